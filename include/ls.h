@@ -350,6 +350,85 @@ int ls_op_prefill_attention(const void *q_bf16_dev, int32_t R, int32_t pos0, int
                             int32_t max_seq, const void *k_pages_dev, const void *v_pages_dev,
                             void *out_bf16_dev, int32_t *status_dev, void *cuda_stream);
 
+/* ------------------------------------------------------------------------------
+ * 4-bit weights and a 4-bit KV cache.  Decoding is bound by the bytes of weights and cached k, v
+ * (Sec. 4.3's loop reads all of them for a handful of rows); these operations read 4.1 to 4.5
+ * bits per value instead of 16.  Rotary embedding, norms and residuals stay as they are.
+ *
+ * Number format.  A group of values shares a scale s, the group's largest |x| divided by 7 and
+ * rounded UP to 5 significant bits, kept as bf16; a value stands for c * s with an integer
+ * c = rint(x / s) in -7..7 (ties to even), stored as the nibble c + 8.  c * s is exactly a bf16
+ * number, so expanding loses nothing.  A group with a NaN or an infinity stands for NaN.
+ * Groups are 32 consecutive channels of a head (cache) or 32, 64 or 128 consecutive columns (weights).
+ *
+ * Packed weights of a matrix [N, K] (K a multiple of 8): blocks of 16 rows x 128 columns, the
+ * ceil(K / 128) blocks of 16 rows one after the other, then the next 16 rows; rows and columns
+ * beyond N and K hold c = 0, s = 0.  A block is 16 rows of 64 bytes of codes, then the scales
+ * bf16 [16][128 / group].  In a row's 64 bytes the 32-bit word 4 t + j (t, j = 0..3) holds columns
+ * 32 j + 8 t .. + 7, column e of the eight at nibble e / 2 + 4 (e % 2).  Any scale that bf16 holds may be
+ * used in weights packed by other means (then c * s is rounded to bf16 by ls_op_expand_w4 only).
+ *
+ * Pages of the cache: [n_pages][Hkv][page_size / 16] tiles of 16 (hd + hd / 8) bytes, 16 tokens of
+ * one KV head each: K codes, 16 rows of hd / 2 bytes (as above; hd 64: word 2 t + j); K scales bf16
+ * [16][hd / 32]; V codes, pieces of hd / 8 channels, lowest nibble first, piece g of token i at
+ * index ((i / 8 * 8 + g) * 4 + i / 2 % 4) * 2 + i % 2; V scales bf16 [hd / 32][16].
+ *
+ * The cache operations take n_seq sequences of M rows; row m of sequence b sits at position
+ * pos0_dev[b] + m (device int32: the calls can be captured and replayed at other positions).
+ * page_table_dev [n_seq][table_stride] maps a sequence's logical pages, table_stride >=
+ * ceil(max_seq / page_size); several sequences may share pages that are only read.  max_seq <=
+ * LS_KV4_MAX_SEQ, page_size a power of two 16..1024, hd 64 or 128.
+ * A row at a negative position is padding.  A position >= max_seq or a table entry outside
+ * [0, n_pages) is refused by the kernel: the access is skipped and status_dev (device int32, may be
+ * NULL, never cleared by the library) receives 2 or 4.
+ * ------------------------------------------------------------------------------ */
+#define LS_KV4_MAX_SEQ (1 << 20)
+
+/* Bytes of the packed weights of an [N, K] matrix; 0 for a shape or group the format does not cover. */
+size_t ls_op_w4_bytes(int32_t N, int32_t K, int32_t group);
+/* bf16 [N, K] -> packed weights, and back to bf16 [N, K] (for ls_op_gemm: the prompt pass).  Weights
+ * are packed once; packed_dev 16-byte aligned. */
+int ls_op_quantize_w4(const void *w_bf16_dev, int32_t N, int32_t K, int32_t group, void *packed_dev,
+                      void *cuda_stream);
+int ls_op_expand_w4(const void *packed_dev, int32_t N, int32_t K, int32_t group, void *out_bf16_dev,
+                    void *cuda_stream);
+/* ls_op_linear on packed weights: out[m,n] (+)= sum_k c[n,k] s[n,k / group] h[m,k]; h bf16 [M,K], M <=
+ * LS_MAX_ROWS, out fp32 [M,N], residual != 0 adds.  The codes enter the tensor cores as integers
+ * and the scales multiply fp32 sums: nothing is rounded but the fp32 accumulation.  A row's
+ * result never depends on how many rows share the pass. */
+int ls_op_linear_w4(const void *packed_dev, const void *h_bf16_dev, int32_t M, int32_t N, int32_t K,
+                    int32_t group, float *out_dev, int32_t residual, void *cuda_stream);
+
+/* Bytes of a page; 0 for a shape the format does not cover. */
+size_t ls_op_kv4_page_bytes(int32_t Hkv, int32_t hd, int32_t page_size);
+/* Append: k, v (bf16, k already rotated) of row m, KV head i of sequence b at element b * seq_stride +
+ * m * row_stride + i * head_stride of either tensor (strides multiples of 8, channels
+ * contiguous, 16-byte aligned: a contiguous [n_seq][M][Hkv][hd], or a page of a bf16 cache that
+ * ls_op_rope_append wrote).  Any M.  Rows of padding are left out; nothing else in the pages
+ * changes.  Two rows of one call must not fall on the same slot of the same page. */
+int ls_op_append_kv4(const void *k_bf16_dev, const void *v_bf16_dev, int64_t seq_stride, int64_t row_stride,
+                     int64_t head_stride, int32_t n_seq, int32_t M, const int32_t *pos0_dev, int32_t Hkv,
+                     int32_t hd, int32_t page_size, const int32_t *page_table_dev, int32_t table_stride,
+                     int32_t max_seq, void *pages_dev, int32_t n_pages, int32_t *status_dev, void *cuda_stream);
+/* The rows' values to a bf16 cache of the same page size with a page table of its own (same
+ * stride; k_pages / v_pages [n_out_pages][Hkv][page_size][hd], as ls_op_prefill_attention and
+ * ls_op_attention read them).  Rows of padding and all other slots are left as they were. */
+int ls_op_expand_kv4(const void *pages_dev, int32_t n_pages, int32_t n_seq, int32_t M, const int32_t *pos0_dev,
+                     int32_t Hkv, int32_t hd, int32_t page_size, const int32_t *page_table_dev,
+                     int32_t table_stride, int32_t max_seq, const int32_t *out_page_table_dev,
+                     void *k_pages_dev, void *v_pages_dev, int32_t n_out_pages, int32_t *status_dev,
+                     void *cuda_stream);
+/* Causal attention as ls_op_attention, over the 4-bit cache, for several sequences: row m of
+ * sequence b sees positions 0..pos0_dev[b] + m; a row that sees none, or is refused, is all zeros.
+ * q, out bf16 [n_seq][M][Hq * hd], M <= LS_MAX_ROWS, Hq / Hkv <= 8.  Slots beyond a sequence's last row
+ * are never used, whatever bits they hold; a row whose table entries are refused leaves out
+ * those positions.  No scratch memory.  A row's result depends on its position, n_seq, Hkv and
+ * max_seq (which fix how the positions are dealt to CTAs), never on M or on the other rows. */
+int ls_op_attention_kv4(const void *q_bf16_dev, int32_t n_seq, int32_t M, const int32_t *pos0_dev, int32_t Hq,
+                        int32_t Hkv, int32_t hd, int32_t page_size, const int32_t *page_table_dev,
+                        int32_t table_stride, int32_t max_seq, const void *pages_dev, int32_t n_pages,
+                        void *out_bf16_dev, int32_t *status_dev, void *cuda_stream);
+
 /* match + crop of Appendix A.4 on device arrays: n = number of leading i < d with
  * draft[i] == verified[i]; appends draft[0..n-1], verified[n] to out_ids (truncated at
  * max_new, and after the first eos_id if eos_id >= 0).

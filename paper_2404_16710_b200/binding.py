@@ -28,7 +28,8 @@ EXPORTS = (
     "ls_generate_batch", "ls_prefill_batch", "ls_decode_batch", "ls_read_output_seq", "ls_debug_logits", "ls_debug_next_logits", "ls_get_stats", "ls_op_embed", "ls_op_rmsnorm",
     "ls_op_linear", "ls_op_gate_up_swiglu", "ls_op_lm_head_scratch_bytes", "ls_op_lm_head_argmax",
     "ls_op_lm_head_argmax_static", "ls_op_rope_append", "ls_op_qkv_rope_append", "ls_op_attention", "ls_op_accept",
-    "ls_op_gemm", "ls_op_prefill_attention", "ls_op_chain",
+    "ls_op_gemm", "ls_op_prefill_attention", "ls_op_chain", "ls_op_w4_bytes", "ls_op_quantize_w4", "ls_op_expand_w4",
+    "ls_op_linear_w4", "ls_op_kv4_page_bytes", "ls_op_append_kv4", "ls_op_expand_kv4", "ls_op_attention_kv4",
 )
 
 
@@ -74,6 +75,7 @@ def lib():
             raise RuntimeError(f"{LIB_PATH} is missing: run `python -m paper_2404_16710_b200.build` "
                                "(there is no CPU fallback)")
         L = C.CDLL(str(LIB_PATH))
+        i64 = C.c_int64
         i32, vp, ip, fp = C.c_int32, C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_float)
         sig = {
             "ls_strerror": (C.c_char_p, [C.c_int]),
@@ -115,6 +117,14 @@ def lib():
             "ls_op_accept": (C.c_int, [vp, vp, i32, vp, vp, vp, vp]),
             "ls_op_gemm": (C.c_int, [vp, vp, i32, i32, i32, vp, i32, i32, vp, vp]),
             "ls_op_prefill_attention": (C.c_int, [vp, i32, i32, i32, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp]),
+            "ls_op_w4_bytes": (C.c_size_t, [i32, i32, i32]),
+            "ls_op_quantize_w4": (C.c_int, [vp, i32, i32, i32, vp, vp]),
+            "ls_op_expand_w4": (C.c_int, [vp, i32, i32, i32, vp, vp]),
+            "ls_op_linear_w4": (C.c_int, [vp, vp, i32, i32, i32, i32, vp, i32, vp]),
+            "ls_op_kv4_page_bytes": (C.c_size_t, [i32, i32, i32]),
+            "ls_op_append_kv4": (C.c_int, [vp, vp, i64, i64, i64, i32, i32, vp, i32, i32, i32, vp, i32, i32, vp, i32, vp, vp]),
+            "ls_op_expand_kv4": (C.c_int, [vp, i32, i32, i32, vp, i32, i32, i32, vp, i32, i32, vp, vp, vp, i32, vp, vp]),
+            "ls_op_attention_kv4": (C.c_int, [vp, i32, i32, vp, i32, i32, i32, i32, vp, i32, i32, vp, i32, vp, vp, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -399,6 +409,112 @@ def ls_op_prefill_attention(q, pos0, Hq, Hkv, hd, page_size, page_table, max_seq
     _ck(lib().ls_op_prefill_attention(_dev(q), q.shape[0], pos0, Hq, Hkv, hd, page_size, _dev(page_table), max_seq,
                                       _dev(k_pages), _dev(v_pages), _dev(out), _dev(status), _stream()),
         "ls_op_prefill_attention")
+
+
+# ---- 4-bit weights and the 4-bit cache
+def _bad(what):
+    raise LsError(LS_ERR_INVALID_ARG, what)
+
+
+def _arg(t, dtype, what):
+    """device pointer of a contiguous CUDA tensor of the type the entry point reads (None -> NULL)"""
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous() or str(t.dtype) != dtype:
+        _bad(f"{what}: a contiguous {dtype} CUDA tensor is needed")
+    return t.data_ptr()
+
+
+_BF16, _F32, _INT, _U8 = "torch.bfloat16", "torch.float32", "torch.int32", "torch.uint8"
+
+
+def ls_op_w4_bytes(N, K, group):
+    return lib().ls_op_w4_bytes(N, K, group)
+
+
+def _packed(packed, N, K, group):
+    """device pointer of packed weights (uint8), which must be large enough for [N, K]"""
+    if packed.numel() < ls_op_w4_bytes(N, K, group):
+        raise LsError(LS_ERR_CAPACITY, "packed weights")
+    return _arg(packed, _U8, "packed weights")
+
+
+def ls_op_quantize_w4(w, group, packed):
+    """bf16 [N, K] -> packed 4-bit weights (uint8, ls_op_w4_bytes(N, K, group) of them)"""
+    N, K = w.shape
+    p = _packed(packed, N, K, group)
+    _ck(lib().ls_op_quantize_w4(_arg(w, _BF16, "w"), N, K, group, p, _stream()), "ls_op_quantize_w4")
+
+
+def ls_op_expand_w4(packed, group, out):
+    N, K = out.shape
+    p = _packed(packed, N, K, group)
+    _ck(lib().ls_op_expand_w4(p, N, K, group, _arg(out, _BF16, "out"), _stream()), "ls_op_expand_w4")
+
+
+def ls_op_linear_w4(packed, group, h, out, residual=False):
+    """out[M, N] (+)= h[M, K] @ W.T of the packed weights W [N, K]"""
+    (M, K), (rows, N) = h.shape, out.shape
+    if rows != M:
+        _bad("ls_op_linear_w4: rows of h and out")
+    p = _packed(packed, N, K, group)
+    _ck(lib().ls_op_linear_w4(p, _arg(h, _BF16, "h"), M, N, K, group, _arg(out, _F32, "out"), int(residual), _stream()),
+        "ls_op_linear_w4")
+
+
+def ls_op_kv4_page_bytes(Hkv, hd, page_size):
+    return lib().ls_op_kv4_page_bytes(Hkv, hd, page_size)
+
+
+def _pool(pages, Hkv, hd, page_size):
+    """number of pages of a pool (uint8, whole pages)"""
+    per, size = ls_op_kv4_page_bytes(Hkv, hd, page_size), pages.numel()
+    if per == 0 or size % per:
+        _bad("pages of a 4-bit cache")
+    return size // per
+
+
+def _rows(pos0, table, n_seq):
+    """entries per sequence of a page table int32 [n_seq, entries]; pos0 int32 [n_seq]"""
+    if pos0.numel() != n_seq or table.dim() != 2 or table.shape[0] != n_seq:
+        _bad("pos0 [n_seq] and page table [n_seq, entries]")
+    return table.shape[1]
+
+
+def ls_op_append_kv4(k, v, pos0, page_size, table, max_seq, pages, status=None):
+    """k, v bf16 [n_seq, M, Hkv, hd], of any strides but equal ones, channels contiguous"""
+    n_seq, M, Hkv, hd = k.shape
+    n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
+    if v.shape != k.shape or v.stride() != k.stride() or k.stride(3) != 1 or not (k.is_cuda and v.is_cuda) or \
+            str(k.dtype) != _BF16 or str(v.dtype) != _BF16:
+        _bad("ls_op_append_kv4: k and v")
+    _ck(lib().ls_op_append_kv4(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), n_seq, M,
+                               _arg(pos0, _INT, "pos0"), Hkv, hd, page_size, _arg(table, _INT, "page table"), entries, max_seq,
+                               _arg(pages, _U8, "pages"), n_pages, _arg(status, _INT, "status"), _stream()), "ls_op_append_kv4")
+
+
+def ls_op_expand_kv4(pages, pos0, M, page_size, table, max_seq, out_table, k_pages, v_pages, status=None):
+    """k_pages, v_pages bf16 [n_out_pages, Hkv, page_size, hd]"""
+    n_out, Hkv, ps, hd = k_pages.shape
+    n_seq = table.shape[0]
+    n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
+    if ps != page_size or v_pages.shape != k_pages.shape or out_table.shape != table.shape:
+        _bad("ls_op_expand_kv4: k_pages, v_pages and their table")
+    _ck(lib().ls_op_expand_kv4(_arg(pages, _U8, "pages"), n_pages, n_seq, M, _arg(pos0, _INT, "pos0"), Hkv, hd, page_size,
+                               _arg(table, _INT, "page table"), entries, max_seq, _arg(out_table, _INT, "out page table"),
+                               _arg(k_pages, _BF16, "k_pages"), _arg(v_pages, _BF16, "v_pages"), n_out,
+                               _arg(status, _INT, "status"), _stream()), "ls_op_expand_kv4")
+
+
+def ls_op_attention_kv4(q, pos0, Hkv, hd, page_size, table, max_seq, pages, out, status=None):
+    """q, out bf16 [n_seq, M, Hq * hd]"""
+    n_seq, M, width = q.shape
+    n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
+    if width % hd or out.shape != q.shape:
+        _bad("ls_op_attention_kv4: q and out")
+    _ck(lib().ls_op_attention_kv4(_arg(q, _BF16, "q"), n_seq, M, _arg(pos0, _INT, "pos0"), width // hd, Hkv, hd, page_size,
+                                  _arg(table, _INT, "page table"), entries, max_seq, _arg(pages, _U8, "pages"), n_pages,
+                                  _arg(out, _BF16, "out"), _arg(status, _INT, "status"), _stream()), "ls_op_attention_kv4")
 
 
 def ls_op_accept(draft, verified, d, state, out_ids, accepted):

@@ -24,6 +24,7 @@
 
 #include "ls.h"
 #include "ls_attention.cuh"
+#include "ls_kv4.cuh"
 #include "ls_linear.cuh"
 #include "ls_prefill.cuh"
 #include "ls_prefill_attn.cuh"
@@ -1834,6 +1835,190 @@ int ls_op_prefill_attention(const void* q, int32_t R, int32_t pos0, int32_t Hq, 
     return prefill_attn_launch((const uint16_t*)q, (const uint16_t*)kp, (const uint16_t*)vp, page_table, pos0, R, Hq,
                                Hkv, hd, log2_exact(page_size), (max_seq + page_size - 1) / page_size, (uint16_t*)out, status,
                                (cudaStream_t)stream);
+}
+
+// ---- 4-bit weights and the 4-bit cache (ls_q4.cuh, ls_w4.cuh, ls_kv4.cuh)
+static bool w4_shape_ok(int N, int K, int group)
+{
+    return N >= 1 && K >= 8 && K % 8 == 0 && (group == 32 || group == 64 || group == 128);
+}
+static int w4_kblocks(int K) { return (int)(((int64_t)K + kQ4Cols - 1) / kQ4Cols); }
+static int64_t w4_blocks(int N, int K) { return ((int64_t)N + kQ4Rows - 1) / kQ4Rows * w4_kblocks(K); }
+
+size_t ls_op_w4_bytes(int32_t N, int32_t K, int32_t group)
+{
+    if (!w4_shape_ok(N, K, group)) return 0;
+    return (size_t)w4_blocks(N, K) * w4_block_bytes(kQ4Cols / group);
+}
+
+int ls_op_quantize_w4(const void* w, int32_t N, int32_t K, int32_t group, void* packed, void* stream)
+{
+    if (!w4_shape_ok(N, K, group) || !aligned16(w) || !aligned16(packed)) return LS_ERR_INVALID_ARG;
+    const int64_t blocks = w4_blocks(N, K);
+    if ((blocks + 7) / 8 > 0x7fffffff) return LS_ERR_UNSUPPORTED;
+    auto* kernel = group == 32 ? quantize_w4_kernel<4> : group == 64 ? quantize_w4_kernel<2> : quantize_w4_kernel<1>;
+    LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, kernel, dim3((unsigned)((blocks + 7) / 8)), dim3(256), 0,
+                 (const uint16_t*)w, N, K, w4_kblocks(K), blocks, (unsigned char*)packed));
+    return LS_OK;
+}
+
+int ls_op_expand_w4(const void* packed, int32_t N, int32_t K, int32_t group, void* out, void* stream)
+{
+    if (!w4_shape_ok(N, K, group) || !aligned16(packed) || !aligned16(out)) return LS_ERR_INVALID_ARG;
+    const int64_t blocks = w4_blocks(N, K);
+    if ((blocks + 7) / 8 > 0x7fffffff) return LS_ERR_UNSUPPORTED;
+    auto* kernel = group == 32 ? expand_w4_kernel<4> : group == 64 ? expand_w4_kernel<2> : expand_w4_kernel<1>;
+    LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, kernel, dim3((unsigned)((blocks + 7) / 8)), dim3(256), 0,
+                 (const unsigned char*)packed, N, K, w4_kblocks(K), blocks, (uint16_t*)out));
+    return LS_OK;
+}
+
+int ls_op_linear_w4(const void* packed, const void* h, int32_t M, int32_t N, int32_t K, int32_t group, float* out,
+                    int32_t residual, void* stream)
+{
+    if (!w4_shape_ok(N, K, group) || M < 1 || M > LS_MAX_ROWS || !aligned16(packed) || !aligned16(h) || !out ||
+        ((uintptr_t)out & 3u))
+        return LS_ERR_INVALID_ARG;
+    auto* kernel = M <= 8 ? (group == 32 ? linear_w4_kernel<4, 1> : group == 64 ? linear_w4_kernel<2, 1> : linear_w4_kernel<1, 1>)
+                          : (group == 32 ? linear_w4_kernel<4, 2> : group == 64 ? linear_w4_kernel<2, 2> : linear_w4_kernel<1, 2>);
+    LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, kernel, dim3((unsigned)((N + (int64_t)15) / 16)),
+                 dim3(kW4Warps * 32), 0, (const unsigned char*)packed, (const uint16_t*)h, M, N, K, w4_kblocks(K), out, residual));
+    return LS_OK;
+}
+
+static int log2_page(int page_size)
+{
+    return page_size < 16 || page_size > 1024 ? -1 : log2_exact(page_size);
+}
+
+size_t ls_op_kv4_page_bytes(int32_t Hkv, int32_t hd, int32_t page_size)
+{
+    if (Hkv < 1 || (hd != 64 && hd != 128) || log2_page(page_size) < 0) return 0;
+    return (size_t)Hkv * (page_size / 16) * kv4_tile_bytes(hd);
+}
+
+// what the three cache operations check alike; the rows of a call are n_seq x M
+static int kv4_check(int n_seq, int M, const int32_t* pos0, int Hkv, int hd, int page_size, const int32_t* table,
+                     int table_stride, int max_seq, const void* pages, int n_pages, Kv4Cache* c)
+{
+    if (n_seq < 1 || M < 1 || Hkv < 1 || (hd != 64 && hd != 128) || log2_page(page_size) < 0 || !pos0 || !table ||
+        !aligned16(pages) || n_pages < 1)
+        return LS_ERR_INVALID_ARG;
+    if (max_seq < 1 || max_seq > LS_KV4_MAX_SEQ || n_seq > 65535 || Hkv > 4095) return LS_ERR_CAPACITY;
+    if (table_stride < (max_seq + page_size - 1) / page_size) return LS_ERR_INVALID_ARG;
+    *c = Kv4Cache{table, table_stride, log2_page(page_size), max_seq, n_pages, Hkv};
+    return LS_OK;
+}
+static int kv4_warps(int M) { return M >= 57 ? 8 : (M + 7) / 8; }  // 8 rows a warp
+
+int ls_op_append_kv4(const void* k, const void* v, int64_t seq_stride, int64_t row_stride, int64_t head_stride,
+                     int32_t n_seq, int32_t M, const int32_t* pos0, int32_t Hkv, int32_t hd, int32_t page_size,
+                     const int32_t* table, int32_t table_stride, int32_t max_seq, void* pages, int32_t n_pages,
+                     int32_t* status, void* stream)
+{
+    Kv4Cache c;
+    LS_TRY(kv4_check(n_seq, M, pos0, Hkv, hd, page_size, table, table_stride, max_seq, pages, n_pages, &c));
+    if (!aligned16(k) || !aligned16(v) || seq_stride % 8 || row_stride % 8 || head_stride % 8) return LS_ERR_INVALID_ARG;
+    const int w = kv4_warps(M);
+    LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, hd == 128 ? append_kv4_kernel<128> : append_kv4_kernel<64>,
+                 dim3((unsigned)((M + (int64_t)8 * w - 1) / (8 * w)), Hkv, n_seq), dim3(32 * w), 0, (const uint16_t*)k,
+                 (const uint16_t*)v, (long long)seq_stride, (long long)row_stride, (long long)head_stride, M, pos0, c,
+                 (unsigned char*)pages, status));
+    return LS_OK;
+}
+
+int ls_op_expand_kv4(const void* pages, int32_t n_pages, int32_t n_seq, int32_t M, const int32_t* pos0, int32_t Hkv,
+                     int32_t hd, int32_t page_size, const int32_t* table, int32_t table_stride, int32_t max_seq,
+                     const int32_t* out_table, void* kp, void* vp, int32_t n_out_pages, int32_t* status, void* stream)
+{
+    Kv4Cache c;
+    LS_TRY(kv4_check(n_seq, M, pos0, Hkv, hd, page_size, table, table_stride, max_seq, pages, n_pages, &c));
+    if (!out_table || !aligned16(kp) || !aligned16(vp) || n_out_pages < 1) return LS_ERR_INVALID_ARG;
+    Kv4Cache d = c;
+    d.table = out_table;
+    d.n_pages = n_out_pages;
+    const int w = kv4_warps(M);
+    LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, hd == 128 ? expand_kv4_kernel<128> : expand_kv4_kernel<64>,
+                 dim3((unsigned)((M + (int64_t)8 * w - 1) / (8 * w)), Hkv, n_seq), dim3(32 * w), 0,
+                 (const unsigned char*)pages, M, pos0, c, d, (uint16_t*)kp, (uint16_t*)vp, status));
+    return LS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// CTAs a (sequence, KV head) is spread over: enough for about two CTAs per SM, no more than the cache has
+// rounds of chunks for, at most 16 (the largest cluster).  Never a function of the rows of the call.
+int kv4_cluster(int n_seq, int Hkv, int max_seq)
+{
+    int S = 1;
+    while (S < 16 && (int64_t)S * Hkv * n_seq < 256 && S * kKv4Warps * kKv4Chunk < max_seq) S *= 2;
+    return S;
+}
+
+template <int HD, int NT>
+int kv4_attn_launch(int S, int qtiles, int n_seq, const uint16_t* q, int M, int G, const int32_t* pos0,
+                           const Kv4Cache& c, const unsigned char* pages, uint16_t* out, int32_t* status, const LaunchCtx& lc)
+{
+    constexpr size_t smem = kv4_smem_bytes<HD, NT>();
+    // once per device: shared memory beyond 48 KB, clusters of 16
+    static std::mutex mu;
+    static bool ready[64] = {};
+    int dev = 0;
+    LS_CK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return LS_ERR_UNSUPPORTED;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!ready[dev]) {
+            LS_CK(cudaFuncSetAttribute(attention_kv4_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+            LS_CK(cudaFuncSetAttribute(attention_kv4_kernel<HD, NT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+            ready[dev] = true;
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(S, c.Hkv * qtiles, n_seq);
+    cfg.blockDim = dim3(kKv4Threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = lc.st;
+    cudaLaunchAttribute at[3];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = S;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeClusterSchedulingPolicyPreference;  // several CTAs of a cluster per SM: see attn_launch_t
+    at[1].val.clusterSchedulingPolicyPreference = cudaClusterSchedulingPolicyLoadBalancing;
+    at[2].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[2].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = lc.pdl ? 3 : 2;
+    LS_CK(cudaLaunchKernelEx(&cfg, attention_kv4_kernel<HD, NT>, q, M, G, pos0, c, pages, out, status));
+    return LS_OK;
+}
+
+template <int HD>
+int kv4_attn_launch_hd(int n_seq, const uint16_t* q, int M, int G, const int32_t* pos0, const Kv4Cache& c,
+                              const unsigned char* pages, uint16_t* out, int32_t* status, const LaunchCtx& lc)
+{
+    const int S = kv4_cluster(n_seq, c.Hkv, c.max_seq), Q = M * G;  // queries of a KV head, in tiles of 8
+    if (Q <= 8) return kv4_attn_launch<HD, 1>(S, 1, n_seq, q, M, G, pos0, c, pages, out, status, lc);
+    return kv4_attn_launch<HD, 2>(S, (Q + 15) / 16, n_seq, q, M, G, pos0, c, pages, out, status, lc);
+}
+
+}  // namespace
+
+extern "C" {
+
+int ls_op_attention_kv4(const void* q, int32_t n_seq, int32_t M, const int32_t* pos0, int32_t Hq, int32_t Hkv, int32_t hd,
+                        int32_t page_size, const int32_t* table, int32_t table_stride, int32_t max_seq, const void* pages,
+                        int32_t n_pages, void* out, int32_t* status, void* stream)
+{
+    Kv4Cache c;
+    LS_TRY(kv4_check(n_seq, M, pos0, Hkv, hd, page_size, table, table_stride, max_seq, pages, n_pages, &c));
+    if (M > LS_MAX_ROWS || Hq < 1 || Hq % Hkv || Hq / Hkv > 8 || !aligned16(q) || !aligned16(out)) return LS_ERR_INVALID_ARG;
+    const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
+    return (hd == 128 ? kv4_attn_launch_hd<128> : kv4_attn_launch_hd<64>)(
+        n_seq, (const uint16_t*)q, M, Hq / Hkv, pos0, c, (const unsigned char*)pages, (uint16_t*)out, status, lc);
 }
 
 int ls_op_accept(const int32_t* draft, const int32_t* verified, int32_t d, int32_t* state, int32_t* out_ids,

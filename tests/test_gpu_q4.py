@@ -1,0 +1,484 @@
+"""4-bit weights and the 4-bit cache against the format's definition and 64-bit arithmetic (tests/q4_reference.py).
+
+Conversions are exact: bytes and values have to be equal.  Tolerances of the computed results, derived:
+* linear: exact products (8-bit by 3-bit significands), fp32 sums. Every one of the K / 16 tensor-core sums, the
+  K / group scaled additions and the 16 at the end is off by at most one unit of its result's last place (the tensor
+  cores may truncate), 2^-23, of a partial sum that is at most sum |c s h|.
+* attention: the scores are fp32 sums as above, so the exponent is off by at most (hd / 16 + hd / 32 + 4) 2^-23 of
+  sum |q k| scale; the weights enter the product as two bf16 numbers (2^-16), the exponential is good to 2^-21, the
+  sums to 2^-23 a term in a chunk; together well below 2^-12 of sum_i a_i |v_i| for these inputs.  The bf16 result
+  is rounded once (2^-8 of its value).
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2404_16710_b200 import binding as B
+from tests import q4_reference as R
+from tests.helpers import vals
+
+pytestmark = pytest.mark.gpu
+
+
+def rnd(shape, seed, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda") * scale
+
+
+def from_bits(u):
+    return torch.from_numpy(np.ascontiguousarray(u, np.uint16).view(np.int16)).cuda().view(torch.bfloat16)
+
+
+def awkward(shape, seed):
+    """bf16 values over the whole range, with exact borders, zeros, denormals, the largest number, NaN, infinities"""
+    rng = np.random.default_rng(seed)
+    x = (rng.standard_normal(shape) * np.exp2(rng.integers(-140, 120, shape[:-1] + (1,)))).astype(np.float32)
+    u = (x.view(np.uint32) >> 16).astype(np.uint16)
+    flat = u.reshape(-1, 16, 8)  # blocks of 128 values: the widest group
+    n = flat.shape[0]
+    # 7 steps of a scale with 5 significant bits, and borders (k + 1/2) of it (6.5: next to one, as 9 bits do not fit)
+    s = np.float32(21 * 2.0 ** -9)
+    flat[n // 3] = ((np.float32([7, 0.5, 1.5, 2.5, -3.5, 4.5, -5.5, 6.5]) * s).view(np.uint32) >> 16)
+    flat[n // 2] = 0
+    flat[n // 2 + 1] = [1, 0x8001, 2, 0x7F, 0x80, 0, 0x8000, 3]
+    flat[(2 * n) // 3] = [0x7F7F, 0xFF7F, 0x7F00, 0x4000, 0, 1, 0x3F80, 0xBF80]
+    flat[(3 * n) // 4, 5] = [0x7F80, 0x3F80, 0x3F80, 0, 0, 0, 0, 0]
+    flat[(4 * n) // 5, 9] = [0x3F80, 0x7FC1, 0x3F80, 0, 0, 0, 0, 0xFF80]
+    return from_bits(flat.reshape(shape))
+
+
+def quantised(w, group):
+    N, K = w.shape
+    packed = torch.full((B.ls_op_w4_bytes(N, K, group),), 0xEE, dtype=torch.uint8, device="cuda")
+    B.ls_op_quantize_w4(w, group, packed)
+    return packed
+
+
+# ------------------------------------------------------------------ weights
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N,K", [(1, 8), (16, 128), (17, 136), (33, 1000), (100, 72), (5, 2056)])
+def test_quantize_and_expand_weights(N, K, group):
+    w = rnd((N, K), N + K, 0.02).bfloat16()
+    packed = quantised(w, group)
+    assert np.array_equal(packed.cpu().numpy(), R.pack_weight(vals(w), group))
+    out = torch.full((N, K), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.ls_op_expand_w4(packed, group, out)
+    assert np.array_equal(vals(out), R.values(*R.quantise(vals(w), group), group))
+
+
+@pytest.mark.parametrize("group", [32, 128])
+def test_quantize_weights_at_the_ends_of_the_range(group):
+    w = awkward((40, 1024), 3)
+    packed = quantised(w, group)
+    assert np.array_equal(packed.cpu().numpy(), R.pack_weight(vals(w), group))
+    out = torch.empty_like(w)
+    B.ls_op_expand_w4(packed, group, out)
+    assert np.array_equal(vals(out), R.values(*R.quantise(vals(w), group), group), equal_nan=True)
+
+
+def linear_reference(w, group, h):
+    v = R.values(*R.quantise(vals(w), group), group)
+    hv = vals(h)
+    return hv @ v.T, np.abs(hv) @ np.abs(v).T
+
+
+def linear_tol(K, group, spread):
+    return (K / 16 + K / group + 20) * 2.0 ** -23 * spread
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N,K", [(1, 16, 128), (1, 1, 8), (2, 200, 88), (7, 333, 1000), (8, 64, 4096), (9, 48, 2000),
+                                   (16, 130, 520), (5, 1000, 14336), (16, 4096, 1376), (1, 4100, 4096)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_linear(M, N, K, group, residual):
+    w, h = rnd((N, K), 1 + N, 0.02).bfloat16(), rnd((M, K), 2 + K).bfloat16()
+    out = rnd((M, N), 3) if residual else torch.full((M, N), float("nan"), device="cuda")
+    base = out.cpu().numpy().astype(np.float64) if residual else 0.0
+    B.ls_op_linear_w4(quantised(w, group), group, h, out, residual)
+    ref, spread = linear_reference(w, group, h)
+    got = out.cpu().numpy().astype(np.float64)
+    tol = linear_tol(K, group, spread) + (2.0 ** -23 * np.abs(base + ref) if residual else 0.0)
+    assert (np.abs(got - base - ref) <= tol).all(), np.abs(got - base - ref).max()
+    assert np.linalg.norm(got - base - ref) <= 1e-5 * np.linalg.norm(ref)
+
+
+def test_linear_large_vocabulary_sampled_rows():
+    N, K, group, M = 128256, 4096, 64, 13
+    w, h = rnd((N, K), 5, 0.02).bfloat16(), rnd((M, K), 6).bfloat16()
+    out = torch.empty((M, N), device="cuda")
+    B.ls_op_linear_w4(quantised(w, group), group, h, out)
+    rows = np.unique(np.concatenate([[0, 15, 16, N - 1], np.random.default_rng(0).integers(0, N, 40)]))
+    ref, spread = linear_reference(w[torch.from_numpy(rows).cuda()], group, h)
+    assert (np.abs(out.cpu().numpy()[:, rows] - ref) <= linear_tol(K, group, spread)).all()
+
+
+@pytest.mark.parametrize("N,K,group", [(304, 1384, 32), (4096, 4096, 128), (5000, 264, 64), (16, 11008, 32)])
+def test_linear_rows_do_not_depend_on_pass_size(N, K, group):
+    packed = quantised(rnd((N, K), 7, 0.05).bfloat16(), group)
+    h = rnd((16, K), 8).bfloat16()
+    full = torch.empty((16, N), device="cuda")
+    B.ls_op_linear_w4(packed, group, h, full)
+    for m0, M in ((0, 1), (3, 2), (0, 4), (5, 7), (8, 8), (2, 9), (0, 15)):
+        out = torch.empty((M, N), device="cuda")
+        B.ls_op_linear_w4(packed, group, h[m0:m0 + M].contiguous(), out)
+        assert torch.equal(out, full[m0:m0 + M]), M
+
+
+def test_linear_scales_of_other_packers_and_values_that_are_not_finite():
+    """any bf16 scale may stand in the packed weights; a NaN group, an infinite h make NaN where the formula does"""
+    N, K, group = 40, 256, 64
+    w = rnd((N, K), 9, 0.02).bfloat16()
+    packed = quantised(w, group).cpu().numpy().reshape(-1, 1024 + 64)
+    scales = np.random.default_rng(1).integers(0x3A00, 0x3C00, (packed.shape[0], 32)).astype("<u2")
+    packed[:, 1024:] = scales.view(np.uint8)
+    dev = torch.from_numpy(packed.reshape(-1).copy()).cuda()
+    codes, _ = R.quantise(vals(w), group)
+    S = (scales.astype(np.uint32) << 16).view(np.float32).astype(np.float64).reshape(3, 2, 16, 2)
+    S = S.transpose(0, 2, 1, 3).reshape(48, 4)[:N]
+    h = rnd((3, K), 10).bfloat16()
+    out = torch.empty((3, N), device="cuda")
+    B.ls_op_linear_w4(dev, group, h, out)
+    v = R.values(codes, S, group)
+    assert (np.abs(out.cpu().numpy() - vals(h) @ v.T) <= linear_tol(K, group, np.abs(vals(h)) @ np.abs(v).T)).all()
+    w[5, 70] = float("nan")
+    w[6, 3] = float("inf")
+    h[1, 9] = float("inf")
+    B.ls_op_linear_w4(quantised(w, group), group, h, out)
+    got = out.cpu().numpy()
+    assert np.isnan(got[:, [5, 6]]).all() and not np.isfinite(got[1]).any()
+    rest = [n for n in range(N) if n not in (5, 6)]
+    assert np.isfinite(got[[0, 2]][:, rest]).all()
+
+
+# ------------------------------------------------------------------ the cache: append, expand
+def empty_pool(n_pages, Hkv, hd, page, fill=0xFF):
+    return torch.full((n_pages, B.ls_op_kv4_page_bytes(Hkv, hd, page)), fill, dtype=torch.uint8, device="cuda")
+
+
+def reference_append(pool, k, v, pos0, table, page, max_seq):
+    """the appended pool by the definition; pool [n_pages, page bytes] uint8, k, v float64 [n_seq, M, Hkv, hd]"""
+    n_seq, M, Hkv, hd = k.shape
+    tiles = pool.reshape(pool.shape[0], Hkv, page // 16, R.tile_bytes(hd))
+    for b in range(n_seq):
+        for m in range(M):
+            p = pos0[b] + m
+            if 0 <= p < max_seq and 0 <= table[b, p // page] < pool.shape[0]:
+                for i in range(Hkv):
+                    R.put_token(tiles[table[b, p // page], i, p % page // 16], p % 16, k[b, m, i], v[b, m, i], hd)
+    return pool
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n_seq,M,Hkv,page,pos", [(1, 1, 2, 16, [0]), (1, 1, 1, 64, [77]), (3, 5, 2, 16, [14, 0, 40]),
+                                                  (2, 70, 1, 32, [3, 25]), (4, 3, 2, 64, [-1, -3, 93, 60])])
+def test_append_and_expand(n_seq, M, Hkv, page, pos, hd):
+    max_seq = 96
+    n_tab = -(-max_seq // page)
+    table = np.random.default_rng(5).permutation(n_seq * n_tab + 3)[:n_seq * n_tab].reshape(n_seq, n_tab).astype(np.int32)
+    k, v = rnd((n_seq, M, Hkv, hd), 11, 3.0).bfloat16(), rnd((n_seq, M, Hkv, hd), 12).bfloat16()
+    pool = empty_pool(n_seq * n_tab + 3, Hkv, hd, page, 0x5A)
+    want = reference_append(pool.cpu().numpy().copy(), vals(k), vals(v), pos, table, page, max_seq)
+    td, pd = torch.from_numpy(table).cuda(), torch.tensor(pos, dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.ls_op_append_kv4(k, v, pd, page, td, max_seq, pool, status)
+    assert np.array_equal(pool.cpu().numpy(), want) and int(status) == 0
+    # back, to pages in another order; slots that no row covers stay as they were
+    out_table = np.random.default_rng(6).permutation(n_seq * n_tab).reshape(n_seq, n_tab).astype(np.int32)
+    kp = torch.full((n_seq * n_tab, Hkv, page, hd), 3.0, dtype=torch.bfloat16, device="cuda")
+    vp = torch.full_like(kp, 5.0)
+    wk, wv = vals(kp), vals(vp)
+    for b in range(n_seq):
+        for m in range(M):
+            p = pos[b] + m
+            if p >= 0:
+                at = out_table[b, p // page], slice(None), p % page
+                wk[at] = R.values(*R.quantise(vals(k[b, m]), 32), 32)
+                wv[at] = R.values(*R.quantise(vals(v[b, m]), 32), 32)
+    B.ls_op_expand_kv4(pool, pd, M, page, td, max_seq, torch.from_numpy(out_table).cuda(), kp, vp, status)
+    assert np.array_equal(vals(kp), wk) and np.array_equal(vals(vp), wv) and int(status) == 0
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_append_strided_rows_and_the_ends_of_the_range(hd):
+    """rows of a fused q|k|v buffer and of a bf16 cache page (heads outermost), values over the whole range"""
+    Hkv, page, M = 2, 32, 20
+    table, pd = torch.tensor([[1, 0]], dtype=torch.int32, device="cuda"), torch.tensor([7], dtype=torch.int32, device="cuda")
+    fused = awkward((M, 6 * Hkv * hd), 13)
+    heads = awkward((2, Hkv, 32, hd), 14)
+    for k, v in ((fused.view(1, M, 6 * Hkv, hd)[:, :, Hkv:2 * Hkv], fused.view(1, M, 6 * Hkv, hd)[:, :, 4 * Hkv:5 * Hkv]),
+                 (heads[0].transpose(0, 1)[None, 4:4 + M], heads[1].transpose(0, 1)[None, 4:4 + M])):
+        pool = empty_pool(2, Hkv, hd, page)
+        want = reference_append(pool.cpu().numpy().copy(), vals(k), vals(v), [7], table.cpu().numpy(), page, 64)
+        B.ls_op_append_kv4(k, v, pd, page, table, 64, pool)
+        assert np.array_equal(pool.cpu().numpy(), want)
+
+
+def test_positions_and_pages_out_of_range_are_refused():
+    Hkv, hd, page, max_seq = 2, 128, 16, 64
+    table = torch.tensor([[0, 1, 2, 3], [4, 9, -1, 5], [6, 7, 8, 2 ** 31 - 1]], dtype=torch.int32, device="cuda")
+    k, v = rnd((3, 6, Hkv, hd), 15).bfloat16(), rnd((3, 6, Hkv, hd), 16).bfloat16()
+    q = rnd((3, 6, 4 * hd), 17).bfloat16()
+    kp = torch.zeros((9, Hkv, page, hd), dtype=torch.bfloat16, device="cuda")
+    for pos, code in (([60, 0, 2 ** 31 - 1], 2), ([0, 12, 0], 4), ([0, 30, 0], 4), ([0, 0, 46], 4)):
+        pd = torch.tensor(pos, dtype=torch.int32, device="cuda")
+        for which in range(3):
+            status = torch.zeros(1, dtype=torch.int32, device="cuda")
+            pool = empty_pool(9, Hkv, hd, page, 0x11)
+            if which == 0:
+                want = reference_append(pool.cpu().numpy().copy(), vals(k), vals(v), pos, table.cpu().numpy(), page, max_seq)
+                B.ls_op_append_kv4(k, v, pd, page, table, max_seq, pool, status)
+                assert np.array_equal(pool.cpu().numpy(), want)
+            elif which == 1:
+                B.ls_op_expand_kv4(pool, pd, 6, page, table, max_seq, table, kp, kp.clone(), status)
+            else:
+                out = torch.full_like(q, 9.0)
+                B.ls_op_attention_kv4(q, pd, Hkv, hd, page, table, max_seq, pool, out, status)
+                got = vals(out)
+                for b in range(3):
+                    for m in range(6):
+                        if pos[b] + m >= max_seq:
+                            assert (got[b, m] == 0).all(), (pos, b, m)
+            assert int(status) == code, (pos, which)
+
+
+# ------------------------------------------------------------------ attention
+class Cache:
+    """n_seq sequences of random k, v in 4 bits: appended by the library (its bytes are tested above) to pages whose
+    other slots hold 0xff bytes, i.e. NaN scales"""
+
+    def __init__(self, lens, Hkv, hd, page, seed, max_seq=None, loud=1.0):
+        self.Hkv, self.hd, self.page, self.lens = Hkv, hd, page, lens
+        n_seq, T = len(lens), max(max(lens), 1)
+        self.max_seq = max_seq or -(-T // page) * page
+        n_tab = -(-self.max_seq // page)
+        order = np.random.default_rng(seed).permutation(n_seq * n_tab).astype(np.int32)
+        self.table = torch.from_numpy(order.reshape(n_seq, n_tab)).cuda()
+        self.pool = empty_pool(n_seq * n_tab, Hkv, hd, page)
+        self.k = [rnd((max(n, 1), Hkv, hd), seed + 10 * b, loud).bfloat16() for b, n in enumerate(lens)]
+        self.v = [rnd((max(n, 1), Hkv, hd), seed + 10 * b + 1).bfloat16() for b, n in enumerate(lens)]
+        for b, n in enumerate(lens):
+            if n:
+                B.ls_op_append_kv4(self.k[b][None, :n], self.v[b][None, :n], torch.zeros(1, dtype=torch.int32, device="cuda"),
+                                   page, self.table[b:b + 1], self.max_seq, self.pool)
+
+    def values(self, b):
+        return [R.values(*R.quantise(vals(x[b]), 32), 32) for x in (self.k, self.v)]
+
+    def run(self, q, M, status=None):
+        out = torch.full_like(q, float("nan"))
+        pos = torch.tensor([n - M for n in self.lens], dtype=torch.int32, device="cuda")
+        B.ls_op_attention_kv4(q, pos, self.Hkv, self.hd, self.page, self.table, self.max_seq, self.pool, out, status)
+        return out
+
+
+def check_attention(c, q, out, M, G):
+    got, qv = vals(out), vals(q)
+    for b, n in enumerate(c.lens):
+        k, v = c.values(b)
+        for m in range(M):
+            ref, spread = R.attention(qv[b, m].reshape(-1, c.hd), k, v, n - M + m, G)
+            err = np.abs(got[b, m].reshape(-1, c.hd) - ref)
+            assert (err <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -12 * spread).all(), (b, m, n, err.max())
+
+
+@pytest.mark.parametrize("Hkv,G,hd", [(2, 1, 128), (1, 8, 128), (2, 4, 64), (3, 2, 128)])
+@pytest.mark.parametrize("M,lens,page", [(1, [1], 16), (1, [15, 16, 17], 16), (1, [31, 32, 33], 32), (3, [2, 3, 4], 16),
+                                         (7, [300], 64), (16, [16, 1000], 32), (1, [0, 257, 256, 255], 64),
+                                         (5, [0, 0, 4, 130], 16), (16, [1100, 7], 256), (2, [4099], 64)])
+def test_attention(Hkv, G, hd, M, lens, page):
+    c = Cache(lens, Hkv, hd, page, 20)
+    q = rnd((len(lens), M, Hkv * G * hd), 21).bfloat16()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = c.run(q, M, status)
+    check_attention(c, q, out, M, G)
+    assert int(status) == 0
+
+
+@pytest.mark.parametrize("n_seq", [1, 40])
+def test_attention_clusters_of_every_size_and_peaked_scores(n_seq):
+    """one to 16 CTAs a head (by the number of sequences and heads), scores that differ by hundreds"""
+    for Hkv in (1, 2, 8):
+        c = Cache([700 - 13 * b for b in range(n_seq)], Hkv, 128, 64, 30, max_seq=4096, loud=6.0)
+        q = rnd((n_seq, 2, Hkv * 2 * 128), 31, 2.0).bfloat16()
+        check_attention(c, q, c.run(q, 2), 2, 2)
+
+
+@pytest.mark.parametrize("Hkv,G,hd", [(2, 1, 128), (2, 4, 64), (4, 8, 128)])
+def test_attention_rows_do_not_depend_on_pass_size(Hkv, G, hd):
+    c = Cache([1000], Hkv, hd, 64, 40, max_seq=2048)
+    q = rnd((1, 16, Hkv * G * hd), 41).bfloat16()
+    full = c.run(q, 16)
+    for m0, M in ((0, 1), (15, 1), (4, 3), (0, 8), (7, 9)):
+        out = torch.empty((1, M, q.shape[2]), dtype=torch.bfloat16, device="cuda")
+        B.ls_op_attention_kv4(q[:, m0:m0 + M].contiguous(), torch.tensor([984 + m0], dtype=torch.int32, device="cuda"), Hkv, hd, 64,
+                              c.table, 2048, c.pool, out)
+        assert torch.equal(out, full[:, m0:m0 + M]), (m0, M)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attention_values_that_are_not_finite_reach_only_the_rows_that_see_them(hd):
+    Hkv, G, M, n = 1, 2, 4, 90
+    for what in ("k", "v"):
+        c = Cache([n], Hkv, hd, 32, 50)
+        bad = rnd((1, 2, Hkv, hd), 51).bfloat16()
+        good = rnd((1, 2, Hkv, hd), 52).bfloat16()
+        bad[0, 0, 0, 40] = float("nan")
+        bad[0, 1, 0, 3] = float("inf")
+        pos = torch.tensor([n - 2], dtype=torch.int32, device="cuda")
+        k, v = (bad, good) if what == "k" else (good, bad)
+        B.ls_op_append_kv4(k, v, pos, 32, c.table, c.max_seq, c.pool)
+        c.k[0][n - 2:], c.v[0][n - 2:] = k[0], v[0]
+        q = rnd((1, M, G * hd), 53).bfloat16()
+        out = c.run(q, M)
+        got = vals(out).reshape(M, G, hd)
+        kk, vv = c.values(0)
+        for m in range(2):
+            ref, spread = R.attention(vals(q)[0, m].reshape(G, hd), kk[:n - 2], vv[:n - 2], n - M + m, G)
+            assert (np.abs(got[m] - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -12 * spread).all()
+        if what == "k":
+            assert np.isnan(got[2:]).all()
+        else:  # the groups of channels 40 and 3
+            assert np.isnan(got[2, :, 32:64]).all() and np.isfinite(got[2, :, :32]).all() and np.isfinite(got[2, :, 64:]).all()
+            assert np.isnan(got[3, :, :64]).all() and np.isfinite(got[3, :, 64:]).all()
+
+
+def test_attention_pages_beyond_32_bits_of_offset():
+    """a pool of more than 4 GB whose used pages are the last ones"""
+    Hkv, hd, page, n = 8, 128, 1024, 1500
+    per = B.ls_op_kv4_page_bytes(Hkv, hd, page)
+    n_pages = (1 << 32) // per + 8
+    small = Cache([n], Hkv, hd, page, 60, max_seq=4096)
+    pool = torch.zeros((n_pages, per), dtype=torch.uint8, device="cuda")
+    far = torch.tensor([[n_pages - 1, n_pages - 3, n_pages - 2, 0]], dtype=torch.int32, device="cuda")
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.ls_op_append_kv4(small.k[0][None], small.v[0][None], zero, page, far, 4096, pool)
+    assert not bool(pool[:n_pages - 3].any())
+    q = rnd((1, 1, 16 * hd), 61).bfloat16()
+    a, pos = torch.empty_like(q), torch.tensor([n - 1], dtype=torch.int32, device="cuda")
+    B.ls_op_attention_kv4(q, pos, Hkv, hd, page, far, 4096, pool, a)
+    assert torch.equal(a, small.run(q, 1))
+    kp = torch.zeros((4, Hkv, page, hd), dtype=torch.bfloat16, device="cuda")
+    vp = torch.zeros_like(kp)
+    B.ls_op_expand_kv4(pool, zero, n, page, far, 4096, torch.tensor([[0, 1, 2, 3]], dtype=torch.int32, device="cuda"), kp, vp)
+    k, _ = small.values(0)
+    assert np.array_equal(vals(kp).transpose(0, 2, 1, 3).reshape(-1, Hkv, hd)[:n], k)
+
+
+def test_captured_and_replayed_at_other_positions_on_another_stream():
+    """append and attention in one CUDA graph, positions advanced on the device between replays; a second sequence
+    shares the pages of the first for what both only read"""
+    Hkv, G, hd, page, max_seq = 2, 2, 128, 16, 160
+    c = Cache([100], Hkv, hd, page, 70, max_seq=max_seq)
+    st = torch.cuda.Stream()
+    table = torch.cat([c.table, c.table])
+    pool = torch.cat([c.pool, empty_pool(4, Hkv, hd, page)])
+    n_own = c.pool.shape[0]
+    table[1, 6:10] = torch.arange(n_own, n_own + 4, device="cuda", dtype=torch.int32)
+    pool[table[1, 6].long()] = pool[table[0, 6].long()]  # positions 96..99 are copied, 0..95 shared
+    k, v = rnd((2, 1, Hkv, hd), 71).bfloat16(), rnd((2, 1, Hkv, hd), 72).bfloat16()
+    q, out = rnd((2, 1, Hkv * G * hd), 73).bfloat16(), torch.zeros((2, 1, Hkv * G * hd), dtype=torch.bfloat16, device="cuda")
+    pos = torch.tensor([100, 100], dtype=torch.int32, device="cuda")
+
+    def step():
+        B.ls_op_append_kv4(k, v, pos, page, table, max_seq, pool)
+        B.ls_op_attention_kv4(q, pos, Hkv, hd, page, table, max_seq, pool, out)
+        pos.add_(1)
+
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        step()  # first use outside a capture
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            step()
+        pos.fill_(100)
+        steps = []
+        for i in range(20):
+            k.copy_(rnd((2, 1, Hkv, hd), 200 + i))
+            v.copy_(rnd((2, 1, Hkv, hd), 300 + i))
+            q.copy_(rnd((2, 1, Hkv * G * hd), 400 + i))
+            steps.append((vals(k), vals(v), vals(q)))
+            graph.replay()
+            steps[-1] += (vals(out),)
+    st.synchronize()
+    ck, cv = c.values(0)
+    for b in range(2):
+        kk, vv = ck, cv
+        for ks, vs, qs, got in steps:
+            kk = np.concatenate([kk, R.values(*R.quantise(ks[b], 32), 32)])
+            vv = np.concatenate([vv, R.values(*R.quantise(vs[b], 32), 32)])
+            ref, spread = R.attention(qs[b, 0].reshape(-1, hd), kk, vv, kk.shape[0] - 1, G)
+            assert (np.abs(got[b, 0].reshape(-1, hd) - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -12 * spread).all()
+
+
+# ------------------------------------------------------------------ together
+@pytest.mark.parametrize("chained", [False, True])
+def test_a_layer_of_draft_and_verify_passes_on_4_bit_weights_and_cache(chained):
+    """A prompt and then passes of 1, 1 and 3 rows through one layer's attention block, as a decode loop runs them:
+    norm, q|k|v projections, rotary embedding (into a bf16 page), append, attention, output projection with the
+    residual.  The prompt's rows go through the prompt-pass operations on expanded weights and cache.  Every step is
+    checked against 64-bit arithmetic on what the step before it left; chained: with the operations linked by
+    programmatic dependent launch."""
+    D, Hq, Hkv, hd, page, max_seq, group, theta = 256, 4, 2, 64, 16, 96, 32, 1e4
+    qw, kw = Hq * hd, Hkv * hd
+    wqkv, wo = rnd((qw + 2 * kw, D), 80, 0.06).bfloat16(), rnd((D, qw), 81, 0.06).bfloat16()
+    pqkv, po = quantised(wqkv, group), quantised(wo, group)
+    gain = (1 + 0.1 * rnd((D,), 82)).bfloat16()
+    table = torch.tensor([[3, 0, 5, 1, 4, 2]], dtype=torch.int32, device="cuda")
+    pool = empty_pool(6, Hkv, hd, page)
+    stage = torch.zeros((2, 1, Hkv, page, hd), dtype=torch.bfloat16, device="cuda")  # one bf16 page for new k, one for v
+    at_stage = torch.zeros(6, dtype=torch.int32, device="cuda")
+    x = rnd((16 + 1 + 1 + 3, D), 83)
+    pos, left = 0, []
+    B.ls_op_chain(chained)
+    try:
+        for M in (16, 1, 1, 3):
+            rows = x[pos:pos + M].clone()
+            h = torch.empty((M, D), dtype=torch.bfloat16, device="cuda")
+            qkv = torch.empty((M, qw + 2 * kw), device="cuda")
+            q, o = torch.empty((1, M, qw), dtype=torch.bfloat16, device="cuda"), torch.empty((1, M, qw), dtype=torch.bfloat16, device="cuda")
+            pd = torch.tensor([pos], dtype=torch.int32, device="cuda")
+            before = rows.clone()
+            B.ls_op_rmsnorm(rows, gain, 1e-5, h)
+            B.ls_op_linear_w4(pqkv, group, h, qkv)
+            B.ls_op_rope_append(qkv, pos, Hq, Hkv, hd, theta, page, at_stage, max_seq, q, stage[0], stage[1])
+            s0 = pos % page  # rows of a pass stay within the staging page here: 0..15, 0, 1, 2..4
+            k, v = (stage[i, 0].transpose(0, 1)[None, s0:s0 + M] for i in range(2))
+            B.ls_op_append_kv4(k, v, pd, page, table, max_seq, pool)
+            B.ls_op_attention_kv4(q, pd, Hkv, hd, page, table, max_seq, pool, o)
+            B.ls_op_linear_w4(po, group, o[0], rows, True)
+            torch.cuda.synchronize()
+            left.append((pos, M, before, h, qkv, q, o, rows, k.clone(), v.clone()))
+            pos += M
+    finally:
+        B.ls_op_chain(False)
+    ks, vs = [], []
+    for pos, M, before, h, qkv, q, o, rows, k, v in left:
+        ref, spread = linear_reference(wqkv, group, h)
+        assert (np.abs(qkv.cpu().numpy() - ref) <= linear_tol(D, group, spread)).all()
+        ks.append(R.values(*R.quantise(vals(k[0]), 32), 32))
+        vs.append(R.values(*R.quantise(vals(v[0]), 32), 32))
+        kk, vv = np.concatenate(ks), np.concatenate(vs)
+        for m in range(M):
+            ref, spread = R.attention(vals(q)[0, m].reshape(Hq, hd), kk, vv, pos + m, Hq // Hkv)
+            assert (np.abs(vals(o)[0, m].reshape(Hq, hd) - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -12 * spread).all()
+        ref, spread = linear_reference(wo, group, o[0])
+        base = before.cpu().numpy().astype(np.float64)
+        assert (np.abs(rows.cpu().numpy() - base - ref) <= linear_tol(qw, group, spread) + 2.0 ** -23 * np.abs(base + ref)).all()
+    # the prompt again by the prompt-pass operations on expanded weights and an expanded cache
+    _, M, _, h, qkv, q, o, *_ = left[0]
+    wide = torch.empty_like(wqkv)
+    B.ls_op_expand_w4(pqkv, group, wide)
+    c, status = torch.empty_like(qkv), torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.ls_op_gemm(h, wide, c, False, status)
+    _, spread = linear_reference(wqkv, group, h)
+    assert (np.abs((c - qkv).cpu().numpy()) <= 2 * linear_tol(D, group, spread)).all()
+    kp = torch.full((6, Hkv, page, hd), float("nan"), dtype=torch.bfloat16, device="cuda")
+    vp = torch.full_like(kp, float("nan"))
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.ls_op_expand_kv4(pool, zero, 21, page, table, max_seq, table, kp, vp, status)
+    a = torch.empty_like(q[0])
+    B.ls_op_prefill_attention(q[0], 0, Hq, Hkv, hd, page, table[0], max_seq, kp, vp, a, status)
+    for m in range(M):  # both within their bounds of the same values: bf16 weights p there (2^-9), two results rounded
+        ref, spread = R.attention(vals(q)[0, m].reshape(Hq, hd), kk, vv, m, Hq // Hkv)
+        assert (np.abs(vals(a)[m].reshape(Hq, hd) - ref) <= 2.0 ** -8 * np.abs(ref).max() + 2.0 ** -8 * spread).all()
+    assert int(status) == 0
