@@ -1873,17 +1873,76 @@ int ls_op_expand_w4(const void* packed, int32_t N, int32_t K, int32_t group, voi
     return LS_OK;
 }
 
+}  // extern "C"
+
+namespace {
+
+// log2 of the warps that share a tile of 16 rows.  A function of the matrix alone: it enters a row's arithmetic.
+// Few tiles: all 16 warps of an SM on its one tile (64 tiles, K = 4096: 3.6 us, 4.7 with 8 warps); up to a few
+// tiles an SM: 8 (256 tiles: 5.1 us, with 16 warps 5.5, with 4 6.7); beyond, 4, which saves additions of sums
+// (8016 tiles: 58.6 us, with 8 warps 63.8, with 16 77.5, with 1 60.2).
+int w4_split(int n_tiles)
+{
+    return n_tiles <= 148 ? 4 : n_tiles < 1024 ? 3 : 2;
+}
+
+template <int NG, int NT, int D, bool HS>
+int w4_launch(const unsigned char* packed, const uint16_t* h, int M, int N, int K, float* out, int residual,
+              const LaunchCtx& lc)
+{
+    auto* kernel = linear_w4_kernel<NG, NT, D, HS>;
+    static std::mutex mu;
+    static int sms[64] = {};  // SMs of the device; asked for once, when the kernel's shared memory is raised
+    int dev = 0;
+    LS_CK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return LS_ERR_UNSUPPORTED;
+    int n_sm;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!sms[dev]) {
+            LS_CK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kW4SmemMax));
+            LS_CK(cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev));
+        }
+        n_sm = sms[dev];
+    }
+    const int n_tiles = (int)(((int64_t)N + 15) / 16), kb = w4_kblocks(K), lks = w4_split(n_tiles);
+    const int teams = kW4Warps >> lks, grid = (n_tiles + teams - 1) / teams;
+    const size_t smem = w4_part_bytes<NT>() + w4_ring_bytes<NG>(D) + (HS ? (size_t)M * w4_h_stride(kb) : 0);
+    LS_CK(launch(lc, kernel, dim3((unsigned)(grid < n_sm ? grid : n_sm)), dim3(kW4Warps * 32), smem, packed, h, M, N, K, kb,
+                 n_tiles, lks, out, residual));
+    return LS_OK;
+}
+
+template <int NG, int NT>
+int w4_launch_nt(const unsigned char* packed, const uint16_t* h, int M, int N, int K, float* out, int residual,
+                 const LaunchCtx& lc)
+{
+    const int64_t room = kW4SmemMax - w4_part_bytes<NT>() - (int64_t)M * w4_h_stride(w4_kblocks(K));
+    if (room >= w4_ring_bytes<NG>(6)) return w4_launch<NG, NT, 6, true>(packed, h, M, N, K, out, residual, lc);
+    if (room >= w4_ring_bytes<NG>(3)) return w4_launch<NG, NT, 3, true>(packed, h, M, N, K, out, residual, lc);
+    return w4_launch<NG, NT, 6, false>(packed, h, M, N, K, out, residual, lc);
+}
+
+template <int NG>
+int w4_launch_ng(const unsigned char* packed, const uint16_t* h, int M, int N, int K, float* out, int residual,
+                 const LaunchCtx& lc)
+{
+    return (M <= 8 ? w4_launch_nt<NG, 1> : w4_launch_nt<NG, 2>)(packed, h, M, N, K, out, residual, lc);
+}
+
+}  // namespace
+
+extern "C" {
+
 int ls_op_linear_w4(const void* packed, const void* h, int32_t M, int32_t N, int32_t K, int32_t group, float* out,
                     int32_t residual, void* stream)
 {
     if (!w4_shape_ok(N, K, group) || M < 1 || M > LS_MAX_ROWS || !aligned16(packed) || !aligned16(h) || !out ||
         ((uintptr_t)out & 3u))
         return LS_ERR_INVALID_ARG;
-    auto* kernel = M <= 8 ? (group == 32 ? linear_w4_kernel<4, 1> : group == 64 ? linear_w4_kernel<2, 1> : linear_w4_kernel<1, 1>)
-                          : (group == 32 ? linear_w4_kernel<4, 2> : group == 64 ? linear_w4_kernel<2, 2> : linear_w4_kernel<1, 2>);
-    LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, kernel, dim3((unsigned)((N + (int64_t)15) / 16)),
-                 dim3(kW4Warps * 32), 0, (const unsigned char*)packed, (const uint16_t*)h, M, N, K, w4_kblocks(K), out, residual));
-    return LS_OK;
+    const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
+    return (group == 32 ? w4_launch_ng<4> : group == 64 ? w4_launch_ng<2> : w4_launch_ng<1>)(
+        (const unsigned char*)packed, (const uint16_t*)h, M, N, K, out, residual, lc);
 }
 
 static int log2_page(int page_size)

@@ -62,9 +62,9 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
 {
     constexpr int NJ = HD / 32;   // groups of a row
     constexpr int CT = HD / 16;   // 16-channel tiles of O^T
-    extern __shared__ __align__(16) float sm[];
-    float* sO = sm;                                       // [4][NT * 8][HD]
-    float* sM = sm + kv4_o_floats<HD, NT>();              // [warps][NT * 8], then the CTA's max and sum
+    extern __shared__ __align__(16) float kv4_smem[];
+    float* sO = kv4_smem;                                       // [4][NT * 8][HD]
+    float* sM = kv4_smem + kv4_o_floats<HD, NT>();              // [warps][NT * 8], then the CTA's max and sum
     float* sML = sM + kKv4Warps * NT * 8;                 // [2][NT * 8]
     uint4* sQ = reinterpret_cast<uint4*>(sML + 2 * NT * 8);  // [NT][NJ][32 lanes]
     pdl_launch_dependents();

@@ -2,13 +2,31 @@
 // M <= 16 rows (LayerSkip Sec. 4.3: a draft pass has one row, a verify pass num_draft + 1).  Format and
 // block layout: ls_q4.cuh.
 #pragma once
+#include "ls_prefill.cuh"
 #include "ls_q4.cuh"
 
 namespace ls {
 
-constexpr int kW4Warps = 8;
-
-// D = A * B + C on one tile; with C a constant zero the first product of a group starts a new sum
+// contiguous bytes (a multiple of 16, both ends 16-byte aligned) to shared memory, announced on an mbarrier
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ uint2 lds8(uint32_t addr)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds4(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+    return v;
+}
+// D = A * B: the first product of a sum
 __device__ __forceinline__ void mma_bf16_16816_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                                    uint32_t b0, uint32_t b1)
 {
@@ -18,73 +36,187 @@ __device__ __forceinline__ void mma_bf16_16816_new(float (&d)[4], uint32_t a0, u
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
+constexpr int kW4Warps = 16;
+constexpr int kW4SmemMax = 227 * 1024;
 
-// One CTA per 16 weight rows; its warps take the 128-column blocks in turn.  The codes are the A operand
-// (exact small integers in bf16), the rows of h the B operand; a group's products are summed on the tensor
-// cores in fp32 and multiplied by the group's scale (per weight row: a lane holds rows g and g + 8) when
-// they join the running sum.  Which blocks a warp adds, and in which order the warps' sums are added,
-// depends on K only, so a row's result does not depend on how many rows share the pass.
+// shared memory: the warps' sums of a tile, then D blocks a warp, then (HS) the rows of h, each padded by 64 bytes
+// (two rows' 64-byte pieces then fall on different banks)
+template <int NT>
+__host__ __device__ constexpr int w4_part_bytes() { return kW4Warps * 32 * NT * 16; }
+template <int NG>
+__host__ __device__ constexpr int w4_ring_bytes(int D) { return kW4Warps * D * w4_block_bytes(NG); }
+__host__ __device__ constexpr int w4_h_stride(int kblocks) { return kblocks * kQ4Cols * 2 + 64; }
+
+// what a lane reads of a block: the codes of rows g and g + 8 (its 16-byte pieces) and the rows' scales
+template <int NG>
+struct W4Regs {
+    uint4 lo, hi;
+    uint32_t s_lo[(NG + 1) / 2], s_hi[(NG + 1) / 2];
+    __device__ __forceinline__ void load(uint32_t blk, int lane)  // of a block in shared memory
+    {
+        lo = lds16(blk + lane * 16);
+        hi = lds16(blk + kQ4CodeBytes / 2 + lane * 16);
+        const uint32_t sd = blk + kQ4CodeBytes + (lane >> 2) * NG * 2;
+        if (NG == 4) {
+            const uint2 x = lds8(sd), y = lds8(sd + 8 * NG * 2);
+            s_lo[0] = x.x, s_lo[(NG + 1) / 2 - 1] = x.y, s_hi[0] = y.x, s_hi[(NG + 1) / 2 - 1] = y.y;
+        } else if (NG == 2) {
+            s_lo[0] = lds4(sd), s_hi[0] = lds4(sd + 8 * NG * 2);
+        } else {
+            uint16_t x, y;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(sd));
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(sd + 8 * NG * 2));
+            s_lo[0] = x, s_hi[0] = y;
+        }
+    }
+    __device__ __forceinline__ static float scale(const uint32_t (&s)[(NG + 1) / 2], int i)
+    {
+        return i & 1 ? bf16hi(s[i / 2]) : bf16lo(s[i / 2]);
+    }
+};
+
+// acc (rows g, g + 8 x columns 2 t, 2 t + 1) += the block's values times the NT * 8 rows of h in b
 template <int NG, int NT>
-__global__ void __launch_bounds__(kW4Warps * 32)
-linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __restrict__ h, int M, int N, int K,
-                 int kblocks, float* __restrict__ out, int residual)
+__device__ __forceinline__ void w4_block_mma(const W4Regs<NG>& w, const uint4 (&b)[NT][4], float (&acc)[NT][4])
 {
-    __shared__ float part[kW4Warps][NT * 8][17];
-    pdl_launch_dependents();
-    pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const unsigned char* rows = packed + (long long)blockIdx.x * kblocks * w4_block_bytes(NG);
-    float acc[NT][4] = {};
-    for (int kb = warp; kb < kblocks; kb += kW4Warps) {
-        const unsigned char* blk = rows + (long long)kb * w4_block_bytes(NG);
-        const uint4 lo = ld_stream16(blk + lane * 16), hi = ld_stream16(blk + kQ4CodeBytes / 2 + lane * 16);
-        uint32_t s_lo[NG], s_hi[NG];
-        q4_row_scales<NG>(blk + kQ4CodeBytes + g * NG * 2, s_lo);
-        q4_row_scales<NG>(blk + kQ4CodeBytes + (g + 8) * NG * 2, s_hi);
-        const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
-        float c[NT][4];
+    const uint32_t wl[4] = {w.lo.x, w.lo.y, w.lo.z, w.lo.w}, wh[4] = {w.hi.x, w.hi.y, w.hi.z, w.hi.w};
+    float c[NT][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int k = kb * kQ4Cols + 32 * j + 8 * t;
-            uint32_t a[8];
+    for (int j = 0; j < 4; ++j) {
+        uint32_t a[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[2 * i] = q4_bf16x2(wl[j], i), a[2 * i + 1] = q4_bf16x2(wh[j], i);
+        for (int p = 0; p < 4; ++p) a[2 * p] = q4_bf16x2(wl[j], p), a[2 * p + 1] = q4_bf16x2(wh[j], p);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                uint4 b = make_uint4(0, 0, 0, 0);
-                if (nt * 8 + g < M && k < K) b = ld_reuse16(h + (long long)(nt * 8 + g) * K + k);
-                if (j % (4 / NG) == 0)
-                    mma_bf16_16816_new(c[nt], a[0], a[1], a[2], a[3], b.x, b.y);
-                else
-                    mma_bf16_16816(c[nt], a[0], a[1], a[2], a[3], b.x, b.y);
-                mma_bf16_16816(c[nt], a[4], a[5], a[6], a[7], b.z, b.w);
-                if ((j + 1) % (4 / NG) == 0) {
-                    const float s0 = bf16lo(s_lo[j * NG / 4]), s1 = bf16lo(s_hi[j * NG / 4]);
-                    acc[nt][0] = fmaf(s0, c[nt][0], acc[nt][0]);
-                    acc[nt][1] = fmaf(s0, c[nt][1], acc[nt][1]);
-                    acc[nt][2] = fmaf(s1, c[nt][2], acc[nt][2]);
-                    acc[nt][3] = fmaf(s1, c[nt][3], acc[nt][3]);
-                }
+        for (int nt = 0; nt < NT; ++nt) {
+            if (j % (4 / NG) == 0)
+                mma_bf16_16816_new(c[nt], a[0], a[1], a[2], a[3], b[nt][j].x, b[nt][j].y);
+            else
+                mma_bf16_16816(c[nt], a[0], a[1], a[2], a[3], b[nt][j].x, b[nt][j].y);
+            mma_bf16_16816(c[nt], a[4], a[5], a[6], a[7], b[nt][j].z, b[nt][j].w);
+            if ((j + 1) % (4 / NG) == 0) {
+                const float s0 = W4Regs<NG>::scale(w.s_lo, j * NG / 4), s1 = W4Regs<NG>::scale(w.s_hi, j * NG / 4);
+                acc[nt][0] = fmaf(s0, c[nt][0], acc[nt][0]);
+                acc[nt][1] = fmaf(s0, c[nt][1], acc[nt][1]);
+                acc[nt][2] = fmaf(s1, c[nt][2], acc[nt][2]);
+                acc[nt][3] = fmaf(s1, c[nt][3], acc[nt][3]);
             }
         }
     }
+}
+
+// One CTA per SM; its 16 warps form teams of 2^lks, and a team takes every (teams of the grid)-th tile of 16
+// rows.  Of a tile's blocks each warp of the team has a fixed share, consecutive along K, and keeps the
+// next D of its sequence of blocks (which runs on across tiles) in flight in a ring of its own; the team
+// meets once per tile, to add its sums up.  HS: h is copied to shared memory once (columns beyond K as
+// zeros); otherwise, for h larger than that, it comes through L1.
+// The codes are the A operand of mma.sync (exact small integers in bf16), the rows of h the B operand; a
+// group's products are summed in fp32 by the tensor cores and multiplied by the group's scale (a lane holds
+// rows g and g + 8 of a tile) when they join the running sum.  Which blocks a warp adds, and in which order the
+// warps' sums are added, depends on N and K only: a row's result does not depend on how many rows share
+// the pass.
+template <int NG, int NT, int D, bool HS>
+__global__ void __launch_bounds__(kW4Warps * 32, 1)
+linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __restrict__ h, int M, int N, int K,
+                 int kblocks, int n_tiles, int lks, float* __restrict__ out, int residual)
+{
+    constexpr int BB = w4_block_bytes(NG);
+    extern __shared__ __align__(128) unsigned char w4_smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int KS = 1 << lks, ks = warp & (KS - 1), team = warp >> lks;
+    float4* part = reinterpret_cast<float4*>(w4_smem) + (team << lks) * 32 * NT;  // [warp of the team][NT][lane]
+    const uint32_t ring = smem_u32(w4_smem) + w4_part_bytes<NT>() + warp * D * BB;
+    pdl_launch_dependents();
+
+    const int kb0 = kblocks * ks >> lks, nkb = (kblocks * (ks + 1) >> lks) - kb0;
+    const int tile0 = team * gridDim.x + blockIdx.x, tile_step = (kW4Warps >> lks) * gridDim.x;
+    // the sequence of blocks, D ahead of their use: a lane copies its own two pieces, lanes below 2 NG the scales
+    int in_tile = nkb ? tile0 : n_tiles, in_left = nkb;
+    uint32_t in_at = ring + lane * 16;
+    const unsigned char* src = packed + ((long long)tile0 * kblocks + kb0) * BB + lane * 16;
+    const long long jump = ((long long)tile_step * kblocks - nkb) * BB;
+    auto fetch = [&]() {
+        if (in_tile < n_tiles) {
+            cp_async16_cg(in_at, src, 16);
+            cp_async16_cg(in_at + kQ4CodeBytes / 2, src + kQ4CodeBytes / 2, 16);
+            if (lane < 2 * NG) cp_async16_cg(in_at + kQ4CodeBytes, src + kQ4CodeBytes, 16);
+            src += BB;
+            if (--in_left == 0) in_left = nkb, in_tile += tile_step, src += jump;
+            in_at += BB;
+            if (in_at == ring + D * BB + lane * 16) in_at = ring + lane * 16;
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < D - 1; ++i) fetch();  // weights: no kernel before this one writes them
+    pdl_wait();
+
+    const uint32_t hs = smem_u32(w4_smem) + w4_part_bytes<NT>() + w4_ring_bytes<NG>(D);
+    const int stride = w4_h_stride(kblocks);
+    if (HS) {
+        for (int i = threadIdx.x; i < kblocks * 16; i += kW4Warps * 32) {
+            const int bytes = 8 * i < K ? 16 : 0;
+            const uint16_t* s = h + (bytes ? 8 * i : 0);
+            uint32_t d = hs + i * 16;
+            for (int m = 0; m < M; ++m, s += K, d += stride) cp_async16_ca(d, s, bytes);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        __syncthreads();
+    }
+    // B operand of a block: rows nt * 8 + g of h, columns 32 j + 8 t.  Rows beyond M repeat the last one (their
+    // columns of the product are not stored).
+    uint32_t hoff[NT];
+    const uint16_t* hrow[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        part[warp][nt * 8 + 2 * t][g] = acc[nt][0];
-        part[warp][nt * 8 + 2 * t + 1][g] = acc[nt][1];
-        part[warp][nt * 8 + 2 * t][g + 8] = acc[nt][2];
-        part[warp][nt * 8 + 2 * t + 1][g + 8] = acc[nt][3];
+        const int m = min(nt * 8 + g, M - 1);
+        hoff[nt] = hs + m * stride + t * 16;
+        hrow[nt] = h + (long long)m * K + 8 * t;
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < NT * 8 * 16; i += kW4Warps * 32) {
-        const int m = i / 16, r = i % 16;
-        const long long n = (long long)blockIdx.x * kQ4Rows + r;
-        if (m >= M || n >= N) continue;
-        float s = 0.f;
+
+    uint32_t at = ring;
+    for (int tile = tile0; tile < n_tiles; tile += tile_step) {
+        float acc[NT][4] = {};
+        for (int kb = kb0; kb < kb0 + nkb; ++kb) {
+            fetch();
+            cp_async_wait<D - 1>();  // the oldest of the D blocks in flight
+            __syncwarp();
+            W4Regs<NG> w;
+            w.load(at, lane);
+            at += BB;
+            if (at == ring + D * BB) at = ring;
+            uint4 b[NT][4];
+            if (HS) {
 #pragma unroll
-        for (int w = 0; w < kW4Warps; ++w) s += part[w][m][r];
-        float* o = out + (long long)m * N + n;
-        *o = residual ? *o + s : s;
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) b[nt][j] = lds16(hoff[nt] + kb * 256 + j * 64);
+            } else {
+                const bool whole = (kb + 1) * kQ4Cols <= K;  // only the last block has columns beyond K
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        b[nt][j] = whole || kb * kQ4Cols + 32 * j + 8 * t < K ? ld_reuse16(hrow[nt] + kb * kQ4Cols + 32 * j)
+                                                                              : make_uint4(0, 0, 0, 0);
+            }
+            w4_block_mma<NG, NT>(w, b, acc);
+            __syncwarp();  // every lane has read the block before the ring comes round to it
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) part[(ks * NT + nt) * 32 + lane] = make_float4(acc[nt][0], acc[nt][1], acc[nt][2], acc[nt][3]);
+        asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(KS * 32) : "memory");
+        const float* sums = reinterpret_cast<const float*>(part);
+        for (int x = ks * 32 + lane; x < 128 * NT; x += KS * 32) {
+            const int e = x & 3, l = x >> 2 & 31, m = (x >> 7) * 8 + 2 * (l & 3) + (e & 1);
+            const int n = tile * kQ4Rows + (l >> 2) + 8 * (e >> 1);
+            if (m >= M || n >= N) continue;
+            float s = 0.f;
+            for (int v = 0; v < KS; ++v) s += sums[v * 128 * NT + x];
+            float* o = out + (long long)m * N + n;
+            *o = residual ? *o + s : s;
+        }
+        asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(KS * 32) : "memory");  // the sums are read
     }
 }
 
