@@ -422,12 +422,18 @@ int ls_op_expand_kv4(const void *pages_dev, int32_t n_pages, int32_t n_seq, int3
  * sequence b sees positions 0..pos0_dev[b] + m; a row that sees none, or is refused, is all zeros.
  * q, out bf16 [n_seq][M][Hq * hd], M <= LS_MAX_ROWS, Hq / Hkv <= 8.  Slots beyond a sequence's last row
  * are never used, whatever bits they hold; a row whose table entries are refused leaves out
- * those positions.  No scratch memory.  A row's result depends on its position, n_seq, Hkv and
- * max_seq (which fix how the positions are dealt to CTAs), never on M or on the other rows. */
+ * those positions.  Few heads over a long cache leave SMs idle unless their positions are split
+ * over more CTAs than a cluster holds, which needs scratch_dev (16-byte aligned,
+ * ls_op_attention_kv4_scratch_bytes() bytes, of any content, used by one call at a time); with
+ * NULL, or where that function returns 0 (no split is worth it), none is used.  A row's result
+ * depends on its position, n_seq, Hkv, max_seq and whether there is scratch (which fix how the
+ * positions are dealt to CTAs), never on M or on the other rows. */
+size_t ls_op_attention_kv4_scratch_bytes(int32_t n_seq, int32_t M, int32_t Hq, int32_t Hkv, int32_t hd,
+                                         int32_t max_seq);
 int ls_op_attention_kv4(const void *q_bf16_dev, int32_t n_seq, int32_t M, const int32_t *pos0_dev, int32_t Hq,
                         int32_t Hkv, int32_t hd, int32_t page_size, const int32_t *page_table_dev,
                         int32_t table_stride, int32_t max_seq, const void *pages_dev, int32_t n_pages,
-                        void *out_bf16_dev, int32_t *status_dev, void *cuda_stream);
+                        void *out_bf16_dev, void *scratch_dev, int32_t *status_dev, void *cuda_stream);
 
 /* match + crop of Appendix A.4 on device arrays: n = number of leading i < d with
  * draft[i] == verified[i]; appends draft[0..n-1], verified[n] to out_ids (truncated at

@@ -30,6 +30,7 @@ EXPORTS = (
     "ls_op_lm_head_argmax_static", "ls_op_rope_append", "ls_op_qkv_rope_append", "ls_op_attention", "ls_op_accept",
     "ls_op_gemm", "ls_op_prefill_attention", "ls_op_chain", "ls_op_w4_bytes", "ls_op_quantize_w4", "ls_op_expand_w4",
     "ls_op_linear_w4", "ls_op_kv4_page_bytes", "ls_op_append_kv4", "ls_op_expand_kv4", "ls_op_attention_kv4",
+    "ls_op_attention_kv4_scratch_bytes",
 )
 
 
@@ -124,7 +125,8 @@ def lib():
             "ls_op_kv4_page_bytes": (C.c_size_t, [i32, i32, i32]),
             "ls_op_append_kv4": (C.c_int, [vp, vp, i64, i64, i64, i32, i32, vp, i32, i32, i32, vp, i32, i32, vp, i32, vp, vp]),
             "ls_op_expand_kv4": (C.c_int, [vp, i32, i32, i32, vp, i32, i32, i32, vp, i32, i32, vp, vp, vp, i32, vp, vp]),
-            "ls_op_attention_kv4": (C.c_int, [vp, i32, i32, vp, i32, i32, i32, i32, vp, i32, i32, vp, i32, vp, vp, vp]),
+            "ls_op_attention_kv4": (C.c_int, [vp, i32, i32, vp, i32, i32, i32, i32, vp, i32, i32, vp, i32, vp, vp, vp, vp]),
+            "ls_op_attention_kv4_scratch_bytes": (C.c_size_t, [i32, i32, i32, i32, i32, i32]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -509,15 +511,28 @@ def ls_op_expand_kv4(pages, pos0, M, page_size, table, max_seq, out_table, k_pag
                                _arg(status, _INT, "status"), _stream()), "ls_op_expand_kv4")
 
 
-def ls_op_attention_kv4(q, pos0, Hkv, hd, page_size, table, max_seq, pages, out, status=None):
-    """q, out bf16 [n_seq, M, Hq * hd]"""
+def ls_op_attention_kv4_scratch_bytes(n_seq, M, Hq, Hkv, hd, max_seq):
+    return lib().ls_op_attention_kv4_scratch_bytes(n_seq, M, Hq, Hkv, hd, max_seq)
+
+
+def ls_op_attention_kv4(q, pos0, Hkv, hd, page_size, table, max_seq, pages, out, status=None, scratch=None):
+    """q, out bf16 [n_seq, M, Hq * hd].  scratch: uint8, ls_op_attention_kv4_scratch_bytes of them; None allocates them
+    where the call can use any (torch's allocator hands them out and takes them back in stream order)."""
     n_seq, M, width = q.shape
     n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
     if width % hd or out.shape != q.shape:
         _bad("ls_op_attention_kv4: q and out")
-    _ck(lib().ls_op_attention_kv4(_arg(q, _BF16, "q"), n_seq, M, _arg(pos0, _INT, "pos0"), width // hd, Hkv, hd, page_size,
+    Hq = width // hd
+    need = ls_op_attention_kv4_scratch_bytes(n_seq, M, Hq, Hkv, hd, max_seq)
+    if scratch is None and need:
+        import torch
+        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+    elif scratch is not None and scratch.numel() < need:
+        raise LsError(LS_ERR_CAPACITY, "ls_op_attention_kv4: scratch")
+    _ck(lib().ls_op_attention_kv4(_arg(q, _BF16, "q"), n_seq, M, _arg(pos0, _INT, "pos0"), Hq, Hkv, hd, page_size,
                                   _arg(table, _INT, "page table"), entries, max_seq, _arg(pages, _U8, "pages"), n_pages,
-                                  _arg(out, _BF16, "out"), _arg(status, _INT, "status"), _stream()), "ls_op_attention_kv4")
+                                  _arg(out, _BF16, "out"), _arg(scratch, _U8, "scratch"), _arg(status, _INT, "status"),
+                                  _stream()), "ls_op_attention_kv4")
 
 
 def ls_op_accept(draft, verified, d, state, out_ids, accepted):

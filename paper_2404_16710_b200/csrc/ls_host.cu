@@ -2007,22 +2007,33 @@ int ls_op_expand_kv4(const void* pages, int32_t n_pages, int32_t n_seq, int32_t 
 
 namespace {
 
-// CTAs a (sequence, KV head) is spread over: enough for about two CTAs per SM, no more than the cache has
-// rounds of chunks for, at most 16 (the largest cluster).  Never a function of the rows of the call.
-int kv4_cluster(int n_seq, int Hkv, int max_seq)
+// How the positions of a (sequence, KV head) are spread: splits x S CTAs, enough for about two CTAs per SM, no more
+// than the cache has rounds of chunks for.  Never a function of the rows of the call.
+struct Kv4Plan {
+    int S, splits;
+};
+Kv4Plan kv4_plan(int n_seq, int Hkv, int max_seq, bool may_split)
 {
-    int S = 1;
-    while (S < 16 && (int64_t)S * Hkv * n_seq < 256 && S * kKv4Warps * kKv4Chunk < max_seq) S *= 2;
-    return S;
+    Kv4Plan p = {1, 1};
+    const int64_t pairs = (int64_t)n_seq * Hkv;
+    const int round = kKv4Warps * kKv4Chunk;
+    while (p.S < 8 && p.S * pairs < 256 && p.S * round < max_seq) p.S *= 2;
+    if (may_split)
+        while (p.splits < 64 && p.splits * p.S * pairs < 256 && 4 * p.splits * p.S * round < max_seq) p.splits *= 2;
+    if (getenv("LS_KV4_S")) p.S = atoi(getenv("LS_KV4_S"));
+    if (getenv("LS_KV4_C") && may_split) p.splits = atoi(getenv("LS_KV4_C"));
+    return p;
 }
+int kv4_query_tile(int Q) { return Q <= 8 ? 1 : 2; }  // tiles of 8 queries a CTA takes
+int kv4_rows(int Q, int Hkv) { return (Q + 8 * kv4_query_tile(Q) - 1) / (8 * kv4_query_tile(Q)) * Hkv; }
 
 template <int HD, int NT>
-int kv4_attn_launch(int S, int qtiles, int n_seq, const uint16_t* q, int M, int G, const int32_t* pos0,
-                           const Kv4Cache& c, const unsigned char* pages, uint16_t* out, int32_t* status, const LaunchCtx& lc)
+int kv4_attn_launch(const Kv4Plan& plan, int n_seq, const uint16_t* q, int M, int G, const int32_t* pos0, const Kv4Cache& c,
+                    const unsigned char* pages, uint16_t* out, float* scratch, int32_t* status, const LaunchCtx& lc)
 {
-    constexpr size_t smem = kv4_smem_bytes<HD, NT>();
-    // once per device: shared memory beyond 48 KB, clusters of 16
-    static std::mutex mu;
+    auto* kernel = attention_kv4_kernel<HD, NT>;
+    constexpr int smem = Kv4Smem<HD, NT>::kBytes;
+    static std::mutex mu;  // once per device: shared memory beyond 48 KB
     static bool ready[64] = {};
     int dev = 0;
     LS_CK(cudaGetDevice(&dev));
@@ -2030,19 +2041,19 @@ int kv4_attn_launch(int S, int qtiles, int n_seq, const uint16_t* q, int M, int 
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!ready[dev]) {
-            LS_CK(cudaFuncSetAttribute(attention_kv4_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-            LS_CK(cudaFuncSetAttribute(attention_kv4_kernel<HD, NT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+            LS_CK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
             ready[dev] = true;
         }
     }
+    const int rows = kv4_rows(M * G, c.Hkv);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(S, c.Hkv * qtiles, n_seq);
-    cfg.blockDim = dim3(kKv4Threads);
+    cfg.gridDim = dim3(plan.splits * plan.S, rows, n_seq);
+    cfg.blockDim = dim3(kKv4Warps * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = lc.st;
     cudaLaunchAttribute at[3];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = S;
+    at[0].val.clusterDim.x = plan.S;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
     at[1].id = cudaLaunchAttributeClusterSchedulingPolicyPreference;  // several CTAs of a cluster per SM: see attn_launch_t
@@ -2051,33 +2062,49 @@ int kv4_attn_launch(int S, int qtiles, int n_seq, const uint16_t* q, int M, int 
     at[2].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = lc.pdl ? 3 : 2;
-    LS_CK(cudaLaunchKernelEx(&cfg, attention_kv4_kernel<HD, NT>, q, M, G, pos0, c, pages, out, status));
+    LS_CK(cudaLaunchKernelEx(&cfg, kernel, q, M, G, pos0, c, pages, plan.S, out, scratch, status));
+    if (plan.splits > 1)  // may move in while the splits finish; it waits for them before it reads
+        LS_CK(launch(LaunchCtx{lc.st, true}, combine_kv4_kernel<HD>, dim3(M, G * c.Hkv, n_seq), dim3(HD / 2), 0, scratch, G, pos0,
+                     c.max_seq, NT, c.Hkv, rows, plan.splits, out));
     return LS_OK;
 }
 
 template <int HD>
-int kv4_attn_launch_hd(int n_seq, const uint16_t* q, int M, int G, const int32_t* pos0, const Kv4Cache& c,
-                              const unsigned char* pages, uint16_t* out, int32_t* status, const LaunchCtx& lc)
+int kv4_attn_launch_hd(const Kv4Plan& plan, int n_seq, const uint16_t* q, int M, int G, const int32_t* pos0, const Kv4Cache& c,
+                       const unsigned char* pages, uint16_t* out, float* scratch, int32_t* status, const LaunchCtx& lc)
 {
-    const int S = kv4_cluster(n_seq, c.Hkv, c.max_seq), Q = M * G;  // queries of a KV head, in tiles of 8
-    if (Q <= 8) return kv4_attn_launch<HD, 1>(S, 1, n_seq, q, M, G, pos0, c, pages, out, status, lc);
-    return kv4_attn_launch<HD, 2>(S, (Q + 15) / 16, n_seq, q, M, G, pos0, c, pages, out, status, lc);
+    return (kv4_query_tile(M * G) == 1 ? kv4_attn_launch<HD, 1> : kv4_attn_launch<HD, 2>)(plan, n_seq, q, M, G, pos0, c, pages, out,
+                                                                                   scratch, status, lc);
 }
 
 }  // namespace
 
 extern "C" {
 
+size_t ls_op_attention_kv4_scratch_bytes(int32_t n_seq, int32_t M, int32_t Hq, int32_t Hkv, int32_t hd, int32_t max_seq)
+{
+    if (n_seq < 1 || n_seq > 65535 || M < 1 || M > LS_MAX_ROWS || Hkv < 1 || Hkv > 4095 || Hq < 1 || Hq % Hkv || Hq / Hkv > 8 ||
+        (hd != 64 && hd != 128) || max_seq < 1 || max_seq > LS_KV4_MAX_SEQ)
+        return 0;
+    const Kv4Plan p = kv4_plan(n_seq, Hkv, max_seq, true);
+    const int Q = M * (Hq / Hkv);
+    if (p.splits == 1) return 0;
+    return sizeof(float) * (size_t)n_seq * kv4_rows(Q, Hkv) * p.splits * kv4_query_tile(Q) * 8 * (hd + 2);
+}
+
 int ls_op_attention_kv4(const void* q, int32_t n_seq, int32_t M, const int32_t* pos0, int32_t Hq, int32_t Hkv, int32_t hd,
                         int32_t page_size, const int32_t* table, int32_t table_stride, int32_t max_seq, const void* pages,
-                        int32_t n_pages, void* out, int32_t* status, void* stream)
+                        int32_t n_pages, void* out, void* scratch, int32_t* status, void* stream)
 {
     Kv4Cache c;
     LS_TRY(kv4_check(n_seq, M, pos0, Hkv, hd, page_size, table, table_stride, max_seq, pages, n_pages, &c));
-    if (M > LS_MAX_ROWS || Hq < 1 || Hq % Hkv || Hq / Hkv > 8 || !aligned16(q) || !aligned16(out)) return LS_ERR_INVALID_ARG;
+    if (M > LS_MAX_ROWS || Hq < 1 || Hq % Hkv || Hq / Hkv > 8 || !aligned16(q) || !aligned16(out) ||
+        (scratch && ((uintptr_t)scratch & 15u)))
+        return LS_ERR_INVALID_ARG;
     const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
     return (hd == 128 ? kv4_attn_launch_hd<128> : kv4_attn_launch_hd<64>)(
-        n_seq, (const uint16_t*)q, M, Hq / Hkv, pos0, c, (const unsigned char*)pages, (uint16_t*)out, status, lc);
+        kv4_plan(n_seq, Hkv, max_seq, scratch != nullptr), n_seq, (const uint16_t*)q, M, Hq / Hkv, pos0, c,
+        (const unsigned char*)pages, (uint16_t*)out, (float*)scratch, status, lc);
 }
 
 int ls_op_accept(const int32_t* draft, const int32_t* verified, int32_t d, int32_t* state, int32_t* out_ids,

@@ -4,17 +4,29 @@
 //   o[m] = sum_i p_i v_i / sum_i p_i,  p_i = exp(q[m] . k_i / sqrt(hd)) for the positions i <= pos0 + m
 //
 // Tokens are the 16-row operand of mma.sync in both products, queries (row, head of the KV group) the
-// 8-column one: S^T = K Q^T with K's codes as A; O^T = V^T P^T with V^T's values as A -- a tile stores V so
-// that a lane finds two neighbouring tokens of a channel in the same nibble of two words, so the
-// transposition costs one byte permutation.
+// 8-column one: S^T = K Q^T and O^T = V^T P^T.  At 4 bits a value the kernel is bound by the instructions
+// that turn nibbles into operands, so both products run in f16, whose formats make those few:
+// * K: a nibble u = c + 8 left where it is, all other bits cleared, IS an f16 number, u 2^-24 (bits 0..3) or
+//   u 2^-20 (bits 4..7), a denormal, which the tensor cores take exactly.  No offset, no conversion: 5
+//   instructions for 8 codes.  The queries' columns that meet the second kind are scaled by 2^-4, and the
+//   sum of a scale group starts at -8 sum q instead of 0.  Queries are scaled by powers of two of their own
+//   so that the largest component is in [2^14, 2^15): what f16 then cannot hold is 2^-39 of it.
+// * V: a nibble moved to bits 4..7 or-ed to 1024 is 1024 + 16 u, and one multiply-add makes c s of it:
+//   (1024 + 16 u) (s / 16) - 72 s.  A scale has 5 significant bits, so every step is exact, for scales down to 2^-25
+//   of the largest one the warp has met (the power of two it is divided by is kept beside O).
+// * p <= 1 is rounded to f16's 11 bits (2^-12; 2^-25 absolute below 2^-14), well below the rounding of a
+//   bf16 result.  Scores, maxima, sums and O are fp32.
 #pragma once
+#include <cuda_fp16.h>
+
+#include "ls_attention.cuh"
 #include "ls_w4.cuh"
 
 namespace ls {
 
+constexpr int kKv4Chunk = 32;   // positions a warp takes at a time: two tiles
 constexpr int kKv4Warps = 8;
-constexpr int kKv4Threads = kKv4Warps * 32;
-constexpr int kKv4Chunk = 32;  // positions a warp takes at a time: two tiles
+constexpr int kKv4Stages = 2;   // chunks of a warp's ring
 
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
 {
@@ -28,11 +40,15 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr)
+// 2^e, 0 below the denormals
+__device__ __forceinline__ float exp2_int(int e)
 {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
+    if (e >= -126) return __uint_as_float((uint32_t)(min(e, 127) + 127) << 23);
+    return e >= -149 ? __uint_as_float(1u << (e + 149)) : 0.f;
+}
+__device__ __forceinline__ void st_cluster_f4(uint32_t addr, float4 v)
+{
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 __device__ __forceinline__ uint32_t map_cluster(uint32_t addr, int rank)
 {
@@ -40,50 +56,121 @@ __device__ __forceinline__ uint32_t map_cluster(uint32_t addr, int rank)
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-
-// shared memory, in floats: the halves of the warps' outputs while they are added up, then the CTA's (O, m, l)
-template <int HD, int NT>
-__host__ __device__ constexpr int kv4_o_floats() { return (kKv4Warps / 2) * NT * 8 * HD; }
-template <int HD, int NT>
-constexpr size_t kv4_smem_bytes()
+// D (fp32, 16x8) = A (f16, 16x16) * B (f16, 16x8) + C
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                              uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3)
 {
-    return sizeof(float) * (kv4_o_floats<HD, NT>() + (kKv4Warps + 2) * NT * 8) + NT * 8 * HD * 2;
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+        "{%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+// c s of nibble i of the two halves of w, as f16: s16 = s / 16, s72 = -72 s
+__device__ __forceinline__ uint32_t q4_scaled_f16x2(uint32_t w, int i, uint32_t s16, uint32_t s72)
+{
+    uint32_t r;
+    asm("lop3.b32 %0, %1, 0x00f000f0, 0x64006400, 0xea;" : "=r"(r) : "r"(i == 0 ? w << 4 : w >> (4 * i - 4)));
+    return fma_f16x2(r, s16, s72);
 }
 
-// grid (S, Hkv * query tiles, n_seq) in clusters of S CTAs.  The warps of a cluster take the 32-position
-// chunks of the cache in turn by absolute position, each with a running (max, sum, O) of its own; the warps'
-// results are added up in a fixed order, then the CTAs' through distributed shared memory.  A row's result
-// depends on its position and on S, not on M or the other rows.
+// shared memory of a CTA: rings (later each warp's O in its own), queries, their offsets and factors, the
+// warps' statistics, and what the CTAs of the cluster send one another
+constexpr int kKv4MaxCluster = 16;
 template <int HD, int NT>
-__global__ void __launch_bounds__(kKv4Threads)
-attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t* __restrict__ pos0_dev,
-                     const Kv4Cache cache, const unsigned char* __restrict__ pages, uint16_t* __restrict__ out,
-                     int32_t* status)
+struct Kv4Smem {
+    static constexpr int W = kKv4Warps;
+    static constexpr int kTile = kv4_tile_bytes(HD);
+    static constexpr int kWarpRing = kKv4Stages * 2 * kTile;
+    static constexpr int kItems = NT * HD / 16 * 32;           // float4 pieces of O: [NT][HD / 16][lane]
+    static constexpr int kRing = W * kWarpRing;
+    static constexpr int kQ = NT * HD / 32 * 32 * 16;          // [NT][group][lane] 16 bytes
+    static constexpr int kInbox = kItems * 16;                 // [CTA][its share of the pieces]
+    static constexpr int kInit = NT * 8 * (HD / 32) * 4;       // -8 sum q [query][group]
+    static constexpr int kFactor = NT * 8 * 4;                 // 2^e [query]
+    static constexpr int kStat = W * NT * 8 * 8 + W * 4;       // (max, sum) of the warps, exponents of their O
+    static constexpr int kInStat = kKv4MaxCluster * NT * 8 * 8;  // (max, sum) of the CTAs
+    static constexpr int kBytes = kRing + kQ + kInbox + kInit + kFactor + kStat + kInStat;
+    static_assert(kItems / (NT * 32) * 512 * NT <= kWarpRing, "a warp's O fits its ring");
+};
+
+// where the results of split s of (sequence b, block row y of the grid) stand in the scratch memory
+__device__ __forceinline__ long long kv4_partial(int b, int rows, int y, int splits, int s)
 {
+    return ((long long)b * rows + y) * splits + s;
+}
+// log2(e) / sqrt(hd), and the 2^10 that the operands' units leave (see the kernel)
+__device__ __forceinline__ float kv4_unit(int hd) { return 1024.f * 1.4426950408889634f / sqrtf((float)hd); }
+
+// grid (splits * S, Hkv * query tiles, n_seq) in clusters of S CTAs.  The warps of a (sequence, KV head) take
+// the 32-position chunks of the cache in turn by absolute position, each through a cp.async ring of its own and
+// with a running (max, sum, O) of its own.  At the end every thread adds up, in warp order, the pieces of O it is
+// given and sends them to the CTA of the cluster that finishes them, through distributed shared memory: one
+// CTA barrier, one cluster barrier.  With one split that is the result; clusters hold at most 16 CTAs, so that
+// few heads over a long cache take several splits, which a second kernel joins.  A row's result depends on its
+// position and on the grid, not on M or the other rows: what other rows add to the tokens a CTA looks at has weight 0, and all factors that are shared
+// are powers of two.
+template <int HD, int NT>
+__global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1)
+attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t* __restrict__ pos0_dev,
+                     const Kv4Cache cache, const unsigned char* __restrict__ pages, int S, uint16_t* __restrict__ out,
+                     float* __restrict__ scratch, int32_t* status)
+{
+    using SM = Kv4Smem<HD, NT>;
+    constexpr int W = kKv4Warps;
     constexpr int NJ = HD / 32;   // groups of a row
     constexpr int CT = HD / 16;   // 16-channel tiles of O^T
-    extern __shared__ __align__(16) float kv4_smem[];
-    float* sO = kv4_smem;                                       // [4][NT * 8][HD]
-    float* sM = kv4_smem + kv4_o_floats<HD, NT>();              // [warps][NT * 8], then the CTA's max and sum
-    float* sML = sM + kKv4Warps * NT * 8;                 // [2][NT * 8]
-    uint4* sQ = reinterpret_cast<uint4*>(sML + 2 * NT * 8);  // [NT][NJ][32 lanes]
+    constexpr int TB = SM::kTile, D = kKv4Stages;
+    extern __shared__ __align__(128) unsigned char kv4_smem[];
+    unsigned char* at = kv4_smem + SM::kRing;
+    uint4* sQ = reinterpret_cast<uint4*>(at);
+    float4* sIn = reinterpret_cast<float4*>(at += SM::kQ);
+    float* sInit = reinterpret_cast<float*>(at += SM::kInbox);
+    float* sF = reinterpret_cast<float*>(at += SM::kInit);
+    float2* sStat = reinterpret_cast<float2*>(at += SM::kFactor);   // [W][NT * 8]
+    int* sExp = reinterpret_cast<int*>(sStat + W * NT * 8);         // [W]
+    float2* sInStat = reinterpret_cast<float2*>(at += SM::kStat);   // [CTA][NT * 8]
     pdl_launch_dependents();
     pdl_wait();
-    const int S = gridDim.x, rank = blockIdx.x, b = blockIdx.z;
+    const int splits = gridDim.x / S, split = blockIdx.x / S, rank = blockIdx.x % S, b = blockIdx.z;
+    if (S > 1) cluster_arrive_relaxed();  // this CTA is there
     const int head = blockIdx.y % cache.Hkv, q0 = blockIdx.y / cache.Hkv * (NT * 8);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int Q = M * G, Hq = cache.Hkv * G, pos0 = pos0_dev[b];
+    const int Q = M * G, Hq = cache.Hkv * G;
 
-    for (int i = threadIdx.x; i < NT * NJ * 32; i += kKv4Threads) {
-        const int l = i % 32, j = i / 32 % NJ, qi = q0 + i / 32 / NJ * 8 + (l >> 2);
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (qi < Q)
-            v = *reinterpret_cast<const uint4*>(q + (((long long)b * M + qi / G) * Hq + head * G + qi % G) * HD + 32 * j +
-                                                8 * (l & 3));
-        sQ[i] = v;
-    }
-    // last visible position of this lane's two queries of each tile, and of all queries of the CTA
-    int lim[NT][2], top = -1;
+    // page-table entries of this warp's next chunk (a chunk lies in one page, unless pages are of 16), read before
+    // anything says whether it is needed: the positions below max_seq have entries
+    const int step = gridDim.x * W * kKv4Chunk, base0 = (blockIdx.x * W + warp) * kKv4Chunk;
+    const int32_t* table = cache.table + (long long)b * cache.table_stride;
+    int next_page[2];
+    auto look_up = [&](int base) {
+        next_page[0] = base < cache.max_seq ? table[base >> cache.page_shift] : 0;
+        next_page[1] = next_page[0];
+        if (cache.page_shift == 4) next_page[1] = base + 16 < cache.max_seq ? table[(base + 16) >> 4] : 0;
+    };
+    look_up(base0);
+    const int pos0 = pos0_dev[b];
+
+    // last position that this lane's two queries of each 8 see, and over the CTA's queries the last and the first of those
+    int lim[NT][2], top = -1, low = 0x7fffffff;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -91,137 +178,226 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             const int qi = q0 + nt * 8 + 2 * t + e;
             lim[nt][e] = qi < Q ? kv4_position(pos0, qi / G, cache.max_seq, status) : -1;
             top = max(top, lim[nt][e]);
+            if (qi < Q) low = min(low, lim[nt][e]);
         }
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    low = min(low, __shfl_xor_sync(0xffffffffu, low, 1));
+    low = min(low, __shfl_xor_sync(0xffffffffu, low, 2));
+
+    // the ring: chunks of this warp, D - 1 ahead of their use.  ok_bits: which tiles of the chunks in flight exist
+    const uint32_t ring = smem_u32(kv4_smem) + warp * D * 2 * TB;
+    int in_base = base0, in_stage = 0, in_count = 0;
+    uint32_t ok_bits = 0;
+    const unsigned char* mine = pages + ((long long)head << (cache.page_shift - 4)) * TB + lane * 16;
+    const uint32_t page_bytes = (uint32_t)(cache.Hkv << (cache.page_shift - 4)) * TB, tile_mask = (1u << (cache.page_shift - 4)) - 1;
+    auto fetch = [&]() {
+        if (in_base <= top) {
+            const uint32_t dst = ring + in_stage * 2 * TB + lane * 16;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int p = in_base + 16 * u;
+                if (p > top) continue;
+                if ((unsigned)next_page[u] >= (unsigned)cache.n_pages) {
+                    if (status) *status = DEV_BAD_PAGE;
+                    continue;
+                }
+                ok_bits |= 1u << (2 * in_count + u);
+                const unsigned char* src = mine + (unsigned long long)page_bytes * (uint32_t)next_page[u] + ((uint32_t)(p >> 4) & tile_mask) * TB;
+#pragma unroll
+                for (int i = 0; i < TB / 512; ++i) cp_async16_cg(dst + u * TB + 512 * i, src + 512 * i, 16);
+                if (lane < TB % 512 / 16) cp_async16_cg(dst + u * TB + TB / 512 * 512, src + TB / 512 * 512, 16);
+            }
+            in_base += step;
+            ++in_count;
+            if (++in_stage == D) in_stage = 0;
+            look_up(in_base);
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < D - 1; ++i) fetch();
+
+    // Queries as B operands: lane 4 g + t of group j holds channels 32 j + 8 t .. + 7 of query g, columns 2, 3, 6 and 7
+    // of the eight times 2^-4.  A query is shared by the NJ x 4 threads that make it.
+    constexpr int PER = NJ * 4;
+    for (int i = threadIdx.x; i < NT * 8 * PER; i += W * 32) {
+        const int qq = i / PER, j = i % PER / 4, tt = i % 4, qi = q0 + qq;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (qi < Q)
+            v = *reinterpret_cast<const uint4*>(q + (((long long)b * M + qi / G) * Hq + head * G + qi % G) * HD + 32 * j +
+                                                8 * tt);
+        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+        uint32_t am = 0;  // the largest finite component
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = x[k] & 0x7fffu, hi = x[k] >> 16 & 0x7fffu;
+            am = max(am, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+        }
+#pragma unroll
+        for (int o = 1; o < PER; o *= 2) am = max(am, __shfl_xor_sync(0xffffffffu, am, o));
+        const int e = max((int)(am >> 7), 15) - 127;  // |q| < 2^(e + 1)
+        const float up = exp2_int(14 - e);
+        float y[8], sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            y[k] = (k & 1 ? bf16hi(x[k / 2]) : bf16lo(x[k / 2])) * up;
+            sum += y[k];
+            if (k & 2) y[k] *= 0.0625f;
+        }
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        sQ[((qq / 8) * NJ + j) * 32 + (qq % 8) * 4 + tt] =
+            make_uint4(pack_f16(y[0], y[1]), pack_f16(y[2], y[3]), pack_f16(y[4], y[5]), pack_f16(y[6], y[7]));
+        if (tt == 0) sInit[qq * NJ + j] = sum * -0x1p-21f;  // -8 sum q, in units of 2^-24
+        if (i % PER == 0) sF[qq] = exp2_int(e);
+    }
     __syncthreads();
+    float init[NT][NJ][2], fa[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int c = nt * 8 + 2 * t + e;
+            fa[nt][e] = sF[c];
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) init[nt][j][e] = sInit[c * NJ + j];
+        }
+    // score * log2(e) = sum_g s_g c_g * 2^e * fb
+    const float fb = kv4_unit(HD);
 
     float o[NT][CT][4] = {}, mx[NT][2], sum[NT][2] = {};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = -INFINITY;
-    const float scale = 1.4426950408889634f / sqrtf((float)HD);
+    int vexp = 17;  // O is kept in units of 2^(vexp - 135); vexp: exponent field of the largest V scale so far, at least 17
 
-    for (int base = (rank * kKv4Warps + warp) * kKv4Chunk; base <= top; base += S * kKv4Warps * kKv4Chunk) {
-        const unsigned char* tile[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int p = base + 16 * u, page = p <= top ? kv4_page(cache, b, p, status) : -1;
-            tile[u] = page >= 0 ? pages + kv4_tile_offset<HD>(cache, page, p, head) : nullptr;
-        }
+    int stage = 0;
+    for (int base = base0; base <= top; base += step) {
+        fetch();
+        cp_async_wait<D - 1>();
+        __syncwarp();
+        const uint32_t ok = ok_bits & 3u;
+        ok_bits >>= 2;
+        --in_count;
+        const uint32_t chunk = ring + stage * 2 * TB;
+        if (++stage == D) stage = 0;
+        const bool whole = ok == 3u && base + kKv4Chunk - 1 <= low;  // every query sees every token
+
         float s[NT][2][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            uint32_t wl[4] = {}, wh[4] = {}, s_lo[NJ] = {}, s_hi[NJ] = {};
-            if (tile[u]) {
-                if (HD == 128) {
-                    const uint4 x = ld_stream16(tile[u] + lane * 16), y = ld_stream16(tile[u] + 512 + lane * 16);
-                    wl[0] = x.x, wl[1] = x.y, wl[2] = x.z, wl[3] = x.w;
-                    wh[0] = y.x, wh[1] = y.y, wh[2] = y.z, wh[3] = y.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(tile[u] + lane * 8);
-                    const uint2 y = *reinterpret_cast<const uint2*>(tile[u] + 256 + lane * 8);
-                    wl[0] = x.x, wl[1] = x.y;
-                    wh[0] = y.x, wh[1] = y.y;
-                }
-                q4_row_scales<NJ>(tile[u] + 8 * HD + g * (HD / 16), s_lo);
-                q4_row_scales<NJ>(tile[u] + 8 * HD + (g + 8) * (HD / 16), s_hi);
+            const uint32_t tile = chunk + u * TB;
+            uint32_t wl[NJ], wh[NJ];
+            if (HD == 128) {
+                const uint4 x = lds16(tile + lane * 16), y = lds16(tile + 512 + lane * 16);
+                wl[0] = x.x, wl[1] = x.y, wl[2 % NJ] = x.z, wl[3 % NJ] = x.w;
+                wh[0] = y.x, wh[1] = y.y, wh[2 % NJ] = y.z, wh[3 % NJ] = y.w;
+            } else {
+                const uint2 x = lds8(tile + lane * 8), y = lds8(tile + 256 + lane * 8);
+                wl[0] = x.x, wl[1] = x.y;
+                wh[0] = y.x, wh[1] = y.y;
+            }
+            float s_lo[NJ], s_hi[NJ];
+            const uint32_t sd = tile + 8 * HD + g * (HD / 16);
+            if (HD == 128) {
+                const uint2 x = lds8(sd), y = lds8(sd + 8 * (HD / 16));
+                s_lo[0] = bf16lo(x.x), s_lo[1] = bf16hi(x.x), s_lo[2 % NJ] = bf16lo(x.y), s_lo[3 % NJ] = bf16hi(x.y);
+                s_hi[0] = bf16lo(y.x), s_hi[1] = bf16hi(y.x), s_hi[2 % NJ] = bf16lo(y.y), s_hi[3 % NJ] = bf16hi(y.y);
+            } else {
+                const uint32_t x = lds4(sd), y = lds4(sd + 8 * (HD / 16));
+                s_lo[0] = bf16lo(x), s_lo[1] = bf16hi(x);
+                s_hi[0] = bf16lo(y), s_hi[1] = bf16hi(y);
             }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[nt][u][0] = s[nt][u][1] = s[nt][u][2] = s[nt][u][3] = 0.f;
-#pragma unroll
             for (int j = 0; j < NJ; ++j) {
-                uint32_t a[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) a[2 * i] = q4_bf16x2(wl[j], i), a[2 * i + 1] = q4_bf16x2(wh[j], i);
-                const float s0 = bf16lo(s_lo[j]), s1 = bf16lo(s_hi[j]);
+                const uint32_t l8 = wl[j] >> 8, h8 = wh[j] >> 8;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const uint4 bq = sQ[(nt * NJ + j) * 32 + lane];
                     float c[4];
-                    mma_bf16_16816_new(c, a[0], a[1], a[2], a[3], bq.x, bq.y);
-                    mma_bf16_16816(c, a[4], a[5], a[6], a[7], bq.z, bq.w);
-                    s[nt][u][0] = fmaf(s0, c[0], s[nt][u][0]);
-                    s[nt][u][1] = fmaf(s0, c[1], s[nt][u][1]);
-                    s[nt][u][2] = fmaf(s1, c[2], s[nt][u][2]);
-                    s[nt][u][3] = fmaf(s1, c[3], s[nt][u][3]);
+                    mma_f16_16816(c, wl[j] & 0x000f000fu, wh[j] & 0x000f000fu, wl[j] & 0x00f000f0u, wh[j] & 0x00f000f0u, bq.x,
+                                  bq.y, init[nt][j][0], init[nt][j][1], init[nt][j][0], init[nt][j][1]);
+                    mma_f16_16816(c, l8 & 0x000f000fu, h8 & 0x000f000fu, l8 & 0x00f000f0u, h8 & 0x00f000f0u, bq.z, bq.w, c[0],
+                                  c[1], c[2], c[3]);
+                    if (j == 0) {
+                        s[nt][u][0] = s_lo[j] * c[0], s[nt][u][1] = s_lo[j] * c[1];
+                        s[nt][u][2] = s_hi[j] * c[2], s[nt][u][3] = s_hi[j] * c[3];
+                    } else {
+                        s[nt][u][0] = fmaf(s_lo[j], c[0], s[nt][u][0]);
+                        s[nt][u][1] = fmaf(s_lo[j], c[1], s[nt][u][1]);
+                        s[nt][u][2] = fmaf(s_hi[j], c[2], s[nt][u][2]);
+                        s[nt][u][3] = fmaf(s_hi[j], c[3], s[nt][u][3]);
+                    }
                 }
             }
         }
-        // running softmax; a score that its query does not see is -inf whatever the tile holds there
+        // V scales of this lane's group, tokens 2 t, 2 t + 1 and 8 more of each tile
+        uint32_t sc[2][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int r = 0; r < 2; ++r)
+                sc[u][r] = lds4(chunk + u * TB + 17 * HD + g * (HD / 8) / 32 * 32 + r * 16 + t * 4);
+        if (!whole) {
+            // a score that its query does not see is -inf, the V scale of a token that none sees 0, whatever
+            // bits the tile holds there
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int p = base + 16 * u + g + 8 * (e >> 1);
-                    s[nt][u][e] = tile[u] && p <= lim[nt][e & 1] ? s[nt][u][e] * scale : -INFINITY;
+            for (int u = 0; u < 2; ++u) {
+                const bool here = ok >> u & 1u;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!here || base + 16 * u + g + 8 * (e >> 1) > lim[nt][e & 1]) s[nt][u][e] = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int p = base + 16 * u + 8 * r + 2 * t;
+                    if (!here || p > top) sc[u][r] &= 0xffff0000u;
+                    if (!here || p + 1 > top) sc[u][r] &= 0x0000ffffu;
                 }
+            }
+        }
+        // running softmax, in units of 1 / fb
+        float alpha[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) s[nt][u][e] *= fa[nt][e], s[nt][u][e + 2] *= fa[nt][e];
                 float m = fmaxf(fmaxf(s[nt][0][e], s[nt][0][e + 2]), fmaxf(s[nt][1][e], s[nt][1][e + 2]));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
                 m = fmaxf(m, mx[nt][e]);
                 const float ref = m == -INFINITY ? 0.f : m;  // nothing seen so far
-                const float alpha = exp2_fast(mx[nt][e] - ref);
+                alpha[nt][e] = exp2_fast((mx[nt][e] - ref) * fb);
                 mx[nt][e] = m;
+                const float off = -ref * fb;
                 float add = 0.f;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    s[nt][u][e] = exp2_fast(s[nt][u][e] - ref);
-                    s[nt][u][e + 2] = exp2_fast(s[nt][u][e + 2] - ref);
+                    s[nt][u][e] = exp2_fast(fmaf(s[nt][u][e], fb, off));
+                    s[nt][u][e + 2] = exp2_fast(fmaf(s[nt][u][e + 2], fb, off));
                     add += s[nt][u][e] + s[nt][u][e + 2];
                 }
-                sum[nt][e] = sum[nt][e] * alpha + add;
-#pragma unroll
-                for (int i = 0; i < CT; ++i) o[nt][i][e] *= alpha, o[nt][i][e + 2] *= alpha;
+                sum[nt][e] = sum[nt][e] * alpha[nt][e] + add;
             }
-        }
+        // the largest V scale; scales that are not finite belong to values that are not: 0 in the product, and
+        // NaN for the queries that see them
+        auto largest = [&]() {
+            const uint32_t m2 = __vmaxu2(__vmaxu2(sc[0][0], sc[0][1]), __vmaxu2(sc[1][0], sc[1][1]));
+            return __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16));
+        };
+        uint32_t vmax = largest();
+        float poison[NT][2] = {};
+        const bool odd = vmax >= 0x7f80u;
+        if (odd) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if (!tile[u]) continue;  // the whole warp
-            // p as the sum of two bf16 numbers (16 bits): rounding it to one would cost as much as the
-            // rounding of the result
-            uint32_t ph[NT][2], pl[NT][2];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const float x = s[nt][u][2 * r], y = s[nt][u][2 * r + 1];
-                    const uint32_t hi = pack_bf16(x, y);
-                    ph[nt][r] = movmatrix_trans(hi);
-                    pl[nt][r] = movmatrix_trans(pack_bf16(x - bf16lo(hi), y - bf16hi(hi)));
-                }
-            constexpr int W = HD / 64;  // code words of a lane's piece: channels (HD / 8) g ..
-            const unsigned char* vc = tile[u] + 9 * HD + lane * (HD / 8);
-            const unsigned char* vs = tile[u] + 17 * HD + g * (HD / 8) / 32 * 32 + t * 4;
-            uint32_t w[2][2][W], sc[2];  // [tokens 2 t, 2 t + 1 | 2 t + 8, 2 t + 9][token][word]
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                if (HD == 128) {
-                    const uint4 x = ld_stream16(vc + r * 512);
-                    w[r][0][0] = x.x, w[r][0][W - 1] = x.y, w[r][1][0] = x.z, w[r][1][W - 1] = x.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(vc + r * 256);
-                    w[r][0][0] = x.x, w[r][1][0] = x.y;
-                }
-                sc[r] = *reinterpret_cast<const uint32_t*>(vs + r * 16);
-            }
-            // Scales that are not finite: those of slots behind the last token (whatever bits are there),
-            // and of values that are not finite themselves.  0 in the product for both; the latter make
-            // NaN of what the queries that see them sum up.
-            bool odd = false;
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-                odd |= (sc[r] & 0x7f80u) == 0x7f80u || (sc[r] & 0x7f800000u) == 0x7f800000u;
-            float poison[NT][2] = {};
-            const bool any_odd = __any_sync(0xffffffffu, odd);
-            if (any_odd) {
-                const uint16_t* gs = reinterpret_cast<const uint16_t*>(tile[u] + 17 * HD + g * (HD / 8) / 32 * 32);
+            for (int u = 0; u < 2; ++u) {
                 for (int i = 0; i < 16; ++i) {
-                    if ((gs[i] & 0x7f80u) != 0x7f80u) continue;
+                    const uint32_t x = lds4(chunk + u * TB + 17 * HD + g * (HD / 8) / 32 * 32 + (i & ~1) * 2) >> (16 * (i & 1));
+                    if ((x & 0x7f80u) != 0x7f80u || !(ok >> u & 1u)) continue;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -230,8 +406,48 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
                 }
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    if ((sc[r] & 0x7f80u) == 0x7f80u) sc[r] &= 0xffff0000u;
-                    if ((sc[r] & 0x7f800000u) == 0x7f800000u) sc[r] &= 0xffffu;
+                    if ((sc[u][r] & 0x7f80u) == 0x7f80u) sc[u][r] &= 0xffff0000u;
+                    if ((sc[u][r] & 0x7f800000u) == 0x7f800000u) sc[u][r] &= 0x0000ffffu;
+                }
+            }
+            vmax = largest();
+        }
+        const int vnew = max(vexp, (int)(vmax >> 7));
+        const float shrink = exp2_int(vexp - vnew);  // 1 almost always
+        vexp = vnew;
+        bool keep = shrink == 1.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) keep = keep && alpha[nt][0] == 1.f && alpha[nt][1] == 1.f;
+        if (!__all_sync(0xffffffffu, keep)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float f = alpha[nt][e] * shrink;
+#pragma unroll
+                    for (int i = 0; i < CT; ++i) o[nt][i][e] *= f, o[nt][i][e + 2] *= f;
+                }
+        }
+        const float vscale = exp2_int(135 - vexp);  // the largest scale to [2^8, 2^9)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            constexpr int CW = HD / 64;  // code words of a lane's piece: channels (HD / 8) g ..
+            uint32_t p[NT][2], s16[2], s72[2], w[2][2][CW];  // w: [tokens 2 t, 2 t + 1 | 8 more][token][word]
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) p[nt][r] = movmatrix_trans(pack_f16(s[nt][u][2 * r], s[nt][u][2 * r + 1]));
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const uint32_t vs = pack_f16(bf16lo(sc[u][r]) * vscale, bf16hi(sc[u][r]) * vscale);
+                s16[r] = mul_f16x2(vs, 0x2c002c00u), s72[r] = mul_f16x2(vs, 0xd480d480u);  // 1 / 16, -72
+                const uint32_t vc = chunk + u * TB + 9 * HD + r * (4 * HD) + lane * (HD / 8);
+                if (HD == 128) {
+                    const uint4 x = lds16(vc);
+                    w[r][0][0] = x.x, w[r][0][CW - 1] = x.y, w[r][1][0] = x.z, w[r][1][CW - 1] = x.w;
+                } else {
+                    const uint2 x = lds8(vc);
+                    w[r][0][0] = x.x, w[r][1][0] = x.y;
                 }
             }
 #pragma unroll
@@ -240,122 +456,129 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const uint32_t two = __byte_perm(w[r][0][i / 4], w[r][1][i / 4], i % 4 < 2 ? 0x5410 : 0x7632);
-                    a[2 * r] = mul_bf16x2(q4_bf16x2(two, 2 * (i % 2)), sc[r]);
-                    a[2 * r + 1] = mul_bf16x2(q4_bf16x2(two, 2 * (i % 2) + 1), sc[r]);
+                    a[2 * r] = q4_scaled_f16x2(two, 2 * (i % 2), s16[r], s72[r]);
+                    a[2 * r + 1] = q4_scaled_f16x2(two, 2 * (i % 2) + 1, s16[r], s72[r]);
                 }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    mma_bf16_16816(o[nt][i], a[0], a[1], a[2], a[3], ph[nt][0], ph[nt][1]);
-                    mma_bf16_16816(o[nt][i], a[0], a[1], a[2], a[3], pl[nt][0], pl[nt][1]);
-                }
-            }
-            if (any_odd) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int i = 0; i < CT; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[nt][i][e] += poison[nt][e & 1];
+                    mma_f16_16816(o[nt][i], a[0], a[1], a[2], a[3], p[nt][0], p[nt][1], o[nt][i][0], o[nt][i][1], o[nt][i][2],
+                                  o[nt][i][3]);
             }
         }
+        if (odd) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < CT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[nt][i][e] += poison[nt][e & 1];
+        }
+        __syncwarp();  // every lane has read the chunk before the ring comes round to it
     }
 
-    // ---- the warps of the CTA: common maximum, then halves added in a fixed order
+    // ---- the warps' results, each where its ring was
+    cp_async_wait<0>();
+    __syncwarp();
+    float4* mineO = reinterpret_cast<float4*>(kv4_smem + warp * SM::kWarpRing);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int i = 0; i < CT; ++i)
+            mineO[(nt * CT + i) * 32 + lane] = make_float4(o[nt][i][0], o[nt][i][1], o[nt][i][2], o[nt][i][3]);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 4);
             sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 8);
             sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 16);
-            if (g == 0) sM[warp * NT * 8 + nt * 8 + 2 * t + e] = mx[nt][e];
+            if (g == 0) sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e]);
         }
-    __syncthreads();
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int c = nt * 8 + 2 * t + e;
-            float m = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < kKv4Warps; ++w) m = fmaxf(m, sM[w * NT * 8 + c]);
-            const float f = m == -INFINITY ? 0.f : exp2_fast(mx[nt][e] - m);
-            sum[nt][e] *= f;
-#pragma unroll
-            for (int i = 0; i < CT; ++i) o[nt][i][e] *= f, o[nt][i][e + 2] *= f;
-            if (warp == 0 && g == 0) sML[c] = m;
-        }
-    __syncthreads();
-    for (int half = kKv4Warps / 2; half >= 1; half /= 2) {
-        if (warp >= half && warp < 2 * half) {
-            float* dst = sO + (warp - half) * NT * 8 * HD;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float* d = dst + (nt * 8 + 2 * t + e) * HD + g * (HD / 8);
-#pragma unroll
-                    for (int i = 0; i < CT; ++i)
-                        *reinterpret_cast<float2*>(d + 2 * i) = make_float2(o[nt][i][e], o[nt][i][e + 2]);
-                    if (g == 0) sM[(warp - half) * NT * 8 + nt * 8 + 2 * t + e] = sum[nt][e];
-                }
-        }
-        __syncthreads();
-        if (warp < half) {
-            const float* src = sO + warp * NT * 8 * HD;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float* d = src + (nt * 8 + 2 * t + e) * HD + g * (HD / 8);
-#pragma unroll
-                    for (int i = 0; i < CT; ++i) {
-                        const float2 v = *reinterpret_cast<const float2*>(d + 2 * i);
-                        o[nt][i][e] += v.x, o[nt][i][e + 2] += v.y;
-                    }
-                    sum[nt][e] += sM[warp * NT * 8 + nt * 8 + 2 * t + e];
-                }
-        }
-        __syncthreads();
     }
-    if (warp == 0) {
+    if (lane == 0) sExp[warp] = vexp;
+    if (S > 1) cluster_wait();  // the others are there
+    __syncthreads();
+    // ---- the CTA's, sent to the CTA that finishes them: piece x holds two queries x two channels
+    const int share = SM::kItems / S;
+    for (int x = threadIdx.x; x < SM::kItems; x += W * 32) {
+        const int c = x / (CT * 32) * 8 + 2 * (x & 3);  // its first query
+        float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int w = 0; w < W; ++w) m0 = fmaxf(m0, sStat[w * NT * 8 + c].x), m1 = fmaxf(m1, sStat[w * NT * 8 + c + 1].x);
+        float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+        float l0 = 0.f, l1 = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int c = nt * 8 + 2 * t + e;
-#pragma unroll
-                for (int i = 0; i < CT; ++i)
-                    *reinterpret_cast<float2*>(sO + c * HD + g * (HD / 8) + 2 * i) =
-                        make_float2(o[nt][i][e], o[nt][i][e + 2]);
-                if (g == 0) sML[NT * 8 + c] = sum[nt][e];
+        for (int w = 0; w < W; ++w) {
+            const float4 v = *reinterpret_cast<const float4*>(kv4_smem + w * SM::kWarpRing + x * 16);
+            const float2 s0 = sStat[w * NT * 8 + c], s1 = sStat[w * NT * 8 + c + 1];
+            const float f0 = m0 == -INFINITY ? 0.f : exp2_fast((s0.x - m0) * fb);
+            const float f1 = m1 == -INFINITY ? 0.f : exp2_fast((s1.x - m1) * fb);
+            const float unit = exp2_int(sExp[w] - 135);  // O was kept in units of this
+            l0 = fmaf(f0, s0.y, l0), l1 = fmaf(f1, s1.y, l1);
+            r.x = fmaf(f0 * unit, v.x, r.x), r.z = fmaf(f0 * unit, v.z, r.z);
+            r.y = fmaf(f1 * unit, v.y, r.y), r.w = fmaf(f1 * unit, v.w, r.w);
+        }
+        const int to = x / share;
+        st_cluster_f4(map_cluster(smem_u32(sIn) + (rank * share + x - to * share) * 16, to), r);
+        if ((x / 4) % (CT * 8) == 0)  // one of the pieces with these queries: their statistics, to all
+            for (int d = 0; d < S; ++d) {
+                const uint32_t a = map_cluster(smem_u32(sInStat) + (rank * NT * 8 + c) * 8, d);
+                st_cluster_f2(a, m0, l0);
+                st_cluster_f2(a + 8, m1, l1);
             }
     }
-    // ---- the CTAs of the cluster: CTA r finishes every S-th pair of output elements
     if (S > 1)
-        cluster_sync_all();
+        cluster_sync_all();  // after it nobody touches another CTA's memory
     else
         __syncthreads();
-    const uint32_t aO = (uint32_t)__cvta_generic_to_shared(sO), aML = (uint32_t)__cvta_generic_to_shared(sML);
-    for (int i = rank * kKv4Threads + threadIdx.x; i < NT * 8 * HD / 2; i += S * kKv4Threads) {
-        const int c = i / (HD / 2), ch = 2 * (i % (HD / 2)), qi = q0 + c;
+    for (int y = threadIdx.x; y < 2 * share; y += W * 32) {  // one query and two channels a thread
+        const int x = rank * share + y / 2, e = y & 1, l = x & 31, c = x / (CT * 32) * 8 + 2 * (l & 3) + e, qi = q0 + c;
         if (qi >= Q) continue;
-        float m = -INFINITY;
-        for (int r = 0; r < S; ++r) m = fmaxf(m, ld_cluster_f32(map_cluster(aML + 4 * c, r)));
-        float l = 0.f, x = 0.f, y = 0.f;
+        float m = -INFINITY, sum_l = 0.f, v0 = 0.f, v1 = 0.f;
+        for (int r = 0; r < S; ++r) m = fmaxf(m, sInStat[r * NT * 8 + c].x);
+#pragma unroll 4
         for (int r = 0; r < S; ++r) {
-            const float mr = ld_cluster_f32(map_cluster(aML + 4 * c, r));
-            const float f = m == -INFINITY ? 0.f : exp2_fast(mr - m);
-            l = fmaf(f, ld_cluster_f32(map_cluster(aML + 4 * (NT * 8 + c), r)), l);
-            x = fmaf(f, ld_cluster_f32(map_cluster(aO + 4 * (c * HD + ch), r)), x);
-            y = fmaf(f, ld_cluster_f32(map_cluster(aO + 4 * (c * HD + ch + 1), r)), y);
+            const float2 st = sInStat[r * NT * 8 + c];
+            const float f = m == -INFINITY ? 0.f : exp2_fast((st.x - m) * fb);
+            const float* v = reinterpret_cast<const float*>(sIn + r * share + y / 2);
+            sum_l = fmaf(f, st.y, sum_l), v0 = fmaf(f, v[e], v0), v1 = fmaf(f, v[e + 2], v1);
         }
-        const int m_row = qi / G;
-        const bool none = (long long)pos0 + m_row < 0 || (long long)pos0 + m_row >= cache.max_seq;
-        const uint32_t v = none ? 0u : pack_bf16(x / l, y / l);
-        *reinterpret_cast<uint32_t*>(out + (((long long)b * M + m_row) * Hq + head * G + qi % G) * HD + ch) = v;
+        const int row = qi / G, ch = (l >> 2) * (HD / 8) + 2 * (x / 32 % CT);
+        if (splits > 1) {  // to be finished by combine_kv4_kernel
+            float* to = scratch + (kv4_partial(b, gridDim.y, blockIdx.y, splits, split) * (NT * 8) + c) * (HD + 2);
+            *reinterpret_cast<float2*>(to + ch) = make_float2(v0, v1);
+            if (ch == 0) *reinterpret_cast<float2*>(to + HD) = make_float2(m, sum_l);
+            continue;
+        }
+        const bool none = (long long)pos0 + row < 0 || (long long)pos0 + row >= cache.max_seq;
+        const uint32_t v = none ? 0u : pack_bf16(v0 / sum_l, v1 / sum_l);
+        *reinterpret_cast<uint32_t*>(out + (((long long)b * M + row) * Hq + head * G + qi % G) * HD + ch) = v;
     }
-    if (S > 1) cluster_sync_all();  // no CTA leaves while another still reads its results
+}
+
+// Joins the splits.  grid (M, Hq, n_seq), block HD / 2: a thread has two channels of a row.  NT, rows (gridDim.y), splits:
+// of the attention kernel's launch.
+template <int HD>
+__global__ void __launch_bounds__(HD / 2)
+combine_kv4_kernel(const float* __restrict__ scratch, int G, const int32_t* __restrict__ pos0_dev, int max_seq, int NT, int Hkv,
+                   int rows, int splits, uint16_t* __restrict__ out)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int m = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, ch = 2 * threadIdx.x;
+    const int qi = m * G + hq % G, y = qi / (NT * 8) * Hkv + hq / G, c = qi % (NT * 8);
+    const float* from = scratch + (kv4_partial(b, rows, y, splits, 0) * (NT * 8) + c) * (HD + 2);
+    const long long stride = (long long)NT * 8 * (HD + 2), p = (long long)pos0_dev[b] + m;
+    const float fb = kv4_unit(HD);
+    float top = -INFINITY, l = 0.f, x = 0.f, y0 = 0.f;
+    for (int s = 0; s < splits; ++s) top = fmaxf(top, from[s * stride + HD]);
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+        const float2 st = *reinterpret_cast<const float2*>(from + s * stride + HD);
+        const float2 v = *reinterpret_cast<const float2*>(from + s * stride + ch);
+        const float f = top == -INFINITY ? 0.f : exp2_fast((st.x - top) * fb);
+        l = fmaf(f, st.y, l), x = fmaf(f, v.x, x), y0 = fmaf(f, v.y, y0);
+    }
+    const uint32_t r = p < 0 || p >= max_seq ? 0u : pack_bf16(x / l, y0 / l);
+    *reinterpret_cast<uint32_t*>(out + (((long long)b * gridDim.x + m) * gridDim.y + hq) * HD + ch) = r;
 }
 
 }  // namespace ls

@@ -100,12 +100,12 @@ def test_cache_operations_refuse_bad_arguments():
         (0, None, BAD), (1, 0, BAD), (2, 0, BAD), (3, 0, BAD), (4, None, BAD), (5, 0, BAD), (6, 80, BAD), (7, 24, BAD),
         (8, None, BAD), (9, 3, BAD), (10, 1 << 21, CAP), (11, None, BAD), (12, None, BAD), (12, P + 8, BAD), (13, None, BAD),
         (14, 0, BAD)])
-    # q, n_seq, M, pos0, Hq, Hkv, hd, page_size, table, stride, max_seq, pages, n_pages, out, status, stream
-    good = [P, 1, 1, P, 8, 2, 128, 64, P, 4, 256, P, 4, P, None, None]
+    # q, n_seq, M, pos0, Hq, Hkv, hd, page_size, table, stride, max_seq, pages, n_pages, out, scratch, status, stream
+    good = [P, 1, 1, P, 8, 2, 128, 64, P, 4, 256, P, 4, P, None, None, None]
     refused(L.ls_op_attention_kv4, good, [
         (0, None, BAD), (0, P + 8, BAD), (1, 0, BAD), (2, 0, BAD), (2, 17, BAD), (3, None, BAD), (4, 0, BAD), (4, 7, BAD),
         (4, 18, BAD), (5, 0, BAD), (6, 256, BAD), (7, 100, BAD), (8, None, BAD), (9, 3, BAD), (10, 0, CAP), (11, None, BAD),
-        (12, 0, BAD), (13, None, BAD), (13, P + 4, BAD)])
+        (12, 0, BAD), (13, None, BAD), (13, P + 4, BAD), (14, P + 8, BAD)])
 
 
 def test_the_binding_refuses_what_does_not_fit():
