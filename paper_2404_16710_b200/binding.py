@@ -9,6 +9,7 @@ missing the first call raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from pathlib import Path
 
 import numpy as np
@@ -148,10 +149,22 @@ def _dev(t):
     return C.c_void_p(t.data_ptr())
 
 
+_torch = None
+
+
+def _t():
+    """torch, imported at the first call that needs it"""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _stream():
-    """the current CUDA stream.  torch.cuda.current_stream() builds a Stream object for it (3.4 us a call, as much as a
-    launch); the raw handle costs 0.3 us."""
-    import torch
+    """handle of the current CUDA stream.  torch.cuda.current_stream() builds a Stream object for it (3.4 us a call, as
+    much as a launch); the raw handle costs 0.3 us."""
+    torch = _torch or _t()
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
 
@@ -422,17 +435,20 @@ def _bad(what):
 
 
 def _arg(t, dtype, what):
-    """device pointer of a contiguous CUDA tensor of the type the entry point reads (None -> NULL)"""
-    if t is None:
-        return None
-    if not t.is_cuda or not t.is_contiguous() or str(t.dtype) != dtype:
-        _bad(f"{what}: a contiguous {dtype} CUDA tensor is needed")
-    return t.data_ptr()
+    """device pointer of a contiguous CUDA tensor of the type the entry point reads"""
+    if t.is_cuda and t.is_contiguous() and t.dtype is getattr(_torch or _t(), dtype):
+        return t.data_ptr()
+    _bad(f"{what}: a contiguous {dtype} CUDA tensor is needed")
 
 
-_BF16, _F32, _INT, _U8 = "torch.bfloat16", "torch.float32", "torch.int32", "torch.uint8"
+def _status(t):
+    return None if t is None else _arg(t, _INT, "status")
 
 
+_BF16, _F32, _INT, _U8 = "bfloat16", "float32", "int32", "uint8"
+
+
+@functools.lru_cache(maxsize=4096)
 def ls_op_w4_bytes(N, K, group):
     return lib().ls_op_w4_bytes(N, K, group)
 
@@ -491,11 +507,11 @@ def ls_op_append_kv4(k, v, pos0, page_size, table, max_seq, pages, status=None):
     n_seq, M, Hkv, hd = k.shape
     n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
     if v.shape != k.shape or v.stride() != k.stride() or k.stride(3) != 1 or not (k.is_cuda and v.is_cuda) or \
-            str(k.dtype) != _BF16 or str(v.dtype) != _BF16:
+            k.dtype is not _t().bfloat16 or v.dtype is not _t().bfloat16:
         _bad("ls_op_append_kv4: k and v")
     _ck(lib().ls_op_append_kv4(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), n_seq, M,
                                _arg(pos0, _INT, "pos0"), Hkv, hd, page_size, _arg(table, _INT, "page table"), entries, max_seq,
-                               _arg(pages, _U8, "pages"), n_pages, _arg(status, _INT, "status"), _stream()), "ls_op_append_kv4")
+                               _arg(pages, _U8, "pages"), n_pages, _status(status), _stream()), "ls_op_append_kv4")
 
 
 def ls_op_expand_kv4(pages, pos0, M, page_size, table, max_seq, out_table, k_pages, v_pages, status=None):
@@ -508,9 +524,10 @@ def ls_op_expand_kv4(pages, pos0, M, page_size, table, max_seq, out_table, k_pag
     _ck(lib().ls_op_expand_kv4(_arg(pages, _U8, "pages"), n_pages, n_seq, M, _arg(pos0, _INT, "pos0"), Hkv, hd, page_size,
                                _arg(table, _INT, "page table"), entries, max_seq, _arg(out_table, _INT, "out page table"),
                                _arg(k_pages, _BF16, "k_pages"), _arg(v_pages, _BF16, "v_pages"), n_out,
-                               _arg(status, _INT, "status"), _stream()), "ls_op_expand_kv4")
+                               _status(status), _stream()), "ls_op_expand_kv4")
 
 
+@functools.lru_cache(maxsize=4096)
 def ls_op_attention_kv4_scratch_bytes(n_seq, M, Hq, Hkv, hd, max_seq):
     return lib().ls_op_attention_kv4_scratch_bytes(n_seq, M, Hq, Hkv, hd, max_seq)
 
@@ -525,13 +542,12 @@ def ls_op_attention_kv4(q, pos0, Hkv, hd, page_size, table, max_seq, pages, out,
     Hq = width // hd
     need = ls_op_attention_kv4_scratch_bytes(n_seq, M, Hq, Hkv, hd, max_seq)
     if scratch is None and need:
-        import torch
-        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+        scratch = _t().empty(need, dtype=_t().uint8, device=q.device)
     elif scratch is not None and scratch.numel() < need:
         raise LsError(LS_ERR_CAPACITY, "ls_op_attention_kv4: scratch")
     _ck(lib().ls_op_attention_kv4(_arg(q, _BF16, "q"), n_seq, M, _arg(pos0, _INT, "pos0"), Hq, Hkv, hd, page_size,
                                   _arg(table, _INT, "page table"), entries, max_seq, _arg(pages, _U8, "pages"), n_pages,
-                                  _arg(out, _BF16, "out"), _arg(scratch, _U8, "scratch"), _arg(status, _INT, "status"),
+                                  _arg(out, _BF16, "out"), None if scratch is None else _arg(scratch, _U8, "scratch"), _status(status),
                                   _stream()), "ls_op_attention_kv4")
 
 

@@ -106,7 +106,7 @@ struct Kv4Smem {
     static constexpr int kInbox = kItems * 16;                 // [CTA][its share of the pieces]
     static constexpr int kInit = NT * 8 * (HD / 32) * 4;       // -8 sum q [query][group]
     static constexpr int kFactor = NT * 8 * 4;                 // 2^e [query]
-    static constexpr int kStat = W * NT * 8 * 8 + W * 4;       // (max, sum) of the warps, exponents of their O
+    static constexpr int kStat = W * NT * 8 * 8 + W * 4;       // (max, sum) of the warps, units of their O
     static constexpr int kInStat = kKv4MaxCluster * NT * 8 * 8;  // (max, sum) of the CTAs
     static constexpr int kBytes = kRing + kQ + kInbox + kInit + kFactor + kStat + kInStat;
     static_assert(kItems / (NT * 32) * 512 * NT <= kWarpRing, "a warp's O fits its ring");
@@ -146,7 +146,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     float* sInit = reinterpret_cast<float*>(at += SM::kInbox);
     float* sF = reinterpret_cast<float*>(at += SM::kInit);
     float2* sStat = reinterpret_cast<float2*>(at += SM::kFactor);   // [W][NT * 8]
-    int* sExp = reinterpret_cast<int*>(sStat + W * NT * 8);         // [W]
+    float* sUnit = reinterpret_cast<float*>(sStat + W * NT * 8);     // [W]
     float2* sInStat = reinterpret_cast<float2*>(at += SM::kStat);   // [CTA][NT * 8]
     pdl_launch_dependents();
     pdl_wait();
@@ -156,6 +156,15 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int Q = M * G, Hq = cache.Hkv * G;
 
+    // The first accesses to memory, all before the first use of any: this thread's piece of a query, the page-table
+    // entries of its warp's first chunk, the position.
+    constexpr int PER = NJ * 4;  // threads that make a query's operand: channels 32 j + 8 t .. + 7
+    static_assert(NT * 8 * PER <= W * 32, "a thread has one piece");
+    const int piece_q = threadIdx.x / PER, piece_j = threadIdx.x % PER / 4, piece_t = threadIdx.x % 4;
+    uint4 piece = make_uint4(0, 0, 0, 0);
+    if (piece_q < NT * 8 && q0 + piece_q < Q)
+        piece = *reinterpret_cast<const uint4*>(q + (((long long)b * M + (q0 + piece_q) / G) * Hq + head * G + (q0 + piece_q) % G) * HD +
+                                                32 * piece_j + 8 * piece_t);
     // page-table entries of this warp's next chunk (a chunk lies in one page, unless pages are of 16), read before
     // anything says whether it is needed: the positions below max_seq have entries
     const int step = gridDim.x * W * kKv4Chunk, base0 = (blockIdx.x * W + warp) * kKv4Chunk;
@@ -219,15 +228,9 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     for (int i = 0; i < D - 1; ++i) fetch();
 
     // Queries as B operands: lane 4 g + t of group j holds channels 32 j + 8 t .. + 7 of query g, columns 2, 3, 6 and 7
-    // of the eight times 2^-4.  A query is shared by the NJ x 4 threads that make it.
-    constexpr int PER = NJ * 4;
-    for (int i = threadIdx.x; i < NT * 8 * PER; i += W * 32) {
-        const int qq = i / PER, j = i % PER / 4, tt = i % 4, qi = q0 + qq;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (qi < Q)
-            v = *reinterpret_cast<const uint4*>(q + (((long long)b * M + qi / G) * Hq + head * G + qi % G) * HD + 32 * j +
-                                                8 * tt);
-        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+    // of the eight times 2^-4.
+    if (piece_q < NT * 8) {  // whole warps
+        const uint32_t x[4] = {piece.x, piece.y, piece.z, piece.w};
         uint32_t am = 0;  // the largest finite component
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -247,10 +250,10 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
         }
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        sQ[((qq / 8) * NJ + j) * 32 + (qq % 8) * 4 + tt] =
+        sQ[((piece_q / 8) * NJ + piece_j) * 32 + (piece_q % 8) * 4 + piece_t] =
             make_uint4(pack_f16(y[0], y[1]), pack_f16(y[2], y[3]), pack_f16(y[4], y[5]), pack_f16(y[6], y[7]));
-        if (tt == 0) sInit[qq * NJ + j] = sum * -0x1p-21f;  // -8 sum q, in units of 2^-24
-        if (i % PER == 0) sF[qq] = exp2_int(e);
+        if (piece_t == 0) sInit[piece_q * NJ + piece_j] = sum * -0x1p-21f;  // -8 sum q, in units of 2^-24
+        if (threadIdx.x % PER == 0) sF[piece_q] = exp2_int(e);
     }
     __syncthreads();
     float init[NT][NJ][2], fa[NT][2];
@@ -493,13 +496,14 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             if (g == 0) sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e]);
         }
     }
-    if (lane == 0) sExp[warp] = vexp;
+    if (lane == 0) sUnit[warp] = exp2_int(vexp - 135);  // O was kept in units of this
     if (S > 1) cluster_wait();  // the others are there
     __syncthreads();
     // ---- the CTA's, sent to the CTA that finishes them: piece x holds two queries x two channels
     const int share = SM::kItems / S;
     for (int x = threadIdx.x; x < SM::kItems; x += W * 32) {
         const int c = x / (CT * 32) * 8 + 2 * (x & 3);  // its first query
+        if (q0 + c >= Q) continue;
         float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
         for (int w = 0; w < W; ++w) m0 = fmaxf(m0, sStat[w * NT * 8 + c].x), m1 = fmaxf(m1, sStat[w * NT * 8 + c + 1].x);
@@ -511,7 +515,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             const float2 s0 = sStat[w * NT * 8 + c], s1 = sStat[w * NT * 8 + c + 1];
             const float f0 = m0 == -INFINITY ? 0.f : exp2_fast((s0.x - m0) * fb);
             const float f1 = m1 == -INFINITY ? 0.f : exp2_fast((s1.x - m1) * fb);
-            const float unit = exp2_int(sExp[w] - 135);  // O was kept in units of this
+            const float unit = sUnit[w];
             l0 = fmaf(f0, s0.y, l0), l1 = fmaf(f1, s1.y, l1);
             r.x = fmaf(f0 * unit, v.x, r.x), r.z = fmaf(f0 * unit, v.z, r.z);
             r.y = fmaf(f1 * unit, v.y, r.y), r.w = fmaf(f1 * unit, v.w, r.w);

@@ -7,8 +7,8 @@
 // s is kept as bf16.  A code has 3 significant bits, so c * s has at most 8: it IS a bf16 number, and the
 // bf16 operators (the prompt pass) see on expanded data exactly the values the 4-bit operators use.  The
 // price is a step up to 6 % wider (3 % on average) than a / 7.  Codes decide exactly in fp32: x has 8
-// significant bits and a border (k + 1/2) s at most 9, so |x| either is the border or differs from it by
-// more than 2^-17 of its value.
+// significant bits and a border (k + 1/2) s at most 9, so x / s either is k + 1/2 or differs from it by at least
+// 2^-17 of its value, 2^-18 or more.
 // Ends of the range: s = 0 (all codes 0) if a = 0; s >= 2^-126, so that c * s never is a subnormal number;
 // s <= 1.125 * 2^125, so that 7 s is finite.  A group with a NaN or an infinity gets a NaN scale and stands
 // for NaN.  A nibble holds c + 8.
@@ -37,26 +37,31 @@ __host__ __device__ constexpr int kv4_tile_bytes(int hd) { return kQ4Rows * (hd 
 // scale of a group whose largest |x| has the bf16 bits amax (sign bit clear)
 __device__ __forceinline__ float q4_scale(uint32_t amax)
 {
-    if (amax >= 0x7f80u) return __uint_as_float(0x7fff0000u);  // an infinity or a NaN in the group
-    if (amax == 0) return 0.f;
-    const float q = __fdiv_rn(__uint_as_float(amax << 16), 7.f);
+    // a / 7 from below: a has 8 significant bits, so a / 7 either has 5 or is farther than 2^-11 of its value
+    // from every number that does, and a product short of it by less than 2^-19 rounds up to the same one
+    const float q = __uint_as_float(amax << 16) * 0.14285700f;
     // up to the next multiple of 2^19 ulps: 4 of the 23 mantissa bits stay
-    const float s = __uint_as_float((__float_as_uint(q) + 0x7ffffu) & ~0x7ffffu);
-    return fminf(fmaxf(s, 0x1p-126f), 1.125f * 0x1p125f);
+    float s = __uint_as_float((__float_as_uint(q) + 0x7ffffu) & ~0x7ffffu);
+    s = fminf(fmaxf(s, 0x1p-126f), 1.125f * 0x1p125f);
+    if (amax == 0) s = 0.f;
+    return amax >= 0x7f80u ? __uint_as_float(0x7fff0000u) : s;  // an infinity or a NaN in the group
 }
-// c + 8 of the bf16 value x; r = 1 / s to within an ulp (0 for s = 0 or NaN: every code is then 0).  |x| r
-// is within 2^-22 of |x| / s, so k = floor(|x| r) is the code below the border that decides, or the
-// border is farther than the error; (k + 1/2) s is exact.
-__device__ __forceinline__ uint32_t q4_code(uint32_t x, float s, float r)
+// 1 / s to within an ulp; 0 for s = 0 or NaN: every code is then 0
+__device__ __forceinline__ float q4_rcp(float s)
 {
-    const float v = __uint_as_float(x << 16), a = fabsf(v);
-    const float k = floorf(a * r), mid = (k + 0.5f) * s;
-    int c = (int)k;
-    c += (a > mid || (a == mid && (c & 1))) ? 1 : 0;
-    c = min(c, 7);
-    return (uint32_t)(8 + (v < 0.f ? -c : c));
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    return s > 0.f ? r : 0.f;
 }
-__device__ __forceinline__ float q4_rcp(float s) { return s > 0.f ? __frcp_rn(s) : 0.f; }
+// A float whose bits are kQ4Base + u, u = c + 8, for the bf16 value v; r = q4_rcp(s).  v r + 24 is rounded to a multiple
+// of 2^-19: the product is off by at most 7.1 * 2^-23 < 2^-20, so what lies on a border (k + 1/2) comes out on
+// it, and what does not lies at least 2^-18 off and stays off.  Adding 3 * 2^22 then rounds to an integer, borders
+// to the even one, and leaves 24 + c in the low bits.
+constexpr uint32_t kQ4Base = 0x4b400000u + 16u;
+__device__ __forceinline__ uint32_t q4_code_bits(float v, float r)
+{
+    return __float_as_uint(__fadd_rn(__fmaf_rn(v, r, 24.f), 12582912.f));
+}
 
 __device__ __forceinline__ uint32_t absmax_bf16x2(uint32_t m, uint32_t w)  // bits, not values: NaN counts as largest
 {
@@ -66,21 +71,22 @@ __device__ __forceinline__ uint32_t absmax8(const uint4& v)
 {
     return absmax_bf16x2(absmax_bf16x2(absmax_bf16x2(absmax_bf16x2(0, v.x), v.y), v.z), v.w);
 }
-// codes of two neighbouring values in the row order: columns 2 i, 2 i + 1 at nibbles i and i + 4
-__device__ __forceinline__ uint32_t q4_pair(uint32_t w, float s, float r)
+// Codes of 8 values as a word, value e at nibble e / 2 + 4 (e % 2) (ROW) or e: the sum of the codes' bits in their places,
+// less what kQ4Base adds to each.  Under a NaN scale all codes are 0.
+template <bool ROW>
+__device__ __forceinline__ uint32_t q4_word8(const uint4& v, float s, float r)
 {
-    return q4_code(w & 0xffffu, s, r) | (q4_code(w >> 16, s, r) << 16);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t word = 0u - kQ4Base * 0x11111111u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int pos = ROW ? e / 2 + 4 * (e % 2) : e;
+        word += q4_code_bits(e & 1 ? bf16hi(w[e / 2]) : bf16lo(w[e / 2]), r) << (4 * pos);
+    }
+    return s == s ? word : 0x88888888u;
 }
-__device__ __forceinline__ uint32_t q4_word(const uint4& v, float s, float r)
-{
-    return q4_pair(v.x, s, r) | (q4_pair(v.y, s, r) << 4) | (q4_pair(v.z, s, r) << 8) | (q4_pair(v.w, s, r) << 12);
-}
-// codes of 8 values lowest nibble first (V)
-__device__ __forceinline__ uint32_t q4_word_plain(const uint4& v, float s, float r)
-{
-    auto two = [&](uint32_t w) { return q4_code(w & 0xffffu, s, r) | (q4_code(w >> 16, s, r) << 4); };
-    return two(v.x) | (two(v.y) << 8) | (two(v.z) << 16) | (two(v.w) << 24);
-}
+__device__ __forceinline__ uint32_t q4_word(const uint4& v, float s, float r) { return q4_word8<true>(v, s, r); }         // a row's
+__device__ __forceinline__ uint32_t q4_word_plain(const uint4& v, float s, float r) { return q4_word8<false>(v, s, r); }  // lowest first (V)
 
 // codes i and i + 4 of a word as two bf16 numbers c (exact): 0x4300 | u is 128 + u
 __device__ __forceinline__ uint32_t q4_bf16x2(uint32_t w, int i)
@@ -244,29 +250,33 @@ __global__ void __launch_bounds__(256) append_kv4_kernel(const uint16_t* __restr
     pdl_wait();
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, head = blockIdx.y, b = blockIdx.z;
     const int m = (blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32) * 8 + g;
-    int p = m < M ? kv4_position(pos0[b], m, cache.max_seq, status) : -1;
-    const int page = p >= 0 ? kv4_page(cache, b, p, status) : -1;
-    if (page < 0) p = -1;  // the row is left out, but its lanes stay for the shuffles
+    constexpr int G = HD / 32, O = HD / 64;  // groups of a row, octets of a V piece
+    // the row's values first: they wait for nothing
     const long long at = b * seq_stride + (long long)m * row_stride + head * head_stride;
-    unsigned char* tile = pages + (p >= 0 ? kv4_tile_offset<HD>(cache, page, p, head) : 0);
+    uint4 xk[G], xv[2][O];
+#pragma unroll
+    for (int j = 0; j < G; ++j) xk[j] = m < M ? *reinterpret_cast<const uint4*>(k + at + 32 * j + 8 * t) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int o = 0; o < O; ++o)
+            xv[h][o] = m < M ? *reinterpret_cast<const uint4*>(v + at + (t + 4 * h) * (HD / 8) + 8 * o) : make_uint4(0, 0, 0, 0);
+    const int p = m < M ? kv4_position(pos0[b], m, cache.max_seq, status) : -1;
+    const int page = p >= 0 ? kv4_page(cache, b, p, status) : -1;  // -1: the row is left out, its lanes stay for the shuffles
+    unsigned char* tile = pages + (page >= 0 ? kv4_tile_offset<HD>(cache, page, p, head) : 0);
     const int i = p & 15;
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    constexpr int G = HD / 32;
     {
-        uint4 x[G];
         uint32_t words[G], sc[G];
 #pragma unroll
-        for (int j = 0; j < G; ++j) x[j] = p >= 0 ? *reinterpret_cast<const uint4*>(k + at + 32 * j + 8 * t) : zero;
-#pragma unroll
         for (int j = 0; j < G; ++j) {
-            uint32_t am = absmax8(x[j]);
+            uint32_t am = absmax8(xk[j]);
             am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
             am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
             const float s = q4_scale(am), r = q4_rcp(s);
             sc[j] = __float_as_uint(s) >> 16;
-            words[j] = q4_word(x[j], s, r);
+            words[j] = q4_word(xk[j], s, r);
         }
-        if (p >= 0) {
+        if (page >= 0) {
             unsigned char* cd = tile + i * (HD / 2) + t * (HD / 8);
             unsigned char* sd = tile + 8 * HD + i * (HD / 16);
             if (HD == 128) {
@@ -281,21 +291,16 @@ __global__ void __launch_bounds__(256) append_kv4_kernel(const uint16_t* __restr
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int piece = t + 4 * h;  // of HD / 8 channels: two pieces to a group (HD = 128) or four
-        constexpr int O = HD / 64;    // octets of a piece
-        uint4 x[O];
-#pragma unroll
-        for (int o = 0; o < O; ++o)
-            x[o] = p >= 0 ? *reinterpret_cast<const uint4*>(v + at + piece * (HD / 8) + 8 * o) : zero;
-        uint32_t am = absmax8(x[0]);
-        if (O == 2) am = max(am, absmax8(x[O - 1]));
+        uint32_t am = absmax8(xv[h][0]);
+        if (O == 2) am = max(am, absmax8(xv[h][O - 1]));
         am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
         if (HD == 64) am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
         const float s = q4_scale(am), r = q4_rcp(s);
-        if (p < 0) continue;
+        if (page < 0) continue;
         unsigned char* cd = tile + kv4_v_piece<HD>(i, piece);
-        const uint32_t w0 = q4_word_plain(x[0], s, r);
+        const uint32_t w0 = q4_word_plain(xv[h][0], s, r);
         if (O == 2)
-            *reinterpret_cast<uint2*>(cd) = make_uint2(w0, q4_word_plain(x[O - 1], s, r));
+            *reinterpret_cast<uint2*>(cd) = make_uint2(w0, q4_word_plain(xv[h][O - 1], s, r));
         else
             *reinterpret_cast<uint32_t*>(cd) = w0;
         const int grp = piece * (HD / 8) / 32;

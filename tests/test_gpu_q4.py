@@ -77,6 +77,27 @@ def test_quantize_weights_at_the_ends_of_the_range(group):
     assert np.array_equal(vals(out), R.values(*R.quantise(vals(w), group), group), equal_nan=True)
 
 
+def test_quantize_every_border_of_every_scale():
+    """all 16 mantissas a scale can have, small and large exponents, and every value within two steps of bf16 of every
+    border (k + 1/2) s: the codes are those of exact arithmetic, borders to the even code"""
+    rows = []
+    for n in range(16, 32):
+        for e in (-120, -20, -3, 0, 17, 100):
+            s = np.float32(n * 2.0 ** e)
+            x = np.zeros((8, 32), np.float32)
+            x[:, 0] = 7 * s  # the group's largest: fixes the scale
+            for k in range(7):
+                border = np.float32((k + 0.5) * s)
+                u = int(border.view(np.uint32)) >> 16
+                x[k, 1:11] = (np.arange(u - 4, u + 6, dtype=np.uint32) << 16).view(np.float32)
+            x[:, 11:21] = -x[:, 1:11]
+            rows.append(x)
+    x = np.concatenate(rows)
+    w = from_bits((x.view(np.uint32) >> 16).astype(np.uint16))
+    assert np.array_equal(vals(w), x.astype(np.float64))
+    assert np.array_equal(quantised(w, 32).cpu().numpy(), R.pack_weight(vals(w), 32))
+
+
 def linear_reference(w, group, h):
     v = R.values(*R.quantise(vals(w), group), group)
     hv = vals(h)
