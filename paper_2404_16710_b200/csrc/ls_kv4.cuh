@@ -14,8 +14,8 @@
 // * V: a nibble moved to bits 4..7 or-ed to 1024 is 1024 + 16 u, and one multiply-add makes c s of it:
 //   (1024 + 16 u) (s / 16) - 72 s.  A scale has 5 significant bits, so every step is exact, for scales down to 2^-25
 //   of the largest one the warp has met (the power of two it is divided by is kept beside O).
-// * p <= 1 is rounded to f16's 11 bits (2^-12; 2^-25 absolute below 2^-14), well below the rounding of a
-//   bf16 result.  Scores, maxima, sums and O are fp32.
+// * p is rounded to f16's 11 bits (2^-12 of it; 2^-25 absolute below 2^-14, when the largest p so far is 1 or
+//   more), well below the rounding of a bf16 result.  Scores, maxima, sums and O are fp32.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -203,19 +203,30 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     auto fetch = [&]() {
         if (in_base <= top) {
             const uint32_t dst = ring + in_stage * 2 * TB + lane * 16;
+            auto source = [&](int p, int page) {
+                return mine + (unsigned long long)page_bytes * (uint32_t)page + ((uint32_t)(p >> 4) & tile_mask) * TB;
+            };
+            if (in_base + 16 <= top && cache.page_shift > 4 && (unsigned)next_page[0] < (unsigned)cache.n_pages) {
+                const unsigned char* src = source(in_base, next_page[0]);  // two tiles in a row
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int p = in_base + 16 * u;
-                if (p > top) continue;
-                if ((unsigned)next_page[u] >= (unsigned)cache.n_pages) {
-                    if (status) *status = DEV_BAD_PAGE;
-                    continue;
+                for (int i = 0; i < 2 * TB / 512; ++i) cp_async16_cg(dst + 512 * i, src + 512 * i, 16);
+                if (2 * TB % 512 && lane < 2 * TB % 512 / 16) cp_async16_cg(dst + 2 * TB / 512 * 512, src + 2 * TB / 512 * 512, 16);
+                ok_bits |= 3u << (2 * in_count);
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int p = in_base + 16 * u;
+                    if (p > top) continue;
+                    if ((unsigned)next_page[u] >= (unsigned)cache.n_pages) {
+                        if (status) *status = DEV_BAD_PAGE;
+                        continue;
+                    }
+                    ok_bits |= 1u << (2 * in_count + u);
+                    const unsigned char* src = source(p, next_page[u]);
+#pragma unroll
+                    for (int i = 0; i < TB / 512; ++i) cp_async16_cg(dst + u * TB + 512 * i, src + 512 * i, 16);
+                    if (lane < TB % 512 / 16) cp_async16_cg(dst + u * TB + TB / 512 * 512, src + TB / 512 * 512, 16);
                 }
-                ok_bits |= 1u << (2 * in_count + u);
-                const unsigned char* src = mine + (unsigned long long)page_bytes * (uint32_t)next_page[u] + ((uint32_t)(p >> 4) & tile_mask) * TB;
-#pragma unroll
-                for (int i = 0; i < TB / 512; ++i) cp_async16_cg(dst + u * TB + 512 * i, src + 512 * i, 16);
-                if (lane < TB % 512 / 16) cp_async16_cg(dst + u * TB + TB / 512 * 512, src + TB / 512 * 512, 16);
             }
             in_base += step;
             ++in_count;
@@ -272,7 +283,9 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     float o[NT][CT][4] = {}, mx[NT][2], sum[NT][2] = {};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = -INFINITY;
+    float top_m[NT][2];
     int vexp = 17;  // O is kept in units of 2^(vexp - 135); vexp: exponent field of the largest V scale so far, at least 17
+    float vscale = exp2_int(135 - vexp);  // brings the largest scale to [2^8, 2^9)
 
     int stage = 0;
     for (int base = base0; base <= top; base += step) {
@@ -360,8 +373,9 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
                 }
             }
         }
-        // running softmax, in units of 1 / fb
-        float alpha[NT][2];
+        // Running softmax, in units of 1 / fb.  A query's reference moves up only when its maximum has outgrown it by
+        // 2^8, so that O is rarely rescaled: p <= 2^8 then, and some p so far has been 1 or more.
+        bool grown = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -371,67 +385,72 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
                 float m = fmaxf(fmaxf(s[nt][0][e], s[nt][0][e + 2]), fmaxf(s[nt][1][e], s[nt][1][e + 2]));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                m = fmaxf(m, mx[nt][e]);
-                const float ref = m == -INFINITY ? 0.f : m;  // nothing seen so far
-                alpha[nt][e] = exp2_fast((mx[nt][e] - ref) * fb);
-                mx[nt][e] = m;
-                const float off = -ref * fb;
-                float add = 0.f;
+                top_m[nt][e] = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                grown |= top_m[nt][e] * fb > fmaf(mx[nt][e], fb, 8.f);
+            }
+        // V scales beyond what O's unit allows for, or not finite (of values that are not)
+        const uint32_t m2 = __vmaxu2(__vmaxu2(sc[0][0], sc[0][1]), __vmaxu2(sc[1][0], sc[1][1]));
+        grown |= max(m2 & 0xffffu, m2 >> 16) >> 7 > (uint32_t)vexp;
+        bool odd = false;
+        float poison[NT][2] = {};
+        if (__any_sync(0xffffffffu, grown)) {
+            auto largest = [&]() {
+                const uint32_t x = __vmaxu2(__vmaxu2(sc[0][0], sc[0][1]), __vmaxu2(sc[1][0], sc[1][1]));
+                return __reduce_max_sync(0xffffffffu, max(x & 0xffffu, x >> 16));
+            };
+            uint32_t vmax = largest();
+            odd = vmax >= 0x7f80u;
+            if (odd) {  // 0 in the product, and NaN for the queries that see them
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    s[nt][u][e] = exp2_fast(fmaf(s[nt][u][e], fb, off));
-                    s[nt][u][e + 2] = exp2_fast(fmaf(s[nt][u][e + 2], fb, off));
-                    add += s[nt][u][e] + s[nt][u][e + 2];
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t x = lds4(chunk + u * TB + 17 * HD + g * (HD / 8) / 32 * 32 + (i & ~1) * 2) >> (16 * (i & 1));
+                        if ((x & 0x7f80u) != 0x7f80u || !(ok >> u & 1u)) continue;
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                if (base + 16 * u + i <= lim[nt][e]) poison[nt][e] = __uint_as_float(0x7fffffffu);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        if ((sc[u][r] & 0x7f80u) == 0x7f80u) sc[u][r] &= 0xffff0000u;
+                        if ((sc[u][r] & 0x7f800000u) == 0x7f800000u) sc[u][r] &= 0x0000ffffu;
+                    }
                 }
-                sum[nt][e] = sum[nt][e] * alpha[nt][e] + add;
+                vmax = largest();
             }
-        // the largest V scale; scales that are not finite belong to values that are not: 0 in the product, and
-        // NaN for the queries that see them
-        auto largest = [&]() {
-            const uint32_t m2 = __vmaxu2(__vmaxu2(sc[0][0], sc[0][1]), __vmaxu2(sc[1][0], sc[1][1]));
-            return __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16));
-        };
-        uint32_t vmax = largest();
-        float poison[NT][2] = {};
-        const bool odd = vmax >= 0x7f80u;
-        if (odd) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t x = lds4(chunk + u * TB + 17 * HD + g * (HD / 8) / 32 * 32 + (i & ~1) * 2) >> (16 * (i & 1));
-                    if ((x & 0x7f80u) != 0x7f80u || !(ok >> u & 1u)) continue;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            if (base + 16 * u + i <= lim[nt][e]) poison[nt][e] = __uint_as_float(0x7fffffffu);
-                }
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    if ((sc[u][r] & 0x7f80u) == 0x7f80u) sc[u][r] &= 0xffff0000u;
-                    if ((sc[u][r] & 0x7f800000u) == 0x7f800000u) sc[u][r] &= 0x0000ffffu;
-                }
-            }
-            vmax = largest();
-        }
-        const int vnew = max(vexp, (int)(vmax >> 7));
-        const float shrink = exp2_int(vexp - vnew);  // 1 almost always
-        vexp = vnew;
-        bool keep = shrink == 1.f;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) keep = keep && alpha[nt][0] == 1.f && alpha[nt][1] == 1.f;
-        if (!__all_sync(0xffffffffu, keep)) {
+            const int vnew = max(vexp, (int)(vmax >> 7));
+            const float shrink = exp2_int(vexp - vnew);
+            vexp = vnew;
+            vscale = exp2_int(135 - vexp);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float f = alpha[nt][e] * shrink;
+                    float alpha = 1.f;
+                    if (top_m[nt][e] * fb > fmaf(mx[nt][e], fb, 8.f)) {
+                        alpha = exp2_fast((mx[nt][e] - top_m[nt][e]) * fb);
+                        mx[nt][e] = top_m[nt][e];
+                    }
+                    sum[nt][e] *= alpha;
+                    alpha *= shrink;
 #pragma unroll
-                    for (int i = 0; i < CT; ++i) o[nt][i][e] *= f, o[nt][i][e + 2] *= f;
+                    for (int i = 0; i < CT; ++i) o[nt][i][e] *= alpha, o[nt][i][e + 2] *= alpha;
                 }
         }
-        const float vscale = exp2_int(135 - vexp);  // the largest scale to [2^8, 2^9)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float off = mx[nt][e] == -INFINITY ? 0.f : -mx[nt][e] * fb;  // nothing seen so far: every score is -inf
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    s[nt][u][e] = exp2_fast(fmaf(s[nt][u][e], fb, off));
+                    s[nt][u][e + 2] = exp2_fast(fmaf(s[nt][u][e + 2], fb, off));
+                    sum[nt][e] += s[nt][u][e] + s[nt][u][e + 2];
+                }
+            }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             constexpr int CW = HD / 64;  // code words of a lane's piece: channels (HD / 8) g ..
