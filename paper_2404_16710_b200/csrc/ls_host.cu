@@ -2024,6 +2024,7 @@ Kv4Plan kv4_plan(int n_seq, int Hkv, int max_seq, bool may_split)
     if (getenv("LS_KV4_C") && may_split) p.splits = atoi(getenv("LS_KV4_C"));
     return p;
 }
+uint32_t divisor(int d) { return d > 1 ? 0xffffffffu / (uint32_t)d + 1u : 0u; }  // for fastdiv on the device
 int kv4_query_tile(int Q) { return Q <= 8 ? 1 : 2; }  // tiles of 8 queries a CTA takes
 int kv4_rows(int Q, int Hkv) { return (Q + 8 * kv4_query_tile(Q) - 1) / (8 * kv4_query_tile(Q)) * Hkv; }
 
@@ -2062,7 +2063,8 @@ int kv4_attn_launch(const Kv4Plan& plan, int n_seq, const uint16_t* q, int M, in
     at[2].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = lc.pdl ? 3 : 2;
-    LS_CK(cudaLaunchKernelEx(&cfg, kernel, q, M, G, pos0, c, pages, plan.S, out, scratch, status));
+    LS_CK(cudaLaunchKernelEx(&cfg, kernel, q, M, G, pos0, c, pages, log2_exact(plan.S), divisor(G), divisor(c.Hkv), out,
+                             scratch, status));
     if (plan.splits > 1)  // may move in while the splits finish; it waits for them before it reads
         LS_CK(launch(LaunchCtx{lc.st, true}, combine_kv4_kernel<HD>, dim3(M, G * c.Hkv, n_seq), dim3(HD / 2), 0, scratch, G, pos0,
                      c.max_seq, NT, c.Hkv, rows, plan.splits, out));

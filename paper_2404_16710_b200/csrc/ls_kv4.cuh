@@ -40,6 +40,12 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ int ld_now(const int32_t* p)
+{
+    int v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
 // 2^e, 0 below the denormals
 __device__ __forceinline__ float exp2_int(int e)
 {
@@ -131,8 +137,8 @@ __device__ __forceinline__ float kv4_unit(int hd) { return 1024.f * 1.4426950408
 template <int HD, int NT>
 __global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1)
 attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t* __restrict__ pos0_dev,
-                     const Kv4Cache cache, const unsigned char* __restrict__ pages, int S, uint16_t* __restrict__ out,
-                     float* __restrict__ scratch, int32_t* status)
+                     const Kv4Cache cache, const unsigned char* __restrict__ pages, int log2_S, uint32_t div_G, uint32_t div_Hkv,
+                     uint16_t* __restrict__ out, float* __restrict__ scratch, int32_t* status)
 {
     using SM = Kv4Smem<HD, NT>;
     constexpr int W = kKv4Warps;
@@ -150,33 +156,35 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     float2* sInStat = reinterpret_cast<float2*>(at += SM::kStat);   // [CTA][NT * 8]
     pdl_launch_dependents();
     pdl_wait();
-    const int splits = gridDim.x / S, split = blockIdx.x / S, rank = blockIdx.x % S, b = blockIdx.z;
+    const int S = 1 << log2_S, splits = gridDim.x >> log2_S, split = blockIdx.x >> log2_S, rank = blockIdx.x & (S - 1), b = blockIdx.z;
     if (S > 1) cluster_arrive_relaxed();  // this CTA is there
-    const int head = blockIdx.y % cache.Hkv, q0 = blockIdx.y / cache.Hkv * (NT * 8);
+    const int tile_y = fastdiv(blockIdx.y, cache.Hkv, div_Hkv), head = blockIdx.y - tile_y * cache.Hkv, q0 = tile_y * (NT * 8);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int Q = M * G, Hq = cache.Hkv * G;
 
-    // The first accesses to memory, all before the first use of any: this thread's piece of a query, the page-table
-    // entries of its warp's first chunk, the position.
+    // The first accesses to memory, all before the first use of any (volatile: the compiler moves plain loads down to
+    // their use, one latency after the other): this thread's piece of a query, the page-table entries of its warp's first
+    // chunk, the position.
     constexpr int PER = NJ * 4;  // threads that make a query's operand: channels 32 j + 8 t .. + 7
     static_assert(NT * 8 * PER <= W * 32, "a thread has one piece");
     const int piece_q = threadIdx.x / PER, piece_j = threadIdx.x % PER / 4, piece_t = threadIdx.x % 4;
     uint4 piece = make_uint4(0, 0, 0, 0);
-    if (piece_q < NT * 8 && q0 + piece_q < Q)
-        piece = *reinterpret_cast<const uint4*>(q + (((long long)b * M + (q0 + piece_q) / G) * Hq + head * G + (q0 + piece_q) % G) * HD +
-                                                32 * piece_j + 8 * piece_t);
+    if (piece_q < NT * 8 && q0 + piece_q < Q) {
+        const int row = fastdiv(q0 + piece_q, G, div_G), in_group = q0 + piece_q - row * G;
+        piece = ld_reuse16(q + (((long long)b * M + row) * Hq + head * G + in_group) * HD + 32 * piece_j + 8 * piece_t);
+    }
     // page-table entries of this warp's next chunk (a chunk lies in one page, unless pages are of 16), read before
     // anything says whether it is needed: the positions below max_seq have entries
     const int step = gridDim.x * W * kKv4Chunk, base0 = (blockIdx.x * W + warp) * kKv4Chunk;
     const int32_t* table = cache.table + (long long)b * cache.table_stride;
     int next_page[2];
     auto look_up = [&](int base) {
-        next_page[0] = base < cache.max_seq ? table[base >> cache.page_shift] : 0;
-        next_page[1] = next_page[0];
-        if (cache.page_shift == 4) next_page[1] = base + 16 < cache.max_seq ? table[(base + 16) >> 4] : 0;
+        next_page[0] = next_page[1] = 0;
+        if (base < cache.max_seq) next_page[0] = ld_now(table + (base >> cache.page_shift));
+        if (cache.page_shift == 4 && base + 16 < cache.max_seq) next_page[1] = ld_now(table + ((base + 16) >> 4));
     };
     look_up(base0);
-    const int pos0 = pos0_dev[b];
+    const int pos0 = ld_now(pos0_dev + b);
 
     // last position that this lane's two queries of each 8 see, and over the CTA's queries the last and the first of those
     int lim[NT][2], top = -1, low = 0x7fffffff;
@@ -185,7 +193,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int qi = q0 + nt * 8 + 2 * t + e;
-            lim[nt][e] = qi < Q ? kv4_position(pos0, qi / G, cache.max_seq, status) : -1;
+            lim[nt][e] = qi < Q ? kv4_position(pos0, fastdiv(qi, G, div_G), cache.max_seq, status) : -1;
             top = max(top, lim[nt][e]);
             if (qi < Q) low = min(low, lim[nt][e]);
         }
@@ -217,12 +225,13 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
                 for (int u = 0; u < 2; ++u) {
                     const int p = in_base + 16 * u;
                     if (p > top) continue;
-                    if ((unsigned)next_page[u] >= (unsigned)cache.n_pages) {
+                    const int page = cache.page_shift > 4 ? next_page[0] : next_page[u];
+                    if ((unsigned)page >= (unsigned)cache.n_pages) {
                         if (status) *status = DEV_BAD_PAGE;
                         continue;
                     }
                     ok_bits |= 1u << (2 * in_count + u);
-                    const unsigned char* src = source(p, next_page[u]);
+                    const unsigned char* src = source(p, page);
 #pragma unroll
                     for (int i = 0; i < TB / 512; ++i) cp_async16_cg(dst + u * TB + 512 * i, src + 512 * i, 16);
                     if (lane < TB % 512 / 16) cp_async16_cg(dst + u * TB + TB / 512 * 512, src + TB / 512 * 512, 16);
@@ -519,7 +528,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     if (S > 1) cluster_wait();  // the others are there
     __syncthreads();
     // ---- the CTA's, sent to the CTA that finishes them: piece x holds two queries x two channels
-    const int share = SM::kItems / S;
+    const int share = SM::kItems >> log2_S;
     for (int x = threadIdx.x; x < SM::kItems; x += W * 32) {
         const int c = x / (CT * 32) * 8 + 2 * (x & 3);  // its first query
         if (q0 + c >= Q) continue;
@@ -539,7 +548,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             r.x = fmaf(f0 * unit, v.x, r.x), r.z = fmaf(f0 * unit, v.z, r.z);
             r.y = fmaf(f1 * unit, v.y, r.y), r.w = fmaf(f1 * unit, v.w, r.w);
         }
-        const int to = x / share;
+        const int to = x / (SM::kItems / 16) >> (4 - log2_S);  // x / share
         st_cluster_f4(map_cluster(smem_u32(sIn) + (rank * share + x - to * share) * 16, to), r);
         if ((x / 4) % (CT * 8) == 0)  // one of the pieces with these queries: their statistics, to all
             for (int d = 0; d < S; ++d) {
@@ -564,7 +573,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             const float* v = reinterpret_cast<const float*>(sIn + r * share + y / 2);
             sum_l = fmaf(f, st.y, sum_l), v0 = fmaf(f, v[e], v0), v1 = fmaf(f, v[e + 2], v1);
         }
-        const int row = qi / G, ch = (l >> 2) * (HD / 8) + 2 * (x / 32 % CT);
+        const int row = fastdiv(qi, G, div_G), ch = (l >> 2) * (HD / 8) + 2 * (x / 32 % CT);
         if (splits > 1) {  // to be finished by combine_kv4_kernel
             float* to = scratch + (kv4_partial(b, gridDim.y, blockIdx.y, splits, split) * (NT * 8) + c) * (HD + 2);
             *reinterpret_cast<float2*>(to + ch) = make_float2(v0, v1);
@@ -572,8 +581,9 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             continue;
         }
         const bool none = (long long)pos0 + row < 0 || (long long)pos0 + row >= cache.max_seq;
-        const uint32_t v = none ? 0u : pack_bf16(v0 / sum_l, v1 / sum_l);
-        *reinterpret_cast<uint32_t*>(out + (((long long)b * M + row) * Hq + head * G + qi % G) * HD + ch) = v;
+        const float inv = 1.f / sum_l;
+        const uint32_t v = none ? 0u : pack_bf16(v0 * inv, v1 * inv);
+        *reinterpret_cast<uint32_t*>(out + (((long long)b * M + row) * Hq + head * G + qi - row * G) * HD + ch) = v;
     }
 }
 
@@ -600,7 +610,8 @@ combine_kv4_kernel(const float* __restrict__ scratch, int G, const int32_t* __re
         const float f = top == -INFINITY ? 0.f : exp2_fast((st.x - top) * fb);
         l = fmaf(f, st.y, l), x = fmaf(f, v.x, x), y0 = fmaf(f, v.y, y0);
     }
-    const uint32_t r = p < 0 || p >= max_seq ? 0u : pack_bf16(x / l, y0 / l);
+    const float inv = 1.f / l;
+    const uint32_t r = p < 0 || p >= max_seq ? 0u : pack_bf16(x * inv, y0 * inv);
     *reinterpret_cast<uint32_t*>(out + (((long long)b * gridDim.x + m) * gridDim.y + hq) * HD + ch) = r;
 }
 
