@@ -17,8 +17,6 @@
 // * p is rounded to f16's 11 bits (2^-12 of it; 2^-25 absolute below 2^-14, when the largest p so far is 1 or
 //   more), well below the rounding of a bf16 result.  Scores, maxima, sums and O are fp32.
 #pragma once
-#include <cuda_fp16.h>
-
 #include "ls_attention.cuh"
 #include "ls_w4.cuh"
 
@@ -60,22 +58,6 @@ __device__ __forceinline__ uint32_t map_cluster(uint32_t addr, int rank)
 {
     uint32_t r;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-// D (fp32, 16x8) = A (f16, 16x16) * B (f16, 16x8) + C
-__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                              uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3)
-{
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-        "{%10,%11,%12,%13};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b)

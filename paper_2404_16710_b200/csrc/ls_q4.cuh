@@ -109,6 +109,23 @@ __device__ __forceinline__ uint4 q4_values(uint32_t w, uint32_t s2)
                       mul_bf16x2(q4_bf16x2(w, 2), s2), mul_bf16x2(q4_bf16x2(w, 3), s2));
 }
 
+// D (fp32, 16x8) = A (f16, 16x16) * B (f16, 16x8) + C
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                              uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+        "{%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
 // ------------------------------------------------------------------ weights: bf16 -> blocks, blocks -> bf16
 // One warp per block of 16 rows x 128 columns: lane 4 g + t holds rows g and g + 8, columns 32 j + 8 t .. + 7.
 // NG groups of 128 / NG columns per block.  grid.x * warps covers the blocks of all rows, row blocks slowest.
