@@ -1886,11 +1886,11 @@ int w4_split(int n_tiles)
     return n_tiles <= 148 ? 4 : n_tiles < 1024 ? 3 : 2;
 }
 
-template <int NG, int NT, int D, bool HS, bool F16, int TG>
+template <int NG, int NT, int D, bool HS, int TG>
 int w4_launch(const unsigned char* packed, const uint16_t* h, int M, int N, int K, float* out, int residual,
               const LaunchCtx& lc)
 {
-    auto* kernel = linear_w4_kernel<NG, NT, D, HS, F16, TG>;
+    auto* kernel = linear_w4_kernel<NG, NT, D, HS, TG>;
     static std::mutex mu;
     static int sms[64] = {};  // SMs of the device; asked for once, when the kernel's shared memory is raised
     int dev = 0;
@@ -1907,8 +1907,7 @@ int w4_launch(const unsigned char* packed, const uint16_t* h, int M, int N, int 
     }
     const int n_tiles = (int)(((int64_t)N + 15) / 16), kb = w4_kblocks(K), lks = w4_split(n_tiles);
     const int teams = kW4Warps >> lks, grid = ((n_tiles + TG - 1) / TG + teams - 1) / teams;
-    const size_t smem = w4_part_bytes<NT>() + w4_ring_bytes<NG>(D) + (HS ? (size_t)M * w4_h_stride(kb) : 0) +
-                        (F16 ? w4_aux_bytes<NG>(kb) : 0);
+    const size_t smem = w4_part_bytes<NT>() + w4_ring_bytes<NG>(D) + (HS ? (size_t)M * w4_h_stride(kb) : 0);
     LS_CK(launch(lc, kernel, dim3((unsigned)(grid < n_sm ? grid : n_sm)), dim3(kW4Warps * 32), smem, packed, h, M, N, K, kb,
                  n_tiles, lks, out, residual));
     return LS_OK;
@@ -1918,20 +1917,15 @@ template <int NG, int NT>
 int w4_launch_nt(const unsigned char* packed, const uint16_t* h, int M, int N, int K, float* out, int residual,
                  const LaunchCtx& lc)
 {
-    const int kb = w4_kblocks(K);
-    const int64_t room = kW4SmemMax - w4_part_bytes<NT>() - (int64_t)M * w4_h_stride(kb);
-    // f16 operands where an SM has at least some 7 tiles to make up for turning h into f16, and h fits for any M (the
-    // choice may not depend on M): K <= 5120
-    if (N > 16 * 1023 && kb <= 40) {
-        const int64_t left = room - w4_aux_bytes<NG>(kb);
-        constexpr int TG = NT;  // two tiles at a time where h has more than 8 rows
-        if (left >= w4_ring_bytes<NG>(6)) return w4_launch<NG, NT, 6, true, true, TG>(packed, h, M, N, K, out, residual, lc);
-        if (left >= w4_ring_bytes<NG>(4)) return w4_launch<NG, NT, 4, true, true, TG>(packed, h, M, N, K, out, residual, lc);
-        return w4_launch<NG, NT, 2, true, true, 1>(packed, h, M, N, K, out, residual, lc);
-    }
-    if (room >= w4_ring_bytes<NG>(6)) return w4_launch<NG, NT, 6, true, false, 1>(packed, h, M, N, K, out, residual, lc);
-    if (room >= w4_ring_bytes<NG>(3)) return w4_launch<NG, NT, 3, true, false, 1>(packed, h, M, N, K, out, residual, lc);
-    return w4_launch<NG, NT, 6, false, false, 1>(packed, h, M, N, K, out, residual, lc);
+    const int64_t room = kW4SmemMax - w4_part_bytes<NT>() - (int64_t)M * w4_h_stride(w4_kblocks(K));
+    // more than 8 rows through a large matrix: two tiles at a time (128256 x 4096, 16 rows: 71.4 us, one at a time 75.2);
+    // with few tiles an SM the teams would run out of pairs
+    if (NT == 2 && N > 16 * 1023 && room >= w4_ring_bytes<NG>(4))
+        return room >= w4_ring_bytes<NG>(6) ? w4_launch<NG, 2, 6, true, 2>(packed, h, M, N, K, out, residual, lc)
+                                            : w4_launch<NG, 2, 4, true, 2>(packed, h, M, N, K, out, residual, lc);
+    if (room >= w4_ring_bytes<NG>(6)) return w4_launch<NG, NT, 6, true, 1>(packed, h, M, N, K, out, residual, lc);
+    if (room >= w4_ring_bytes<NG>(3)) return w4_launch<NG, NT, 3, true, 1>(packed, h, M, N, K, out, residual, lc);
+    return w4_launch<NG, NT, 6, false, 1>(packed, h, M, N, K, out, residual, lc);
 }
 
 template <int NG>

@@ -6,11 +6,11 @@
 // Tokens are the 16-row operand of mma.sync in both products, queries (row, head of the KV group) the
 // 8-column one: S^T = K Q^T and O^T = V^T P^T.  At 4 bits a value the kernel is bound by the instructions
 // that turn nibbles into operands, so both products run in f16, whose formats make those few:
-// * K: a nibble u = c + 8 left where it is, all other bits cleared, IS an f16 number, u 2^-24 (bits 0..3) or
-//   u 2^-20 (bits 4..7), a denormal, which the tensor cores take exactly.  No offset, no conversion: 5
-//   instructions for 8 codes.  The queries' columns that meet the second kind are scaled by 2^-4, and the
-//   sum of a scale group starts at -8 sum q instead of 0.  Queries are scaled by powers of two of their own
-//   so that the largest component is in [2^14, 2^15): what f16 then cannot hold is 2^-39 of it.
+// * K: a nibble u = c + 8 or-ed to 1024 is 1024 + u (bits 0..3) or 1024 + 16 u (bits 4..7), and one instruction makes
+//   c of it: 9 instructions for 8 codes, 11 in bf16, which has too few bits for the second kind.  (The bare nibble is
+//   an f16 denormal, u 2^-24, that the tensor cores multiply without any conversion -- but they align products by
+//   exponent fields, and sums of denormals came out with an error of 2^-20 instead of 2^-24.)  Queries are scaled by
+//   powers of two of their own so that the largest component is in [2^14, 2^15): what f16 then cannot hold is 2^-39 of it.
 // * V: a nibble moved to bits 4..7 or-ed to 1024 is 1024 + 16 u, and one multiply-add makes c s of it:
 //   (1024 + 16 u) (s / 16) - 72 s.  A scale has 5 significant bits, so every step is exact, for scales down to 2^-25
 //   of the largest one the warp has met (the power of two it is divided by is kept beside O).
@@ -80,7 +80,7 @@ __device__ __forceinline__ uint32_t q4_scaled_f16x2(uint32_t w, int i, uint32_t 
     return fma_f16x2(r, s16, s72);
 }
 
-// shared memory of a CTA: rings (later each warp's O in its own), queries, their offsets and factors, the
+// shared memory of a CTA: rings (later each warp's O in its own), queries and their factors, the
 // warps' statistics, and what the CTAs of the cluster send one another
 constexpr int kKv4MaxCluster = 16;
 template <int HD, int NT>
@@ -92,11 +92,10 @@ struct Kv4Smem {
     static constexpr int kRing = W * kWarpRing;
     static constexpr int kQ = NT * HD / 32 * 32 * 16;          // [NT][group][lane] 16 bytes
     static constexpr int kInbox = kItems * 16;                 // [CTA][its share of the pieces]
-    static constexpr int kInit = NT * 8 * (HD / 32) * 4;       // -8 sum q [query][group]
     static constexpr int kFactor = NT * 8 * 4;                 // 2^e [query]
     static constexpr int kStat = W * NT * 8 * 8 + W * 4;       // (max, sum) of the warps, units of their O
     static constexpr int kInStat = kKv4MaxCluster * NT * 8 * 8;  // (max, sum) of the CTAs
-    static constexpr int kBytes = kRing + kQ + kInbox + kInit + kFactor + kStat + kInStat;
+    static constexpr int kBytes = kRing + kQ + kInbox + kFactor + kStat + kInStat;
     static_assert(kItems / (NT * 32) * 512 * NT <= kWarpRing, "a warp's O fits its ring");
 };
 
@@ -105,8 +104,8 @@ __device__ __forceinline__ long long kv4_partial(int b, int rows, int y, int spl
 {
     return ((long long)b * rows + y) * splits + s;
 }
-// log2(e) / sqrt(hd), and the 2^10 that the operands' units leave (see the kernel)
-__device__ __forceinline__ float kv4_unit(int hd) { return 1024.f * 1.4426950408889634f / sqrtf((float)hd); }
+// log2(e) / sqrt(hd), over the 2^14 that queries are scaled to
+__device__ __forceinline__ float kv4_unit(int hd) { return 0x1p-14f * 1.4426950408889634f / sqrtf((float)hd); }
 
 // grid (splits * S, Hkv * query tiles, n_seq) in clusters of S CTAs.  The warps of a (sequence, KV head) take
 // the 32-position chunks of the cache in turn by absolute position, each through a cp.async ring of its own and
@@ -131,8 +130,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     unsigned char* at = kv4_smem + SM::kRing;
     uint4* sQ = reinterpret_cast<uint4*>(at);
     float4* sIn = reinterpret_cast<float4*>(at += SM::kQ);
-    float* sInit = reinterpret_cast<float*>(at += SM::kInbox);
-    float* sF = reinterpret_cast<float*>(at += SM::kInit);
+    float* sF = reinterpret_cast<float*>(at += SM::kInbox);
     float2* sStat = reinterpret_cast<float2*>(at += SM::kFactor);   // [W][NT * 8]
     float* sUnit = reinterpret_cast<float*>(sStat + W * NT * 8);     // [W]
     float2* sInStat = reinterpret_cast<float2*>(at += SM::kStat);   // [CTA][NT * 8]
@@ -229,8 +227,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
 #pragma unroll
     for (int i = 0; i < D - 1; ++i) fetch();
 
-    // Queries as B operands: lane 4 g + t of group j holds channels 32 j + 8 t .. + 7 of query g, columns 2, 3, 6 and 7
-    // of the eight times 2^-4.
+    // Queries as B operands: lane 4 g + t of group j holds channels 32 j + 8 t .. + 7 of query g.
     if (piece_q < NT * 8) {  // whole warps
         const uint32_t x[4] = {piece.x, piece.y, piece.z, piece.w};
         uint32_t am = 0;  // the largest finite component
@@ -243,31 +240,19 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
         for (int o = 1; o < PER; o *= 2) am = max(am, __shfl_xor_sync(0xffffffffu, am, o));
         const int e = max((int)(am >> 7), 15) - 127;  // |q| < 2^(e + 1)
         const float up = exp2_int(14 - e);
-        float y[8], sum = 0.f;
+        float y[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            y[k] = (k & 1 ? bf16hi(x[k / 2]) : bf16lo(x[k / 2])) * up;
-            sum += y[k];
-            if (k & 2) y[k] *= 0.0625f;
-        }
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        for (int k = 0; k < 8; ++k) y[k] = (k & 1 ? bf16hi(x[k / 2]) : bf16lo(x[k / 2])) * up;
         sQ[((piece_q / 8) * NJ + piece_j) * 32 + (piece_q % 8) * 4 + piece_t] =
             make_uint4(pack_f16(y[0], y[1]), pack_f16(y[2], y[3]), pack_f16(y[4], y[5]), pack_f16(y[6], y[7]));
-        if (piece_t == 0) sInit[piece_q * NJ + piece_j] = sum * -0x1p-21f;  // -8 sum q, in units of 2^-24
         if (threadIdx.x % PER == 0) sF[piece_q] = exp2_int(e);
     }
     __syncthreads();
-    float init[NT][NJ][2], fa[NT][2];
+    float fa[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int c = nt * 8 + 2 * t + e;
-            fa[nt][e] = sF[c];
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) init[nt][j][e] = sInit[c * NJ + j];
-        }
+        for (int e = 0; e < 2; ++e) fa[nt][e] = sF[nt * 8 + 2 * t + e];
     // score * log2(e) = sum_g s_g c_g * 2^e * fb
     const float fb = kv4_unit(HD);
 
@@ -317,15 +302,18 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             }
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
-                const uint32_t l8 = wl[j] >> 8, h8 = wh[j] >> 8;
+                uint32_t a[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    a[2 * i] = q4_f16x2(wl[j] >> (8 * (i / 2)), i % 2);
+                    a[2 * i + 1] = q4_f16x2(wh[j] >> (8 * (i / 2)), i % 2);
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const uint4 bq = sQ[(nt * NJ + j) * 32 + lane];
                     float c[4];
-                    mma_f16_16816(c, wl[j] & 0x000f000fu, wh[j] & 0x000f000fu, wl[j] & 0x00f000f0u, wh[j] & 0x00f000f0u, bq.x,
-                                  bq.y, init[nt][j][0], init[nt][j][1], init[nt][j][0], init[nt][j][1]);
-                    mma_f16_16816(c, l8 & 0x000f000fu, h8 & 0x000f000fu, l8 & 0x00f000f0u, h8 & 0x00f000f0u, bq.z, bq.w, c[0],
-                                  c[1], c[2], c[3]);
+                    mma_f16_16816(c, a[0], a[1], a[2], a[3], bq.x, bq.y, 0.f, 0.f, 0.f, 0.f);
+                    mma_f16_16816(c, a[4], a[5], a[6], a[7], bq.z, bq.w, c[0], c[1], c[2], c[3]);
                     if (j == 0) {
                         s[nt][u][0] = s_lo[j] * c[0], s[nt][u][1] = s_lo[j] * c[1];
                         s[nt][u][2] = s_hi[j] * c[2], s[nt][u][3] = s_hi[j] * c[3];

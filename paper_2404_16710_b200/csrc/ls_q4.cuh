@@ -96,6 +96,19 @@ __device__ __forceinline__ uint32_t q4_bf16x2(uint32_t w, int i)
     asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(r), "r"(0x43084308u));  // - 136
     return r;
 }
+// codes of nibbles 0 (i = 0) or 1 (i = 1) of the two halves of w as f16 numbers c (exact), which has bits enough for both
+__device__ __forceinline__ uint32_t q4_f16x2(uint32_t w, int i)
+{
+    uint32_t r;
+    if (i == 0) {
+        asm("lop3.b32 %0, %1, 0x000f000f, 0x64006400, 0xea;" : "=r"(r) : "r"(w));
+        asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(r), "r"(0xe408e408u));  // 1024 + u - 1032
+    } else {
+        asm("lop3.b32 %0, %1, 0x00f000f0, 0x64006400, 0xea;" : "=r"(r) : "r"(w));
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(r), "r"(0x2c002c00u), "r"(0xd480d480u));  // (1024 + 16 u) / 16 - 72
+    }
+    return r;
+}
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
 {
     uint32_t r;

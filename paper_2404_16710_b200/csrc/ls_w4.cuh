@@ -2,8 +2,6 @@
 // M <= 16 rows (LayerSkip Sec. 4.3: a draft pass has one row, a verify pass num_draft + 1).  Format and
 // block layout: ls_q4.cuh.
 #pragma once
-#include <type_traits>
-
 #include "ls_prefill.cuh"
 #include "ls_q4.cuh"
 
@@ -48,8 +46,6 @@ __host__ __device__ constexpr int w4_part_bytes() { return kW4Warps * 32 * NT * 
 template <int NG>
 __host__ __device__ constexpr int w4_ring_bytes(int D) { return kW4Warps * D * w4_block_bytes(NG); }
 __host__ __device__ constexpr int w4_h_stride(int kblocks) { return kblocks * kQ4Cols * 2 + 64; }
-template <int NG>
-__host__ __device__ constexpr int w4_aux_bytes(int kblocks) { return kblocks * (NG + 1) * 16 * 4; }
 
 // what a lane reads of a block: the codes of rows g and g + 8 (its 16-byte pieces) and the rows' scales
 template <int NG>
@@ -108,100 +104,6 @@ __device__ __forceinline__ void w4_block_mma(const W4Regs<NG>& w, const uint4 (&
     }
 }
 
-// The same on raw nibbles.  A nibble u = c + 8 left where it is, all other bits of the half cleared, IS an f16
-// number, u 2^-24 (bits 0..3) or u 2^-20 (bits 4..7), a denormal, which the tensor cores take exactly: 5 instructions
-// for 8 codes instead of 11.  The second kind meets columns of h scaled by 2^-4, and a group's sum starts at -8 sum h
-// instead of 0 (init).
-// TG tiles share what is read of h: rows of h in f16 (32-column group j of row nt * 8 + g at b + j * 64 +
-// nt * rows8 bytes), scaled per row and block by a power of two that f undoes.
-template <int NG, int NT, int TG>
-__device__ __forceinline__ void w4_block_mma_f16(const W4Regs<NG> (&w)[TG], const uint32_t (&b)[NT], const float* aux,
-                                                 float (&acc)[TG][NT][4])
-{
-    float c[TG][NT][4], sum[TG][NT][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint4 bj[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            bj[nt] = lds16(b[nt] + j * 64);
-            if (j % (4 / NG) == 0) {
-                const float2 z = *reinterpret_cast<const float2*>(aux + j * NG / 4 * 16 + nt * 8);
-#pragma unroll
-                for (int u = 0; u < TG; ++u) c[u][nt][0] = c[u][nt][2] = z.x, c[u][nt][1] = c[u][nt][3] = z.y;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < TG; ++u) {
-            const uint32_t wl = j == 0 ? w[u].lo.x : j == 1 ? w[u].lo.y : j == 2 ? w[u].lo.z : w[u].lo.w;
-            const uint32_t wh = j == 0 ? w[u].hi.x : j == 1 ? w[u].hi.y : j == 2 ? w[u].hi.z : w[u].hi.w;
-            const uint32_t l8 = wl >> 8, h8 = wh >> 8;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float(&d)[4] = c[u][nt];
-                mma_f16_16816(d, wl & 0x000f000fu, wh & 0x000f000fu, wl & 0x00f000f0u, wh & 0x00f000f0u, bj[nt].x, bj[nt].y, d[0],
-                              d[1], d[2], d[3]);
-                mma_f16_16816(d, l8 & 0x000f000fu, h8 & 0x000f000fu, l8 & 0x00f000f0u, h8 & 0x00f000f0u, bj[nt].z, bj[nt].w, d[0],
-                              d[1], d[2], d[3]);
-                if ((j + 1) % (4 / NG) == 0) {
-                    const float s0 = W4Regs<NG>::scale(w[u].s_lo, j * NG / 4), s1 = W4Regs<NG>::scale(w[u].s_hi, j * NG / 4);
-                    const bool first = j == 4 / NG - 1;
-                    float(&r)[4] = sum[u][nt];
-                    r[0] = first ? s0 * d[0] : fmaf(s0, d[0], r[0]);
-                    r[1] = first ? s0 * d[1] : fmaf(s0, d[1], r[1]);
-                    r[2] = first ? s1 * d[2] : fmaf(s1, d[2], r[2]);
-                    r[3] = first ? s1 * d[3] : fmaf(s1, d[3], r[3]);
-                }
-            }
-        }
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const float2 f = *reinterpret_cast<const float2*>(aux + NG * 16 + nt * 8);
-#pragma unroll
-        for (int u = 0; u < TG; ++u) {
-            acc[u][nt][0] = fmaf(f.x, sum[u][nt][0], acc[u][nt][0]);
-            acc[u][nt][1] = fmaf(f.y, sum[u][nt][1], acc[u][nt][1]);
-            acc[u][nt][2] = fmaf(f.x, sum[u][nt][2], acc[u][nt][2]);
-            acc[u][nt][3] = fmaf(f.y, sum[u][nt][3], acc[u][nt][3]);
-        }
-    }
-}
-
-// Eight neighbouring values of a row of h as that B operand; the 16 lanes of a half warp hold the 128 columns of a
-// block.  The largest finite value goes to [2^14, 2^15): what f16 then cannot hold is 2^-39 of it, far below what an
-// fp32 sum can.  sum: -8 2^-24 times the sum over this lane's group of 128 / NG columns, in the scaled units; f: 2^e.
-template <int NG>
-__device__ __forceinline__ uint4 w4_h_f16(const uint4& v, float& sum, float& f)
-{
-    const uint32_t half = 0xffffu << (threadIdx.x & 16), x[4] = {v.x, v.y, v.z, v.w};
-    uint32_t a[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] = x[k] & 0x7fff7fffu;
-    uint32_t m2 = __vmaxu2(__vmaxu2(a[0], a[1]), __vmaxu2(a[2], a[3])), am = max(m2 & 0xffffu, m2 >> 16);
-    if (__any_sync(half, am >= 0x7f80u)) {  // an infinity or a NaN: it stays one; the others count
-        am = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = a[k] & 0xffffu, hi = a[k] >> 16;
-            am = max(am, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-        }
-    }
-#pragma unroll
-    for (int o = 1; o < 16; o *= 2) am = max(am, __shfl_xor_sync(half, am, o));
-    const uint32_t e = max(am >> 7, 15u);  // exponent field
-    f = __uint_as_float(e << 23);
-    const float up = __uint_as_float((268u - e) << 23), up4 = up * 0.0625f;
-    float y[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) y[k] = (k & 1 ? bf16hi(x[k / 2]) : bf16lo(x[k / 2])) * (k & 2 ? up4 : up);
-    sum = fmaf(16.f, (y[2] + y[3]) + (y[6] + y[7]), (y[0] + y[1]) + (y[4] + y[5]));
-#pragma unroll
-    for (int o = 1; o < 16 / NG; o *= 2) sum += __shfl_xor_sync(half, sum, o);
-    sum *= -0x1p-21f;
-    return make_uint4(pack_f16(y[0], y[1]), pack_f16(y[2], y[3]), pack_f16(y[4], y[5]), pack_f16(y[6], y[7]));
-}
-
 // One CTA per SM; its 16 warps form teams of 2^lks, and a team takes every (teams of the grid)-th group of TG tiles of
 // 16 rows (TG = 2 halves what is read of h in shared memory, which bounds the kernel for 16 rows of h).  Of a tile's blocks each warp of the team has a fixed share, consecutive along K, and keeps the
 // next D of its sequence of blocks (which runs on across tiles) in flight in a ring of its own; the team
@@ -209,11 +111,11 @@ __device__ __forceinline__ uint4 w4_h_f16(const uint4& v, float& sum, float& f)
 // zeros); otherwise, for h larger than that, it comes through L1.
 // The codes are the A operand of mma.sync, the rows of h the B operand; a group's products are summed in fp32 by
 // the tensor cores and multiplied by the group's scale (a lane holds rows g and g + 8 of a tile) when they join
-// the running sum.  Turning codes into operands bounds the kernel: as exact small integers in bf16, or (F16) as
-// raw nibbles, for which every CTA first turns all of h into f16 -- worth it where a CTA has many tiles.  Which blocks a warp adds, and in which order the
+// the running sum.  Turning codes into operands (11 instructions for 8 codes, 7 of them on a pipe of half rate) bounds
+// the kernel.  Which blocks a warp adds, and in which order the
 // warps' sums are added, depends on N and K only: a row's result does not depend on how many rows share
 // the pass.
-template <int NG, int NT, int D, bool HS, bool F16, int TG>
+template <int NG, int NT, int D, bool HS, int TG>
 __global__ void __launch_bounds__(kW4Warps * 32, 1)
 linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __restrict__ h, int M, int N, int K,
                  int kblocks, int n_tiles, int lks, float* __restrict__ out, int residual)
@@ -253,42 +155,12 @@ linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __res
     };
     static_assert(D % TG == 0, "whole groups of blocks in the ring");
 #pragma unroll
-    for (int i = 0; i < D / TG; ++i) fetch();  // weights: no kernel before this one writes them
+    for (int i = 0; i < D / TG - 1; ++i) fetch();  // weights: no kernel before this one writes them
     pdl_wait();
 
     const uint32_t hs = smem_u32(w4_smem) + w4_part_bytes<NT>() + w4_ring_bytes<NG>(D);
     const int stride = w4_h_stride(kblocks);
-    float* aux = reinterpret_cast<float*>(w4_smem + w4_part_bytes<NT>() + w4_ring_bytes<NG>(D) + M * stride);  // F16: [block][NG + 1][16 rows]
-    if (F16) {
-        for (int i = threadIdx.x; i < kblocks * 16; i += kW4Warps * 32) {
-            const int r = i & 15;  // lane of the half warp: columns 8 r .. of block i / 16
-            auto rows = [&](int m0, auto count) {  // count rows at a time: their shuffles overlap
-                constexpr int U = decltype(count)::value;
-                uint4 v[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    v[u] = m0 + u < M && 8 * i < K ? *reinterpret_cast<const uint4*>(h + (long long)(m0 + u) * K + 8 * i)
-                                                   : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    float sum, f;
-                    v[u] = w4_h_f16<NG>(v[u], sum, f);
-                    if (m0 + u >= M) continue;
-                    *reinterpret_cast<uint4*>(w4_smem + (hs - smem_u32(w4_smem)) + (m0 + u) * stride + i * 16) = v[u];
-                    float* to = aux + (i >> 4) * (NG + 1) * 16 + m0 + u;
-                    if (r % (16 / NG) == 0) to[r / (16 / NG) * 16] = sum;
-                    if (r == 0) to[NG * 16] = f;
-                }
-            };
-            if (M <= 2)
-                for (int m = 0; m < M; ++m) rows(m, std::integral_constant<int, 1>());
-            else if (M <= 4)
-                rows(0, std::integral_constant<int, 4>());
-            else
-                for (int m = 0; m < M; m += 8) rows(m, std::integral_constant<int, 8>());
-        }
-        __syncthreads();
-    } else if (HS) {
+    if (HS) {
         for (int i = threadIdx.x; i < kblocks * 16; i += kW4Warps * 32) {
             const int bytes = 8 * i < K ? 16 : 0;
             const uint16_t* s = h + (bytes ? 8 * i : 0);
@@ -314,6 +186,7 @@ linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __res
     for (int group = group0; group < n_groups; group += group_step) {
         float acc[TG][NT][4] = {};
         for (int kb = kb0; kb < kb0 + nkb; ++kb) {
+            fetch();
             cp_async_wait<D / TG - 1>();  // the oldest of the blocks in flight
             __syncwarp();
             W4Regs<NG> w[TG];
@@ -321,32 +194,24 @@ linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __res
             for (int u = 0; u < TG; ++u) w[u].load(at + u * BB, lane);
             at += TG * BB;
             if (at == ring + D * BB) at = ring;
-            __syncwarp();  // every lane has them in registers: their place is free
-            fetch();
-            if constexpr (F16) {
-                uint32_t b[NT];
+            uint4 b[NT][4];
+            if (HS) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) b[nt] = hoff[nt] + kb * 256;
-                w4_block_mma_f16<NG, NT, TG>(w, b, aux + kb * (NG + 1) * 16 + 2 * t, acc);
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) b[nt][j] = lds16(hoff[nt] + kb * 256 + j * 64);
             } else {
-                uint4 b[NT][4];
-                if (HS) {
+                const bool whole = (kb + 1) * kQ4Cols <= K;  // only the last block has columns beyond K
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) b[nt][j] = lds16(hoff[nt] + kb * 256 + j * 64);
-                } else {
-                    const bool whole = (kb + 1) * kQ4Cols <= K;  // only the last block has columns beyond K
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            b[nt][j] = whole || kb * kQ4Cols + 32 * j + 8 * t < K ? ld_reuse16(hrow[nt] + kb * kQ4Cols + 32 * j)
-                                                                                  : make_uint4(0, 0, 0, 0);
-                }
-#pragma unroll
-                for (int u = 0; u < TG; ++u) w4_block_mma<NG, NT>(w[u], b, acc[u]);
+                    for (int j = 0; j < 4; ++j)
+                        b[nt][j] = whole || kb * kQ4Cols + 32 * j + 8 * t < K ? ld_reuse16(hrow[nt] + kb * kQ4Cols + 32 * j)
+                                                                              : make_uint4(0, 0, 0, 0);
             }
+#pragma unroll
+            for (int u = 0; u < TG; ++u) w4_block_mma<NG, NT>(w[u], b, acc[u]);
+            __syncwarp();  // every lane has read the blocks before the ring comes round to them
         }
 #pragma unroll
         for (int u = 0; u < TG; ++u) {
@@ -362,7 +227,6 @@ linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __res
                 if (m >= M || n >= N) continue;
                 float s = 0.f;
                 for (int v = 0; v < KS; ++v) s += sums[v * 128 * NT + x];
-                if (F16) s *= 1024.f;  // 2^24 of the nibbles over 2^14 of h
                 float* o = out + (long long)m * N + n;
                 *o = residual ? *o + s : s;
             }
