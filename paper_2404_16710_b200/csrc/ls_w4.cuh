@@ -36,15 +36,14 @@ __device__ __forceinline__ void mma_bf16_16816_new(float (&d)[4], uint32_t a0, u
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-constexpr int kW4Warps = 16;
 constexpr int kW4SmemMax = 227 * 1024;
 
 // shared memory: the warps' sums of a tile, then D blocks a warp, then (HS) the rows of h, each padded by 64 bytes
 // (two rows' 64-byte pieces then fall on different banks)
-template <int NT>
-__host__ __device__ constexpr int w4_part_bytes() { return kW4Warps * 32 * NT * 16; }
-template <int NG>
-__host__ __device__ constexpr int w4_ring_bytes(int D) { return kW4Warps * D * w4_block_bytes(NG); }
+template <int NT, int W>
+__host__ __device__ constexpr int w4_part_bytes() { return W * 32 * NT * 16; }
+template <int NG, int W>
+__host__ __device__ constexpr int w4_ring_bytes(int D) { return W * D * w4_block_bytes(NG); }
 __host__ __device__ constexpr int w4_h_stride(int kblocks) { return kblocks * kQ4Cols * 2 + 64; }
 
 // what a lane reads of a block: the codes of rows g and g + 8 (its 16-byte pieces) and the rows' scales
@@ -104,7 +103,7 @@ __device__ __forceinline__ void w4_block_mma(const W4Regs<NG>& w, const uint4 (&
     }
 }
 
-// One CTA per SM; its 16 warps form teams of 2^lks, and a team takes every (teams of the grid)-th group of TG tiles of
+// One CTA per SM; its W warps form teams of 2^lks, and a team takes every (teams of the grid)-th group of TG tiles of
 // 16 rows (TG = 2 halves what is read of h in shared memory, which bounds the kernel for 16 rows of h).  Of a tile's blocks each warp of the team has a fixed share, consecutive along K, and keeps the
 // next D of its sequence of blocks (which runs on across tiles) in flight in a ring of its own; the team
 // meets once per tile, to add its sums up.  HS: h is copied to shared memory once (columns beyond K as
@@ -115,8 +114,8 @@ __device__ __forceinline__ void w4_block_mma(const W4Regs<NG>& w, const uint4 (&
 // the kernel.  Which blocks a warp adds, and in which order the
 // warps' sums are added, depends on N and K only: a row's result does not depend on how many rows share
 // the pass.
-template <int NG, int NT, int D, bool HS, int TG>
-__global__ void __launch_bounds__(kW4Warps * 32, 1)
+template <int NG, int NT, int W, int D, bool HS, int TG>
+__global__ void __launch_bounds__(W * 32, 1)
 linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __restrict__ h, int M, int N, int K,
                  int kblocks, int n_tiles, int lks, float* __restrict__ out, int residual)
 {
@@ -125,11 +124,11 @@ linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __res
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int KS = 1 << lks, ks = warp & (KS - 1), team = warp >> lks;
     float4* part = reinterpret_cast<float4*>(w4_smem) + (team << lks) * 32 * NT;  // [warp of the team][NT][lane]; a tile at a time
-    const uint32_t ring = smem_u32(w4_smem) + w4_part_bytes<NT>() + warp * D * BB;
+    const uint32_t ring = smem_u32(w4_smem) + w4_part_bytes<NT, W>() + warp * D * BB;
     pdl_launch_dependents();
 
     const int kb0 = kblocks * ks >> lks, nkb = (kblocks * (ks + 1) >> lks) - kb0;
-    const int n_groups = (n_tiles + TG - 1) / TG, group0 = team * gridDim.x + blockIdx.x, group_step = (kW4Warps >> lks) * gridDim.x;
+    const int n_groups = (n_tiles + TG - 1) / TG, group0 = team * gridDim.x + blockIdx.x, group_step = (W >> lks) * gridDim.x;
     // the sequence of blocks (of TG tiles in turn), D ahead of their use: a lane copies its own two pieces, lanes below
     // 2 NG the scales
     int in_group = nkb ? group0 : n_groups, in_left = nkb;
@@ -158,10 +157,10 @@ linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __res
     for (int i = 0; i < D / TG - 1; ++i) fetch();  // weights: no kernel before this one writes them
     pdl_wait();
 
-    const uint32_t hs = smem_u32(w4_smem) + w4_part_bytes<NT>() + w4_ring_bytes<NG>(D);
+    const uint32_t hs = smem_u32(w4_smem) + w4_part_bytes<NT, W>() + w4_ring_bytes<NG, W>(D);
     const int stride = w4_h_stride(kblocks);
     if (HS) {
-        for (int i = threadIdx.x; i < kblocks * 16; i += kW4Warps * 32) {
+        for (int i = threadIdx.x; i < kblocks * 16; i += W * 32) {
             const int bytes = 8 * i < K ? 16 : 0;
             const uint16_t* s = h + (bytes ? 8 * i : 0);
             uint32_t d = hs + i * 16;
