@@ -2016,8 +2016,10 @@ int ls_op_expand_kv4(const void* pages, int32_t n_pages, int32_t n_seq, int32_t 
 
 namespace {
 
-// How the positions of a (sequence, KV head) are spread: splits x S CTAs, enough for about two CTAs per SM, no more
-// than the cache has rounds of chunks for.  Never a function of the rows of the call.
+// How the positions of a (sequence, KV head) are spread: splits x S CTAs, enough for about two CTAs per SM.  A CTA
+// pays for its start and its share of the joining (32 heads, 1030 positions: 8 CTAs a head 6.5 us, 4 of them, with
+// two chunks for a warp, 6.9; 1024 positions: 6.6, 5.3); splits cost a second kernel, some 2 us (8 heads, 4 splits: 4096
+// positions 9.0 us, without 7.0; 8192: 10.0, 11.0; 131072: 44, 104).  Never a function of the rows of the call.
 struct Kv4Plan {
     int S, splits;
 };
@@ -2027,14 +2029,12 @@ Kv4Plan kv4_plan(int n_seq, int Hkv, int max_seq, bool may_split)
     const int64_t pairs = (int64_t)n_seq * Hkv;
     const int round = kKv4Warps * kKv4Chunk;
     while (p.S < 8 && p.S * pairs < 256 && p.S * round < max_seq) p.S *= 2;
-    if (may_split)
-        while (p.splits < 64 && p.splits * p.S * pairs < 256 && 4 * p.splits * p.S * round < max_seq) p.splits *= 2;
-    if (getenv("LS_KV4_S")) p.S = atoi(getenv("LS_KV4_S"));
-    if (getenv("LS_KV4_C") && may_split) p.splits = atoi(getenv("LS_KV4_C"));
+    if (may_split && max_seq >= 4 * p.S * round)
+        while (p.splits < 64 && p.splits * p.S * pairs < 256 && 2 * p.splits * p.S * round <= max_seq) p.splits *= 2;
     return p;
 }
 uint32_t divisor(int d) { return d > 1 ? 0xffffffffu / (uint32_t)d + 1u : 0u; }  // for fastdiv on the device
-int kv4_query_tile(int Q) { return Q <= 8 ? 1 : 2; }  // tiles of 8 queries a CTA takes
+int kv4_query_tile(int Q) { return Q <= 8 ? 1 : Q <= 16 ? 2 : Q <= 24 ? 3 : 4; }  // tiles of 8 queries a CTA takes
 int kv4_rows(int Q, int Hkv) { return (Q + 8 * kv4_query_tile(Q) - 1) / (8 * kv4_query_tile(Q)) * Hkv; }
 
 template <int HD, int NT>
@@ -2084,8 +2084,9 @@ template <int HD>
 int kv4_attn_launch_hd(const Kv4Plan& plan, int n_seq, const uint16_t* q, int M, int G, const int32_t* pos0, const Kv4Cache& c,
                        const unsigned char* pages, uint16_t* out, float* scratch, int32_t* status, const LaunchCtx& lc)
 {
-    return (kv4_query_tile(M * G) == 1 ? kv4_attn_launch<HD, 1> : kv4_attn_launch<HD, 2>)(plan, n_seq, q, M, G, pos0, c, pages, out,
-                                                                                   scratch, status, lc);
+    const int nt = kv4_query_tile(M * G);
+    return (nt == 1 ? kv4_attn_launch<HD, 1> : nt == 2 ? kv4_attn_launch<HD, 2> : nt == 3 ? kv4_attn_launch<HD, 3> : kv4_attn_launch<HD, 4>)(
+        plan, n_seq, q, M, G, pos0, c, pages, out, scratch, status, lc);
 }
 
 }  // namespace

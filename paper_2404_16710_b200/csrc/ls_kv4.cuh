@@ -24,7 +24,6 @@ namespace ls {
 
 constexpr int kKv4Chunk = 32;   // positions a warp takes at a time: two tiles
 constexpr int kKv4Warps = 8;
-constexpr int kKv4Stages = 2;   // chunks of a warp's ring
 
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
 {
@@ -86,8 +85,9 @@ constexpr int kKv4MaxCluster = 16;
 template <int HD, int NT>
 struct Kv4Smem {
     static constexpr int W = kKv4Warps;
+    static constexpr int kStages = NT <= 2 ? 2 : 4;            // chunks of a warp's ring
     static constexpr int kTile = kv4_tile_bytes(HD);
-    static constexpr int kWarpRing = kKv4Stages * 2 * kTile;
+    static constexpr int kWarpRing = kStages * 2 * kTile;
     static constexpr int kItems = NT * HD / 16 * 32;           // float4 pieces of O: [NT][HD / 16][lane]
     static constexpr int kRing = W * kWarpRing;
     static constexpr int kQ = NT * HD / 32 * 32 * 16;          // [NT][group][lane] 16 bytes
@@ -125,7 +125,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     constexpr int W = kKv4Warps;
     constexpr int NJ = HD / 32;   // groups of a row
     constexpr int CT = HD / 16;   // 16-channel tiles of O^T
-    constexpr int TB = SM::kTile, D = kKv4Stages;
+    constexpr int TB = SM::kTile, D = SM::kStages;
     extern __shared__ __align__(128) unsigned char kv4_smem[];
     unsigned char* at = kv4_smem + SM::kRing;
     uint4* sQ = reinterpret_cast<uint4*>(at);
@@ -145,13 +145,14 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     // The first accesses to memory, all before the first use of any (volatile: the compiler moves plain loads down to
     // their use, one latency after the other): this thread's piece of a query, the page-table entries of its warp's first
     // chunk, the position.
-    constexpr int PER = NJ * 4;  // threads that make a query's operand: channels 32 j + 8 t .. + 7
-    static_assert(NT * 8 * PER <= W * 32, "a thread has one piece");
-    const int piece_q = threadIdx.x / PER, piece_j = threadIdx.x % PER / 4, piece_t = threadIdx.x % 4;
-    uint4 piece = make_uint4(0, 0, 0, 0);
-    if (piece_q < NT * 8 && q0 + piece_q < Q) {
-        const int row = fastdiv(q0 + piece_q, G, div_G), in_group = q0 + piece_q - row * G;
-        piece = ld_reuse16(q + (((long long)b * M + row) * Hq + head * G + in_group) * HD + 32 * piece_j + 8 * piece_t);
+    constexpr int PER = NJ * 4, PIECES = (NT * 8 * PER + W * 32 - 1) / (W * 32);  // threads that make a query's operand; a thread's share
+    uint4 piece[PIECES];
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+        const int i = threadIdx.x + k * W * 32, qi = q0 + i / PER, row = fastdiv(qi, G, div_G);
+        piece[k] = make_uint4(0, 0, 0, 0);
+        if (i < NT * 8 * PER && qi < Q)
+            piece[k] = ld_reuse16(q + (((long long)b * M + row) * Hq + head * G + qi - row * G) * HD + 8 * (i % PER));
     }
     // page-table entries of this warp's next chunk (a chunk lies in one page, unless pages are of 16), read before
     // anything says whether it is needed: the positions below max_seq have entries
@@ -228,12 +229,15 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     for (int i = 0; i < D - 1; ++i) fetch();
 
     // Queries as B operands: lane 4 g + t of group j holds channels 32 j + 8 t .. + 7 of query g.
-    if (piece_q < NT * 8) {  // whole warps
-        const uint32_t x[4] = {piece.x, piece.y, piece.z, piece.w};
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+        const int i = threadIdx.x + k * W * 32, qq = i / PER, j = i % PER / 4, tt = i % 4;
+        if (i >= NT * 8 * PER) break;  // whole warps
+        const uint32_t x[4] = {piece[k].x, piece[k].y, piece[k].z, piece[k].w};
         uint32_t am = 0;  // the largest finite component
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = x[k] & 0x7fffu, hi = x[k] >> 16 & 0x7fffu;
+        for (int v = 0; v < 4; ++v) {
+            const uint32_t lo = x[v] & 0x7fffu, hi = x[v] >> 16 & 0x7fffu;
             am = max(am, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
         }
 #pragma unroll
@@ -242,10 +246,10 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
         const float up = exp2_int(14 - e);
         float y[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = (k & 1 ? bf16hi(x[k / 2]) : bf16lo(x[k / 2])) * up;
-        sQ[((piece_q / 8) * NJ + piece_j) * 32 + (piece_q % 8) * 4 + piece_t] =
+        for (int v = 0; v < 8; ++v) y[v] = (v & 1 ? bf16hi(x[v / 2]) : bf16lo(x[v / 2])) * up;
+        sQ[((qq / 8) * NJ + j) * 32 + (qq % 8) * 4 + tt] =
             make_uint4(pack_f16(y[0], y[1]), pack_f16(y[2], y[3]), pack_f16(y[4], y[5]), pack_f16(y[6], y[7]));
-        if (threadIdx.x % PER == 0) sF[piece_q] = exp2_int(e);
+        if (i % PER == 0) sF[qq] = exp2_int(e);
     }
     __syncthreads();
     float fa[NT][2];
