@@ -358,7 +358,9 @@ int ls_op_prefill_attention(const void *q_bf16_dev, int32_t R, int32_t pos0, int
  * Number format.  A group of values shares a scale s, the group's largest |x| divided by 7 and
  * rounded UP to 5 significant bits, kept as bf16; a value stands for c * s with an integer
  * c = rint(x / s) in -7..7 (ties to even), stored as the nibble c + 8.  c * s is exactly a bf16
- * number, so expanding loses nothing.  A group with a NaN or an infinity stands for NaN.
+ * number, so expanding loses nothing.  A group with a NaN or an infinity stands for NaN.  Values up to
+ * 2^127 are represented; operations compute as if in fp32 and overflow as it does (attention: queries times
+ * k scales beyond 2^100).
  * Groups are 32 consecutive channels of a head (cache) or 32, 64 or 128 consecutive columns (weights).
  *
  * Packed weights of a matrix [N, K] (K a multiple of 8): blocks of 16 rows x 128 columns, the
@@ -427,7 +429,8 @@ int ls_op_expand_kv4(const void *pages_dev, int32_t n_pages, int32_t n_seq, int3
  * ls_op_attention_kv4_scratch_bytes() bytes, of any content, used by one call at a time); with
  * NULL, or where that function returns 0 (no split is worth it), none is used.  A row's result
  * depends on its position, n_seq, Hkv, max_seq and whether there is scratch (which fix how the
- * positions are dealt to CTAs), never on M or on the other rows. */
+ * positions are dealt to CTAs), never on M or on the other rows.  Softmax weights enter the second
+ * product in f16, V exactly, unless its scale is more than 2^25 below the largest of the head. */
 size_t ls_op_attention_kv4_scratch_bytes(int32_t n_seq, int32_t M, int32_t Hq, int32_t Hkv, int32_t hd,
                                          int32_t max_seq);
 int ls_op_attention_kv4(const void *q_bf16_dev, int32_t n_seq, int32_t M, const int32_t *pos0_dev, int32_t Hq,

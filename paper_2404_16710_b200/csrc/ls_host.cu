@@ -2028,7 +2028,7 @@ Kv4Plan kv4_plan(int n_seq, int Hkv, int max_seq, bool may_split)
     Kv4Plan p = {1, 1};
     const int64_t pairs = (int64_t)n_seq * Hkv;
     const int round = kKv4Warps * kKv4Chunk;
-    while (p.S < 8 && p.S * pairs < 256 && p.S * round < max_seq) p.S *= 2;
+    while (p.S < kKv4MaxCluster && p.S * pairs < 256 && p.S * round < max_seq) p.S *= 2;
     if (may_split && max_seq >= 4 * p.S * round)
         while (p.splits < 64 && p.splits * p.S * pairs < 256 && 2 * p.splits * p.S * round <= max_seq) p.splits *= 2;
     return p;

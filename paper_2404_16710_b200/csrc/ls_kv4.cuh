@@ -81,7 +81,7 @@ __device__ __forceinline__ uint32_t q4_scaled_f16x2(uint32_t w, int i, uint32_t 
 
 // shared memory of a CTA: rings (later each warp's O in its own), queries and their factors, the
 // warps' statistics, and what the CTAs of the cluster send one another
-constexpr int kKv4MaxCluster = 16;
+constexpr int kKv4MaxCluster = 8;
 template <int HD, int NT>
 struct Kv4Smem {
     static constexpr int W = kKv4Warps;
@@ -111,10 +111,11 @@ __device__ __forceinline__ float kv4_unit(int hd) { return 0x1p-14f * 1.44269504
 // the 32-position chunks of the cache in turn by absolute position, each through a cp.async ring of its own and
 // with a running (max, sum, O) of its own.  At the end every thread adds up, in warp order, the pieces of O it is
 // given and sends them to the CTA of the cluster that finishes them, through distributed shared memory: one
-// CTA barrier, one cluster barrier.  With one split that is the result; clusters hold at most 16 CTAs, so that
-// few heads over a long cache take several splits, which a second kernel joins.  A row's result depends on its
-// position and on the grid, not on M or the other rows: what other rows add to the tokens a CTA looks at has weight 0, and all factors that are shared
-// are powers of two.
+// CTA barrier, one cluster barrier.  With one split that is the result; a GPC has room for few large clusters
+// (148 SMs: 33 of 8 CTAs, 7 of 16 where one fills an SM), so that few heads over a long cache take several splits,
+// which a second kernel joins.  A row's result depends on its position and on the grid, not on M or the other
+// rows: what other rows add to the tokens a CTA looks at has weight 0, and all factors that are shared are powers
+// of two.
 template <int HD, int NT>
 __global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1)
 attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t* __restrict__ pos0_dev,
@@ -522,7 +523,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             r.x = fmaf(f0 * unit, v.x, r.x), r.z = fmaf(f0 * unit, v.z, r.z);
             r.y = fmaf(f1 * unit, v.y, r.y), r.w = fmaf(f1 * unit, v.w, r.w);
         }
-        const int to = x / (SM::kItems / 16) >> (4 - log2_S);  // x / share
+        const int to = x / (SM::kItems / kKv4MaxCluster) >> (3 - log2_S);  // x / share
         st_cluster_f4(map_cluster(smem_u32(sIn) + (rank * share + x - to * share) * 16, to), r);
         if ((x / 4) % (CT * 8) == 0)  // one of the pieces with these queries: their statistics, to all
             for (int d = 0; d < S; ++d) {

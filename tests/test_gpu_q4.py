@@ -134,7 +134,8 @@ def test_linear_large_vocabulary_sampled_rows():
     assert (np.abs(out.cpu().numpy()[:, rows] - ref) <= linear_tol(K, group, spread)).all()
 
 
-@pytest.mark.parametrize("N,K,group", [(304, 1384, 32), (4096, 4096, 128), (5000, 264, 64), (16, 11008, 32)])
+@pytest.mark.parametrize("N,K,group", [(304, 1384, 32), (4096, 4096, 128), (5000, 264, 64), (16, 11008, 32), (16400, 520, 32),
+                                       (16500, 14336, 128), (33, 30000, 64)])
 def test_linear_rows_do_not_depend_on_pass_size(N, K, group):
     packed = quantised(rnd((N, K), 7, 0.05).bfloat16(), group)
     h = rnd((16, K), 8).bfloat16()
@@ -307,7 +308,7 @@ def check_attention(c, q, out, M, G):
             assert (err <= (attention_tol(ref, spread, v) if n - M + m >= 0 else 0)).all(), (b, m, n, err.max())
 
 
-@pytest.mark.parametrize("Hkv,G,hd", [(2, 1, 128), (1, 8, 128), (2, 4, 64), (3, 2, 128)])
+@pytest.mark.parametrize("Hkv,G,hd", [(2, 1, 128), (1, 8, 128), (2, 4, 64), (3, 2, 128), (1, 7, 64)])
 @pytest.mark.parametrize("M,lens,page", [(1, [1], 16), (1, [15, 16, 17], 16), (1, [31, 32, 33], 32), (3, [2, 3, 4], 16),
                                          (7, [300], 64), (16, [16, 1000], 32), (1, [0, 257, 256, 255], 64),
                                          (5, [0, 0, 4, 130], 16), (16, [1100, 7], 256), (2, [4099], 64)])
@@ -334,7 +335,7 @@ def test_attention_rows_do_not_depend_on_pass_size(Hkv, G, hd):
     c = Cache([1000], Hkv, hd, 64, 40, max_seq=2048)
     q = rnd((1, 16, Hkv * G * hd), 41).bfloat16()
     full = c.run(q, 16)
-    for m0, M in ((0, 1), (15, 1), (4, 3), (0, 8), (7, 9)):
+    for m0, M in ((0, 1), (15, 1), (4, 3), (3, 5), (9, 6), (0, 8), (7, 9)):
         out = torch.empty((1, M, q.shape[2]), dtype=torch.bfloat16, device="cuda")
         B.ls_op_attention_kv4(q[:, m0:m0 + M].contiguous(), torch.tensor([984 + m0], dtype=torch.int32, device="cuda"), Hkv, hd, 64,
                               c.table, 2048, c.pool, out)
@@ -434,6 +435,99 @@ def test_captured_and_replayed_at_other_positions_on_another_stream():
             vv = np.concatenate([vv, R.values(*R.quantise(vs[b], 32), 32)])
             ref, spread = R.attention(qs[b, 0].reshape(-1, hd), kk, vv, kk.shape[0] - 1, G)
             assert (np.abs(got[b, 0].reshape(-1, hd) - ref) <= attention_tol(ref, spread, vv)).all()
+
+
+def test_attention_values_and_keys_of_very_different_sizes():
+    """tokens and channel groups whose k and v differ by factors up to 2^20 and 2^24, queries too: the kernel's shared
+    powers of two must lose nothing.  The loudest values sit under the smallest weights."""
+    Hkv, G, hd, n, M = 2, 4, 128, 700, 3
+    c = Cache([n], Hkv, hd, 64, 90)
+    rng = np.random.default_rng(91)
+    size = torch.from_numpy(np.exp2(rng.uniform(-12, 12, (n, Hkv, 4)))).float().cuda()
+    c.v[0] = (c.v[0].float() * size.repeat_interleave(32, 2)).bfloat16()
+    c.k[0] = (c.k[0].float() * torch.from_numpy(np.exp2(rng.uniform(-20, 0, (n, Hkv, 1)))).float().cuda()).bfloat16()
+    q = (rnd((1, M, Hkv * G * hd), 92) * torch.from_numpy(np.exp2(rng.uniform(-30, 2, (1, M, Hkv * G, 1)))).float().cuda()
+         .expand(1, M, Hkv * G, hd).reshape(1, M, -1)).bfloat16()
+    loud = int(np.argmax(vals(c.v[0]).max((1, 2))))
+    c.k[0][loud] = -3.0 * q[0, 0].view(Hkv, G, hd)[:, 0].sign()  # as far from the queries as can be
+    B.ls_op_append_kv4(c.k[0][None], c.v[0][None], torch.zeros(1, dtype=torch.int32, device="cuda"), 64, c.table, c.max_seq, c.pool)
+    check_attention(c, q, c.run(q, M), M, G)
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 6, 16])
+def test_attention_over_a_cache_long_enough_to_be_split(M):
+    """16384 positions of one KV head: several splits joined by the second kernel, with scratch of the caller's and of
+    the binding's; without any, one cluster does it.  Both within the bound; rows as in a pass of 16."""
+    Hkv, G, hd, page, n = 1, 4, 64, 64, 12345
+    c = Cache([n], Hkv, hd, page, 95, max_seq=16384)
+    q = rnd((1, 16, Hkv * G * hd), 96).bfloat16()
+    need = B.ls_op_attention_kv4_scratch_bytes(1, M, Hkv * G, Hkv, hd, 16384)
+    assert need > 0 and B.ls_op_attention_kv4_scratch_bytes(1, M, Hkv * G, Hkv, hd, 4096) == 0
+    pos = torch.tensor([n - M], dtype=torch.int32, device="cuda")
+    mine = q[:, 16 - M:].contiguous()
+    outs = []
+    for scratch in (None, torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")):
+        out = torch.empty_like(mine)
+        B.ls_op_attention_kv4(mine, pos, Hkv, hd, page, c.table, 16384, c.pool, out, None, scratch)
+        outs.append(out)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], c.run(q, 16)[:, 16 - M:])
+    check_attention(c, mine, outs[0], M, G)
+    alone = torch.empty_like(mine)
+    L, p = B.lib(), lambda t: t.data_ptr()
+    assert L.ls_op_attention_kv4(p(mine), 1, M, p(pos), Hkv * G, Hkv, hd, page, p(c.table), c.table.shape[1], 16384, p(c.pool),
+                                 c.pool.shape[0], p(alone), None, None, B._stream()) == 0
+    check_attention(c, mine, alone, M, G)
+    with pytest.raises(B.LsError):
+        B.ls_op_attention_kv4(mine, pos, Hkv, hd, page, c.table, 16384, c.pool, alone, None, torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+
+
+def test_attention_split_rows_without_keys_and_captured():
+    """two sequences over split caches, one with nothing to see: zeros; and the same from a replayed graph, whose scratch
+    the binding takes from the graph's own memory, while an eager call uses another"""
+    Hkv, G, hd, page = 1, 8, 128, 64
+    c = Cache([9000, 0], Hkv, hd, page, 97, max_seq=8192 + 4096)
+    q = rnd((2, 2, Hkv * G * hd), 98).bfloat16()
+    assert B.ls_op_attention_kv4_scratch_bytes(2, 2, Hkv * G, Hkv, hd, c.max_seq) > 0
+    eager = c.run(q, 2)
+    check_attention(c, q, eager, 2, G)
+    pos = torch.tensor([8998, -2], dtype=torch.int32, device="cuda")
+    st, out = torch.cuda.Stream(), torch.zeros_like(q)
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            B.ls_op_attention_kv4(q, pos, Hkv, hd, page, c.table, c.max_seq, c.pool, out)
+            B.ls_op_attention_kv4(q, pos, Hkv, hd, page, c.table, c.max_seq, c.pool, out)
+        for _ in range(3):
+            out.fill_(7.0)
+            graph.replay()
+    again = c.run(q, 2)  # at the same time as the last replay
+    st.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(out, eager) and torch.equal(again, eager)
+
+
+def test_two_streams_at_once():
+    """linear and attention calls on two streams, neither waiting for the other, give what each gives alone"""
+    N, K = 4096, 2048
+    packed, h = quantised(rnd((N, K), 100, 0.02).bfloat16(), 32), rnd((2, 8, K), 101).bfloat16()
+    c = Cache([3000, 2500], 4, 128, 64, 102)
+    q = rnd((2, 4, 8 * 128), 103).bfloat16()
+    want = torch.empty((2, 8, N), device="cuda")
+    for i in range(2):
+        B.ls_op_linear_w4(packed, 32, h[i], want[i])
+    ref = c.run(q, 4)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], []
+    for _ in range(5):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                o = torch.empty((8, N), device="cuda")
+                B.ls_op_linear_w4(packed, 32, h[i], o)
+                outs.append((o, want[i], c.run(q, 4)))
+    torch.cuda.synchronize()
+    for o, w, a in outs:
+        assert torch.equal(o, w) and torch.equal(a, ref)
 
 
 # ------------------------------------------------------------------ together
