@@ -1,6 +1,7 @@
 """Time single kernels of the decode path on a workload's shapes, through the C ABI.
 
     python -m paper_2404_16710_b200.opbench --workload llama2-7b --layers 4 --ops gate_up_swiglu --rows 7
+    python -m paper_2404_16710_b200.opbench --workload llama3-8b --bits 4 --rows 1,5
 
 Each op is launched ``iters`` times (as one CUDA graph) with CUDA events around the batch,
 rotating over the weights of ``layers`` layers so that no launch finds its weights in L2 (one 7B-shaped
@@ -92,6 +93,52 @@ def op_cases(shape, w, path, M, n_ctx=1030):
     }
 
 
+Q4_OPS = ("gate_w4", "down_residual_w4", "qkv_w4", "o_residual_w4", "lm_head_w4", "append_kv4", "attention_kv4")
+
+
+def q4_cases(shape, w, M, n_ctx=1030, group=64):
+    """The same on 4-bit weights and a 4-bit cache: name -> (callable(layer index), algorithmic bytes per launch, number of
+    distinct weights).  The bytes are those of the packed weights, of the rows appended, of the tiles attention must read."""
+    D, F, V = shape.d_model, shape.d_ffn, shape.vocab
+    L = len(w["wq"])
+    Hq, Hkv, hd, ps = shape.n_heads, shape.n_kv_heads, shape.head_dim, 64
+    g = torch.Generator(device="cuda").manual_seed(7)
+
+    def pack(m):
+        packed = torch.empty(B.ls_op_w4_bytes(m.shape[0], m.shape[1], group), dtype=torch.uint8, device="cuda")
+        B.ls_op_quantize_w4(m.contiguous(), group, packed)
+        return packed
+
+    mats = {"gate_w4": w["w_gate"], "down_residual_w4": w["w_down"], "o_residual_w4": w["wo"], "lm_head_w4": [w["lm_head"], w["tok_embed"]],
+            "qkv_w4": [torch.cat([w["wq"][i], w["wk"][i], w["wv"][i]]) for i in range(L)]}
+    cases = {}
+    for name, ms in mats.items():
+        # small matrices: further copies, so that no launch finds its weights in L2
+        packed = [pack(m) for m in ms]
+        packed += [packed[i % len(ms)].clone() for i in range(max(0, 160_000_000 // packed[0].numel() - len(ms)))]
+        N, K = ms[0].shape
+        h = torch.randn((M, K), device="cuda", generator=g).bfloat16()
+        out = torch.zeros((M, N), dtype=torch.float32, device="cuda")
+        fn = lambda i, packed=packed, h=h, out=out, r="residual" in name: B.ls_op_linear_w4(packed[i], group, h, out, r)  # noqa: E731
+        cases[name] = (fn, packed[0].numel(), len(packed))
+    max_seq = n_ctx + M + 1
+    n_pages = -(-max_seq // ps)
+    per = B.ls_op_kv4_page_bytes(Hkv, hd, ps)
+    kvl = max(2, min(48, 160_000_000 // (n_pages * per)))
+    pools = [torch.empty((n_pages, per), dtype=torch.uint8, device="cuda") for _ in range(kvl)]
+    table = torch.arange(n_pages, dtype=torch.int32, device="cuda")[None]
+    zero, pos = (torch.full((1,), n, dtype=torch.int32, device="cuda") for n in (0, n_ctx))
+    k, v = (torch.randn((1, n_ctx + M, Hkv, hd), device="cuda", generator=g).bfloat16() for _ in range(2))
+    for p in pools:
+        B.ls_op_append_kv4(k, v, zero, ps, table, max_seq, p)
+    q = (torch.randn((1, M, Hq * hd), device="cuda", generator=g) * 0.3).bfloat16()
+    o = torch.empty_like(q)
+    row = Hkv * (hd + hd // 8)  # bytes of a cached token
+    cases["append_kv4"] = (lambda i: B.ls_op_append_kv4(k[:, :M], v[:, :M], pos, ps, table, max_seq, pools[i]), M * (row + 4 * Hkv * hd), kvl)
+    cases["attention_kv4"] = (lambda i: B.ls_op_attention_kv4(q, pos, Hkv, hd, ps, table, max_seq, pools[i], o), (n_ctx + M) * row, kvl)
+    return cases
+
+
 PROMPT_OPS = ("prompt_gemm_qkv", "prompt_gemm_gate", "prompt_gemm_down", "prompt_attention")
 
 
@@ -134,14 +181,14 @@ def prompt_rates(shape, w, R, ops=PROMPT_OPS, iters=20, warm=3):
     return out
 
 
-def kernel_rooflines(shape, w, path, rows, peak_gbs, ops=OPS, iters=40, warm=5, chained=True):
+def kernel_rooflines(shape, w, path, rows, peak_gbs, ops=OPS, iters=40, warm=5, chained=True, bits=16):
     """Per op and pass size: one launch alone (launches serialised: each starts when the one before
     has drained) and, with ``chained``, the same launches linked by programmatic dependent launch as
     inside the decode loop (``ms_chained``: a launch's CTAs move in and prefetch while its
     predecessor's last CTAs finish).  Fractions are algorithmic bytes / time / peak_gbs."""
     out = {}
     for M in rows:
-        cases = op_cases(shape, w, path, M)
+        cases = op_cases(shape, w, path, M) if bits == 16 else q4_cases(shape, w, M)
         for name in ops:
             fn, nbytes, rot = cases[name]
             ms = time_op(fn, rot, iters, warm)
@@ -163,7 +210,8 @@ def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--workload", default="llama2-7b", choices=sorted(synth.WORKLOADS))
     ap.add_argument("--layers", type=int, default=4, help="layers of weights to create and rotate over")
-    ap.add_argument("--ops", default=",".join(OPS))
+    ap.add_argument("--ops", default="", help="of " + ", ".join(OPS) + "; with --bits 4 of " + ", ".join(Q4_OPS))
+    ap.add_argument("--bits", type=int, default=16, choices=[16, 4], help="4: packed 4-bit weights and the 4-bit cache")
     ap.add_argument("--rows", default="1,7")
     ap.add_argument("--path", default="mma", choices=["fma", "mma"])
     ap.add_argument("--iters", type=int, default=40)
@@ -186,7 +234,7 @@ def main():
         print(json.dumps(res))
         return
     res = kernel_rooflines(shape, w, path, [int(r) for r in a.rows.split(",")], a.peak,
-                           [o for o in a.ops.split(",") if o], a.iters, a.warm)
+                           [o for o in a.ops.split(",") if o] or (OPS if a.bits == 16 else Q4_OPS), a.iters, a.warm, bits=a.bits)
     for k, v in res.items():
         print(f"{k:28s} {v['ms'] * 1e3:8.2f} us  {v['GB/s']:8.1f} GB/s  {v['frac']:.3f} of {a.peak:.0f}   chained "
               f"{v['ms_chained'] * 1e3:8.2f} us  {v['frac_chained']:.3f}")
