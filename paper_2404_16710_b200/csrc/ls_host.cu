@@ -1886,11 +1886,11 @@ int w4_split(int n_tiles)
     return n_tiles <= 148 ? 4 : n_tiles < 1024 ? 3 : 2;
 }
 
-template <int NG, int NT, int W, int D, bool HS, int TG>
+template <int NG, int NT, int W, int D, int CB, bool HS, int TG>
 int w4_launch(const unsigned char* packed, const uint16_t* h, int M, int N, int K, float* out, int residual,
               const LaunchCtx& lc)
 {
-    auto* kernel = linear_w4_kernel<NG, NT, W, D, HS, TG>;
+    auto* kernel = linear_w4_kernel<NG, NT, W, D, CB, HS, TG>;
     static std::mutex mu;
     static int sms[64] = {};  // SMs of the device; asked for once, when the kernel's shared memory is raised
     int dev = 0;
@@ -1923,20 +1923,22 @@ int w4_launch_ng(const unsigned char* packed, const uint16_t* h, int M, int N, i
         // 24 warps, what 64 to 80 registers allow, make a third team of 8 warps: of use with more than two tiles an SM
         // (320 tiles, K = 5120: 7.4 us, 16 warps 8.4; 688 tiles: 9.2, 9.9; but 256 tiles, K = 4096: 5.8, 5.2)
         if (N > 16 * 296 && ring24 >= w4_ring_bytes<NG, 24>(4))
-            return w4_launch<NG, 1, 24, 4, true, 1>(packed, h, M, N, K, out, residual, lc);
-        if (ring16 >= w4_ring_bytes<NG, 16>(6)) return w4_launch<NG, 1, 16, 6, true, 1>(packed, h, M, N, K, out, residual, lc);
-        if (ring16 >= w4_ring_bytes<NG, 16>(3)) return w4_launch<NG, 1, 16, 3, true, 1>(packed, h, M, N, K, out, residual, lc);
-        return w4_launch<NG, 1, 16, 6, false, 1>(packed, h, M, N, K, out, residual, lc);
+            return w4_launch<NG, 1, 24, 4, 2, true, 1>(packed, h, M, N, K, out, residual, lc);
+        if (ring16 >= w4_ring_bytes<NG, 16>(6)) return w4_launch<NG, 1, 16, 6, 2, true, 1>(packed, h, M, N, K, out, residual, lc);
+        if (ring16 >= w4_ring_bytes<NG, 16>(4)) return w4_launch<NG, 1, 16, 4, 2, true, 1>(packed, h, M, N, K, out, residual, lc);
+        if (ring16 >= w4_ring_bytes<NG, 16>(3)) return w4_launch<NG, 1, 16, 3, 1, true, 1>(packed, h, M, N, K, out, residual, lc);
+        return w4_launch<NG, 1, 16, 6, 2, false, 1>(packed, h, M, N, K, out, residual, lc);
     }
     const int64_t ring = room - w4_part_bytes<2, 16>();
     // more than 8 rows through a large matrix: two tiles at a time (128256 x 4096, 16 rows: 71.4 us, one at a time 75.2);
     // with few tiles an SM the teams would run out of pairs
     if (N > 16 * 1023 && ring >= w4_ring_bytes<NG, 16>(4))
-        return ring >= w4_ring_bytes<NG, 16>(6) ? w4_launch<NG, 2, 16, 6, true, 2>(packed, h, M, N, K, out, residual, lc)
-                                                : w4_launch<NG, 2, 16, 4, true, 2>(packed, h, M, N, K, out, residual, lc);
-    if (ring >= w4_ring_bytes<NG, 16>(6)) return w4_launch<NG, 2, 16, 6, true, 1>(packed, h, M, N, K, out, residual, lc);
-    if (ring >= w4_ring_bytes<NG, 16>(3)) return w4_launch<NG, 2, 16, 3, true, 1>(packed, h, M, N, K, out, residual, lc);
-    return w4_launch<NG, 2, 16, 6, false, 1>(packed, h, M, N, K, out, residual, lc);
+        return ring >= w4_ring_bytes<NG, 16>(6) ? w4_launch<NG, 2, 16, 6, 1, true, 2>(packed, h, M, N, K, out, residual, lc)
+                                                : w4_launch<NG, 2, 16, 4, 1, true, 2>(packed, h, M, N, K, out, residual, lc);
+    if (ring >= w4_ring_bytes<NG, 16>(6)) return w4_launch<NG, 2, 16, 6, 2, true, 1>(packed, h, M, N, K, out, residual, lc);
+    if (ring >= w4_ring_bytes<NG, 16>(4)) return w4_launch<NG, 2, 16, 4, 2, true, 1>(packed, h, M, N, K, out, residual, lc);
+    if (ring >= w4_ring_bytes<NG, 16>(3)) return w4_launch<NG, 2, 16, 3, 1, true, 1>(packed, h, M, N, K, out, residual, lc);
+    return w4_launch<NG, 2, 16, 6, 2, false, 1>(packed, h, M, N, K, out, residual, lc);
 }
 
 }  // namespace

@@ -2,6 +2,8 @@
 // M <= 16 rows (LayerSkip Sec. 4.3: a draft pass has one row, a verify pass num_draft + 1).  Format and
 // block layout: ls_q4.cuh.
 #pragma once
+#include <type_traits>
+
 #include "ls_prefill.cuh"
 #include "ls_q4.cuh"
 
@@ -105,8 +107,8 @@ __device__ __forceinline__ void w4_block_mma(const W4Regs<NG>& w, const uint4 (&
 
 // One CTA per SM; its W warps form teams of 2^lks, and a team takes every (teams of the grid)-th group of TG tiles of
 // 16 rows (TG = 2 halves what is read of h in shared memory, which bounds the kernel for 16 rows of h).  Of a tile's blocks each warp of the team has a fixed share, consecutive along K, and keeps the
-// next D of its sequence of blocks (which runs on across tiles) in flight in a ring of its own; the team
-// meets once per tile, to add its sums up.  HS: h is copied to shared memory once (columns beyond K as
+// next blocks of its sequence (which runs on across tiles) in flight in a ring of its own, of D blocks; the team meets
+// once per tile, to add its sums up.  HS: h is copied to shared memory once (columns beyond K as
 // zeros); otherwise, for h larger than that, it comes through L1.
 // The codes are the A operand of mma.sync, the rows of h the B operand; a group's products are summed in fp32 by
 // the tensor cores and multiplied by the group's scale (a lane holds rows g and g + 8 of a tile) when they join
@@ -114,7 +116,7 @@ __device__ __forceinline__ void w4_block_mma(const W4Regs<NG>& w, const uint4 (&
 // the kernel.  Which blocks a warp adds, and in which order the
 // warps' sums are added, depends on N and K only: a row's result does not depend on how many rows share
 // the pass.
-template <int NG, int NT, int W, int D, bool HS, int TG>
+template <int NG, int NT, int W, int D, int CB, bool HS, int TG>
 __global__ void __launch_bounds__(W * 32, 1)
 linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __restrict__ h, int M, int N, int K,
                  int kblocks, int n_tiles, int lks, float* __restrict__ out, int residual)
@@ -129,32 +131,40 @@ linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __res
 
     const int kb0 = kblocks * ks >> lks, nkb = (kblocks * (ks + 1) >> lks) - kb0;
     const int n_groups = (n_tiles + TG - 1) / TG, group0 = team * gridDim.x + blockIdx.x, group_step = (W >> lks) * gridDim.x;
-    // the sequence of blocks (of TG tiles in turn), D ahead of their use: a lane copies its own two pieces, lanes below
-    // 2 NG the scales
+    // the sequence of stages, kDepth - 1 ahead of their use: CB consecutive blocks of a tile, or (TG = 2) one of each
+    constexpr int kStage = CB * TG, kDepth = D / kStage;
+    static_assert(D % kStage == 0 && (TG == 1 || CB == 1), "whole stages");
     int in_group = nkb ? group0 : n_groups, in_left = nkb;
     uint32_t in_at = ring + lane * 16;
     const long long tile_bytes = (long long)kblocks * BB;
     const unsigned char* src = packed + group0 * TG * tile_bytes + (long long)kb0 * BB + lane * 16;
     const long long jump = group_step * TG * tile_bytes - (long long)nkb * BB;
+    auto copy = [&](uint32_t to, const unsigned char* from, auto blocks) {  // a lane's 16-byte pieces of consecutive blocks
+        constexpr int kBytes = decltype(blocks)::value * BB;
+#pragma unroll
+        for (int i = 0; i < kBytes / 512; ++i) cp_async16_cg(to + 512 * i, from + 512 * i, 16);
+        if (lane < kBytes % 512 / 16) cp_async16_cg(to + kBytes / 512 * 512, from + kBytes / 512 * 512, 16);
+    };
     auto fetch = [&]() {
         if (in_group < n_groups) {
-#pragma unroll
-            for (int u = 0; u < TG; ++u) {  // a last group of fewer tiles reads its first one again
-                const unsigned char* from = src + (u && in_group * TG + u < n_tiles ? u * tile_bytes : 0);
-                cp_async16_cg(in_at, from, 16);
-                cp_async16_cg(in_at + kQ4CodeBytes / 2, from + kQ4CodeBytes / 2, 16);
-                if (lane < 2 * NG) cp_async16_cg(in_at + kQ4CodeBytes, from + kQ4CodeBytes, 16);
-                in_at += BB;
+            if (TG == 2) {  // a last group of fewer tiles reads its first one again
+                copy(in_at, src, std::integral_constant<int, 1>());
+                copy(in_at + BB, src + (in_group * 2 + 1 < n_tiles ? tile_bytes : 0), std::integral_constant<int, 1>());
+            } else if (in_left >= CB) {
+                copy(in_at, src, std::integral_constant<int, CB>());
+            } else {
+                copy(in_at, src, std::integral_constant<int, 1>());
             }
-            src += BB;
-            if (--in_left == 0) in_left = nkb, in_group += group_step, src += jump;
+            src += CB * BB;
+            in_left -= CB;
+            if (in_left <= 0) src += jump + in_left * BB, in_left = nkb, in_group += group_step;
+            in_at += kStage * BB;
             if (in_at == ring + D * BB + lane * 16) in_at = ring + lane * 16;
         }
         cp_async_commit();
     };
-    static_assert(D % TG == 0, "whole groups of blocks in the ring");
 #pragma unroll
-    for (int i = 0; i < D / TG - 1; ++i) fetch();  // weights: no kernel before this one writes them
+    for (int i = 0; i < kDepth - 1; ++i) fetch();  // weights: no kernel before this one writes them
     pdl_wait();
 
     const uint32_t hs = smem_u32(w4_smem) + w4_part_bytes<NT, W>() + w4_ring_bytes<NG, W>(D);
@@ -184,33 +194,39 @@ linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __res
     uint32_t at = ring;
     for (int group = group0; group < n_groups; group += group_step) {
         float acc[TG][NT][4] = {};
-        for (int kb = kb0; kb < kb0 + nkb; ++kb) {
+        for (int kb = kb0; kb < kb0 + nkb; kb += CB) {
             fetch();
-            cp_async_wait<D / TG - 1>();  // the oldest of the blocks in flight
+            cp_async_wait<kDepth - 1>();  // the oldest of the stages in flight
             __syncwarp();
-            W4Regs<NG> w[TG];
 #pragma unroll
-            for (int u = 0; u < TG; ++u) w[u].load(at + u * BB, lane);
-            at += TG * BB;
-            if (at == ring + D * BB) at = ring;
-            uint4 b[NT][4];
-            if (HS) {
+            for (int i = 0; i < CB; ++i) {
+                if (i && kb + i >= kb0 + nkb) break;
+                uint4 b[NT][4];
+                if (HS) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) b[nt][j] = lds16(hoff[nt] + kb * 256 + j * 64);
-            } else {
-                const bool whole = (kb + 1) * kQ4Cols <= K;  // only the last block has columns beyond K
+                        for (int j = 0; j < 4; ++j) b[nt][j] = lds16(hoff[nt] + (kb + i) * 256 + j * 64);
+                } else {
+                    const bool whole = (kb + i + 1) * kQ4Cols <= K;  // only the last block has columns beyond K
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        b[nt][j] = whole || kb * kQ4Cols + 32 * j + 8 * t < K ? ld_reuse16(hrow[nt] + kb * kQ4Cols + 32 * j)
-                                                                              : make_uint4(0, 0, 0, 0);
+                        for (int j = 0; j < 4; ++j)
+                            b[nt][j] = whole || (kb + i) * kQ4Cols + 32 * j + 8 * t < K
+                                           ? ld_reuse16(hrow[nt] + (kb + i) * kQ4Cols + 32 * j)
+                                           : make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int u = 0; u < TG; ++u) {
+                    W4Regs<NG> w;
+                    w.load(at + (i + u) * BB, lane);
+                    w4_block_mma<NG, NT>(w, b, acc[u]);
+                }
             }
-#pragma unroll
-            for (int u = 0; u < TG; ++u) w4_block_mma<NG, NT>(w[u], b, acc[u]);
-            __syncwarp();  // every lane has read the blocks before the ring comes round to them
+            at += kStage * BB;
+            if (at == ring + D * BB) at = ring;
+            __syncwarp();  // every lane has read the stage before the ring comes round to it
         }
 #pragma unroll
         for (int u = 0; u < TG; ++u) {
