@@ -1906,7 +1906,7 @@ int w4_launch(const unsigned char* packed, const uint16_t* h, int M, int N, int 
         n_sm = sms[dev];
     }
     const int n_tiles = (int)(((int64_t)N + 15) / 16), kb = w4_kblocks(K), lks = w4_split(n_tiles);
-    const int teams = W >> lks, grid = ((n_tiles + TG - 1) / TG + teams - 1) / teams;
+    const int grid = (n_tiles + TG - 1) / TG;  // groups of tiles: every SM gets one before any gets a second
     const size_t smem = w4_part_bytes<NT, W>() + w4_ring_bytes<NG, W>(D) + (HS ? (size_t)M * w4_h_stride(kb) : 0);
     LS_CK(launch(lc, kernel, dim3((unsigned)(grid < n_sm ? grid : n_sm)), dim3(W * 32), smem, packed, h, M, N, K, kb,
                  n_tiles, lks, out, residual));

@@ -150,14 +150,15 @@ linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __res
             if (TG == 2) {  // a last group of fewer tiles reads its first one again
                 copy(in_at, src, std::integral_constant<int, 1>());
                 copy(in_at + BB, src + (in_group * 2 + 1 < n_tiles ? tile_bytes : 0), std::integral_constant<int, 1>());
-            } else if (in_left >= CB) {
+            } else if (CB == 1 || in_left >= CB) {
                 copy(in_at, src, std::integral_constant<int, CB>());
             } else {
                 copy(in_at, src, std::integral_constant<int, 1>());
             }
             src += CB * BB;
             in_left -= CB;
-            if (in_left <= 0) src += jump + in_left * BB, in_left = nkb, in_group += group_step;
+            if (CB == 1 ? in_left == 0 : in_left <= 0)
+                src += CB == 1 ? jump : jump + in_left * BB, in_left = nkb, in_group += group_step;
             in_at += kStage * BB;
             if (in_at == ring + D * BB + lane * 16) in_at = ring + lane * 16;
         }
