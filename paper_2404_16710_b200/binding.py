@@ -149,24 +149,27 @@ def _dev(t):
     return C.c_void_p(t.data_ptr())
 
 
-_torch = None
+class _Torch:
+    """what the single operations need of torch, looked up once: a call of a few microseconds notices"""
 
-
-def _t():
-    """torch, imported at the first call that needs it"""
-    global _torch
-    if _torch is None:
+    def load(self):
         import torch
-        _torch = torch
-    return _torch
+        self.bf16, self.f32, self.i32, self.u8, self.empty = torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.empty
+        # torch.cuda.current_stream() builds a Stream object (3.4 us a call, as much as a launch); the raw handle costs 0.2
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.stream = (lambda: raw(torch.cuda.current_device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
+        return self
+
+    def __getattr__(self, name):  # only before load()
+        return getattr(self.load(), name)
+
+
+_torch = _Torch()
 
 
 def _stream():
-    """handle of the current CUDA stream.  torch.cuda.current_stream() builds a Stream object for it (3.4 us a call, as
-    much as a launch); the raw handle costs 0.3 us."""
-    torch = _torch or _t()
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+    """handle of the current CUDA stream"""
+    return _torch.stream()
 
 
 def _i32(a):
@@ -436,16 +439,13 @@ def _bad(what):
 
 def _arg(t, dtype, what):
     """device pointer of a contiguous CUDA tensor of the type the entry point reads"""
-    if t.is_cuda and t.is_contiguous() and t.dtype is getattr(_torch or _t(), dtype):
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous():
         return t.data_ptr()
     _bad(f"{what}: a contiguous {dtype} CUDA tensor is needed")
 
 
 def _status(t):
-    return None if t is None else _arg(t, _INT, "status")
-
-
-_BF16, _F32, _INT, _U8 = "bfloat16", "float32", "int32", "uint8"
+    return None if t is None else _arg(t, _torch.i32, "status")
 
 
 @functools.lru_cache(maxsize=4096)
@@ -457,20 +457,20 @@ def _packed(packed, N, K, group):
     """device pointer of packed weights (uint8), which must be large enough for [N, K]"""
     if packed.numel() < ls_op_w4_bytes(N, K, group):
         raise LsError(LS_ERR_CAPACITY, "packed weights")
-    return _arg(packed, _U8, "packed weights")
+    return _arg(packed, _torch.u8, "packed weights")
 
 
 def ls_op_quantize_w4(w, group, packed):
     """bf16 [N, K] -> packed 4-bit weights (uint8, ls_op_w4_bytes(N, K, group) of them)"""
     N, K = w.shape
     p = _packed(packed, N, K, group)
-    _ck(lib().ls_op_quantize_w4(_arg(w, _BF16, "w"), N, K, group, p, _stream()), "ls_op_quantize_w4")
+    _ck(lib().ls_op_quantize_w4(_arg(w, _torch.bf16, "w"), N, K, group, p, _stream()), "ls_op_quantize_w4")
 
 
 def ls_op_expand_w4(packed, group, out):
     N, K = out.shape
     p = _packed(packed, N, K, group)
-    _ck(lib().ls_op_expand_w4(p, N, K, group, _arg(out, _BF16, "out"), _stream()), "ls_op_expand_w4")
+    _ck(lib().ls_op_expand_w4(p, N, K, group, _arg(out, _torch.bf16, "out"), _stream()), "ls_op_expand_w4")
 
 
 def ls_op_linear_w4(packed, group, h, out, residual=False):
@@ -479,7 +479,7 @@ def ls_op_linear_w4(packed, group, h, out, residual=False):
     if rows != M:
         _bad("ls_op_linear_w4: rows of h and out")
     p = _packed(packed, N, K, group)
-    _ck(lib().ls_op_linear_w4(p, _arg(h, _BF16, "h"), M, N, K, group, _arg(out, _F32, "out"), int(residual), _stream()),
+    _ck(lib().ls_op_linear_w4(p, _arg(h, _torch.bf16, "h"), M, N, K, group, _arg(out, _torch.f32, "out"), int(residual), _stream()),
         "ls_op_linear_w4")
 
 
@@ -497,21 +497,23 @@ def _pool(pages, Hkv, hd, page_size):
 
 def _rows(pos0, table, n_seq):
     """entries per sequence of a page table int32 [n_seq, entries]; pos0 int32 [n_seq]"""
-    if pos0.numel() != n_seq or table.dim() != 2 or table.shape[0] != n_seq:
+    shape = table.shape
+    if pos0.numel() != n_seq or len(shape) != 2 or shape[0] != n_seq:
         _bad("pos0 [n_seq] and page table [n_seq, entries]")
-    return table.shape[1]
+    return shape[1]
 
 
 def ls_op_append_kv4(k, v, pos0, page_size, table, max_seq, pages, status=None):
     """k, v bf16 [n_seq, M, Hkv, hd], of any strides but equal ones, channels contiguous"""
     n_seq, M, Hkv, hd = k.shape
     n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
-    if v.shape != k.shape or v.stride() != k.stride() or k.stride(3) != 1 or not (k.is_cuda and v.is_cuda) or \
-            k.dtype is not _t().bfloat16 or v.dtype is not _t().bfloat16:
+    stride = k.stride()
+    if v.shape != k.shape or v.stride() != stride or stride[3] != 1 or not (k.is_cuda and v.is_cuda) or \
+            k.dtype is not _torch.bf16 or v.dtype is not _torch.bf16:
         _bad("ls_op_append_kv4: k and v")
-    _ck(lib().ls_op_append_kv4(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), n_seq, M,
-                               _arg(pos0, _INT, "pos0"), Hkv, hd, page_size, _arg(table, _INT, "page table"), entries, max_seq,
-                               _arg(pages, _U8, "pages"), n_pages, _status(status), _stream()), "ls_op_append_kv4")
+    _ck(lib().ls_op_append_kv4(k.data_ptr(), v.data_ptr(), stride[0], stride[1], stride[2], n_seq, M,
+                               _arg(pos0, _torch.i32, "pos0"), Hkv, hd, page_size, _arg(table, _torch.i32, "page table"), entries, max_seq,
+                               _arg(pages, _torch.u8, "pages"), n_pages, _status(status), _stream()), "ls_op_append_kv4")
 
 
 def ls_op_expand_kv4(pages, pos0, M, page_size, table, max_seq, out_table, k_pages, v_pages, status=None):
@@ -521,9 +523,9 @@ def ls_op_expand_kv4(pages, pos0, M, page_size, table, max_seq, out_table, k_pag
     n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
     if ps != page_size or v_pages.shape != k_pages.shape or out_table.shape != table.shape:
         _bad("ls_op_expand_kv4: k_pages, v_pages and their table")
-    _ck(lib().ls_op_expand_kv4(_arg(pages, _U8, "pages"), n_pages, n_seq, M, _arg(pos0, _INT, "pos0"), Hkv, hd, page_size,
-                               _arg(table, _INT, "page table"), entries, max_seq, _arg(out_table, _INT, "out page table"),
-                               _arg(k_pages, _BF16, "k_pages"), _arg(v_pages, _BF16, "v_pages"), n_out,
+    _ck(lib().ls_op_expand_kv4(_arg(pages, _torch.u8, "pages"), n_pages, n_seq, M, _arg(pos0, _torch.i32, "pos0"), Hkv, hd, page_size,
+                               _arg(table, _torch.i32, "page table"), entries, max_seq, _arg(out_table, _torch.i32, "out page table"),
+                               _arg(k_pages, _torch.bf16, "k_pages"), _arg(v_pages, _torch.bf16, "v_pages"), n_out,
                                _status(status), _stream()), "ls_op_expand_kv4")
 
 
@@ -542,12 +544,12 @@ def ls_op_attention_kv4(q, pos0, Hkv, hd, page_size, table, max_seq, pages, out,
     Hq = width // hd
     need = ls_op_attention_kv4_scratch_bytes(n_seq, M, Hq, Hkv, hd, max_seq)
     if scratch is None and need:
-        scratch = _t().empty(need, dtype=_t().uint8, device=q.device)
+        scratch = _torch.empty(need, dtype=_torch.u8, device=q.device)
     elif scratch is not None and scratch.numel() < need:
         raise LsError(LS_ERR_CAPACITY, "ls_op_attention_kv4: scratch")
-    _ck(lib().ls_op_attention_kv4(_arg(q, _BF16, "q"), n_seq, M, _arg(pos0, _INT, "pos0"), Hq, Hkv, hd, page_size,
-                                  _arg(table, _INT, "page table"), entries, max_seq, _arg(pages, _U8, "pages"), n_pages,
-                                  _arg(out, _BF16, "out"), None if scratch is None else _arg(scratch, _U8, "scratch"), _status(status),
+    _ck(lib().ls_op_attention_kv4(_arg(q, _torch.bf16, "q"), n_seq, M, _arg(pos0, _torch.i32, "pos0"), Hq, Hkv, hd, page_size,
+                                  _arg(table, _torch.i32, "page table"), entries, max_seq, _arg(pages, _torch.u8, "pages"), n_pages,
+                                  _arg(out, _torch.bf16, "out"), None if scratch is None else _arg(scratch, _torch.u8, "scratch"), _status(status),
                                   _stream()), "ls_op_attention_kv4")
 
 
