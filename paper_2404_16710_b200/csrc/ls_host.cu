@@ -2018,22 +2018,24 @@ int ls_op_expand_kv4(const void* pages, int32_t n_pages, int32_t n_seq, int32_t 
 
 namespace {
 
-// How the positions of a (sequence, KV head) are spread: splits x S CTAs, enough for about two CTAs per SM.  A CTA
-// pays for its start and its share of the joining (32 heads, 1030 positions: 8 CTAs a head 6.5 us, 4 of them, with
-// two chunks for a warp, 6.9; 1024 positions: 6.6, 5.3); splits cost a second kernel, some 2 us (8 heads, 4 splits: 4096
-// positions 9.0 us, without 7.0; 8192: 10.0, 11.0; 131072: 44, 104).  Never a function of the rows of the call.
+// How the positions of a (sequence, KV head) are spread: a cluster of S CTAs, so many that all fit one to an SM (with
+// more than 8 queries a CTA fills one: 16 rows of 32 heads over 4103 positions 13.8 us with 128 CTAs, 27.4 with 256;
+// with fewer two fit, and 256 are 5 to 10 % faster), and no more than the cache has rounds of chunks for.  Few heads
+// over a long cache take several such splits: that costs a second kernel, some 2 us (8 heads, 4 splits: 4096 positions
+// 9.0 us, without 7.0; 16384: 13.0, 16.2; 131072: 44, 104).  Never a function of the rows of the call.
 struct Kv4Plan {
     int S, splits;
 };
 Kv4Plan kv4_plan(int n_seq, int Hkv, int max_seq, bool may_split)
 {
-    Kv4Plan p = {1, 1};
-    const int64_t pairs = (int64_t)n_seq * Hkv;
-    const int round = kKv4Warps * kKv4Chunk;
-    while (p.S < kKv4MaxCluster && p.S * pairs < 256 && p.S * round < max_seq) p.S *= 2;
-    if (may_split && max_seq >= 4 * p.S * round)
-        while (p.splits < 64 && p.splits * p.S * pairs < 256 && 2 * p.splits * p.S * round <= max_seq) p.splits *= 2;
-    return p;
+    const int64_t pairs = (int64_t)n_seq * Hkv, round = kKv4Warps * kKv4Chunk, rounds = (max_seq + round - 1) / round;
+    int64_t S = pairs > 148 ? 1 : 148 / pairs;
+    if (S > kKv4MaxCluster) S = kKv4MaxCluster;
+    if (S > rounds) S = rounds;
+    int splits = 1;
+    if (may_split && S == kKv4MaxCluster && max_seq >= 4 * S * round)
+        while (splits < 64 && 2 * splits * S * pairs <= 296 && 2 * splits * S * round <= max_seq) splits *= 2;
+    return Kv4Plan{(int)S, splits};
 }
 uint32_t divisor(int d) { return d > 1 ? 0xffffffffu / (uint32_t)d + 1u : 0u; }  // for fastdiv on the device
 int kv4_query_tile(int Q) { return Q <= 8 ? 1 : Q <= 16 ? 2 : Q <= 24 ? 3 : 4; }  // tiles of 8 queries a CTA takes
@@ -2074,7 +2076,7 @@ int kv4_attn_launch(const Kv4Plan& plan, int n_seq, const uint16_t* q, int M, in
     at[2].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = lc.pdl ? 3 : 2;
-    LS_CK(cudaLaunchKernelEx(&cfg, kernel, q, M, G, pos0, c, pages, log2_exact(plan.S), divisor(G), divisor(c.Hkv), out,
+    LS_CK(cudaLaunchKernelEx(&cfg, kernel, q, M, G, pos0, c, pages, plan.S, divisor(plan.S), divisor(G), divisor(c.Hkv), out,
                              scratch, status));
     if (plan.splits > 1)  // may move in while the splits finish; it waits for them before it reads
         LS_CK(launch(LaunchCtx{lc.st, true}, combine_kv4_kernel<HD>, dim3(M, G * c.Hkv, n_seq), dim3(HD / 2), 0, scratch, G, pos0,

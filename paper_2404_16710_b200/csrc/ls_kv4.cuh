@@ -91,7 +91,7 @@ struct Kv4Smem {
     static constexpr int kItems = NT * HD / 16 * 32;           // float4 pieces of O: [NT][HD / 16][lane]
     static constexpr int kRing = W * kWarpRing;
     static constexpr int kQ = NT * HD / 32 * 32 * 16;          // [NT][group][lane] 16 bytes
-    static constexpr int kInbox = kItems * 16;                 // [CTA][its share of the pieces]
+    static constexpr int kInbox = (kItems + kKv4MaxCluster) * 16;  // [CTA][a share of the pieces]
     static constexpr int kFactor = NT * 8 * 4;                 // 2^e [query]
     static constexpr int kStat = W * NT * 8 * 8 + W * 4;       // (max, sum) of the warps, units of their O
     static constexpr int kInStat = kKv4MaxCluster * NT * 8 * 8;  // (max, sum) of the CTAs
@@ -119,7 +119,7 @@ __device__ __forceinline__ float kv4_unit(int hd) { return 0x1p-14f * 1.44269504
 template <int HD, int NT>
 __global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1)
 attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t* __restrict__ pos0_dev,
-                     const Kv4Cache cache, const unsigned char* __restrict__ pages, int log2_S, uint32_t div_G, uint32_t div_Hkv,
+                     const Kv4Cache cache, const unsigned char* __restrict__ pages, int S, uint32_t div_S, uint32_t div_G, uint32_t div_Hkv,
                      uint16_t* __restrict__ out, float* __restrict__ scratch, int32_t* status)
 {
     using SM = Kv4Smem<HD, NT>;
@@ -137,7 +137,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     float2* sInStat = reinterpret_cast<float2*>(at += SM::kStat);   // [CTA][NT * 8]
     pdl_launch_dependents();
     pdl_wait();
-    const int S = 1 << log2_S, splits = gridDim.x >> log2_S, split = blockIdx.x >> log2_S, rank = blockIdx.x & (S - 1), b = blockIdx.z;
+    const int splits = fastdiv(gridDim.x, S, div_S), split = fastdiv(blockIdx.x, S, div_S), rank = blockIdx.x - split * S, b = blockIdx.z;
     if (S > 1) cluster_arrive_relaxed();  // this CTA is there
     const int tile_y = fastdiv(blockIdx.y, cache.Hkv, div_Hkv), head = blockIdx.y - tile_y * cache.Hkv, q0 = tile_y * (NT * 8);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -503,7 +503,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     if (S > 1) cluster_wait();  // the others are there
     __syncthreads();
     // ---- the CTA's, sent to the CTA that finishes them: piece x holds two queries x two channels
-    const int share = SM::kItems >> log2_S;
+    const int share = fastdiv(SM::kItems + S - 1, S, div_S);  // pieces a CTA finishes; the last one may have fewer
     for (int x = threadIdx.x; x < SM::kItems; x += W * 32) {
         const int c = x / (CT * 32) * 8 + 2 * (x & 3);  // its first query
         if (q0 + c >= Q) continue;
@@ -523,7 +523,8 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             r.x = fmaf(f0 * unit, v.x, r.x), r.z = fmaf(f0 * unit, v.z, r.z);
             r.y = fmaf(f1 * unit, v.y, r.y), r.w = fmaf(f1 * unit, v.w, r.w);
         }
-        const int to = x / (SM::kItems / kKv4MaxCluster) >> (3 - log2_S);  // x / share
+        int to = 0;  // x / share
+        for (int edge = share; edge <= x; edge += share) ++to;
         st_cluster_f4(map_cluster(smem_u32(sIn) + (rank * share + x - to * share) * 16, to), r);
         if ((x / 4) % (CT * 8) == 0)  // one of the pieces with these queries: their statistics, to all
             for (int d = 0; d < S; ++d) {
@@ -538,7 +539,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
         __syncthreads();
     for (int y = threadIdx.x; y < 2 * share; y += W * 32) {  // one query and two channels a thread
         const int x = rank * share + y / 2, e = y & 1, l = x & 31, c = x / (CT * 32) * 8 + 2 * (l & 3) + e, qi = q0 + c;
-        if (qi >= Q) continue;
+        if (x >= SM::kItems || qi >= Q) continue;
         float m = -INFINITY, sum_l = 0.f, v0 = 0.f, v1 = 0.f;
         for (int r = 0; r < S; ++r) m = fmaxf(m, sInStat[r * NT * 8 + c].x);
 #pragma unroll 4
