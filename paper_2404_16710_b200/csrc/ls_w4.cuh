@@ -112,8 +112,12 @@ __device__ __forceinline__ void w4_block_mma(const W4Regs<NG>& w, const uint4 (&
 // zeros); otherwise, for h larger than that, it comes through L1.
 // The codes are the A operand of mma.sync, the rows of h the B operand; a group's products are summed in fp32 by
 // the tensor cores and multiplied by the group's scale (a lane holds rows g and g + 8 of a tile) when they join
-// the running sum.  Turning codes into operands (11 instructions for 8 codes, 7 of them on a pipe of half rate) bounds
-// the kernel.  Which blocks a warp adds, and in which order the
+// the running sum.  Turning codes into operands bounds the kernel: 11 instructions for 8 codes, 7 of them on the
+// half-rate integer pipe, which is 50 % busy on average and collides with the products of the other warps.  With the
+// conversion left out the loads alone take 43 us for 128256 x 4096 (the copy rate), 4.0 us for 4096 x 4096; with it, one
+// row of h: 55.8 us (0.77 of the measured copy rate) and 5.1 us (0.26: 2 us are the launch).  Tried and not kept: bulk
+// copies with h from L1 (143 us, too few warps), blocks held in registers (94 to 104 us: the loads of several blocks end
+// up waiting for one another), f16 operands (3 to 5 % faster for one row, slower for 16: h has to be converted).  Which blocks a warp adds, and in which order the
 // warps' sums are added, depends on N and K only: a row's result does not depend on how many rows share
 // the pass.
 template <int NG, int NT, int W, int D, int CB, bool HS, int TG>
