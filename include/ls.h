@@ -383,6 +383,8 @@ int ls_op_prefill_attention(const void *q_bf16_dev, int32_t R, int32_t pos0, int
  * A row at a negative position is padding.  A position >= max_seq or a table entry outside
  * [0, n_pages) is refused by the kernel: the access is skipped and status_dev (device int32, may be
  * NULL, never cleared by the library) receives 2 or 4.
+ * The first call of each kernel configuration (the class of M, the group, hd) loads the kernel and sets
+ * its attributes: make it outside any stream capture.
  * ------------------------------------------------------------------------------ */
 #define LS_KV4_MAX_SEQ (1 << 20)
 
@@ -404,9 +406,9 @@ int ls_op_linear_w4(const void *packed_dev, const void *h_bf16_dev, int32_t M, i
 /* Bytes of a page; 0 for a shape the format does not cover. */
 size_t ls_op_kv4_page_bytes(int32_t Hkv, int32_t hd, int32_t page_size);
 /* Append: k, v (bf16, k already rotated) of row m, KV head i of sequence b at element b * seq_stride +
- * m * row_stride + i * head_stride of either tensor (strides multiples of 8, channels
- * contiguous, 16-byte aligned: a contiguous [n_seq][M][Hkv][hd], or a page of a bf16 cache that
- * ls_op_rope_append wrote).  Any M.  Rows of padding are left out; nothing else in the pages
+ * m * row_stride + i * head_stride of either tensor (strides multiples of 8, but for those of
+ * dimensions of one; channels contiguous, 16-byte aligned: a contiguous [n_seq][M][Hkv][hd], or a
+ * page of a bf16 cache that ls_op_rope_append wrote).  Any M.  Rows of padding are left out; nothing else in the pages
  * changes.  Two rows of one call must not fall on the same slot of the same page. */
 int ls_op_append_kv4(const void *k_bf16_dev, const void *v_bf16_dev, int64_t seq_stride, int64_t row_stride,
                      int64_t head_stride, int32_t n_seq, int32_t M, const int32_t *pos0_dev, int32_t Hkv,

@@ -1844,6 +1844,13 @@ static bool w4_shape_ok(int N, int K, int group)
 }
 static int w4_kblocks(int K) { return (int)(((int64_t)K + kQ4Cols - 1) / kQ4Cols); }
 static int64_t w4_blocks(int N, int K) { return ((int64_t)N + kQ4Rows - 1) / kQ4Rows * w4_kblocks(K); }
+// A chained operation may read weights before the one ahead of it has finished (ls_op_chain), so what writes weights is
+// followed by a launch that waits for it to the end and that the next operation overlaps instead.
+static int w4_written(cudaStream_t stream)
+{
+    if (g_op_chain) LS_CK(launch(LaunchCtx{stream, false}, fence_kernel, dim3(1), dim3(32), 0));
+    return LS_OK;
+}
 
 size_t ls_op_w4_bytes(int32_t N, int32_t K, int32_t group)
 {
@@ -1859,7 +1866,7 @@ int ls_op_quantize_w4(const void* w, int32_t N, int32_t K, int32_t group, void* 
     auto* kernel = group == 32 ? quantize_w4_kernel<4> : group == 64 ? quantize_w4_kernel<2> : quantize_w4_kernel<1>;
     LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, kernel, dim3((unsigned)((blocks + 7) / 8)), dim3(256), 0,
                  (const uint16_t*)w, N, K, w4_kblocks(K), blocks, (unsigned char*)packed));
-    return LS_OK;
+    return w4_written((cudaStream_t)stream);
 }
 
 int ls_op_expand_w4(const void* packed, int32_t N, int32_t K, int32_t group, void* out, void* stream)
@@ -1870,7 +1877,7 @@ int ls_op_expand_w4(const void* packed, int32_t N, int32_t K, int32_t group, voi
     auto* kernel = group == 32 ? expand_w4_kernel<4> : group == 64 ? expand_w4_kernel<2> : expand_w4_kernel<1>;
     LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, kernel, dim3((unsigned)((blocks + 7) / 8)), dim3(256), 0,
                  (const unsigned char*)packed, N, K, w4_kblocks(K), blocks, (uint16_t*)out));
-    return LS_OK;
+    return w4_written((cudaStream_t)stream);
 }
 
 }  // extern "C"
@@ -1917,7 +1924,7 @@ template <int NG>
 int w4_launch_ng(const unsigned char* packed, const uint16_t* h, int M, int N, int K, float* out, int residual,
                  const LaunchCtx& lc)
 {
-    const int64_t room = kW4SmemMax - (int64_t)M * w4_h_stride(w4_kblocks(K));
+    const int64_t room = kW4SmemMax - M * ((int64_t)w4_kblocks(K) * kQ4Cols * 2 + 64);  // w4_h_stride, without overflow
     if (M <= 8) {
         const int64_t ring24 = room - w4_part_bytes<1, 24>(), ring16 = room - w4_part_bytes<1, 16>();
         // 24 warps, what 64 to 80 registers allow, make a third team of 8 warps: of use with more than two tiles an SM
@@ -1988,7 +1995,8 @@ int ls_op_append_kv4(const void* k, const void* v, int64_t seq_stride, int64_t r
 {
     Kv4Cache c;
     LS_TRY(kv4_check(n_seq, M, pos0, Hkv, hd, page_size, table, table_stride, max_seq, pages, n_pages, &c));
-    if (!aligned16(k) || !aligned16(v) || seq_stride % 8 || row_stride % 8 || head_stride % 8) return LS_ERR_INVALID_ARG;
+    if (!aligned16(k) || !aligned16(v) || (n_seq > 1 && seq_stride % 8) || (M > 1 && row_stride % 8) || (Hkv > 1 && head_stride % 8))
+        return LS_ERR_INVALID_ARG;
     const int w = kv4_warps(M);
     LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, hd == 128 ? append_kv4_kernel<128> : append_kv4_kernel<64>,
                  dim3((unsigned)((M + (int64_t)8 * w - 1) / (8 * w)), Hkv, n_seq), dim3(32 * w), 0, (const uint16_t*)k,

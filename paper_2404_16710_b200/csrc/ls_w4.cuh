@@ -9,13 +9,6 @@
 
 namespace ls {
 
-// contiguous bytes (a multiple of 16, both ends 16-byte aligned) to shared memory, announced on an mbarrier
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-                 "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
-}
 __device__ __forceinline__ uint2 lds8(uint32_t addr)
 {
     uint2 v;

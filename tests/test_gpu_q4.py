@@ -323,11 +323,25 @@ def test_attention(Hkv, G, hd, M, lens, page):
 
 @pytest.mark.parametrize("n_seq", [1, 40])
 def test_attention_clusters_of_every_size_and_peaked_scores(n_seq):
-    """one to 16 CTAs a head (by the number of sequences and heads), scores that differ by hundreds"""
+    """one to 8 CTAs a head (by the number of sequences and heads), scores that differ by hundreds"""
     for Hkv in (1, 2, 8):
         c = Cache([700 - 13 * b for b in range(n_seq)], Hkv, 128, 64, 30, max_seq=4096, loud=6.0)
         q = rnd((n_seq, 2, Hkv * 2 * 128), 31, 2.0).bfloat16()
         check_attention(c, q, c.run(q, 2), 2, 2)
+
+
+@pytest.mark.parametrize("Hkv,n_seq", [(20, 1), (24, 1), (30, 1), (40, 1), (5, 7), (3, 50), (150, 1)])
+def test_attention_clusters_of_odd_sizes(Hkv, n_seq):
+    """numbers of heads that leave 7, 6, 4, 3 and fewer CTAs each; every row the same in a pass of one as among 8"""
+    c = Cache([900 - 11 * b for b in range(n_seq)], Hkv, 64, 64, 60, max_seq=2048)
+    q = rnd((n_seq, 8, Hkv * 64), 61, 2.0).bfloat16()
+    full = c.run(q, 8)
+    check_attention(c, q, full, 8, 1)
+    for m in (0, 5, 7):
+        out = torch.empty((n_seq, 1, Hkv * 64), dtype=torch.bfloat16, device="cuda")
+        pos = torch.tensor([900 - 11 * b - 8 + m for b in range(n_seq)], dtype=torch.int32, device="cuda")
+        B.ls_op_attention_kv4(q[:, m:m + 1].contiguous(), pos, Hkv, 64, 64, c.table, 2048, c.pool, out)
+        assert torch.equal(out, full[:, m:m + 1]), m
 
 
 @pytest.mark.parametrize("Hkv,G,hd", [(2, 1, 128), (2, 4, 64), (4, 8, 128)])
@@ -505,6 +519,80 @@ def test_attention_split_rows_without_keys_and_captured():
     st.synchronize()
     torch.cuda.synchronize()
     assert torch.equal(out, eager) and torch.equal(again, eager)
+
+
+def test_attention_over_the_longest_cache():
+    """LS_KV4_MAX_SEQ positions, split: against 64-bit torch arithmetic on the expanded cache"""
+    n, hd, page = 1 << 20, 64, 1024
+    table = torch.randperm(n // page, generator=torch.Generator().manual_seed(1)).to(torch.int32).cuda()[None]
+    pool = empty_pool(n // page, 1, hd, page)
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    k, v = rnd((1, n, 1, hd), 110).bfloat16(), rnd((1, n, 1, hd), 111).bfloat16()
+    B.ls_op_append_kv4(k, v, zero, page, table, n, pool)
+    kp, vp = (torch.empty((n // page, 1, page, hd), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    B.ls_op_expand_kv4(pool, zero, n, page, table, n, torch.arange(n // page, dtype=torch.int32, device="cuda")[None], kp, vp)
+    q = rnd((1, 2, 8 * hd), 112, 3.0).bfloat16()
+    out, status = torch.empty_like(q), torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.ls_op_attention_kv4(q, torch.tensor([n - 2], dtype=torch.int32, device="cuda"), 1, hd, page, table, n, pool, out, status)
+    kd, vd = kp.view(n, hd).double(), vp.view(n, hd).double()
+    for m in range(2):
+        a = torch.softmax(q[0, m].view(8, hd).double() @ kd[:n - 1 + m].t() / hd ** 0.5, -1)
+        ref, spread = (a @ vd[:n - 1 + m]).cpu().numpy(), (a @ vd[:n - 1 + m].abs()).cpu().numpy()
+        assert (np.abs(vals(out)[0, m].reshape(8, hd) - ref) <= attention_tol(ref, spread, vals(v[0, :, 0]))).all()
+    assert int(status) == 0
+
+
+def test_packing_right_before_a_chained_linear():
+    """with chained operations, which read weights ahead of time, the weights that the call before packs are the ones used"""
+    N, K = 4096, 2048
+    h = rnd((1, K), 120).bfloat16()
+    ws = [rnd((N, K), 121 + i, 0.02).bfloat16() for i in range(6)]
+    packed, outs, want = torch.zeros(B.ls_op_w4_bytes(N, K, 32), dtype=torch.uint8, device="cuda"), [], []
+    for chained in (False, True):
+        B.ls_op_chain(chained)
+        try:
+            for w in ws:
+                o = torch.zeros((1, N), device="cuda")
+                torch.cuda.synchronize()
+                B.ls_op_quantize_w4(w, 32, packed)
+                B.ls_op_linear_w4(packed, 32, h, o)
+                (outs if chained else want).append(o)
+        finally:
+            B.ls_op_chain(False)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_expanding_right_before_a_chained_bf16_linear():
+    N, K = 4096, 2048
+    h = rnd((1, K), 140).bfloat16()
+    packs = [torch.zeros(B.ls_op_w4_bytes(N, K, 32), dtype=torch.uint8, device="cuda") for _ in range(6)]
+    for i, p in enumerate(packs):
+        B.ls_op_quantize_w4(rnd((N, K), 141 + i, 0.02).bfloat16(), 32, p)
+    w, outs, want = torch.zeros((N, K), dtype=torch.bfloat16, device="cuda"), [], []
+    for chained in (False, True):
+        B.ls_op_chain(chained)
+        try:
+            for p in packs:
+                o = torch.zeros((1, N), device="cuda")
+                torch.cuda.synchronize()
+                B.ls_op_expand_w4(p, 32, w)
+                B.ls_op_linear(B.LS_LINEAR_MMA, w, h, o)
+                (outs if chained else want).append(o)
+        finally:
+            B.ls_op_chain(False)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_rows_of_one_sequence_and_head_with_odd_strides():
+    """strides of dimensions of one do not matter"""
+    x = rnd((3, 5 * 64 + 8), 130).bfloat16()
+    k = x.as_strided((1, 3, 1, 64), (3, 5 * 64 + 8, 7, 1))
+    pool, table = empty_pool(1, 1, 64, 16), torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    want = reference_append(pool.cpu().numpy().copy(), vals(k), vals(k), [2], table.cpu().numpy(), 16, 16)
+    B.ls_op_append_kv4(k, k, torch.tensor([2], dtype=torch.int32, device="cuda"), 16, table, 16, pool)
+    assert np.array_equal(pool.cpu().numpy(), want)
 
 
 def test_two_streams_at_once():

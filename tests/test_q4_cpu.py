@@ -91,9 +91,10 @@ def test_cache_operations_refuse_bad_arguments():
     # k, v, strides, n_seq, M, pos0, Hkv, hd, page_size, table, stride, max_seq, pages, n_pages, status, stream
     good = [P, P, 1024, 256, 128, 1, 4, P, 2, 128, 64, P, 4, 256, P, 4, None, None]
     refused(L.ls_op_append_kv4, good, [
-        (0, None, BAD), (0, P + 8, BAD), (1, None, BAD), (2, 4, BAD), (3, 12, BAD), (4, 1, BAD), (5, 0, BAD), (5, 70000, CAP),
+        (0, None, BAD), (0, P + 8, BAD), (1, None, BAD), (3, 12, BAD), (4, 1, BAD), (5, 0, BAD), (5, 70000, CAP),
         (6, 0, BAD), (7, None, BAD), (8, 0, BAD), (8, 5000, CAP), (9, 96, BAD), (10, 48, BAD), (10, 8, BAD), (11, None, BAD),
         (12, 3, BAD), (13, 0, CAP), (13, (1 << 20) + 1, CAP), (14, None, BAD), (14, P + 8, BAD), (15, 0, BAD)])
+    refused(L.ls_op_append_kv4, good[:5] + [2] + good[6:], [(2, 4, BAD)])
     # pages, n_pages, n_seq, M, pos0, Hkv, hd, page_size, table, stride, max_seq, out_table, kp, vp, n_out, status, stream
     good = [P, 4, 1, 4, P, 2, 128, 64, P, 4, 256, P, P, P, 4, None, None]
     refused(L.ls_op_expand_kv4, good, [
