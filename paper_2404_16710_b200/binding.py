@@ -158,6 +158,7 @@ class _Torch:
         # torch.cuda.current_stream() builds a Stream object (3.4 us a call, as much as a launch); the raw handle costs 0.2
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.stream = (lambda: raw(torch.cuda.current_device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
+        self.device = torch.cuda.current_device
         return self
 
     def __getattr__(self, name):  # only before load()
@@ -437,15 +438,22 @@ def _bad(what):
     raise LsError(LS_ERR_INVALID_ARG, what)
 
 
-def _arg(t, dtype, what):
-    """device pointer of a contiguous CUDA tensor of the type the entry point reads"""
-    if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+def _arg(t, dtype, dev, what):
+    """device pointer of a contiguous CUDA tensor of the type the entry point reads, on device dev"""
+    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
         return t.data_ptr()
-    _bad(f"{what}: a contiguous {dtype} CUDA tensor is needed")
+    _bad(f"{what}: a contiguous {dtype} tensor is needed, on the CUDA device of the others")
 
 
-def _status(t):
-    return None if t is None else _arg(t, _torch.i32, "status")
+def _status(t, dev):
+    return None if t is None else _arg(t, _torch.i32, dev, "status")
+
+
+def _stream_on(dev):
+    """handle of the current stream, which has to be one of the operands' device"""
+    if dev < 0 or dev != _torch.device():
+        _bad("operands on the current CUDA device are needed")
+    return _torch.stream()
 
 
 @functools.lru_cache(maxsize=4096)
@@ -453,33 +461,33 @@ def ls_op_w4_bytes(N, K, group):
     return lib().ls_op_w4_bytes(N, K, group)
 
 
-def _packed(packed, N, K, group):
+def _packed(packed, N, K, group, dev):
     """device pointer of packed weights (uint8), which must be large enough for [N, K]"""
     if packed.numel() < ls_op_w4_bytes(N, K, group):
         raise LsError(LS_ERR_CAPACITY, "packed weights")
-    return _arg(packed, _torch.u8, "packed weights")
+    return _arg(packed, _torch.u8, dev, "packed weights")
 
 
 def ls_op_quantize_w4(w, group, packed):
     """bf16 [N, K] -> packed 4-bit weights (uint8, ls_op_w4_bytes(N, K, group) of them)"""
-    N, K = w.shape
-    p = _packed(packed, N, K, group)
-    _ck(lib().ls_op_quantize_w4(_arg(w, _torch.bf16, "w"), N, K, group, p, _stream()), "ls_op_quantize_w4")
+    (N, K), dev = w.shape, w.get_device()
+    p = _packed(packed, N, K, group, dev)
+    _ck(lib().ls_op_quantize_w4(_arg(w, _torch.bf16, dev, "w"), N, K, group, p, _stream_on(dev)), "ls_op_quantize_w4")
 
 
 def ls_op_expand_w4(packed, group, out):
-    N, K = out.shape
-    p = _packed(packed, N, K, group)
-    _ck(lib().ls_op_expand_w4(p, N, K, group, _arg(out, _torch.bf16, "out"), _stream()), "ls_op_expand_w4")
+    (N, K), dev = out.shape, out.get_device()
+    p = _packed(packed, N, K, group, dev)
+    _ck(lib().ls_op_expand_w4(p, N, K, group, _arg(out, _torch.bf16, dev, "out"), _stream_on(dev)), "ls_op_expand_w4")
 
 
 def ls_op_linear_w4(packed, group, h, out, residual=False):
     """out[M, N] (+)= h[M, K] @ W.T of the packed weights W [N, K]"""
-    (M, K), (rows, N) = h.shape, out.shape
+    (M, K), (rows, N), dev = h.shape, out.shape, h.get_device()
     if rows != M:
         _bad("ls_op_linear_w4: rows of h and out")
-    p = _packed(packed, N, K, group)
-    _ck(lib().ls_op_linear_w4(p, _arg(h, _torch.bf16, "h"), M, N, K, group, _arg(out, _torch.f32, "out"), int(residual), _stream()),
+    p = _packed(packed, N, K, group, dev)
+    _ck(lib().ls_op_linear_w4(p, _arg(h, _torch.bf16, dev, "h"), M, N, K, group, _arg(out, _torch.f32, dev, "out"), int(residual), _stream_on(dev)),
         "ls_op_linear_w4")
 
 
@@ -505,28 +513,28 @@ def _rows(pos0, table, n_seq):
 
 def ls_op_append_kv4(k, v, pos0, page_size, table, max_seq, pages, status=None):
     """k, v bf16 [n_seq, M, Hkv, hd], of any strides but equal ones, channels contiguous"""
-    n_seq, M, Hkv, hd = k.shape
+    (n_seq, M, Hkv, hd), dev = k.shape, k.get_device()
     n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
     stride = k.stride()
-    if v.shape != k.shape or v.stride() != stride or stride[3] != 1 or not (k.is_cuda and v.is_cuda) or \
+    if v.shape != k.shape or v.stride() != stride or stride[3] != 1 or dev < 0 or v.get_device() != dev or \
             k.dtype is not _torch.bf16 or v.dtype is not _torch.bf16:
         _bad("ls_op_append_kv4: k and v")
     _ck(lib().ls_op_append_kv4(k.data_ptr(), v.data_ptr(), stride[0], stride[1], stride[2], n_seq, M,
-                               _arg(pos0, _torch.i32, "pos0"), Hkv, hd, page_size, _arg(table, _torch.i32, "page table"), entries, max_seq,
-                               _arg(pages, _torch.u8, "pages"), n_pages, _status(status), _stream()), "ls_op_append_kv4")
+                               _arg(pos0, _torch.i32, dev, "pos0"), Hkv, hd, page_size, _arg(table, _torch.i32, dev, "page table"), entries, max_seq,
+                               _arg(pages, _torch.u8, dev, "pages"), n_pages, _status(status, dev), _stream_on(dev)), "ls_op_append_kv4")
 
 
 def ls_op_expand_kv4(pages, pos0, M, page_size, table, max_seq, out_table, k_pages, v_pages, status=None):
     """k_pages, v_pages bf16 [n_out_pages, Hkv, page_size, hd]"""
-    n_out, Hkv, ps, hd = k_pages.shape
+    (n_out, Hkv, ps, hd), dev = k_pages.shape, k_pages.get_device()
     n_seq = table.shape[0]
     n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
     if ps != page_size or v_pages.shape != k_pages.shape or out_table.shape != table.shape:
         _bad("ls_op_expand_kv4: k_pages, v_pages and their table")
-    _ck(lib().ls_op_expand_kv4(_arg(pages, _torch.u8, "pages"), n_pages, n_seq, M, _arg(pos0, _torch.i32, "pos0"), Hkv, hd, page_size,
-                               _arg(table, _torch.i32, "page table"), entries, max_seq, _arg(out_table, _torch.i32, "out page table"),
-                               _arg(k_pages, _torch.bf16, "k_pages"), _arg(v_pages, _torch.bf16, "v_pages"), n_out,
-                               _status(status), _stream()), "ls_op_expand_kv4")
+    _ck(lib().ls_op_expand_kv4(_arg(pages, _torch.u8, dev, "pages"), n_pages, n_seq, M, _arg(pos0, _torch.i32, dev, "pos0"), Hkv, hd, page_size,
+                               _arg(table, _torch.i32, dev, "page table"), entries, max_seq, _arg(out_table, _torch.i32, dev, "out page table"),
+                               _arg(k_pages, _torch.bf16, dev, "k_pages"), _arg(v_pages, _torch.bf16, dev, "v_pages"), n_out,
+                               _status(status, dev), _stream_on(dev)), "ls_op_expand_kv4")
 
 
 @functools.lru_cache(maxsize=4096)
@@ -537,7 +545,7 @@ def ls_op_attention_kv4_scratch_bytes(n_seq, M, Hq, Hkv, hd, max_seq):
 def ls_op_attention_kv4(q, pos0, Hkv, hd, page_size, table, max_seq, pages, out, status=None, scratch=None):
     """q, out bf16 [n_seq, M, Hq * hd].  scratch: uint8, ls_op_attention_kv4_scratch_bytes of them; None allocates them
     where the call can use any (torch's allocator hands them out and takes them back in stream order)."""
-    n_seq, M, width = q.shape
+    (n_seq, M, width), dev = q.shape, q.get_device()
     n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
     if width % hd or out.shape != q.shape:
         _bad("ls_op_attention_kv4: q and out")
@@ -547,10 +555,10 @@ def ls_op_attention_kv4(q, pos0, Hkv, hd, page_size, table, max_seq, pages, out,
         scratch = _torch.empty(need, dtype=_torch.u8, device=q.device)
     elif scratch is not None and scratch.numel() < need:
         raise LsError(LS_ERR_CAPACITY, "ls_op_attention_kv4: scratch")
-    _ck(lib().ls_op_attention_kv4(_arg(q, _torch.bf16, "q"), n_seq, M, _arg(pos0, _torch.i32, "pos0"), Hq, Hkv, hd, page_size,
-                                  _arg(table, _torch.i32, "page table"), entries, max_seq, _arg(pages, _torch.u8, "pages"), n_pages,
-                                  _arg(out, _torch.bf16, "out"), None if scratch is None else _arg(scratch, _torch.u8, "scratch"), _status(status),
-                                  _stream()), "ls_op_attention_kv4")
+    _ck(lib().ls_op_attention_kv4(_arg(q, _torch.bf16, dev, "q"), n_seq, M, _arg(pos0, _torch.i32, dev, "pos0"), Hq, Hkv, hd, page_size,
+                                  _arg(table, _torch.i32, dev, "page table"), entries, max_seq, _arg(pages, _torch.u8, dev, "pages"), n_pages,
+                                  _arg(out, _torch.bf16, dev, "out"), None if scratch is None else _arg(scratch, _torch.u8, dev, "scratch"), _status(status, dev),
+                                  _stream_on(dev)), "ls_op_attention_kv4")
 
 
 def ls_op_accept(draft, verified, d, state, out_ids, accepted):

@@ -123,3 +123,38 @@ def test_the_binding_refuses_what_does_not_fit():
         B.ls_op_attention_kv4(torch.zeros((1, 1, 1024), dtype=torch.bfloat16), pos, 2, 128, 64, table, 256, pages, torch.zeros((1, 1, 1024), dtype=torch.bfloat16))
     with pytest.raises(B.LsError):
         B.ls_op_expand_kv4(pages, pos, 4, 64, table, 256, table[:, :2], k.view(1, 2, 4, 128), k.view(1, 2, 4, 128))
+
+
+def test_the_binding_refuses_tensors_of_another_device(monkeypatch):
+    """a kernel is launched on the current device, which another device's memory need not be open to"""
+    import torch
+
+    class On:  # a tensor that says it is on some device
+        def __init__(self, t, dev):
+            self.t, self.dev = t, dev
+
+        is_cuda = True
+
+        def __getattr__(self, name):
+            return getattr(self.t, name)
+
+        def get_device(self):
+            return self.dev
+
+    monkeypatch.setattr(B._torch, "device", lambda: 0)
+    w, packed = torch.zeros((16, 128), dtype=torch.bfloat16), torch.zeros(B.ls_op_w4_bytes(16, 128, 32), dtype=torch.uint8)
+    h, out = w[:1], torch.zeros((1, 16))
+    k, i32 = torch.zeros((1, 1, 2, 64), dtype=torch.bfloat16), torch.zeros((1, 4), dtype=torch.int32)
+    pages, kp = torch.zeros(4 * B.ls_op_kv4_page_bytes(2, 64, 16), dtype=torch.uint8), torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16)
+    q, pos = torch.zeros((1, 1, 128), dtype=torch.bfloat16), i32[0, :1]
+    calls = [(B.ls_op_quantize_w4, [w, 32, packed]), (B.ls_op_expand_w4, [packed, 32, w]), (B.ls_op_linear_w4, [packed, 32, h, out]),
+             (B.ls_op_append_kv4, [k, k, pos, 16, i32, 64, pages, pos]),
+             (B.ls_op_expand_kv4, [pages, pos, 1, 16, i32, 64, i32, kp, kp, pos]),
+             (B.ls_op_attention_kv4, [q, pos, 2, 64, 16, i32, 64, pages, q, pos])]
+    for f, args in calls:
+        tensors = [i for i, a in enumerate(args) if isinstance(a, torch.Tensor)]
+        for odd in (None, *tensors):  # all on device 1, or one of them on device 1 and the rest on the current one
+            a = [On(x, int(odd in (None, i))) if i in tensors else x for i, x in enumerate(args)]
+            with pytest.raises(B.LsError) as e:
+                f(*a)
+            assert e.value.status == BAD, (f.__name__, odd)
