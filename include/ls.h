@@ -363,7 +363,7 @@ int ls_op_prefill_attention(const void *q_bf16_dev, int32_t R, int32_t pos0, int
  * k scales beyond 2^100).
  * Groups are 32 consecutive channels of a head (cache) or 32, 64 or 128 consecutive columns (weights).
  *
- * Packed weights of a matrix [N, K] (K a multiple of 8): blocks of 16 rows x 128 columns, the
+ * Packed weights of a matrix [N, K] (K a multiple of 8, at most 2^28): blocks of 16 rows x 128 columns, the
  * ceil(K / 128) blocks of 16 rows one after the other, then the next 16 rows; rows and columns
  * beyond N and K hold c = 0, s = 0.  A block is 16 rows of 64 bytes of codes, then the scales
  * bf16 [16][128 / group].  In a row's 64 bytes the 32-bit word 4 t + j (t, j = 0..3) holds columns
@@ -408,13 +408,13 @@ size_t ls_op_kv4_page_bytes(int32_t Hkv, int32_t hd, int32_t page_size);
 /* Append: k, v (bf16, k already rotated) of row m, KV head i of sequence b at element b * seq_stride +
  * m * row_stride + i * head_stride of either tensor (strides multiples of 8, but for those of
  * dimensions of one; channels contiguous, 16-byte aligned: a contiguous [n_seq][M][Hkv][hd], or a
- * page of a bf16 cache that ls_op_rope_append wrote).  Any M.  Rows of padding are left out; nothing else in the pages
- * changes.  Two rows of one call must not fall on the same slot of the same page. */
+ * page of a bf16 cache that ls_op_rope_append wrote).  M <= LS_KV4_MAX_SEQ.  Rows of padding are left
+ * out; nothing else in the pages changes.  Two rows of one call must not fall on the same slot of the same page. */
 int ls_op_append_kv4(const void *k_bf16_dev, const void *v_bf16_dev, int64_t seq_stride, int64_t row_stride,
                      int64_t head_stride, int32_t n_seq, int32_t M, const int32_t *pos0_dev, int32_t Hkv,
                      int32_t hd, int32_t page_size, const int32_t *page_table_dev, int32_t table_stride,
                      int32_t max_seq, void *pages_dev, int32_t n_pages, int32_t *status_dev, void *cuda_stream);
-/* The rows' values to a bf16 cache of the same page size with a page table of its own (same
+/* The rows' values (M <= LS_KV4_MAX_SEQ) to a bf16 cache of the same page size with a page table of its own (same
  * stride; k_pages / v_pages [n_out_pages][Hkv][page_size][hd], as ls_op_prefill_attention and
  * ls_op_attention read them).  Rows of padding and all other slots are left as they were. */
 int ls_op_expand_kv4(const void *pages_dev, int32_t n_pages, int32_t n_seq, int32_t M, const int32_t *pos0_dev,
@@ -426,7 +426,7 @@ int ls_op_expand_kv4(const void *pages_dev, int32_t n_pages, int32_t n_seq, int3
  * sequence b sees positions 0..pos0_dev[b] + m; a row that sees none, or is refused, is all zeros.
  * q, out bf16 [n_seq][M][Hq * hd], M <= LS_MAX_ROWS, Hq / Hkv <= 8.  Slots beyond a sequence's last row
  * are never used, whatever bits they hold; a row whose table entries are refused leaves out
- * those positions.  Few heads over a long cache leave SMs idle unless their positions are split
+ * those positions, and is NaN if they are all it has.  Few heads over a long cache leave SMs idle unless their positions are split
  * over more CTAs than a cluster holds, which needs scratch_dev (16-byte aligned,
  * ls_op_attention_kv4_scratch_bytes() bytes, of any content, used by one call at a time); with
  * NULL, or where that function returns 0 (no split is worth it), none is used.  A row's result

@@ -1840,9 +1840,9 @@ int ls_op_prefill_attention(const void* q, int32_t R, int32_t pos0, int32_t Hq, 
 // ---- 4-bit weights and the 4-bit cache (ls_q4.cuh, ls_w4.cuh, ls_kv4.cuh)
 static bool w4_shape_ok(int N, int K, int group)
 {
-    return N >= 1 && K >= 8 && K % 8 == 0 && (group == 32 || group == 64 || group == 128);
+    return N >= 1 && K >= 8 && K <= 1 << 28 && K % 8 == 0 && (group == 32 || group == 64 || group == 128);
 }
-static int w4_kblocks(int K) { return (int)(((int64_t)K + kQ4Cols - 1) / kQ4Cols); }
+static int w4_kblocks(int K) { return (K + kQ4Cols - 1) / kQ4Cols; }
 static int64_t w4_blocks(int N, int K) { return ((int64_t)N + kQ4Rows - 1) / kQ4Rows * w4_kblocks(K); }
 // A chained operation may read weights before the one ahead of it has finished (ls_op_chain), so what writes weights is
 // followed by a launch that waits for it to the end and that the next operation overlaps instead.
@@ -1924,7 +1924,7 @@ template <int NG>
 int w4_launch_ng(const unsigned char* packed, const uint16_t* h, int M, int N, int K, float* out, int residual,
                  const LaunchCtx& lc)
 {
-    const int64_t room = kW4SmemMax - M * ((int64_t)w4_kblocks(K) * kQ4Cols * 2 + 64);  // w4_h_stride, without overflow
+    const int64_t room = kW4SmemMax - (int64_t)M * w4_h_stride(w4_kblocks(K));
     if (M <= 8) {
         const int64_t ring24 = room - w4_part_bytes<1, 24>(), ring16 = room - w4_part_bytes<1, 16>();
         // 24 warps, what 64 to 80 registers allow, make a third team of 8 warps: of use with more than two tiles an SM
@@ -1981,7 +1981,8 @@ static int kv4_check(int n_seq, int M, const int32_t* pos0, int Hkv, int hd, int
     if (n_seq < 1 || M < 1 || Hkv < 1 || (hd != 64 && hd != 128) || log2_page(page_size) < 0 || !pos0 || !table ||
         !aligned16(pages) || n_pages < 1)
         return LS_ERR_INVALID_ARG;
-    if (max_seq < 1 || max_seq > LS_KV4_MAX_SEQ || n_seq > 65535 || Hkv > 4095) return LS_ERR_CAPACITY;
+    if (max_seq < 1 || max_seq > LS_KV4_MAX_SEQ || M > LS_KV4_MAX_SEQ || n_seq > 65535 || Hkv > 4095)
+        return LS_ERR_CAPACITY;
     if (table_stride < (max_seq + page_size - 1) / page_size) return LS_ERR_INVALID_ARG;
     *c = Kv4Cache{table, table_stride, log2_page(page_size), max_seq, n_pages, Hkv};
     return LS_OK;

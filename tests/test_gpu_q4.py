@@ -264,6 +264,16 @@ def test_positions_and_pages_out_of_range_are_refused():
             assert int(status) == code, (pos, which)
 
 
+def test_a_row_all_of_whose_pages_are_refused_is_nan():
+    """softmax of nothing; the status says why.  The other sequence is as ever."""
+    c = Cache([20, 20], 1, 64, 16, 70)
+    q = rnd((2, 2, 128), 71).bfloat16()
+    want, status = c.run(q, 2), torch.zeros(1, dtype=torch.int32, device="cuda")
+    c.table[0] = -1
+    got = c.run(q, 2, status)
+    assert torch.isnan(got[0]).all() and torch.equal(got[1], want[1]) and int(status) == 4
+
+
 # ------------------------------------------------------------------ attention
 class Cache:
     """n_seq sequences of random k, v in 4 bits: appended by the library (its bytes are tested above) to pages whose

@@ -52,7 +52,8 @@ def test_sizes():
     assert B.ls_op_w4_bytes(17, 136, 128) == 2 * 2 * (1024 + 32)
     assert B.ls_op_w4_bytes(4096, 11008, 64) == 256 * 86 * (1024 + 64)
     assert B.ls_op_w4_bytes(2 ** 31 - 1, 8, 32) == 2 ** 27 * 1152  # beyond 32 bits
-    for bad in ((0, 128, 32), (16, 0, 32), (16, 12, 32), (16, 128, 16), (16, 128, 0), (-1, 128, 32)):
+    assert B.ls_op_w4_bytes(1, 1 << 28, 32) == (1 << 21) * 1152
+    for bad in ((0, 128, 32), (1, (1 << 28) + 8, 32), (1, 2 ** 31 - 8, 32), (16, 0, 32), (16, 12, 32), (16, 128, 16), (16, 128, 0), (-1, 128, 32)):
         assert B.ls_op_w4_bytes(*bad) == 0, bad
     assert B.ls_op_kv4_page_bytes(8, 128, 64) == 8 * 4 * 2304
     assert B.ls_op_kv4_page_bytes(3, 64, 16) == 3 * 1152
@@ -72,7 +73,7 @@ def test_weight_operations_refuse_bad_arguments():
         assert f(P, 16, 128, 48, P, None) == BAD
     # packed, h, M, N, K, group, out, residual, stream
     good = [P, P, 1, 16, 128, 32, P, 0, None]
-    for at, v in ((0, None), (0, P + 4), (1, None), (1, P + 8), (2, 0), (2, 17), (2, -1), (3, 0), (4, 4), (4, 0),
+    for at, v in ((0, None), (0, P + 4), (1, None), (1, P + 8), (2, 0), (2, 17), (2, -1), (3, 0), (4, 4), (4, 0), (4, 2 ** 31 - 8),
                   (5, 16), (6, None), (6, P + 2)):
         a = list(good)
         a[at] = v
@@ -92,13 +93,13 @@ def test_cache_operations_refuse_bad_arguments():
     good = [P, P, 1024, 256, 128, 1, 4, P, 2, 128, 64, P, 4, 256, P, 4, None, None]
     refused(L.ls_op_append_kv4, good, [
         (0, None, BAD), (0, P + 8, BAD), (1, None, BAD), (3, 12, BAD), (4, 1, BAD), (5, 0, BAD), (5, 70000, CAP),
-        (6, 0, BAD), (7, None, BAD), (8, 0, BAD), (8, 5000, CAP), (9, 96, BAD), (10, 48, BAD), (10, 8, BAD), (11, None, BAD),
+        (6, 0, BAD), (6, (1 << 20) + 1, CAP), (6, 2 ** 31 - 1, CAP), (7, None, BAD), (8, 0, BAD), (8, 5000, CAP), (9, 96, BAD), (10, 48, BAD), (10, 8, BAD), (11, None, BAD),
         (12, 3, BAD), (13, 0, CAP), (13, (1 << 20) + 1, CAP), (14, None, BAD), (14, P + 8, BAD), (15, 0, BAD)])
     refused(L.ls_op_append_kv4, good[:5] + [2] + good[6:], [(2, 4, BAD)])
     # pages, n_pages, n_seq, M, pos0, Hkv, hd, page_size, table, stride, max_seq, out_table, kp, vp, n_out, status, stream
     good = [P, 4, 1, 4, P, 2, 128, 64, P, 4, 256, P, P, P, 4, None, None]
     refused(L.ls_op_expand_kv4, good, [
-        (0, None, BAD), (1, 0, BAD), (2, 0, BAD), (3, 0, BAD), (4, None, BAD), (5, 0, BAD), (6, 80, BAD), (7, 24, BAD),
+        (0, None, BAD), (1, 0, BAD), (2, 0, BAD), (3, 0, BAD), (3, 2 ** 31 - 1, CAP), (4, None, BAD), (5, 0, BAD), (6, 80, BAD), (7, 24, BAD),
         (8, None, BAD), (9, 3, BAD), (10, 1 << 21, CAP), (11, None, BAD), (12, None, BAD), (12, P + 8, BAD), (13, None, BAD),
         (14, 0, BAD)])
     # q, n_seq, M, pos0, Hq, Hkv, hd, page_size, table, stride, max_seq, pages, n_pages, out, scratch, status, stream
