@@ -2030,8 +2030,11 @@ namespace {
 // How the positions of a (sequence, KV head) are spread: a cluster of S CTAs, so many that all fit one to an SM (with
 // more than 8 queries a CTA fills one: 16 rows of 32 heads over 4103 positions 13.8 us with 128 CTAs, 27.4 with 256;
 // with fewer two fit, and 256 are 5 to 10 % faster), and no more than the cache has rounds of chunks for.  Few heads
-// over a long cache take several such splits: that costs a second kernel, some 2 us (8 heads, 4 splits: 4096 positions
-// 9.0 us, without 7.0; 16384: 13.0, 16.2; 131072: 44, 104).  Never a function of the rows of the call.
+// over a long cache take several splits, each a cluster of 4 (of 8, 15 fit at a time one to an SM, of 4, 32): that costs a
+// second kernel, some 2 us (8 heads, 16384 positions, 1 / 20 / 64 queries: one cluster of 8 14.7 / 27 / 58, 4 splits
+// 12.2 / 20.4 / 40.3).  Beyond 65536 positions there are as many as fit two to an SM (131072: 41.5 / 80 / 208 with 8
+// splits, 45.3 / 73 / 197 with 4); with more than 8 queries a cluster takes several of them one after the other, for
+// which see kv4_at_once.  Never a function of the rows of the call.
 struct Kv4Plan {
     int S, splits;
 };
@@ -2042,13 +2045,28 @@ Kv4Plan kv4_plan(int n_seq, int Hkv, int max_seq, bool may_split)
     if (S > kKv4MaxCluster) S = kKv4MaxCluster;
     if (S > rounds) S = rounds;
     int splits = 1;
-    if (may_split && S == kKv4MaxCluster && max_seq >= 4 * S * round)
-        while (splits < 64 && 2 * splits * S * pairs <= 296 && 2 * splits * S * round <= max_seq) splits *= 2;
+    if (may_split && S == kKv4MaxCluster && max_seq >= 4 * S * round) {
+        S = 4;
+        const int ctas = max_seq < 65536 ? 148 : 296;
+        while (splits < kKv4MaxSplits && 2 * splits * S * pairs <= ctas && 2 * splits * S * round <= max_seq) splits *= 2;
+    }
     return Kv4Plan{(int)S, splits};
 }
 uint32_t divisor(int d) { return d > 1 ? 0xffffffffu / (uint32_t)d + 1u : 0u; }  // for fastdiv on the device
 int kv4_query_tile(int Q) { return Q <= 8 ? 1 : Q <= 16 ? 2 : Q <= 24 ? 3 : 4; }  // tiles of 8 queries a CTA takes
 int kv4_rows(int Q, int Hkv) { return (Q + 8 * kv4_query_tile(Q) - 1) / (8 * kv4_query_tile(Q)) * Hkv; }
+
+// Splits that have a cluster of their own.  With more than 8 queries a CTA fills an SM, and clusters that have to wait for
+// others start late and unevenly (131072 positions, 8 heads, 20 queries: 117 us with 32 clusters of 8, 80 with 4 clusters
+// a head that take two splits each).
+template <int NT>
+int kv4_at_once(const Kv4Plan& plan, int rows, int n_seq)
+{
+    int n = plan.splits;
+    if (NT > 1)
+        while (n % 2 == 0 && (int64_t)n * plan.S * rows * n_seq > 148) n /= 2;
+    return n;
+}
 
 template <int HD, int NT>
 int kv4_attn_launch(const Kv4Plan& plan, int n_seq, const uint16_t* q, int M, int G, const int32_t* pos0, const Kv4Cache& c,
@@ -2070,7 +2088,7 @@ int kv4_attn_launch(const Kv4Plan& plan, int n_seq, const uint16_t* q, int M, in
     }
     const int rows = kv4_rows(M * G, c.Hkv);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(plan.splits * plan.S, rows, n_seq);
+    cfg.gridDim = dim3(kv4_at_once<NT>(plan, rows, n_seq) * plan.S, rows, n_seq);
     cfg.blockDim = dim3(kKv4Warps * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = lc.st;
@@ -2085,10 +2103,10 @@ int kv4_attn_launch(const Kv4Plan& plan, int n_seq, const uint16_t* q, int M, in
     at[2].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = lc.pdl ? 3 : 2;
-    LS_CK(cudaLaunchKernelEx(&cfg, kernel, q, M, G, pos0, c, pages, plan.S, divisor(plan.S), divisor(G), divisor(c.Hkv), out,
+    LS_CK(cudaLaunchKernelEx(&cfg, kernel, q, M, G, pos0, c, pages, plan.S, plan.splits, divisor(plan.S), divisor(G), divisor(c.Hkv), out,
                              scratch, status));
     if (plan.splits > 1)  // may move in while the splits finish; it waits for them before it reads
-        LS_CK(launch(LaunchCtx{lc.st, true}, combine_kv4_kernel<HD>, dim3(M, G * c.Hkv, n_seq), dim3(HD / 2), 0, scratch, G, pos0,
+        LS_CK(launch(LaunchCtx{lc.st, true}, combine_kv4_kernel<HD>, dim3(M, G * c.Hkv, n_seq), dim3(2 * HD), 0, scratch, G, pos0,
                      c.max_seq, NT, c.Hkv, rows, plan.splits, out));
     return LS_OK;
 }

@@ -111,7 +111,7 @@ __device__ __forceinline__ long long kv4_partial(int b, int rows, int y, int spl
 // log2(e) / sqrt(hd), over the 2^14 that queries are scaled to
 __device__ __forceinline__ float kv4_unit(int hd) { return 0x1p-14f * 1.4426950408889634f / sqrtf((float)hd); }
 
-// grid (splits * S, Hkv * query tiles, n_seq) in clusters of S CTAs.  The warps of a (sequence, KV head) take
+// grid (S times the splits, or a part of them, Hkv * query tiles, n_seq) in clusters of S CTAs.  The warps of a (sequence, KV head) take
 // the 32-position chunks of the cache in turn by absolute position, each through a cp.async ring of its own and
 // with a running (max, sum, O) of its own.  At the end every thread adds up, in warp order, the pieces of O it is
 // given and sends them to the CTA of the cluster that finishes them, through distributed shared memory: one
@@ -123,7 +123,7 @@ __device__ __forceinline__ float kv4_unit(int hd) { return 0x1p-14f * 1.44269504
 template <int HD, int NT>
 __global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1)
 attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t* __restrict__ pos0_dev,
-                     const Kv4Cache cache, const unsigned char* __restrict__ pages, int S, uint32_t div_S, uint32_t div_G, uint32_t div_Hkv,
+                     const Kv4Cache cache, const unsigned char* __restrict__ pages, int S, int n_splits, uint32_t div_S, uint32_t div_G, uint32_t div_Hkv,
                      uint16_t* __restrict__ out, float* __restrict__ scratch, int32_t* status)
 {
     using SM = Kv4Smem<HD, NT>;
@@ -141,7 +141,8 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     float2* sInStat = reinterpret_cast<float2*>(at += SM::kStat);   // [CTA][NT * 8]
     pdl_launch_dependents();
     pdl_wait();
-    const int splits = fastdiv(gridDim.x, S, div_S), split = fastdiv(blockIdx.x, S, div_S), rank = blockIdx.x - split * S, b = blockIdx.z;
+    const int splits = NT == 1 ? fastdiv(gridDim.x, S, div_S) : n_splits;
+    const int first_split = fastdiv(blockIdx.x, S, div_S), rank = blockIdx.x - first_split * S, b = blockIdx.z;
     if (S > 1) cluster_arrive_relaxed();  // this CTA is there
     const int tile_y = fastdiv(blockIdx.y, cache.Hkv, div_Hkv), head = blockIdx.y - tile_y * cache.Hkv, q0 = tile_y * (NT * 8);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -161,7 +162,8 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     }
     // page-table entries of this warp's next chunk (a chunk lies in one page, unless pages are of 16), read before
     // anything says whether it is needed: the positions below max_seq have entries
-    const int step = gridDim.x * W * kKv4Chunk, base0 = (blockIdx.x * W + warp) * kKv4Chunk;
+    const int step = (NT == 1 ? gridDim.x : splits * S) * W * kKv4Chunk;
+    int split = first_split, base0 = (blockIdx.x * W + warp) * kKv4Chunk;
     const int32_t* table = cache.table + (long long)b * cache.table_stride;
     int next_page[2];
     auto look_up = [&](int base) {
@@ -265,6 +267,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     // score * log2(e) = sum_g s_g c_g * 2^e * fb
     const float fb = kv4_unit(HD);
 
+    for (;;) {  // one split after the other, where there are fewer clusters than splits
     float o[NT][CT][4] = {}, mx[NT][2], sum[NT][2] = {};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = -INFINITY;
@@ -565,34 +568,63 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
         const uint32_t v = none ? 0u : pack_bf16(v0 * inv, v1 * inv);
         *reinterpret_cast<uint32_t*>(out + (((long long)b * M + row) * Hq + head * G + qi - row * G) * HD + ch) = v;
     }
+    if (NT == 1) break;
+    const int ahead = fastdiv(gridDim.x, S, div_S);
+    if ((split += ahead) >= splits) break;
+    __syncwarp();
+    if (S > 1) cluster_arrive();  // what the others sent here has been read
+    in_base = base0 += ahead * S * W * kKv4Chunk, in_stage = in_count = 0, ok_bits = 0;
+    look_up(base0);
+#pragma unroll
+    for (int i = 0; i < D - 1; ++i) fetch();
+    }
 }
 
-// Joins the splits.  grid (M, Hq, n_seq), block HD / 2: a thread has two channels of a row.  NT, rows (gridDim.y), splits:
-// of the attention kernel's launch.
+// Joins the splits.  grid (M, Hq, n_seq), block 2 HD: a thread has two channels of a row and every fourth split.  NT, rows
+// (gridDim.y), splits: of the attention kernel's launch.
+constexpr int kKv4MaxSplits = 64;
 template <int HD>
-__global__ void __launch_bounds__(HD / 2)
+__global__ void __launch_bounds__(2 * HD)
 combine_kv4_kernel(const float* __restrict__ scratch, int G, const int32_t* __restrict__ pos0_dev, int max_seq, int NT, int Hkv,
                    int rows, int splits, uint16_t* __restrict__ out)
 {
+    __shared__ float2 stat[kKv4MaxSplits];  // (max, sum) of a split, later (weight, weight * sum)
+    __shared__ float2 part[3][HD / 2];
     pdl_launch_dependents();
     pdl_wait();
-    const int m = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, ch = 2 * threadIdx.x;
+    const int m = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, lane = threadIdx.x % (HD / 2), quarter = threadIdx.x / (HD / 2);
     const int qi = m * G + hq % G, y = qi / (NT * 8) * Hkv + hq / G, c = qi % (NT * 8);
     const float* from = scratch + (kv4_partial(b, rows, y, splits, 0) * (NT * 8) + c) * (HD + 2);
     const long long stride = (long long)NT * 8 * (HD + 2), p = (long long)pos0_dev[b] + m;
     const float fb = kv4_unit(HD);
-    float top = -INFINITY, l = 0.f, x = 0.f, y0 = 0.f;
-    for (int s = 0; s < splits; ++s) top = fmaxf(top, from[s * stride + HD]);
-#pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
-        const float2 st = *reinterpret_cast<const float2*>(from + s * stride + HD);
-        const float2 v = *reinterpret_cast<const float2*>(from + s * stride + ch);
+    const bool mine = threadIdx.x < splits;
+    const float2 st = mine ? *reinterpret_cast<const float2*>(from + threadIdx.x * stride + HD) : make_float2(0.f, 0.f);
+    if (mine) stat[threadIdx.x] = st;
+    __syncthreads();
+    float top = -INFINITY;
+    for (int s = 0; s < splits; ++s) top = fmaxf(top, stat[s].x);
+    __syncthreads();
+    if (mine) {
         const float f = top == -INFINITY ? 0.f : exp2_fast((st.x - top) * fb);
-        l = fmaf(f, st.y, l), x = fmaf(f, v.x, x), y0 = fmaf(f, v.y, y0);
+        stat[threadIdx.x] = make_float2(f, f * st.y);
     }
+    __syncthreads();
+    float x0 = 0.f, x1 = 0.f;
+#pragma unroll 4
+    for (int s = quarter; s < splits; s += 4) {
+        const float2 v = *reinterpret_cast<const float2*>(from + s * stride + 2 * lane);
+        x0 = fmaf(stat[s].x, v.x, x0), x1 = fmaf(stat[s].x, v.y, x1);
+    }
+    if (quarter) part[quarter - 1][lane] = make_float2(x0, x1);
+    __syncthreads();
+    if (quarter) return;
+    float l = 0.f;
+    for (int s = 0; s < splits; ++s) l += stat[s].y;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) x0 += part[i][lane].x, x1 += part[i][lane].y;
     const float inv = 1.f / l;
-    const uint32_t r = p < 0 || p >= max_seq ? 0u : pack_bf16(x * inv, y0 * inv);
-    *reinterpret_cast<uint32_t*>(out + (((long long)b * gridDim.x + m) * gridDim.y + hq) * HD + ch) = r;
+    const uint32_t r = p < 0 || p >= max_seq ? 0u : pack_bf16(x0 * inv, x1 * inv);
+    *reinterpret_cast<uint32_t*>(out + (((long long)b * gridDim.x + m) * gridDim.y + hq) * HD + 2 * lane) = r;
 }
 
 }  // namespace ls

@@ -366,6 +366,20 @@ def test_attention_rows_do_not_depend_on_pass_size(Hkv, G, hd):
         assert torch.equal(out, full[:, m0:m0 + M]), (m0, M)
 
 
+@pytest.mark.parametrize("Hkv,hd,M,G", [(8, 128, 12, 2), (5, 64, 6, 8)])
+def test_attention_clusters_that_take_several_splits(Hkv, hd, M, G):
+    """a cache of 65536 positions of which 9000 are used: every split has some; rows as in passes of one"""
+    c = Cache([9000], Hkv, hd, 64, 80, max_seq=1 << 16)
+    q = rnd((1, M, Hkv * G * hd), 81, 2.0).bfloat16()
+    full = c.run(q, M)
+    check_attention(c, q, full, M, G)
+    for m in (0, M // 2, M - 1):
+        out = torch.empty((1, 1, q.shape[2]), dtype=torch.bfloat16, device="cuda")
+        B.ls_op_attention_kv4(q[:, m:m + 1].contiguous(), torch.tensor([9000 - M + m], dtype=torch.int32, device="cuda"), Hkv, hd,
+                              64, c.table, 1 << 16, c.pool, out)
+        assert torch.equal(out, full[:, m:m + 1]), m
+
+
 @pytest.mark.parametrize("hd", [64, 128])
 def test_attention_values_that_are_not_finite_reach_only_the_rows_that_see_them(hd):
     Hkv, G, M, n = 1, 2, 4, 90
