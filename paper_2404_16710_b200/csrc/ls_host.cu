@@ -12,6 +12,7 @@
 // The host launches a batch of step graphs sized to the tokens still missing and only
 // then looks at the control words, so there is no host sync per token; steps launched
 // past the end see the done flag and return at once.
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -2027,30 +2028,40 @@ int ls_op_expand_kv4(const void* pages, int32_t n_pages, int32_t n_seq, int32_t 
 
 namespace {
 
-// How the positions of a (sequence, KV head) are spread: a cluster of S CTAs, so many that all fit one to an SM (with
-// more than 8 queries a CTA fills one: 16 rows of 32 heads over 4103 positions 13.8 us with 128 CTAs, 27.4 with 256;
-// with fewer two fit, and 256 are 5 to 10 % faster), and no more than the cache has rounds of chunks for.  Few heads
-// over a long cache take several splits, each a cluster of 4 (of 8, 15 fit at a time one to an SM, of 4, 32): that costs a
-// second kernel, some 2 us (8 heads, 16384 positions, 1 / 20 / 64 queries: one cluster of 8 14.7 / 27 / 58, 4 splits
-// 12.2 / 20.4 / 40.3).  Beyond 65536 positions there are as many as fit two to an SM (131072: 41.5 / 80 / 208 with 8
-// splits, 45.3 / 73 / 197 with 4); with more than 8 queries a cluster takes several of them one after the other, for
-// which see kv4_at_once.  Never a function of the rows of the call.
+// How the positions of a (sequence, KV head) are spread: never a function of the rows of the call, whose results would
+// depend on it.  With up to 8 queries two CTAs fit on an SM, with more one does, and the plan has to do for both.
+// * A cluster of S CTAs for each, the largest of which all fit one to an SM, and no more than the cache has rounds of chunks
+//   for (16 rows of 32 heads over 4103 positions 13.8 us with clusters of 4, 27.4 with 8, which have to wait for one another;
+//   12 rows of 16 heads over 4000 11.4 with 6, 17.4 with 8).
+// * Few heads over a long cache take several splits, each a cluster of 4: that costs a second kernel, some 2 us (8 heads,
+//   16384 positions, 1 / 20 / 64 queries a head: one cluster of 8 14.7 / 27 / 58, 4 splits 12.2 / 20.4 / 40.3).  From 65536
+//   positions on there are as many as fit two to an SM (131072: 41.5 / 80 / 207 with 8 splits, 45.3 / 73 / 197 with 4).
+// * So many heads that clusters of 1 or 2 are left: over a long cache those that fit two to an SM, which also even out
+//   what 148 is not a multiple of (1 / 20 queries: 64 heads, 16000 positions 42.5 / 68.4 with clusters of 2, 35.7 / 66.5
+//   with 4; 96 heads 77 / 126 with 1, 48 / 88 with 3; 128 heads 77 / 126 with 1, 66 / 121 with 2; but 128 heads, 1000
+//   positions 9.7 / 17.6 and 10.9 / 23.4).
 struct Kv4Plan {
     int S, splits;
 };
+constexpr int kKv4Clusters[] = {148, 74, 45, 33, 26, 22, 15, 15};  // of 1, 2 .. CTAs, that fit a B200 one CTA to an SM
+constexpr int kKv4Clusters2[] = {296, 148, 96, 74, 56};            // and two
 Kv4Plan kv4_plan(int n_seq, int Hkv, int max_seq, bool may_split)
 {
-    const int64_t pairs = (int64_t)n_seq * Hkv, round = kKv4Warps * kKv4Chunk, rounds = (max_seq + round - 1) / round;
-    int64_t S = pairs > 148 ? 1 : 148 / pairs;
-    if (S > kKv4MaxCluster) S = kKv4MaxCluster;
-    if (S > rounds) S = rounds;
-    int splits = 1;
-    if (may_split && S == kKv4MaxCluster && max_seq >= 4 * S * round) {
-        S = 4;
-        const int ctas = max_seq < 65536 ? 148 : 296;
-        while (splits < kKv4MaxSplits && 2 * splits * S * pairs <= ctas && 2 * splits * S * round <= max_seq) splits *= 2;
+    const int64_t pairs = (int64_t)n_seq * Hkv;
+    const int round = kKv4Warps * kKv4Chunk, rounds = (max_seq + round - 1) / round;
+    int S = kKv4MaxCluster;
+    while (S > 1 && pairs > kKv4Clusters[S - 1]) --S;
+    if (may_split && 2 * pairs <= kKv4Clusters[3] && max_seq >= 8192) {
+        int splits = kKv4Clusters[3] / (int)pairs;
+        if (max_seq >= 65536) splits *= 2;
+        return Kv4Plan{4, std::min({splits, kKv4MaxSplits, max_seq / (4 * round)})};
     }
-    return Kv4Plan{(int)S, splits};
+    if (S <= 2) {
+        int more = 5;
+        while (more > S && (pairs > kKv4Clusters2[more - 1] || max_seq < 2048 * more)) --more;
+        S = more;
+    }
+    return Kv4Plan{std::min(S, rounds), 1};
 }
 uint32_t divisor(int d) { return d > 1 ? 0xffffffffu / (uint32_t)d + 1u : 0u; }  // for fastdiv on the device
 int kv4_query_tile(int Q) { return Q <= 8 ? 1 : Q <= 16 ? 2 : Q <= 24 ? 3 : 4; }  // tiles of 8 queries a CTA takes

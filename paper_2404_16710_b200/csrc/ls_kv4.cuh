@@ -116,7 +116,7 @@ __device__ __forceinline__ float kv4_unit(int hd) { return 0x1p-14f * 1.44269504
 // with a running (max, sum, O) of its own.  At the end every thread adds up, in warp order, the pieces of O it is
 // given and sends them to the CTA of the cluster that finishes them, through distributed shared memory: one
 // CTA barrier, one cluster barrier.  With one split that is the result; a GPC has room for few large clusters
-// (148 SMs: 33 of 8 CTAs, 7 of 16 where one fills an SM), so that few heads over a long cache take several splits,
+// (148 SMs: 33 of 4 CTAs, 15 of 8, 7 of 16 where one fills an SM), so that few heads over a long cache take several splits,
 // which a second kernel joins.  A row's result depends on its position and on the grid, not on M or the other
 // rows: what other rows add to the tokens a CTA looks at has weight 0, and all factors that are shared are powers
 // of two.

@@ -340,17 +340,19 @@ def test_attention_clusters_of_every_size_and_peaked_scores(n_seq):
         check_attention(c, q, c.run(q, 2), 2, 2)
 
 
-@pytest.mark.parametrize("Hkv,n_seq", [(20, 1), (24, 1), (30, 1), (40, 1), (5, 7), (3, 50), (150, 1)])
-def test_attention_clusters_of_odd_sizes(Hkv, n_seq):
-    """numbers of heads that leave 7, 6, 4, 3 and fewer CTAs each; every row the same in a pass of one as among 8"""
-    c = Cache([900 - 11 * b for b in range(n_seq)], Hkv, 64, 64, 60, max_seq=2048)
+@pytest.mark.parametrize("Hkv,n_seq,max_seq", [(20, 1, 2048), (24, 1, 2048), (30, 1, 2048), (40, 1, 2048), (5, 7, 2048),
+                                               (3, 50, 2048), (150, 1, 2048), (16, 3, 10240), (8, 8, 8192), (32, 3, 6144),
+                                               (64, 2, 4096), (10, 1, 8192)])
+def test_attention_clusters_of_odd_sizes(Hkv, n_seq, max_seq):
+    """numbers of heads and lengths of caches that take clusters of 1 to 6 and splits of any number; every row the same in a pass of one as among 8"""
+    c = Cache([900 - 11 * b for b in range(n_seq)], Hkv, 64, 64, 60, max_seq=max_seq)
     q = rnd((n_seq, 8, Hkv * 64), 61, 2.0).bfloat16()
     full = c.run(q, 8)
     check_attention(c, q, full, 8, 1)
     for m in (0, 5, 7):
         out = torch.empty((n_seq, 1, Hkv * 64), dtype=torch.bfloat16, device="cuda")
         pos = torch.tensor([900 - 11 * b - 8 + m for b in range(n_seq)], dtype=torch.int32, device="cuda")
-        B.ls_op_attention_kv4(q[:, m:m + 1].contiguous(), pos, Hkv, 64, 64, c.table, 2048, c.pool, out)
+        B.ls_op_attention_kv4(q[:, m:m + 1].contiguous(), pos, Hkv, 64, 64, c.table, max_seq, c.pool, out)
         assert torch.equal(out, full[:, m:m + 1]), m
 
 
