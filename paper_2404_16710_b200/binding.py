@@ -157,7 +157,7 @@ class _Torch:
         self.bf16, self.f32, self.i32, self.u8, self.empty = torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.empty
         # torch.cuda.current_stream() builds a Stream object (3.4 us a call, as much as a launch); the raw handle costs 0.2
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        self.stream = (lambda: raw(torch.cuda.current_device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
+        self.stream = raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
         self.device = torch.cuda.current_device
         return self
 
@@ -170,7 +170,7 @@ _torch = _Torch()
 
 def _stream():
     """handle of the current CUDA stream"""
-    return _torch.stream()
+    return _torch.stream(_torch.device())
 
 
 def _i32(a):
@@ -453,7 +453,7 @@ def _stream_on(dev):
     """handle of the current stream, which has to be one of the operands' device"""
     if dev < 0 or dev != _torch.device():
         _bad("operands on the current CUDA device are needed")
-    return _torch.stream()
+    return _torch.stream(dev)
 
 
 @functools.lru_cache(maxsize=4096)

@@ -123,8 +123,8 @@ __device__ __forceinline__ float kv4_unit(int hd) { return 0x1p-14f * 1.44269504
 template <int HD, int NT>
 __global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1)
 attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t* __restrict__ pos0_dev,
-                     const Kv4Cache cache, const unsigned char* __restrict__ pages, int S, int n_splits, uint32_t div_S, uint32_t div_G, uint32_t div_Hkv,
-                     uint16_t* __restrict__ out, float* __restrict__ scratch, int32_t* status)
+                     const Kv4Cache cache, const unsigned char* __restrict__ pages, int S, int n_splits, uint32_t div_S,
+                     uint32_t div_G, uint32_t div_Hkv, uint16_t* __restrict__ out, float* __restrict__ scratch, int32_t* status)
 {
     using SM = Kv4Smem<HD, NT>;
     constexpr int W = kKv4Warps;
