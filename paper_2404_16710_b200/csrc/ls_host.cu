@@ -1886,12 +1886,14 @@ int ls_op_expand_w4(const void* packed, int32_t N, int32_t K, int32_t group, voi
 namespace {
 
 // log2 of the warps that share a tile of 16 rows.  A function of the matrix alone: it enters a row's arithmetic.
-// Few tiles: all 16 warps of an SM on its one tile (64 tiles, K = 4096: 3.6 us, 4.7 with 8 warps); up to a few
-// tiles an SM: 8 (256 tiles: 5.1 us, with 16 warps 5.5, with 4 6.7); beyond, 4, which saves additions of sums
-// (8016 tiles: 58.6 us, with 8 warps 63.8, with 16 77.5, with 1 60.2).
+// Few tiles: all 16 warps of an SM on its one tile (64 tiles, K = 4096: 3.6 us, 4.7 with 8 warps); up to two tiles an SM:
+// 8 (256 tiles, K = 8192, 1 / 16 rows: 7.6 / 10.5 us, with 4 7.8 / 12.8; K = 4096: 5.1 / 6.7, with 16 5.5 / 7.4, with 4
+// 5.0 / 6.6); beyond, 4, which saves additions of sums and evens out what 148 is not a multiple of (384 tiles, K = 4096,
+// 1 / 16 rows: 5.8 / 8.1 us, with 8 warps 6.2 / 8.7; 512 tiles, K = 8192: 11.0 / 17.7, 12.1 / 18.2; 8016 tiles, one row:
+// 55.9, with 8 59.4, with 16 70).
 int w4_split(int n_tiles)
 {
-    return n_tiles <= 148 ? 4 : n_tiles < 1024 ? 3 : 2;
+    return n_tiles <= 148 ? 4 : n_tiles <= 296 ? 3 : 2;
 }
 
 template <int NG, int NT, int W, int D, int CB, bool HS, int TG>
