@@ -391,7 +391,8 @@ int ls_op_prefill_attention(const void *q_bf16_dev, int32_t R, int32_t pos0, int
 /* Bytes of the packed weights of an [N, K] matrix; 0 for a shape or group the format does not cover. */
 size_t ls_op_w4_bytes(int32_t N, int32_t K, int32_t group);
 /* bf16 [N, K] -> packed weights, and back to bf16 [N, K] (for ls_op_gemm: the prompt pass).  Weights
- * are packed once; packed_dev 16-byte aligned. */
+ * are packed once; packed_dev 16-byte aligned.  With ls_op_chain on, an empty launch follows either,
+ * so that an operation that reads weights ahead of time does not read them half written. */
 int ls_op_quantize_w4(const void *w_bf16_dev, int32_t N, int32_t K, int32_t group, void *packed_dev,
                       void *cuda_stream);
 int ls_op_expand_w4(const void *packed_dev, int32_t N, int32_t K, int32_t group, void *out_bf16_dev,
@@ -409,14 +410,16 @@ size_t ls_op_kv4_page_bytes(int32_t Hkv, int32_t hd, int32_t page_size);
  * m * row_stride + i * head_stride of either tensor (strides multiples of 8, but for those of
  * dimensions of one; channels contiguous, 16-byte aligned: a contiguous [n_seq][M][Hkv][hd], or a
  * page of a bf16 cache that ls_op_rope_append wrote).  M <= LS_KV4_MAX_SEQ.  Rows of padding are left
- * out; nothing else in the pages changes.  Two rows of one call must not fall on the same slot of the same page. */
+ * out; nothing else in the pages changes.  Two rows of one call must not fall on the same slot of
+ * the same page. */
 int ls_op_append_kv4(const void *k_bf16_dev, const void *v_bf16_dev, int64_t seq_stride, int64_t row_stride,
                      int64_t head_stride, int32_t n_seq, int32_t M, const int32_t *pos0_dev, int32_t Hkv,
                      int32_t hd, int32_t page_size, const int32_t *page_table_dev, int32_t table_stride,
                      int32_t max_seq, void *pages_dev, int32_t n_pages, int32_t *status_dev, void *cuda_stream);
-/* The rows' values (M <= LS_KV4_MAX_SEQ) to a bf16 cache of the same page size with a page table of its own (same
- * stride; k_pages / v_pages [n_out_pages][Hkv][page_size][hd], as ls_op_prefill_attention and
- * ls_op_attention read them).  Rows of padding and all other slots are left as they were. */
+/* The rows' values (M <= LS_KV4_MAX_SEQ) to a bf16 cache of the same page size with a page table of
+ * its own (same stride; k_pages / v_pages [n_out_pages][Hkv][page_size][hd], as
+ * ls_op_prefill_attention and ls_op_attention read them).  Rows of padding and all other slots are
+ * left as they were; two rows must not go to the same slot of the same page. */
 int ls_op_expand_kv4(const void *pages_dev, int32_t n_pages, int32_t n_seq, int32_t M, const int32_t *pos0_dev,
                      int32_t Hkv, int32_t hd, int32_t page_size, const int32_t *page_table_dev,
                      int32_t table_stride, int32_t max_seq, const int32_t *out_page_table_dev,
@@ -426,11 +429,11 @@ int ls_op_expand_kv4(const void *pages_dev, int32_t n_pages, int32_t n_seq, int3
  * sequence b sees positions 0..pos0_dev[b] + m; a row that sees none, or is refused, is all zeros.
  * q, out bf16 [n_seq][M][Hq * hd], M <= LS_MAX_ROWS, Hq / Hkv <= 8.  Slots beyond a sequence's last row
  * are never used, whatever bits they hold; a row whose table entries are refused leaves out
- * those positions, and is NaN if they are all it has.  Few heads over a long cache leave SMs idle unless their positions are split
- * over more CTAs than a cluster holds, which needs scratch_dev (16-byte aligned,
- * ls_op_attention_kv4_scratch_bytes() bytes, of any content, used by one call at a time); with
- * NULL, or where that function returns 0 (no split is worth it), none is used.  A row's result
- * depends on its position, n_seq, Hkv, max_seq and whether there is scratch (which fix how the
+ * those positions, and is NaN if they are all it has.  Few heads over a long cache leave SMs idle
+ * unless their positions are split over more CTAs than a cluster holds, which needs scratch_dev
+ * (16-byte aligned, ls_op_attention_kv4_scratch_bytes() bytes, of any content, used by one call at a
+ * time); with NULL, or where that function returns 0 (no split is worth it), none is used.  A row's
+ * result depends on its position, n_seq, Hkv, max_seq and whether there is scratch (which fix how the
  * positions are dealt to CTAs), never on M or on the other rows.  Softmax weights enter the second
  * product in f16, V exactly, unless its scale is more than 2^25 below the largest of the head. */
 size_t ls_op_attention_kv4_scratch_bytes(int32_t n_seq, int32_t M, int32_t Hq, int32_t Hkv, int32_t hd,
