@@ -391,8 +391,9 @@ int ls_op_prefill_attention(const void *q_bf16_dev, int32_t R, int32_t pos0, int
 /* Bytes of the packed weights of an [N, K] matrix; 0 for a shape or group the format does not cover. */
 size_t ls_op_w4_bytes(int32_t N, int32_t K, int32_t group);
 /* bf16 [N, K] -> packed weights, and back to bf16 [N, K] (for ls_op_gemm: the prompt pass).  Weights
- * are packed once; packed_dev 16-byte aligned.  With ls_op_chain on, an empty launch follows either,
- * so that an operation that reads weights ahead of time does not read them half written. */
+ * are packed once; packed_dev 16-byte aligned.  An empty launch follows either, whether ls_op_chain is
+ * on or is turned on later, so that an operation that reads weights ahead of time does not read them
+ * half written. */
 int ls_op_quantize_w4(const void *w_bf16_dev, int32_t N, int32_t K, int32_t group, void *packed_dev,
                       void *cuda_stream);
 int ls_op_expand_w4(const void *packed_dev, int32_t N, int32_t K, int32_t group, void *out_bf16_dev,

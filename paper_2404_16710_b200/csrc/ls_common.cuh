@@ -148,8 +148,11 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t& r0, u
 // Programmatic dependent launch: a kernel launched with the attribute may start while its
 // predecessor on the stream is still running.  pdl_wait() blocks until the predecessor
 // grid has completed and its writes are visible; before it, a kernel may touch only
-// memory that no kernel of the loop writes (weights, page table).  Without the launch
-// attribute both are no-ops.
+// memory that no kernel of the loop writes (weights, page table).  The attribute is the later
+// kernel's: pdl_wait() is a no-op in a kernel launched without it, but pdl_launch_dependents() lets
+// a successor that has it start early however this one was launched.  A kernel that writes
+// what successors read before their pdl_wait() must therefore neither call it nor be the last
+// launch before them (fence_kernel in ls_q4.cuh).
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -1845,11 +1845,13 @@ static bool w4_shape_ok(int N, int K, int group)
 }
 static int w4_kblocks(int K) { return (K + kQ4Cols - 1) / kQ4Cols; }
 static int64_t w4_blocks(int N, int K) { return ((int64_t)N + kQ4Rows - 1) / kQ4Rows * w4_kblocks(K); }
-// A chained operation may read weights before the one ahead of it has finished (ls_op_chain), so what writes weights is
-// followed by a launch that waits for it to the end and that the next operation overlaps instead.
+// An operation launched with the programmatic attribute (ls_op_chain, the model's passes) reads weights before the one ahead of
+// it has finished.  Whether it may start early is its own attribute's matter, and the switch may be turned on after
+// the packing: so what writes weights is always followed by a launch that waits for it to the end and that the next
+// operation overlaps instead.
 static int w4_written(cudaStream_t stream)
 {
-    if (g_op_chain) LS_CK(launch(LaunchCtx{stream, false}, fence_kernel, dim3(1), dim3(32), 0));
+    LS_CK(launch(LaunchCtx{stream, false}, fence_kernel, dim3(1), dim3(32), 0));
     return LS_OK;
 }
 

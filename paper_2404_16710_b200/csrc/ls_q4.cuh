@@ -149,7 +149,6 @@ template <int NG>
 __global__ void __launch_bounds__(256) quantize_w4_kernel(const uint16_t* __restrict__ w, int N, int K, int kblocks,
                                                           long long blocks, unsigned char* __restrict__ packed)
 {
-    pdl_launch_dependents();
     pdl_wait();
     const long long blk = (long long)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
     if (blk >= blocks) return;  // whole warps
@@ -191,7 +190,9 @@ __global__ void __launch_bounds__(256) quantize_w4_kernel(const uint16_t* __rest
     }
 }
 
-__global__ void fence_kernel() {}  // does nothing after what is ahead of it on the stream
+// Does nothing.  Launched without the attribute behind what writes weights: it starts when they are written and visible,
+// and the next operation's early reads of weights start after it.
+__global__ void fence_kernel() {}
 
 // scales of one row of a block in both halves of a register each, group by group
 template <int NG>
@@ -214,7 +215,6 @@ template <int NG>
 __global__ void __launch_bounds__(256) expand_w4_kernel(const unsigned char* __restrict__ packed, int N, int K,
                                                         int kblocks, long long blocks, uint16_t* __restrict__ out)
 {
-    pdl_launch_dependents();
     pdl_wait();
     const long long blk = (long long)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
     if (blk >= blocks) return;

@@ -611,6 +611,78 @@ def test_expanding_right_before_a_chained_bf16_linear():
     assert all(torch.equal(a, b) for a, b in zip(outs, want))
 
 
+@pytest.mark.parametrize("packing", [True, False])
+def test_packing_first_and_chaining_afterwards(packing):
+    """weights packed (or expanded) with chaining off, which is then turned on, and a norm between them and the linear
+    layer: operations that start early use the new weights"""
+    N, K = 4096, 2048
+    x, gain = rnd((1, K), 150), torch.ones(K, device="cuda").bfloat16()
+    ws = [rnd((N, K), 151 + i, 0.02).bfloat16() for i in range(6)]
+    packs = [quantised(w, 32) for w in ws]
+    packed, wide, outs, want = torch.zeros_like(packs[0]), torch.zeros_like(ws[0]), [], []
+    for chained in (False, True):
+        for w, p in zip(ws, packs):
+            h, o = torch.zeros((1, K), device="cuda").bfloat16(), torch.zeros((1, N), device="cuda")
+            torch.cuda.synchronize()
+            if packing:
+                B.ls_op_quantize_w4(w, 32, packed)
+            else:
+                B.ls_op_expand_w4(p, 32, wide)
+            B.ls_op_chain(chained)
+            try:
+                B.ls_op_rmsnorm(x, gain, 1e-5, h)
+                if packing:
+                    B.ls_op_linear_w4(packed, 32, h, o)
+                else:
+                    B.ls_op_linear(B.LS_LINEAR_MMA, wide, h, o)
+            finally:
+                B.ls_op_chain(False)
+            (outs if chained else want).append(o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("packing", [True, False])
+@pytest.mark.parametrize("chained", [False, True])
+def test_no_operation_overlaps_one_that_writes_weights(packing, chained):
+    """the same calls captured and not run: whatever the switch said while packing, the operation that may start early
+    depends on a launch behind the packing's, and that one on the packing's end"""
+    drv = pytest.importorskip("cuda.bindings.driver")
+    N, K = 256, 256
+    x, gain, h = rnd((1, K), 160), torch.ones(K, device="cuda").bfloat16(), torch.zeros((1, K), device="cuda").bfloat16()
+    w, o = rnd((N, K), 161).bfloat16(), torch.zeros((1, N), device="cuda")
+    packed = quantised(w, 32)
+    B.ls_op_expand_w4(packed, 32, w)
+    B.ls_op_linear_w4(packed, 32, h, o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        B.ls_op_chain(chained)
+        try:
+            if packing:
+                B.ls_op_quantize_w4(w, 32, packed)
+            else:
+                B.ls_op_expand_w4(packed, 32, w)
+            B.ls_op_chain(True)
+            B.ls_op_rmsnorm(x, gain, 1e-5, h)
+            B.ls_op_linear_w4(packed, 32, h, o)
+        finally:
+            B.ls_op_chain(False)
+    raw = drv.CUgraph(graph.raw_cuda_graph())
+    err, _, _, _, n = drv.cuGraphGetEdges_v2(raw)
+    assert err == drv.CUresult.CUDA_SUCCESS
+    err, start, end, data, n = drv.cuGraphGetEdges_v2(raw, n)
+    assert err == drv.CUresult.CUDA_SUCCESS and n == 3
+    early = drv.CUgraphDependencyType.CU_GRAPH_DEPENDENCY_TYPE_PROGRAMMATIC
+    after = {int(a): (int(b), int(d.type) == int(early)) for a, b, d in zip(start, end, data)}
+    node = (set(after) - {b for b, _ in after.values()}).pop()  # the packing
+    overlaps = []
+    while node in after:
+        node, overlap = after[node]
+        overlaps.append(overlap)
+    assert overlaps[0] is False and overlaps[2] is True  # the packing's end; rmsnorm and linear are chained as ever
+
+
 def test_rows_of_one_sequence_and_head_with_odd_strides():
     """strides of dimensions of one do not matter"""
     x = rnd((3, 5 * 64 + 8), 130).bfloat16()
