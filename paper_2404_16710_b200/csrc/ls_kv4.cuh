@@ -12,8 +12,9 @@
 //   exponent fields, and sums of denormals came out with an error of 2^-20 instead of 2^-24.)  Queries are scaled by
 //   powers of two of their own so that the largest component is in [2^14, 2^15): what f16 then cannot hold is 2^-39 of it.
 // * V: a nibble moved to bits 4..7 or-ed to 1024 is 1024 + 16 u, and one multiply-add makes c s of it:
-//   (1024 + 16 u) (s / 16) - 72 s.  A scale has 5 significant bits, so every step is exact, for scales down to 2^-25
-//   of the largest one the warp has met (the power of two it is divided by is kept beside O).
+//   (1024 + 16 u) (s / 16) - 72 s.  A scale has 5 significant bits, so every step is exact, for scales down to 2^-24
+//   of the largest one that the warp has met in the channel group (a lane's channels are of one group, and the power of
+//   two it divides by is its own); what is smaller still is off by less than 2^-22 of that one.
 // * p is rounded to f16's 11 bits (2^-12 of it; 2^-25 absolute below 2^-14, when the largest p so far is 1 or
 //   more), well below the rounding of a bf16 result.  Scores, maxima, sums and O are fp32.
 // Some 320 instructions go into a tile of 16 tokens of one KV head (2304 bytes) and up to 8 queries, 85 more for each
@@ -98,7 +99,7 @@ struct Kv4Smem {
     static constexpr int kQ = NT * HD / 32 * 32 * 16;          // [NT][group][lane] 16 bytes
     static constexpr int kInbox = (kItems + kKv4MaxCluster) * 16;  // [CTA][a share of the pieces]
     static constexpr int kFactor = NT * 8 * 4;                 // 2^e [query]
-    static constexpr int kStat = W * NT * 8 * 8 + W * 4;       // (max, sum) of the warps, units of their O
+    static constexpr int kStat = W * NT * 8 * 8 + W * HD / 32 * 4;  // (max, sum) of the warps, units of their O
     static constexpr int kInStat = kKv4MaxCluster * NT * 8 * 8;  // (max, sum) of the CTAs
     static constexpr int kBytes = kRing + kQ + kInbox + kFactor + kStat + kInStat;
     static_assert(kItems / (NT * 32) * 512 * NT <= kWarpRing, "a warp's O fits its ring");
@@ -138,7 +139,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     float4* sIn = reinterpret_cast<float4*>(at += SM::kQ);
     float* sF = reinterpret_cast<float*>(at += SM::kInbox);
     float2* sStat = reinterpret_cast<float2*>(at += SM::kFactor);   // [W][NT * 8]
-    float* sUnit = reinterpret_cast<float*>(sStat + W * NT * 8);     // [W]
+    float* sUnit = reinterpret_cast<float*>(sStat + W * NT * 8);     // [W][channel group]
     float2* sInStat = reinterpret_cast<float2*>(at += SM::kStat);   // [CTA][NT * 8]
     pdl_wait();
     const int splits = NT == 1 ? fastdiv(gridDim.x, S, div_S) : n_splits;
@@ -272,7 +273,9 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = -INFINITY;
     float top_m[NT][2];
-    int vexp = 17;  // O is kept in units of 2^(vexp - 135); vexp: exponent field of the largest V scale so far, at least 17
+    // O is kept in units of 2^(vexp - 135); vexp: exponent field of the largest V scale so far of this lane's channel
+    // group, at least 17
+    int vexp = 17;
     float vscale = exp2_int(135 - vexp);  // brings the largest scale to [2^8, 2^9)
 
     int stage = 0;
@@ -385,12 +388,14 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
         bool odd = false;
         float poison[NT][2] = {};
         if (__any_sync(0xffffffffu, grown)) {
-            auto largest = [&]() {
-                const uint32_t x = __vmaxu2(__vmaxu2(sc[0][0], sc[0][1]), __vmaxu2(sc[1][0], sc[1][1]));
-                return __reduce_max_sync(0xffffffffu, max(x & 0xffffu, x >> 16));
+            auto largest = [&]() {  // scale of this lane's channel group, which 32 / NJ neighbouring lanes share
+                uint32_t x = __vmaxu2(__vmaxu2(sc[0][0], sc[0][1]), __vmaxu2(sc[1][0], sc[1][1]));
+#pragma unroll
+                for (int d = 1; d < 32 / NJ; d *= 2) x = __vmaxu2(x, __shfl_xor_sync(0xffffffffu, x, d));
+                return max(x & 0xffffu, x >> 16);
             };
             uint32_t vmax = largest();
-            odd = vmax >= 0x7f80u;
+            odd = __any_sync(0xffffffffu, vmax >= 0x7f80u);
             if (odd) {  // 0 in the product, and NaN for the queries that see them
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -409,6 +414,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
                         if ((sc[u][r] & 0x7f800000u) == 0x7f800000u) sc[u][r] &= 0x0000ffffu;
                     }
                 }
+                __syncwarp();
                 vmax = largest();
             }
             const int vnew = max(vexp, (int)(vmax >> 7));
@@ -509,7 +515,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             if (g == 0) sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e]);
         }
     }
-    if (lane == 0) sUnit[warp] = exp2_int(vexp - 135);  // O was kept in units of this
+    if (lane % (32 / NJ) == 0) sUnit[warp * NJ + lane / (32 / NJ)] = exp2_int(vexp - 135);  // O was kept in units of this
     if (S > 1) cluster_wait();  // the others are there
     __syncthreads();
     // ---- the CTA's, sent to the CTA that finishes them: piece x holds two queries x two channels
@@ -528,7 +534,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             const float2 s0 = sStat[w * NT * 8 + c], s1 = sStat[w * NT * 8 + c + 1];
             const float f0 = m0 == -INFINITY ? 0.f : exp2_fast((s0.x - m0) * fb);
             const float f1 = m1 == -INFINITY ? 0.f : exp2_fast((s1.x - m1) * fb);
-            const float unit = sUnit[w];
+            const float unit = sUnit[w * NJ + (x & 31) / (32 / NJ)];
             l0 = fmaf(f0, s0.y, l0), l1 = fmaf(f1, s1.y, l1);
             r.x = fmaf(f0 * unit, v.x, r.x), r.z = fmaf(f0 * unit, v.z, r.z);
             r.y = fmaf(f1 * unit, v.y, r.y), r.w = fmaf(f1 * unit, v.w, r.w);

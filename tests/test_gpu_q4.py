@@ -494,6 +494,39 @@ def test_attention_values_and_keys_of_very_different_sizes():
     check_attention(c, q, c.run(q, M), M, G)
 
 
+def refill(c, b=0):
+    """the cache's sequence b again from c.k, c.v"""
+    B.ls_op_append_kv4(c.k[b][None], c.v[b][None], torch.zeros(1, dtype=torch.int32, device="cuda"), c.page, c.table[b:b + 1],
+                       c.max_seq, c.pool)
+
+
+def check_by_group(c, q, out, M, G):
+    """as check_attention, but what a weight below f16's normal numbers loses counts against the largest value of the
+    channel group itself, not of the head"""
+    got, qv = vals(out), vals(q)
+    for b, n in enumerate(c.lens):
+        k, v = c.values(b)
+        top = np.abs(v).reshape(n, c.Hkv, -1, 32).max((0, 3)).repeat(32, 1).repeat(G, 0)
+        for m in range(M):
+            ref, spread = R.attention(qv[b, m].reshape(-1, c.hd), k, v, n - M + m, G)
+            err = np.abs(got[b, m].reshape(-1, c.hd) - ref)
+            tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -13) * spread + n * 2.0 ** -25 * top
+            assert (err <= tol).all(), (b, m, n, (err / tol).max(), np.argmax(err / tol))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("down", [20, 24, 25, 26, 40, 100])
+def test_attention_channel_groups_that_are_always_quiet(hd, down):
+    """one channel group 2^-down of the others in every token: as exact as they are"""
+    Hkv, G, n, M = 2, 3, 333, 2
+    c = Cache([n], Hkv, hd, 32, 170)
+    c.v[0][:, 0, 32:64] *= 2.0 ** -down
+    c.v[0][:, 1, :32] *= 2.0 ** -down
+    refill(c)
+    q = rnd((1, M, Hkv * G * hd), 171).bfloat16()
+    check_by_group(c, q, c.run(q, M), M, G)
+
+
 @pytest.mark.parametrize("M", [1, 2, 3, 4, 6, 16])
 def test_attention_over_a_cache_long_enough_to_be_split(M):
     """16384 positions of one KV head: several splits joined by the second kernel, with scratch of the caller's and of
