@@ -12,9 +12,9 @@
 //   exponent fields, and sums of denormals came out with an error of 2^-20 instead of 2^-24.)  Queries are scaled by
 //   powers of two of their own so that the largest component is in [2^14, 2^15): what f16 then cannot hold is 2^-39 of it.
 // * V: a nibble moved to bits 4..7 or-ed to 1024 is 1024 + 16 u, and one multiply-add makes c s of it:
-//   (1024 + 16 u) (s / 16) - 72 s.  A scale has 5 significant bits, so every step is exact, for scales down to 2^-24
+//   (1024 + 16 u) (s / 16) - 72 s.  A scale has 5 significant bits, so every step is exact, for scales down to 2^-23
 //   of the largest one that the warp has met in the channel group (a lane's channels are of one group, and the power of
-//   two it divides by is its own); what is smaller still is off by less than 2^-22 of that one.
+//   two it divides by is its own); what is smaller still is off by less than 2^-21 of that one.
 // * p is rounded to f16's 11 bits (2^-12 of it; 2^-25 absolute below 2^-14, when the largest p so far is 1 or
 //   more), well below the rounding of a bf16 result.  Scores, maxima, sums and O are fp32.
 // Some 320 instructions go into a tile of 16 tokens of one KV head (2304 bytes) and up to 8 queries, 85 more for each
@@ -29,6 +29,9 @@ namespace ls {
 
 constexpr int kKv4Chunk = 32;   // positions a warp takes at a time: two tiles
 constexpr int kKv4Warps = 8;
+// How far beyond a V scale the unit goes that it raises: units are then raised rarely after a warp's first chunk (4103
+// positions, 7 rows: 0.3 us of 11 less than with 0)
+constexpr int kKv4Headroom = 1;
 
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
 {
@@ -99,7 +102,7 @@ struct Kv4Smem {
     static constexpr int kQ = NT * HD / 32 * 32 * 16;          // [NT][group][lane] 16 bytes
     static constexpr int kInbox = (kItems + kKv4MaxCluster) * 16;  // [CTA][a share of the pieces]
     static constexpr int kFactor = NT * 8 * 4;                 // 2^e [query]
-    static constexpr int kStat = W * NT * 8 * 8 + W * HD / 32 * 4;  // (max, sum) of the warps, units of their O
+    static constexpr int kStat = W * NT * 8 * 8 + W * HD / 32 * NT * 8 * 4;  // (max, sum) of the warps, units of their O
     static constexpr int kInStat = kKv4MaxCluster * NT * 8 * 8;  // (max, sum) of the CTAs
     static constexpr int kBytes = kRing + kQ + kInbox + kFactor + kStat + kInStat;
     static_assert(kItems / (NT * 32) * 512 * NT <= kWarpRing, "a warp's O fits its ring");
@@ -121,7 +124,7 @@ __device__ __forceinline__ float kv4_unit(int hd) { return 0x1p-14f * 1.44269504
 // (148 SMs: 33 of 4 CTAs, 15 of 8, 7 of 16 where one fills an SM), so that few heads over a long cache take several splits,
 // which a second kernel joins.  A row's result depends on its position and on the grid, not on M or the other
 // rows: what other rows add to the tokens a CTA looks at has weight 0, and all factors that are shared are powers
-// of two.
+// of two that lose nothing (where they would, a row has its own: `work`).
 template <int HD, int NT>
 __global__ void __launch_bounds__(kKv4Warps * 32, NT == 1 ? 2 : 1)
 attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t* __restrict__ pos0_dev,
@@ -139,7 +142,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     float4* sIn = reinterpret_cast<float4*>(at += SM::kQ);
     float* sF = reinterpret_cast<float*>(at += SM::kInbox);
     float2* sStat = reinterpret_cast<float2*>(at += SM::kFactor);   // [W][NT * 8]
-    float* sUnit = reinterpret_cast<float*>(sStat + W * NT * 8);     // [W][channel group]
+    float* sUnit = reinterpret_cast<float*>(sStat + W * NT * 8);     // [W][channel group][NT * 8]
     float2* sInStat = reinterpret_cast<float2*>(at += SM::kStat);   // [CTA][NT * 8]
     pdl_wait();
     const int splits = NT == 1 ? fastdiv(gridDim.x, S, div_S) : n_splits;
@@ -175,7 +178,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     look_up(base0);
     const int pos0 = ld_now(pos0_dev + b);
 
-    // last position that this lane's two queries of each 8 see, and over the CTA's queries the last and the first of those
+    // last position that this lane's two queries of each 8 see, and over the CTA's queries that see any the last and the first of those
     int lim[NT][2], top = -1, low = 0x7fffffff;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -184,7 +187,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             const int qi = q0 + nt * 8 + 2 * t + e;
             lim[nt][e] = qi < Q ? kv4_position(pos0, fastdiv(qi, G, div_G), cache.max_seq, status) : -1;
             top = max(top, lim[nt][e]);
-            if (qi < Q) low = min(low, lim[nt][e]);
+            if (lim[nt][e] >= 0) low = min(low, lim[nt][e]);
         }
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -273,21 +276,18 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = -INFINITY;
     float top_m[NT][2];
-    // O is kept in units of 2^(vexp - 135); vexp: exponent field of the largest V scale so far of this lane's channel
-    // group, at least 17
+    // O is kept in units of 2^(vexp - 135); vexp: no less than the exponent field of any V scale so far of this lane's
+    // channel group, at least 17
     int vexp = 17;
-    float vscale = exp2_int(135 - vexp);  // brings the largest scale to [2^8, 2^9)
+    float vscale = exp2_int(135 - vexp);  // scales become less than 2^9, the largest [2^7, 2^8) when it raises vexp
 
-    int stage = 0;
-    for (int base = base0; base <= top; base += step) {
-        fetch();
-        cp_async_wait<D - 1>();
-        __syncwarp();
-        const uint32_t ok = ok_bits & 3u;
-        ok_bits >>= 2;
-        --in_count;
-        const uint32_t chunk = ring + stage * 2 * TB;
-        if (++stage == D) stage = 0;
+    // The products of a chunk, for all queries or (ROW) for those of one row, whose lim is `only`.  True, and nothing done, if
+    // the rows have to be gone through one by one: if later rows' own tokens, which only a warp's last chunk can hold, would
+    // take V's unit so far up that the products of rows which do not see them lose bits.
+    int base = base0;
+    uint32_t ok, chunk;  // tiles of the chunk that exist; where it is
+    auto work = [&](auto row, int only) __attribute__((always_inline)) -> bool {
+        constexpr bool ROW = decltype(row)::value;
         const bool whole = ok == 3u && base + kKv4Chunk - 1 <= low;  // every query sees every token
 
         float s[NT][2][4];
@@ -351,19 +351,22 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
         if (!whole) {
             // a score that its query does not see is -inf, the V scale of a token that none sees 0, whatever
             // bits the tile holds there
+            const int to = ROW ? only : top;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const bool here = ok >> u & 1u;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!here || base + 16 * u + g + 8 * (e >> 1) > lim[nt][e & 1]) s[nt][u][e] = -INFINITY;
+                    for (int e = 0; e < 4; ++e) {
+                        const int l = lim[nt][e & 1];
+                        if (!here || (ROW && l != only) || base + 16 * u + g + 8 * (e >> 1) > l) s[nt][u][e] = -INFINITY;
+                    }
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const int p = base + 16 * u + 8 * r + 2 * t;
-                    if (!here || p > top) sc[u][r] &= 0xffff0000u;
-                    if (!here || p + 1 > top) sc[u][r] &= 0x0000ffffu;
+                    if (!here || p > to) sc[u][r] &= 0xffff0000u;
+                    if (!here || p + 1 > to) sc[u][r] &= 0x0000ffffu;
                 }
             }
         }
@@ -388,15 +391,15 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
         bool odd = false;
         float poison[NT][2] = {};
         if (__any_sync(0xffffffffu, grown)) {
-            auto largest = [&]() {  // scale of this lane's channel group, which 32 / NJ neighbouring lanes share
-                uint32_t x = __vmaxu2(__vmaxu2(sc[0][0], sc[0][1]), __vmaxu2(sc[1][0], sc[1][1]));
+            auto largest = [](const uint32_t (&v)[2][2]) {  // scale of this lane's channel group, which 32 / NJ neighbouring lanes share
+                uint32_t x = __vmaxu2(__vmaxu2(v[0][0], v[0][1]), __vmaxu2(v[1][0], v[1][1]));
 #pragma unroll
                 for (int d = 1; d < 32 / NJ; d *= 2) x = __vmaxu2(x, __shfl_xor_sync(0xffffffffu, x, d));
                 return max(x & 0xffffu, x >> 16);
             };
-            uint32_t vmax = largest();
+            uint32_t vmax = largest(sc);
             odd = __any_sync(0xffffffffu, vmax >= 0x7f80u);
-            if (odd) {  // 0 in the product, and NaN for the queries that see them
+            if (odd) [[unlikely]] {  // 0 in the product, and NaN for the queries that see them
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     for (int i = 0; i < 16; ++i) {
@@ -415,9 +418,25 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
                     }
                 }
                 __syncwarp();
-                vmax = largest();
+                vmax = largest(sc);
             }
-            const int vnew = max(vexp, (int)(vmax >> 7));
+            const int vnew = (int)(vmax >> 7) > vexp ? (int)(vmax >> 7) + kKv4Headroom : vexp;
+            if (!ROW && low < top && base + kKv4Chunk - 1 > low) {
+                // Rows differ in what they see of this chunk.  A unit taken up by tokens that the first does not see changes
+                // nothing for it, being a power of two, while all products stay normal f16 numbers (scales down to 2^-22 of
+                // the largest) and what is in O stays normal (bits below 2^-149 of the unit are not looked after).
+                uint32_t seen[2][2], least = 0xffffffffu;  // scales of what the first row sees; the smallest but 0, less 1
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t x = sc[i / 2][i % 2];
+                    const int p = base + 16 * (i / 2) + 8 * (i % 2) + 2 * t;
+                    seen[i / 2][i % 2] = p < low ? x : p == low ? x & 0xffffu : 0u;
+                    least = __vminu2(least, __vsub2(x, 0x00010001u));
+                }
+                const bool raised = (int)(vmax >> 7) > max(vexp, (int)(largest(seen) >> 7));
+                const int by = vnew - (int)(min(least & 0xffffu, least >> 16) >> 7);
+                if (__any_sync(0xffffffffu, raised && (by > 22 || (base > base0 && vnew - vexp > 22)))) return true;
+            }
             const float shrink = exp2_int(vexp - vnew);
             vexp = vnew;
             vscale = exp2_int(135 - vexp);
@@ -431,7 +450,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
                         mx[nt][e] = top_m[nt][e];
                     }
                     sum[nt][e] *= alpha;
-                    alpha *= shrink;
+                    if (!ROW || lim[nt][e] == only) alpha *= shrink;
 #pragma unroll
                     for (int i = 0; i < CT; ++i) o[nt][i][e] *= alpha, o[nt][i][e + 2] *= alpha;
                 }
@@ -484,7 +503,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
                                   o[nt][i][3]);
             }
         }
-        if (odd) {
+        if (odd) [[unlikely]] {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -492,7 +511,39 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[nt][i][e] += poison[nt][e & 1];
         }
+        return false;
+    };
+    int stage = 0;
+    bool apart = false;
+    for (; base <= top; base += step) {
+        fetch();
+        cp_async_wait<D - 1>();
+        __syncwarp();
+        ok = ok_bits & 3u;
+        ok_bits >>= 2;
+        --in_count;
+        chunk = ring + stage * 2 * TB;
+        if (++stage == D) stage = 0;
+        if ((apart = work(std::false_type(), -1))) break;
         __syncwarp();  // every lane has read the chunk before the ring comes round to it
+    }
+    // where O's units go: of the 32 / NJ lanes of a channel group the first four have two queries of each 8 each
+    float* units = sUnit + (warp * NJ + lane / (32 / NJ)) * NT * 8 + 2 * t;
+    if (apart) {
+        const int before = vexp;
+        for (int only = low; only <= top; ++only) {
+            work(std::true_type(), only);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (lim[nt][e] == only && lane % (32 / NJ) < 4) units[nt * 8 + e] = exp2_int(vexp - 135);
+            vexp = before, vscale = exp2_int(135 - vexp);
+            __syncwarp();
+        }
+    } else if (lane % (32 / NJ) < 4) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<float2*>(units + nt * 8) = make_float2(exp2_int(vexp - 135), exp2_int(vexp - 135));
     }
 
     // The next operation may come in from here on: earlier, its CTAs would take the free SMs two at a time (a layer of 4096
@@ -515,7 +566,6 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             if (g == 0) sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e]);
         }
     }
-    if (lane % (32 / NJ) == 0) sUnit[warp * NJ + lane / (32 / NJ)] = exp2_int(vexp - 135);  // O was kept in units of this
     if (S > 1) cluster_wait();  // the others are there
     __syncthreads();
     // ---- the CTA's, sent to the CTA that finishes them: piece x holds two queries x two channels
@@ -534,10 +584,10 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             const float2 s0 = sStat[w * NT * 8 + c], s1 = sStat[w * NT * 8 + c + 1];
             const float f0 = m0 == -INFINITY ? 0.f : exp2_fast((s0.x - m0) * fb);
             const float f1 = m1 == -INFINITY ? 0.f : exp2_fast((s1.x - m1) * fb);
-            const float unit = sUnit[w * NJ + (x & 31) / (32 / NJ)];
+            const float2 unit = *reinterpret_cast<const float2*>(sUnit + (w * NJ + (x & 31) / (32 / NJ)) * NT * 8 + c);
             l0 = fmaf(f0, s0.y, l0), l1 = fmaf(f1, s1.y, l1);
-            r.x = fmaf(f0 * unit, v.x, r.x), r.z = fmaf(f0 * unit, v.z, r.z);
-            r.y = fmaf(f1 * unit, v.y, r.y), r.w = fmaf(f1 * unit, v.w, r.w);
+            r.x = fmaf(f0 * unit.x, v.x, r.x), r.z = fmaf(f0 * unit.x, v.z, r.z);
+            r.y = fmaf(f1 * unit.y, v.y, r.y), r.w = fmaf(f1 * unit.y, v.w, r.w);
         }
         int to = 0;  // x / share
         for (int edge = share; edge <= x; edge += share) ++to;

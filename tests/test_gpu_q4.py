@@ -527,6 +527,35 @@ def test_attention_channel_groups_that_are_always_quiet(hd, down):
     check_by_group(c, q, c.run(q, M), M, G)
 
 
+@pytest.mark.parametrize("Hkv,G,hd,M,n,max_seq", [(1, 1, 64, 2, 40, 64), (2, 2, 128, 4, 700, 1024), (1, 8, 128, 16, 1010, 1024),
+                                                  (3, 1, 128, 16, 24, 64), (1, 4, 64, 16, 9010, 16384), (1, 8, 64, 7, 70, 128)])
+@pytest.mark.parametrize("up", [1, 12, 25, 40, 110])
+def test_attention_loud_values_of_later_rows(Hkv, G, hd, M, n, max_seq, up):
+    """values of the last rows' own tokens that are louder and louder than what came before (whose sizes differ too): rows
+    that do not see them come out bit for bit as without them"""
+    c = Cache([n], Hkv, hd, 16, 180, max_seq=max_seq)
+    size = np.exp2(np.random.default_rng(181).uniform(-11, 0, (n, Hkv, 1)))
+    for i in range(1, M):  # the token of every row but the first
+        size[n - M + i] = 2.0 ** (up * i / (M - 1))
+    x = c.v[0].float() * torch.from_numpy(size).float().cuda()
+    for i in range(1, M):  # less in one channel group
+        x[n - M + i, :, 32 * (i % (hd // 32)):][:, :32] *= 2.0 ** -3
+    c.v[0] = x.bfloat16()
+    refill(c)
+    q = rnd((1, M, Hkv * G * hd), 182).bfloat16()
+    full = c.run(q, M)
+    for m in range(M):
+        out = torch.empty((1, 1, q.shape[2]), dtype=torch.bfloat16, device="cuda")
+        pos = torch.tensor([n - M + m], dtype=torch.int32, device="cuda")
+        B.ls_op_attention_kv4(q[:, m:m + 1].contiguous(), pos, Hkv, hd, 16, c.table, max_seq, c.pool, out)
+        assert torch.equal(out, full[:, m:m + 1]), m
+        k, v = (y[:n - M + m + 1] for y in c.values(0))
+        ref, spread = R.attention(vals(q)[0, m].reshape(-1, hd), k, v, n - M + m, G)
+        top = np.abs(v).max()
+        err = np.abs(vals(out)[0, 0].reshape(-1, hd) - ref)
+        assert (err <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -13) * spread + n * 2.0 ** -25 * top).all(), m
+
+
 @pytest.mark.parametrize("M", [1, 2, 3, 4, 6, 16])
 def test_attention_over_a_cache_long_enough_to_be_split(M):
     """16384 positions of one KV head: several splits joined by the second kernel, with scratch of the caller's and of
