@@ -436,9 +436,9 @@ int ls_op_expand_kv4(const void *pages_dev, int32_t n_pages, int32_t n_seq, int3
  * time); with NULL, or where that function returns 0 (no split is worth it), none is used.  A row's
  * result depends on its position, n_seq, Hkv, max_seq and whether there is scratch (which fix how the
  * positions are dealt to CTAs), never on M or on the other rows (down to 2^-140 of the largest value of
- * a channel group).  Softmax weights enter the second product in f16, V exactly, unless its scale is
- * more than 2^23 below the largest that the row sees in its channel group (of 32): then it may be off
- * by 2^-21 of that one. */
+ * a channel group).  Softmax weights enter the second product with 11 bits (off by 2^-32 of the largest
+ * at least), V exactly, unless its scale is more than 2^23 below the largest that the row sees in its
+ * channel group (of 32): then it may be off by 2^-21 of that one. */
 size_t ls_op_attention_kv4_scratch_bytes(int32_t n_seq, int32_t M, int32_t Hq, int32_t Hkv, int32_t hd,
                                          int32_t max_seq);
 int ls_op_attention_kv4(const void *q_bf16_dev, int32_t n_seq, int32_t M, const int32_t *pos0_dev, int32_t Hq,

@@ -15,8 +15,9 @@
 //   (1024 + 16 u) (s / 16) - 72 s.  A scale has 5 significant bits, so every step is exact, for scales down to 2^-23
 //   of the largest one that the warp has met in the channel group (a lane's channels are of one group, and the power of
 //   two it divides by is its own); what is smaller still is off by less than 2^-21 of that one.
-// * p is rounded to f16's 11 bits (2^-12 of it; 2^-25 absolute below 2^-14, when the largest p so far is 1 or
-//   more), well below the rounding of a bf16 result.  Scores, maxima, sums and O are fp32.
+// * p is rounded to f16's 11 bits (2^-12 of it), well below the rounding of a bf16 result.  2^7 p stands in f16: p is at most
+//   2^8 and the largest so far 1 or more, so that weights keep those bits down to 2^-21 and are off by 2^-32 below, which
+//   thousands of positions beside one that outweighs them by 2^25 need.  Scores, maxima, sums and O are fp32.
 // Some 320 instructions go into a tile of 16 tokens of one KV head (2304 bytes) and up to 8 queries, 85 more for each
 // further 8; two CTAs of 8 warps an SM issue 2.4 of them a cycle.  131072 tokens, 8 KV heads: 41.7 us (0.55 of the
 // measured copy rate; first form 130); 1030 tokens, 32 heads: 7.0 us, of which the launch is 1.4, the first loads and
@@ -32,6 +33,7 @@ constexpr int kKv4Warps = 8;
 // How far beyond a V scale the unit goes that it raises: units are then raised rarely after a warp's first chunk (4103
 // positions, 7 rows: 0.3 us of 11 less than with 0)
 constexpr int kKv4Headroom = 1;
+constexpr int kKv4WeightBits = 7;  // softmax weights are held times 2^7
 
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
 {
@@ -276,7 +278,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = -INFINITY;
     float top_m[NT][2];
-    // O is kept in units of 2^(vexp - 135); vexp: no less than the exponent field of any V scale so far of this lane's
+    // O is kept in units of 2^(vexp - 135), and 2^7 of it for the weights'; vexp: no less than the exponent field of any V scale so far of this lane's
     // channel group, at least 17
     int vexp = 17;
     float vscale = exp2_int(135 - vexp);  // scales become less than 2^9, the largest [2^7, 2^8) when it raises vexp
@@ -459,7 +461,8 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float off = mx[nt][e] == -INFINITY ? 0.f : -mx[nt][e] * fb;  // nothing seen so far: every score is -inf
+                // 2^7 p; nothing seen so far: every score is -inf
+                const float off = mx[nt][e] == -INFINITY ? 0.f : fmaf(-mx[nt][e], fb, kKv4WeightBits);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     s[nt][u][e] = exp2_fast(fmaf(s[nt][u][e], fb, off));
@@ -529,6 +532,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     }
     // where O's units go: of the 32 / NJ lanes of a channel group the first four have two queries of each 8 each
     float* units = sUnit + (warp * NJ + lane / (32 / NJ)) * NT * 8 + 2 * t;
+    auto unit = [&]() { return exp2_int(vexp - 135 - kKv4WeightBits); };  // no less than 2^-125
     if (apart) {
         const int before = vexp;
         for (int only = low; only <= top; ++only) {
@@ -537,13 +541,13 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                    if (lim[nt][e] == only && lane % (32 / NJ) < 4) units[nt * 8 + e] = exp2_int(vexp - 135);
+                    if (lim[nt][e] == only && lane % (32 / NJ) < 4) units[nt * 8 + e] = unit();
             vexp = before, vscale = exp2_int(135 - vexp);
             __syncwarp();
         }
     } else if (lane % (32 / NJ) < 4) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<float2*>(units + nt * 8) = make_float2(exp2_int(vexp - 135), exp2_int(vexp - 135));
+        for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<float2*>(units + nt * 8) = make_float2(unit(), unit());
     }
 
     // The next operation may come in from here on: earlier, its CTAs would take the free SMs two at a time (a layer of 4096
@@ -563,7 +567,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 4);
             sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 8);
             sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 16);
-            if (g == 0) sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e]);
+            if (g == 0) sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e] * exp2_int(-kKv4WeightBits));
         }
     }
     if (S > 1) cluster_wait();  // the others are there

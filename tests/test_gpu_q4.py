@@ -556,6 +556,28 @@ def test_attention_loud_values_of_later_rows(Hkv, G, hd, M, n, max_seq, up):
         assert (err <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -13) * spread + n * 2.0 ** -25 * top).all(), m
 
 
+@pytest.mark.parametrize("M", [1, 3])
+def test_attention_small_weights_beside_a_key_that_has_nearly_all(M):
+    """the first key (7 steps of 7.25, which the format holds) outweighs each of the others by 2^25.9 and has value 0: what the
+    others, all alike, sum up to is as exact as any result, also in the share of the positions (a 64th: 8 CTAs of 8 warps) that
+    the first key belongs to.  There a weight of 2^-25.9 is off by 2^-32 at most: 2^-6.1 of it, 2^-12.1 of the result."""
+    n, hd, G = 4096, 128, 2
+    c = Cache([n], 1, hd, 64, 190)
+    q = torch.zeros((1, M, G * hd), device="cuda")
+    q[..., 0::hd] = 4.0
+    c.k[0].zero_()
+    c.k[0][0, 0, 0] = 50.75
+    c.v[0] = (1.0 + 0.25 * torch.rand((n, 1, hd), generator=torch.Generator(device="cuda").manual_seed(191), device="cuda")).bfloat16()
+    c.v[0][0] = 0
+    refill(c)
+    got = vals(c.run(q.bfloat16(), M))
+    k, v = c.values(0)
+    for m in range(M):
+        ref, spread = R.attention(vals(q)[0, m].reshape(G, hd), k, v, n - M + m, G)
+        tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + 2.0 ** -13) * spread
+        assert (np.abs(got[0, m].reshape(G, hd) - ref) <= tol).all(), m
+
+
 @pytest.mark.parametrize("M", [1, 2, 3, 4, 6, 16])
 def test_attention_over_a_cache_long_enough_to_be_split(M):
     """16384 positions of one KV head: several splits joined by the second kernel, with scratch of the caller's and of
