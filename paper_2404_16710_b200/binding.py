@@ -512,12 +512,13 @@ def _rows(pos0, table, n_seq):
 
 
 def ls_op_append_kv4(k, v, pos0, page_size, table, max_seq, pages, status=None):
-    """k, v bf16 [n_seq, M, Hkv, hd], of any strides but equal ones, channels contiguous"""
+    """k, v bf16 [n_seq, M, Hkv, hd], of any strides but equal ones (in dimensions of more than one), channels contiguous"""
     (n_seq, M, Hkv, hd), dev = k.shape, k.get_device()
     n_pages, entries = _pool(pages, Hkv, hd, page_size), _rows(pos0, table, n_seq)
     stride = k.stride()
-    if v.shape != k.shape or v.stride() != stride or stride[3] != 1 or dev < 0 or v.get_device() != dev or \
-            k.dtype is not _torch.bf16 or v.dtype is not _torch.bf16:
+    if v.shape != k.shape or stride[3] != 1 or dev < 0 or v.get_device() != dev or \
+            k.dtype is not _torch.bf16 or v.dtype is not _torch.bf16 or \
+            (v.stride() != stride and any(n > 1 and a != b for n, a, b in zip(k.shape, stride, v.stride()))):
         _bad("ls_op_append_kv4: k and v")
     _ck(lib().ls_op_append_kv4(k.data_ptr(), v.data_ptr(), stride[0], stride[1], stride[2], n_seq, M,
                                _arg(pos0, _torch.i32, dev, "pos0"), Hkv, hd, page_size, _arg(table, _torch.i32, dev, "page table"), entries, max_seq,

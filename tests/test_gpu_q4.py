@@ -777,6 +777,19 @@ def test_rows_of_one_sequence_and_head_with_odd_strides():
     assert np.array_equal(pool.cpu().numpy(), want)
 
 
+def test_k_and_v_whose_strides_differ_where_there_is_one():
+    """a row cut out of a longer tensor and one that stands alone; strides that differ elsewhere are refused"""
+    v, k = rnd((1, 9, 2, 64), 131).bfloat16(), rnd((1, 1, 2, 64), 132).bfloat16()
+    table, pd = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.tensor([3], dtype=torch.int32, device="cuda")
+    for a, b in ((k, v[:, 4:5]), (v[:, 4:5], k), (k[:, :, 1:], v[:, 4:5].transpose(1, 2)[:, 1:])):
+        pool = empty_pool(1, a.shape[2], 64, 16)
+        want = reference_append(pool.cpu().numpy().copy(), vals(a), vals(b), [3], table.cpu().numpy(), 16, 16)
+        B.ls_op_append_kv4(a, b, pd, 16, table, 16, pool)
+        assert np.array_equal(pool.cpu().numpy(), want)
+    with pytest.raises(B.LsError):
+        B.ls_op_append_kv4(v[:, :2], v[:, ::4][:, :2], pd, 16, table, 16, empty_pool(1, 2, 64, 16))
+
+
 def test_two_streams_at_once():
     """linear and attention calls on two streams, neither waiting for the other, give what each gives alone"""
     N, K = 4096, 2048
