@@ -652,6 +652,57 @@ def test_attention_over_the_longest_cache():
     assert int(status) == 0
 
 
+def test_every_split_of_the_longest_cache_counts():
+    """LS_KV4_MAX_SEQ positions, 64 splits, in each of which another channel's values are raised by 2: the bound is one that a
+    result without any one of them misses by a factor of 4 or more.
+    A weight's absolute error, 2^-32 of the largest of its warp's 512 positions (64 splits of 4 CTAs of 8 warps), adds up to
+    512 * 2^-32 of max |v| at most, as the warps' largest weights add up to no more than the sum.
+    Then a key that has nearly all the weight, in each split in turn: the result is its value."""
+    n, hd, page, G, M = 1 << 20, 64, 1024, 8, 2
+    table = torch.randperm(n // page, generator=torch.Generator().manual_seed(2)).to(torch.int32).cuda()[None]
+    pool = empty_pool(n // page, 1, hd, page)
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    at = torch.arange(n, device="cuda") // 32 // 8 // 4 % 64  # split of a position: chunks of 32, 8 warps, 4 CTAs
+    k, v = rnd((1, n, 1, hd), 200).bfloat16(), rnd((1, n, 1, hd), 201)
+    v[0, torch.arange(n, device="cuda"), 0, at] += 2
+    v = v.bfloat16()
+    B.ls_op_append_kv4(k, v, zero, page, table, n, pool)
+    kp, vp = (torch.empty((n // page, 1, page, hd), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    B.ls_op_expand_kv4(pool, zero, n, page, table, n, torch.arange(n // page, dtype=torch.int32, device="cuda")[None], kp, vp)
+    q = rnd((1, 1, 1, hd), 202, 2.0).expand(1, M, G, hd).reshape(1, M, G * hd).bfloat16()
+    q[0, :, hd:] = rnd((M, (G - 1) * hd), 203, 2.0).bfloat16()
+    splits = B.ls_op_attention_kv4_scratch_bytes(1, M, G, 1, hd, n) // (4 * 16 * (hd + 2))  # 16 queries: (hd + 2) floats each
+    assert splits == 64
+    pos = torch.tensor([n - M], dtype=torch.int32, device="cuda")
+    kd, vd = kp.view(n, hd).double(), vp.view(n, hd).double()
+
+    def run():
+        out = torch.empty_like(q)
+        B.ls_op_attention_kv4(q, pos, 1, hd, page, table, n, pool, out)
+        return torch.from_numpy(vals(out)).cuda().view(M, G, hd)
+
+    out = run()
+    for m in range(M):
+        w = torch.exp(q[0, m].view(G, hd).double() @ kd[:n - M + 1 + m].t() / hd ** 0.5)
+        vm, am = vd[:n - M + 1 + m], at[:n - M + 1 + m]
+        ref, spread = (w @ vm) / w.sum(1, True), (w @ vm.abs()) / w.sum(1, True)
+        tol = 2.0 ** -8 * ref.abs() + (2.0 ** -11 + 2.0 ** -13) * spread + 512 * 2.0 ** -32 * float(vm.abs().max())
+        assert bool(((out[m] - ref).abs() <= tol).all())
+        for i in range(splits):
+            keep = (am != i).double()
+            wrong = ((w * keep) @ vm) / (w * keep).sum(1, True)
+            assert bool((((wrong - ref).abs() > 4 * tol).any(1)).all()), (m, i)
+    rng = np.random.default_rng(204)
+    for i in range(splits):
+        where = int(at.eq(i).nonzero()[int(rng.integers(0, 16000))])  # of 16384
+        p = torch.tensor([where], dtype=torch.int32, device="cuda")
+        loud = (8 * q[0, 0, :hd]).view(1, 1, 1, hd)  # outweighs all others together by 2^100 for the first head of either row
+        B.ls_op_append_kv4(loud.contiguous(), v[:, where:where + 1].contiguous(), p, page, table, n, pool)
+        got = run()[:, 0]
+        assert bool(((got - vd[where]).abs() <= (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -13) * vd[where].abs() + 2.0 ** -40).all()), i
+        B.ls_op_append_kv4(k[:, where:where + 1].contiguous(), v[:, where:where + 1].contiguous(), p, page, table, n, pool)
+
+
 def test_packing_right_before_a_chained_linear():
     """with chained operations, which read weights ahead of time, the weights that the call before packs are the ones used"""
     N, K = 4096, 2048
