@@ -570,6 +570,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             if (g == 0) sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e] * exp2_int(-kKv4WeightBits));
         }
     }
+    __syncwarp();  // the cluster's barriers want whole warps
     if (S > 1) cluster_wait();  // the others are there
     __syncthreads();
     // ---- the CTA's, sent to the CTA that finishes them: piece x holds two queries x two channels
@@ -603,6 +604,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
                 st_cluster_f2(a + 8, m1, l1);
             }
     }
+    __syncwarp();
     if (S > 1)
         cluster_sync_all();  // after it nobody touches another CTA's memory
     else

@@ -244,6 +244,7 @@ linear_w4_kernel(const unsigned char* __restrict__ packed, const uint16_t* __res
                 float* o = out + (long long)m * N + n;
                 *o = residual ? *o + s : s;
             }
+            __syncwarp();  // the barrier wants whole warps
             asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(KS * 32) : "memory");  // the sums are read
         }
     }
