@@ -47,12 +47,6 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ int ld_now(const int32_t* p)
-{
-    int v;
-    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p));
-    return v;
-}
 // 2^e, 0 below the denormals
 __device__ __forceinline__ float exp2_int(int e)
 {
@@ -660,10 +654,10 @@ combine_kv4_kernel(const float* __restrict__ scratch, int G, const int32_t* __re
     const int m = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, lane = threadIdx.x % (HD / 2), quarter = threadIdx.x / (HD / 2);
     const int qi = m * G + hq % G, y = qi / (NT * 8) * Hkv + hq / G, c = qi % (NT * 8);
     const float* from = scratch + (kv4_partial(b, rows, y, splits, 0) * (NT * 8) + c) * (HD + 2);
-    const long long stride = (long long)NT * 8 * (HD + 2), p = (long long)pos0_dev[b] + m;
+    const long long stride = (long long)NT * 8 * (HD + 2), p = (long long)ld_now(pos0_dev + b) + m;
     const float fb = kv4_unit(HD);
     const bool mine = threadIdx.x < splits;
-    const float2 st = mine ? *reinterpret_cast<const float2*>(from + threadIdx.x * stride + HD) : make_float2(0.f, 0.f);
+    const float2 st = mine ? ld_once<float2>(from + threadIdx.x * stride + HD) : make_float2(0.f, 0.f);
     if (mine) stat[threadIdx.x] = st;
     __syncthreads();
     float top = -INFINITY;
@@ -677,7 +671,7 @@ combine_kv4_kernel(const float* __restrict__ scratch, int G, const int32_t* __re
     float x0 = 0.f, x1 = 0.f;
 #pragma unroll 4
     for (int s = quarter; s < splits; s += 4) {
-        const float2 v = *reinterpret_cast<const float2*>(from + s * stride + 2 * lane);
+        const float2 v = ld_once<float2>(from + s * stride + 2 * lane);
         x0 = fmaf(stat[s].x, v.x, x0), x1 = fmaf(stat[s].x, v.y, x1);
     }
     if (quarter) part[quarter - 1][lane] = make_float2(x0, x1);

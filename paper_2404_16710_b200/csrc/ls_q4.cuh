@@ -139,6 +139,20 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
     return r;
 }
 
+// Coherent loads of data that the kernel before this one may have written, under programmatic dependent launch after this one's
+// CTAs had started (ld_reuse16 says why): positions and page tables, and what is read once, from L2.
+__device__ __forceinline__ int ld_now(const int32_t* p)
+{
+    int v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ T ld_once(const void* p)
+{
+    return __ldcg(reinterpret_cast<const T*>(p));
+}
+
 // ------------------------------------------------------------------ weights: bf16 -> blocks, blocks -> bf16
 // Both are bound by memory: 11008 x 4096, packed and expanded again: 37.5 us in two launches (0.83 of the measured copy
 // rate), 4096 x 4096: 17.6 (0.66).  A code costs about 5 instructions; with a division, floor and comparison each (16,
@@ -165,7 +179,7 @@ __global__ void __launch_bounds__(256) quantize_w4_kernel(const uint16_t* __rest
         for (int j = 0; j < 4; ++j) {
             const int k = k0 + 32 * j + 8 * t;
             v[j] = make_uint4(0, 0, 0, 0);
-            if (n < N && k < K) v[j] = ld_stream16(w + n * K + k);  // K is a multiple of 8: the octet is in or out
+            if (n < N && k < K) v[j] = ld_once<uint4>(w + n * K + k);  // K is a multiple of 8: the octet is in or out
             am[j] = absmax8(v[j]);
         }
         if (NG <= 2) am[0] = am[1] = max(am[0], am[1]), am[2] = am[3] = max(am[2], am[3]);
@@ -199,14 +213,14 @@ template <int NG>
 __device__ __forceinline__ void q4_row_scales(const unsigned char* sd, uint32_t (&s2)[NG])
 {
     if (NG == 4) {
-        const uint2 v = *reinterpret_cast<const uint2*>(sd);
+        const uint2 v = ld_once<uint2>(sd);
         s2[0] = __byte_perm(v.x, 0, 0x1010), s2[1 % NG] = __byte_perm(v.x, 0, 0x3232);
         s2[2 % NG] = __byte_perm(v.y, 0, 0x1010), s2[3 % NG] = __byte_perm(v.y, 0, 0x3232);
     } else if (NG == 2) {
-        const uint32_t v = *reinterpret_cast<const uint32_t*>(sd);
+        const uint32_t v = ld_once<uint32_t>(sd);
         s2[0] = __byte_perm(v, 0, 0x1010), s2[1 % NG] = __byte_perm(v, 0, 0x3232);
     } else {
-        const uint32_t v = *reinterpret_cast<const uint16_t*>(sd);
+        const uint32_t v = ld_once<uint16_t>(sd);
         s2[0] = __byte_perm(v, 0, 0x1010);
     }
 }
@@ -222,17 +236,21 @@ __global__ void __launch_bounds__(256) expand_w4_kernel(const unsigned char* __r
     const long long n0 = blk / kblocks * kQ4Rows;
     const int k0 = (int)(blk % kblocks) * kQ4Cols;
     const unsigned char* src = packed + blk * w4_block_bytes(NG);
+    uint4 c[2];
+    uint32_t s2[2][NG];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        c[half] = ld_once<uint4>(src + half * (kQ4CodeBytes / 2) + lane * 16);
+        q4_row_scales<NG>(src + kQ4CodeBytes + (g + 8 * half) * NG * 2, s2[half]);
+    }
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         const long long n = n0 + g + 8 * half;
-        const uint4 c = *reinterpret_cast<const uint4*>(src + half * (kQ4CodeBytes / 2) + lane * 16);
-        uint32_t s2[NG];
-        q4_row_scales<NG>(src + kQ4CodeBytes + (g + 8 * half) * NG * 2, s2);
-        const uint32_t words[4] = {c.x, c.y, c.z, c.w};
+        const uint32_t words[4] = {c[half].x, c[half].y, c[half].z, c[half].w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int k = k0 + 32 * j + 8 * t;
-            if (n < N && k < K) *reinterpret_cast<uint4*>(out + n * K + k) = q4_values(words[j], s2[j * NG / 4]);
+            if (n < N && k < K) *reinterpret_cast<uint4*>(out + n * K + k) = q4_values(words[j], s2[half][j * NG / 4]);
         }
     }
 }
@@ -250,9 +268,12 @@ __device__ __forceinline__ long long kv4_tile_offset(const Kv4Cache& c, int page
     const int tiles = 1 << (c.page_shift - 4);  // tiles of a page and head
     return (((long long)page * c.Hkv + head) * tiles + ((p >> 4) & (tiles - 1))) * kv4_tile_bytes(HD);
 }
-__device__ __forceinline__ int kv4_page(const Kv4Cache& c, int b, int p, int32_t* status)
+__device__ __forceinline__ int kv4_entry(const Kv4Cache& c, int b, int p)
 {
-    const int page = c.table[(long long)b * c.table_stride + (p >> c.page_shift)];
+    return ld_now(c.table + (long long)b * c.table_stride + (p >> c.page_shift));
+}
+__device__ __forceinline__ int kv4_page(const Kv4Cache& c, int page, int32_t* status)
+{
     if ((unsigned)page < (unsigned)c.n_pages) return page;
     if (status) *status = DEV_BAD_PAGE;
     return -1;
@@ -287,18 +308,19 @@ __global__ void __launch_bounds__(256) append_kv4_kernel(const uint16_t* __restr
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, head = blockIdx.y, b = blockIdx.z;
     const int m = (blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32) * 8 + g;
     constexpr int G = HD / 32, O = HD / 64;  // groups of a row, octets of a V piece
-    // the row's values first: they wait for nothing
+    // the first loads are all on their way before the first is used
+    const int start = ld_now(pos0 + b);
     const long long at = b * seq_stride + (long long)m * row_stride + head * head_stride;
     uint4 xk[G], xv[2][O];
 #pragma unroll
-    for (int j = 0; j < G; ++j) xk[j] = m < M ? *reinterpret_cast<const uint4*>(k + at + 32 * j + 8 * t) : make_uint4(0, 0, 0, 0);
+    for (int j = 0; j < G; ++j) xk[j] = m < M ? ld_once<uint4>(k + at + 32 * j + 8 * t) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int o = 0; o < O; ++o)
-            xv[h][o] = m < M ? *reinterpret_cast<const uint4*>(v + at + (t + 4 * h) * (HD / 8) + 8 * o) : make_uint4(0, 0, 0, 0);
-    const int p = m < M ? kv4_position(pos0[b], m, cache.max_seq, status) : -1;
-    const int page = p >= 0 ? kv4_page(cache, b, p, status) : -1;  // -1: the row is left out, its lanes stay for the shuffles
+            xv[h][o] = m < M ? ld_once<uint4>(v + at + (t + 4 * h) * (HD / 8) + 8 * o) : make_uint4(0, 0, 0, 0);
+    const int p = m < M ? kv4_position(start, m, cache.max_seq, status) : -1;
+    const int page = p >= 0 ? kv4_page(cache, kv4_entry(cache, b, p), status) : -1;  // -1: the row is left out, its lanes stay for the shuffles
     unsigned char* tile = pages + (page >= 0 ? kv4_tile_offset<HD>(cache, page, p, head) : 0);
     const int i = p & 15;
     {
@@ -357,9 +379,10 @@ __global__ void __launch_bounds__(256) expand_kv4_kernel(const unsigned char* __
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, head = blockIdx.y, b = blockIdx.z;
     const int m = (blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32) * 8 + g;
     if (m >= M) return;
-    const int p = kv4_position(pos0[b], m, cache.max_seq, status);
+    const int p = kv4_position(ld_now(pos0 + b), m, cache.max_seq, status);
     if (p < 0) return;
-    const int page = kv4_page(cache, b, p, status), to = kv4_page(dst, b, p, status);
+    const int entry = kv4_entry(cache, b, p), to_entry = kv4_entry(dst, b, p);
+    const int page = kv4_page(cache, entry, status), to = kv4_page(dst, to_entry, status);
     if (page < 0 || to < 0) return;
     const unsigned char* tile = pages + kv4_tile_offset<HD>(cache, page, p, head);
     const int slot = p & ((1 << cache.page_shift) - 1), i = p & 15;
@@ -369,27 +392,32 @@ __global__ void __launch_bounds__(256) expand_kv4_kernel(const unsigned char* __
     q4_row_scales<G>(tile + 8 * HD + i * (HD / 16), s2);
     const unsigned char* cd = tile + i * (HD / 2) + t * (HD / 8);
     if (HD == 128) {
-        const uint4 c = *reinterpret_cast<const uint4*>(cd);
+        const uint4 c = ld_once<uint4>(cd);
         words[0] = c.x, words[1] = c.y, words[2 % G] = c.z, words[3 % G] = c.w;
     } else {
-        const uint2 c = *reinterpret_cast<const uint2*>(cd);
+        const uint2 c = ld_once<uint2>(cd);
         words[0] = c.x, words[1] = c.y;
+    }
+    uint32_t sv[2], wv[2][HD / 64];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int piece = t + 4 * h;
+        sv[h] = ld_once<uint16_t>(tile + 17 * HD + (piece * (HD / 8) / 32 * 16 + i) * 2);
+#pragma unroll
+        for (int o = 0; o < HD / 64; ++o) wv[h][o] = ld_once<uint32_t>(tile + kv4_v_piece<HD>(i, piece) + 4 * o);
     }
 #pragma unroll
     for (int j = 0; j < G; ++j) *reinterpret_cast<uint4*>(kp + at + 32 * j + 8 * t) = q4_values(words[j], s2[j]);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int piece = t + 4 * h;
-        const uint32_t s = *reinterpret_cast<const uint16_t*>(tile + 17 * HD + (piece * (HD / 8) / 32 * 16 + i) * 2);
-        const uint32_t sv = __byte_perm(s, 0, 0x1010);
+        const uint32_t s = __byte_perm(sv[h], 0, 0x1010);
 #pragma unroll
         for (int o = 0; o < HD / 64; ++o) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(tile + kv4_v_piece<HD>(i, piece) + 4 * o);
             // lowest nibble first -> the row order of q4_values: even columns to nibbles 0..3, odd to 4..7
             uint32_t e = 0;
 #pragma unroll
-            for (int n = 0; n < 4; ++n) e |= ((w >> (8 * n)) & 0xfu) << (4 * n) | ((w >> (8 * n + 4)) & 0xfu) << (4 * n + 16);
-            *reinterpret_cast<uint4*>(vp + at + piece * (HD / 8) + 8 * o) = q4_values(e, sv);
+            for (int n = 0; n < 4; ++n) e |= ((wv[h][o] >> (8 * n)) & 0xfu) << (4 * n) | ((wv[h][o] >> (8 * n + 4)) & 0xfu) << (4 * n + 16);
+            *reinterpret_cast<uint4*>(vp + at + (t + 4 * h) * (HD / 8) + 8 * o) = q4_values(e, s);
         }
     }
 }

@@ -818,6 +818,43 @@ def test_no_operation_overlaps_one_that_writes_weights(packing, chained):
     assert overlaps[0] is False and overlaps[2] is True  # the packing's end; rmsnorm and linear are chained as ever
 
 
+def test_chained_conversions_read_what_the_one_ahead_wrote():
+    """append -> expand -> append of what was expanded -> attention, and expand -> pack, over buffers used again and again:
+    the same bytes with operations that start early and ones that do not (the values are the format's own: a second packing
+    changes nothing)"""
+    n, Hkv, hd, page, N, K = 160, 2, 128, 32, 272, 384
+    table, pd = torch.arange(5, dtype=torch.int32, device="cuda")[None], torch.zeros(1, dtype=torch.int32, device="cuda")
+    last = torch.tensor([n - 1], dtype=torch.int32, device="cuda")
+    ks, vs = rnd((6, 1, n, Hkv, hd), 210).bfloat16(), rnd((6, 1, n, Hkv, hd), 211).bfloat16()
+    ws, q = rnd((6, N, K), 212).bfloat16(), rnd((1, 1, 2 * Hkv * hd), 213).bfloat16()
+    packs = [quantised(w, 32) for w in ws]
+    a, b = empty_pool(5, Hkv, hd, page), empty_pool(5, Hkv, hd, page)
+    kp, vp = (torch.zeros((5, Hkv, page, hd), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    wide, again, results = torch.zeros((N, K), dtype=torch.bfloat16, device="cuda"), torch.zeros_like(packs[0]), []
+    for chained in (False, True):
+        left = []
+        for i in range(6):
+            out = torch.zeros_like(q)
+            torch.cuda.synchronize()
+            B.ls_op_chain(chained)
+            try:
+                B.ls_op_append_kv4(ks[i], vs[i], pd, page, table, n, a)
+                B.ls_op_expand_kv4(a, pd, n, page, table, n, table, kp, vp)
+                for j in range(5):  # a page of rows at a time, heads outermost
+                    pj = torch.tensor([j * page], dtype=torch.int32, device="cuda")
+                    B.ls_op_append_kv4(kp[j].transpose(0, 1)[None], vp[j].transpose(0, 1)[None], pj, page, table, n, b)
+                B.ls_op_attention_kv4(q, last, Hkv, hd, page, table, n, b, out)
+                B.ls_op_expand_w4(packs[i], 32, wide)
+                B.ls_op_quantize_w4(wide, 32, again)
+            finally:
+                B.ls_op_chain(False)
+            torch.cuda.synchronize()
+            left.append((a.clone(), b.clone(), out, again.clone()))
+            assert torch.equal(a, b) and torch.equal(again, packs[i])
+        results.append(left)
+    assert all(torch.equal(x, y) for u, v in zip(*results) for x, y in zip(u, v))
+
+
 def test_rows_of_one_sequence_and_head_with_odd_strides():
     """strides of dimensions of one do not matter"""
     x = rnd((3, 5 * 64 + 8), 130).bfloat16()
