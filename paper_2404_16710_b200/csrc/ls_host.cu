@@ -1932,8 +1932,10 @@ int w4_launch_ng(const unsigned char* packed, const uint16_t* h, int M, int N, i
     const int64_t room = kW4SmemMax - (int64_t)M * w4_h_stride(w4_kblocks(K));
     if (M <= 8) {
         const int64_t ring24 = room - w4_part_bytes<1, 24>(), ring16 = room - w4_part_bytes<1, 16>();
-        // 24 warps, what 64 to 80 registers allow, make a third team of 8 warps: of use with more than two tiles an SM
-        // (320 tiles, K = 5120: 7.4 us, 16 warps 8.4; 688 tiles: 9.2, 9.9; but 256 tiles, K = 4096: 5.8, 5.2)
+        // 24 warps, what 64 to 80 registers allow, are six teams of 4 warps instead of four: of use with more than two tiles
+        // an SM (one row, groups of 64: 320 tiles, K = 5120: 6.7 us, 16 warps 7.0; 512 tiles, K = 8192: 10.9, 11.3; 688
+        // tiles, K = 4096: 8.35, 9.5; 768: 9.3, 10.05; 2000: 17.6, 18.2; 8016: 56.1, 57.5; seven rows the same; but 896 tiles,
+        // K = 4096: 11.6, 10.8, where six teams deal the tiles of an SM less evenly)
         if (N > 16 * 296 && ring24 >= w4_ring_bytes<NG, 24>(4))
             return w4_launch<NG, 1, 24, 4, 2, true, 1>(packed, h, M, N, K, out, residual, lc);
         if (ring16 >= w4_ring_bytes<NG, 16>(6)) return w4_launch<NG, 1, 16, 6, 2, true, 1>(packed, h, M, N, K, out, residual, lc);
@@ -1942,9 +1944,10 @@ int w4_launch_ng(const unsigned char* packed, const uint16_t* h, int M, int N, i
         return w4_launch<NG, 1, 16, 6, 2, false, 1>(packed, h, M, N, K, out, residual, lc);
     }
     const int64_t ring = room - w4_part_bytes<2, 16>();
-    // more than 8 rows through a large matrix: two tiles at a time (128256 x 4096, 16 rows: 71.4 us, one at a time 75.2);
-    // with few tiles an SM the teams would run out of pairs
-    if (N > 16 * 1023 && ring >= w4_ring_bytes<NG, 16>(4))
+    // more than 8 rows through a large matrix: two tiles at a time (K = 4096, 16 rows, groups of 64: 8016 tiles 72.6 us, one at a
+    // time 74.2; 2000 tiles 22.4, 22.9); with fewer, here than 13 an SM, pairs are dealt less evenly (1600 tiles 20.2, 18.8; 1200
+    // tiles 19.1, 17.1; 1024 tiles 14.3, 13.6).  Groups of 32 spill 6 registers there (79.9 us for 8016 tiles).
+    if (N > 16 * 13 * 148 && ring >= w4_ring_bytes<NG, 16>(4))
         return ring >= w4_ring_bytes<NG, 16>(6) ? w4_launch<NG, 2, 16, 6, 1, true, 2>(packed, h, M, N, K, out, residual, lc)
                                                 : w4_launch<NG, 2, 16, 4, 1, true, 2>(packed, h, M, N, K, out, residual, lc);
     if (ring >= w4_ring_bytes<NG, 16>(6)) return w4_launch<NG, 2, 16, 6, 2, true, 1>(packed, h, M, N, K, out, residual, lc);

@@ -147,6 +147,22 @@ def test_linear_rows_do_not_depend_on_pass_size(N, K, group):
         assert torch.equal(out, full[m0:m0 + M]), M
 
 
+@pytest.mark.parametrize("N,K,group", [(30784, 136, 64), (30785, 136, 64), (30800, 520, 32), (31000, 8200, 128), (33000, 264, 32)])
+def test_linear_rows_of_large_matrices_do_not_depend_on_pass_size(N, K, group):
+    """on both sides of the number of rows from which two tiles are taken at a time, an odd last pair among them"""
+    w = rnd((N, K), 220, 0.05).bfloat16()
+    packed, h = quantised(w, group), rnd((16, K), 221).bfloat16()
+    full = torch.empty((16, N), device="cuda")
+    B.ls_op_linear_w4(packed, group, h, full)
+    rows = np.unique(np.concatenate([[0, 15, 16, N - 17, N - 1], np.random.default_rng(1).integers(0, N, 40)]))
+    ref, spread = linear_reference(w[torch.from_numpy(rows).cuda()], group, h)
+    assert (np.abs(full.cpu().numpy()[:, rows] - ref) <= linear_tol(K, group, spread)).all()
+    for m0, M in ((0, 1), (5, 7), (8, 8), (2, 9), (0, 15)):
+        out = torch.full((M, N), float("nan"), device="cuda")
+        B.ls_op_linear_w4(packed, group, h[m0:m0 + M].contiguous(), out)
+        assert torch.equal(out, full[m0:m0 + M]), M
+
+
 def test_linear_scales_of_other_packers_and_values_that_are_not_finite():
     """any bf16 scale may stand in the packed weights; a NaN group, an infinite h make NaN where the formula does"""
     N, K, group = 40, 256, 64
