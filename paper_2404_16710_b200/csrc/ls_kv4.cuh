@@ -268,374 +268,374 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     const float fb = kv4_unit(HD);
 
     for (;;) {  // one split after the other, where there are fewer clusters than splits
-    float o[NT][CT][4] = {}, mx[NT][2], sum[NT][2] = {};
+        float o[NT][CT][4] = {}, mx[NT][2], sum[NT][2] = {};
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = -INFINITY;
-    float top_m[NT][2];
-    // O is kept in units of 2^(vexp - 135), and 2^7 of it for the weights'; vexp: no less than the exponent field of any V scale so far of this lane's
-    // channel group, at least 17
-    int vexp = 17;
-    float vscale = exp2_int(135 - vexp);  // scales become less than 2^9, the largest [2^7, 2^8) when it raises vexp
+        for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = -INFINITY;
+        float top_m[NT][2];
+        // O is kept in units of 2^(vexp - 135), and 2^7 of it for the weights'; vexp: no less than the exponent field of any V scale so far of this lane's
+        // channel group, at least 17
+        int vexp = 17;
+        float vscale = exp2_int(135 - vexp);  // scales become less than 2^9, the largest [2^7, 2^8) when it raises vexp
 
-    // The products of a chunk, for all queries or (ROW) for those of one row, whose lim is `only`.  True, and nothing done, if
-    // the rows have to be gone through one by one: if later rows' own tokens, which only a warp's last chunk can hold, would
-    // take V's unit so far up that the products of rows which do not see them lose bits.
-    int base = base0;
-    uint32_t ok, chunk;  // tiles of the chunk that exist; where it is
-    auto work = [&](auto row, int only) __attribute__((always_inline)) -> bool {
-        constexpr bool ROW = decltype(row)::value;
-        const bool whole = ok == 3u && base + kKv4Chunk - 1 <= low;  // every query sees every token
+        // The products of a chunk, for all queries or (ROW) for those of one row, whose lim is `only`.  True, and nothing done, if
+        // the rows have to be gone through one by one: if later rows' own tokens, which only a warp's last chunk can hold, would
+        // take V's unit so far up that the products of rows which do not see them lose bits.
+        int base = base0;
+        uint32_t ok, chunk;  // tiles of the chunk that exist; where it is
+        auto work = [&](auto row, int only) __attribute__((always_inline)) -> bool {
+            constexpr bool ROW = decltype(row)::value;
+            const bool whole = ok == 3u && base + kKv4Chunk - 1 <= low;  // every query sees every token
 
-        float s[NT][2][4];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint32_t tile = chunk + u * TB;
-            uint32_t wl[NJ], wh[NJ];
-            if (HD == 128) {
-                const uint4 x = lds16(tile + lane * 16), y = lds16(tile + 512 + lane * 16);
-                wl[0] = x.x, wl[1] = x.y, wl[2 % NJ] = x.z, wl[3 % NJ] = x.w;
-                wh[0] = y.x, wh[1] = y.y, wh[2 % NJ] = y.z, wh[3 % NJ] = y.w;
-            } else {
-                const uint2 x = lds8(tile + lane * 8), y = lds8(tile + 256 + lane * 8);
-                wl[0] = x.x, wl[1] = x.y;
-                wh[0] = y.x, wh[1] = y.y;
-            }
-            float s_lo[NJ], s_hi[NJ];
-            const uint32_t sd = tile + 8 * HD + g * (HD / 16);
-            if (HD == 128) {
-                const uint2 x = lds8(sd), y = lds8(sd + 8 * (HD / 16));
-                s_lo[0] = bf16lo(x.x), s_lo[1] = bf16hi(x.x), s_lo[2 % NJ] = bf16lo(x.y), s_lo[3 % NJ] = bf16hi(x.y);
-                s_hi[0] = bf16lo(y.x), s_hi[1] = bf16hi(y.x), s_hi[2 % NJ] = bf16lo(y.y), s_hi[3 % NJ] = bf16hi(y.y);
-            } else {
-                const uint32_t x = lds4(sd), y = lds4(sd + 8 * (HD / 16));
-                s_lo[0] = bf16lo(x), s_lo[1] = bf16hi(x);
-                s_hi[0] = bf16lo(y), s_hi[1] = bf16hi(y);
-            }
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                uint32_t a[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    a[2 * i] = q4_f16x2(wl[j] >> (8 * (i / 2)), i % 2);
-                    a[2 * i + 1] = q4_f16x2(wh[j] >> (8 * (i / 2)), i % 2);
-                }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const uint4 bq = sQ[(nt * NJ + j) * 32 + lane];
-                    float c[4];
-                    mma_f16_16816(c, a[0], a[1], a[2], a[3], bq.x, bq.y, 0.f, 0.f, 0.f, 0.f);
-                    mma_f16_16816(c, a[4], a[5], a[6], a[7], bq.z, bq.w, c[0], c[1], c[2], c[3]);
-                    if (j == 0) {
-                        s[nt][u][0] = s_lo[j] * c[0], s[nt][u][1] = s_lo[j] * c[1];
-                        s[nt][u][2] = s_hi[j] * c[2], s[nt][u][3] = s_hi[j] * c[3];
-                    } else {
-                        s[nt][u][0] = fmaf(s_lo[j], c[0], s[nt][u][0]);
-                        s[nt][u][1] = fmaf(s_lo[j], c[1], s[nt][u][1]);
-                        s[nt][u][2] = fmaf(s_hi[j], c[2], s[nt][u][2]);
-                        s[nt][u][3] = fmaf(s_hi[j], c[3], s[nt][u][3]);
-                    }
-                }
-            }
-        }
-        // V scales of this lane's group, tokens 2 t, 2 t + 1 and 8 more of each tile
-        uint32_t sc[2][2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-                sc[u][r] = lds4(chunk + u * TB + 17 * HD + g * (HD / 8) / 32 * 32 + r * 16 + t * 4);
-        if (!whole) {
-            // a score that its query does not see is -inf, the V scale of a token that none sees 0, whatever
-            // bits the tile holds there
-            const int to = ROW ? only : top;
+            float s[NT][2][4];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const bool here = ok >> u & 1u;
+                const uint32_t tile = chunk + u * TB;
+                uint32_t wl[NJ], wh[NJ];
+                if (HD == 128) {
+                    const uint4 x = lds16(tile + lane * 16), y = lds16(tile + 512 + lane * 16);
+                    wl[0] = x.x, wl[1] = x.y, wl[2 % NJ] = x.z, wl[3 % NJ] = x.w;
+                    wh[0] = y.x, wh[1] = y.y, wh[2 % NJ] = y.z, wh[3 % NJ] = y.w;
+                } else {
+                    const uint2 x = lds8(tile + lane * 8), y = lds8(tile + 256 + lane * 8);
+                    wl[0] = x.x, wl[1] = x.y;
+                    wh[0] = y.x, wh[1] = y.y;
+                }
+                float s_lo[NJ], s_hi[NJ];
+                const uint32_t sd = tile + 8 * HD + g * (HD / 16);
+                if (HD == 128) {
+                    const uint2 x = lds8(sd), y = lds8(sd + 8 * (HD / 16));
+                    s_lo[0] = bf16lo(x.x), s_lo[1] = bf16hi(x.x), s_lo[2 % NJ] = bf16lo(x.y), s_lo[3 % NJ] = bf16hi(x.y);
+                    s_hi[0] = bf16lo(y.x), s_hi[1] = bf16hi(y.x), s_hi[2 % NJ] = bf16lo(y.y), s_hi[3 % NJ] = bf16hi(y.y);
+                } else {
+                    const uint32_t x = lds4(sd), y = lds4(sd + 8 * (HD / 16));
+                    s_lo[0] = bf16lo(x), s_lo[1] = bf16hi(x);
+                    s_hi[0] = bf16lo(y), s_hi[1] = bf16hi(y);
+                }
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int j = 0; j < NJ; ++j) {
+                    uint32_t a[8];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int l = lim[nt][e & 1];
-                        if (!here || (ROW && l != only) || base + 16 * u + g + 8 * (e >> 1) > l) s[nt][u][e] = -INFINITY;
+                    for (int i = 0; i < 4; ++i) {
+                        a[2 * i] = q4_f16x2(wl[j] >> (8 * (i / 2)), i % 2);
+                        a[2 * i + 1] = q4_f16x2(wh[j] >> (8 * (i / 2)), i % 2);
                     }
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int p = base + 16 * u + 8 * r + 2 * t;
-                    if (!here || p > to) sc[u][r] &= 0xffff0000u;
-                    if (!here || p + 1 > to) sc[u][r] &= 0x0000ffffu;
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const uint4 bq = sQ[(nt * NJ + j) * 32 + lane];
+                        float c[4];
+                        mma_f16_16816(c, a[0], a[1], a[2], a[3], bq.x, bq.y, 0.f, 0.f, 0.f, 0.f);
+                        mma_f16_16816(c, a[4], a[5], a[6], a[7], bq.z, bq.w, c[0], c[1], c[2], c[3]);
+                        if (j == 0) {
+                            s[nt][u][0] = s_lo[j] * c[0], s[nt][u][1] = s_lo[j] * c[1];
+                            s[nt][u][2] = s_hi[j] * c[2], s[nt][u][3] = s_hi[j] * c[3];
+                        } else {
+                            s[nt][u][0] = fmaf(s_lo[j], c[0], s[nt][u][0]);
+                            s[nt][u][1] = fmaf(s_lo[j], c[1], s[nt][u][1]);
+                            s[nt][u][2] = fmaf(s_hi[j], c[2], s[nt][u][2]);
+                            s[nt][u][3] = fmaf(s_hi[j], c[3], s[nt][u][3]);
+                        }
+                    }
                 }
             }
-        }
-        // Running softmax, in units of 1 / fb.  A query's reference moves up only when its maximum has outgrown it by
-        // 2^8, so that O is rarely rescaled: p <= 2^8 then, and some p so far has been 1 or more.
-        bool grown = false;
+            // V scales of this lane's group, tokens 2 t, 2 t + 1 and 8 more of each tile
+            uint32_t sc[2][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u) s[nt][u][e] *= fa[nt][e], s[nt][u][e + 2] *= fa[nt][e];
-                float m = fmaxf(fmaxf(s[nt][0][e], s[nt][0][e + 2]), fmaxf(s[nt][1][e], s[nt][1][e + 2]));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                top_m[nt][e] = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                grown |= top_m[nt][e] * fb > fmaf(mx[nt][e], fb, 8.f);
-            }
-        // V scales beyond what O's unit allows for, or not finite (of values that are not)
-        const uint32_t m2 = __vmaxu2(__vmaxu2(sc[0][0], sc[0][1]), __vmaxu2(sc[1][0], sc[1][1]));
-        grown |= max(m2 & 0xffffu, m2 >> 16) >> 7 > (uint32_t)vexp;
-        bool odd = false;
-        float poison[NT][2] = {};
-        if (__any_sync(0xffffffffu, grown)) {
-            auto largest = [](const uint32_t (&v)[2][2]) {  // scale of this lane's channel group, which 32 / NJ neighbouring lanes share
-                uint32_t x = __vmaxu2(__vmaxu2(v[0][0], v[0][1]), __vmaxu2(v[1][0], v[1][1]));
-#pragma unroll
-                for (int d = 1; d < 32 / NJ; d *= 2) x = __vmaxu2(x, __shfl_xor_sync(0xffffffffu, x, d));
-                return max(x & 0xffffu, x >> 16);
-            };
-            uint32_t vmax = largest(sc);
-            odd = __any_sync(0xffffffffu, vmax >= 0x7f80u);
-            if (odd) [[unlikely]] {  // 0 in the product, and NaN for the queries that see them
+                for (int r = 0; r < 2; ++r)
+                    sc[u][r] = lds4(chunk + u * TB + 17 * HD + g * (HD / 8) / 32 * 32 + r * 16 + t * 4);
+            if (!whole) {
+                // a score that its query does not see is -inf, the V scale of a token that none sees 0, whatever
+                // bits the tile holds there
+                const int to = ROW ? only : top;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    for (int i = 0; i < 16; ++i) {
-                        const uint32_t x = lds4(chunk + u * TB + 17 * HD + g * (HD / 8) / 32 * 32 + (i & ~1) * 2) >> (16 * (i & 1));
-                        if ((x & 0x7f80u) != 0x7f80u || !(ok >> u & 1u)) continue;
+                    const bool here = ok >> u & 1u;
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                if (base + 16 * u + i <= lim[nt][e]) poison[nt][e] = __uint_as_float(0x7fffffffu);
-                    }
+                        for (int e = 0; e < 4; ++e) {
+                            const int l = lim[nt][e & 1];
+                            if (!here || (ROW && l != only) || base + 16 * u + g + 8 * (e >> 1) > l) s[nt][u][e] = -INFINITY;
+                        }
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        if ((sc[u][r] & 0x7f80u) == 0x7f80u) sc[u][r] &= 0xffff0000u;
-                        if ((sc[u][r] & 0x7f800000u) == 0x7f800000u) sc[u][r] &= 0x0000ffffu;
+                        const int p = base + 16 * u + 8 * r + 2 * t;
+                        if (!here || p > to) sc[u][r] &= 0xffff0000u;
+                        if (!here || p + 1 > to) sc[u][r] &= 0x0000ffffu;
                     }
                 }
-                __syncwarp();
-                vmax = largest(sc);
             }
-            const int vnew = (int)(vmax >> 7) > vexp ? (int)(vmax >> 7) + kKv4Headroom : vexp;
-            if (!ROW && low < top && base + kKv4Chunk - 1 > low) {
-                // Rows differ in what they see of this chunk.  A unit taken up by tokens that the first does not see changes
-                // nothing for it, being a power of two, while all products stay normal f16 numbers (scales down to 2^-22 of
-                // the largest) and what is in O stays normal (bits below 2^-149 of the unit are not looked after).
-                uint32_t seen[2][2], least = 0xffffffffu;  // scales of what the first row sees; the smallest but 0, less 1
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t x = sc[i / 2][i % 2];
-                    const int p = base + 16 * (i / 2) + 8 * (i % 2) + 2 * t;
-                    seen[i / 2][i % 2] = p < low ? x : p == low ? x & 0xffffu : 0u;
-                    least = __vminu2(least, __vsub2(x, 0x00010001u));
-                }
-                const bool raised = (int)(vmax >> 7) > max(vexp, (int)(largest(seen) >> 7));
-                const int by = vnew - (int)(min(least & 0xffffu, least >> 16) >> 7);
-                if (__any_sync(0xffffffffu, raised && (by > 22 || (base > base0 && vnew - vexp > 22)))) return true;
-            }
-            const float shrink = exp2_int(vexp - vnew);
-            vexp = vnew;
-            vscale = exp2_int(135 - vexp);
+            // Running softmax, in units of 1 / fb.  A query's reference moves up only when its maximum has outgrown it by
+            // 2^8, so that O is rarely rescaled: p <= 2^8 then, and some p so far has been 1 or more.
+            bool grown = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float alpha = 1.f;
-                    if (top_m[nt][e] * fb > fmaf(mx[nt][e], fb, 8.f)) {
-                        alpha = exp2_fast((mx[nt][e] - top_m[nt][e]) * fb);
-                        mx[nt][e] = top_m[nt][e];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) s[nt][u][e] *= fa[nt][e], s[nt][u][e + 2] *= fa[nt][e];
+                    float m = fmaxf(fmaxf(s[nt][0][e], s[nt][0][e + 2]), fmaxf(s[nt][1][e], s[nt][1][e + 2]));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                    top_m[nt][e] = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                    grown |= top_m[nt][e] * fb > fmaf(mx[nt][e], fb, 8.f);
+                }
+            // V scales beyond what O's unit allows for, or not finite (of values that are not)
+            const uint32_t m2 = __vmaxu2(__vmaxu2(sc[0][0], sc[0][1]), __vmaxu2(sc[1][0], sc[1][1]));
+            grown |= max(m2 & 0xffffu, m2 >> 16) >> 7 > (uint32_t)vexp;
+            bool odd = false;
+            float poison[NT][2] = {};
+            if (__any_sync(0xffffffffu, grown)) {
+                auto largest = [](const uint32_t (&v)[2][2]) {  // scale of this lane's channel group, which 32 / NJ neighbouring lanes share
+                    uint32_t x = __vmaxu2(__vmaxu2(v[0][0], v[0][1]), __vmaxu2(v[1][0], v[1][1]));
+#pragma unroll
+                    for (int d = 1; d < 32 / NJ; d *= 2) x = __vmaxu2(x, __shfl_xor_sync(0xffffffffu, x, d));
+                    return max(x & 0xffffu, x >> 16);
+                };
+                uint32_t vmax = largest(sc);
+                odd = __any_sync(0xffffffffu, vmax >= 0x7f80u);
+                if (odd) [[unlikely]] {  // 0 in the product, and NaN for the queries that see them
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        for (int i = 0; i < 16; ++i) {
+                            const uint32_t x = lds4(chunk + u * TB + 17 * HD + g * (HD / 8) / 32 * 32 + (i & ~1) * 2) >> (16 * (i & 1));
+                            if ((x & 0x7f80u) != 0x7f80u || !(ok >> u & 1u)) continue;
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e)
+                                    if (base + 16 * u + i <= lim[nt][e]) poison[nt][e] = __uint_as_float(0x7fffffffu);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            if ((sc[u][r] & 0x7f80u) == 0x7f80u) sc[u][r] &= 0xffff0000u;
+                            if ((sc[u][r] & 0x7f800000u) == 0x7f800000u) sc[u][r] &= 0x0000ffffu;
+                        }
                     }
-                    sum[nt][e] *= alpha;
-                    if (!ROW || lim[nt][e] == only) alpha *= shrink;
-#pragma unroll
-                    for (int i = 0; i < CT; ++i) o[nt][i][e] *= alpha, o[nt][i][e + 2] *= alpha;
+                    __syncwarp();
+                    vmax = largest(sc);
                 }
-        }
+                const int vnew = (int)(vmax >> 7) > vexp ? (int)(vmax >> 7) + kKv4Headroom : vexp;
+                if (!ROW && low < top && base + kKv4Chunk - 1 > low) {
+                    // Rows differ in what they see of this chunk.  A unit taken up by tokens that the first does not see changes
+                    // nothing for it, being a power of two, while all products stay normal f16 numbers (scales down to 2^-22 of
+                    // the largest) and what is in O stays normal (bits below 2^-149 of the unit are not looked after).
+                    uint32_t seen[2][2], least = 0xffffffffu;  // scales of what the first row sees; the smallest but 0, less 1
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                // 2^7 p; nothing seen so far: every score is -inf
-                const float off = mx[nt][e] == -INFINITY ? 0.f : fmaf(-mx[nt][e], fb, kKv4WeightBits);
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    s[nt][u][e] = exp2_fast(fmaf(s[nt][u][e], fb, off));
-                    s[nt][u][e + 2] = exp2_fast(fmaf(s[nt][u][e + 2], fb, off));
-                    sum[nt][e] += s[nt][u][e] + s[nt][u][e + 2];
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t x = sc[i / 2][i % 2];
+                        const int p = base + 16 * (i / 2) + 8 * (i % 2) + 2 * t;
+                        seen[i / 2][i % 2] = p < low ? x : p == low ? x & 0xffffu : 0u;
+                        least = __vminu2(least, __vsub2(x, 0x00010001u));
+                    }
+                    const bool raised = (int)(vmax >> 7) > max(vexp, (int)(largest(seen) >> 7));
+                    const int by = vnew - (int)(min(least & 0xffffu, least >> 16) >> 7);
+                    if (__any_sync(0xffffffffu, raised && (by > 22 || (base > base0 && vnew - vexp > 22)))) return true;
                 }
-            }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            constexpr int CW = HD / 64;  // code words of a lane's piece: channels (HD / 8) g ..
-            uint32_t p[NT][2], s16[2], s72[2], w[2][2][CW];  // w: [tokens 2 t, 2 t + 1 | 8 more][token][word]
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) p[nt][r] = movmatrix_trans(pack_f16(s[nt][u][2 * r], s[nt][u][2 * r + 1]));
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const uint32_t vs = pack_f16(bf16lo(sc[u][r]) * vscale, bf16hi(sc[u][r]) * vscale);
-                s16[r] = mul_f16x2(vs, 0x2c002c00u), s72[r] = mul_f16x2(vs, 0xd480d480u);  // 1 / 16, -72
-                const uint32_t vc = chunk + u * TB + 9 * HD + r * (4 * HD) + lane * (HD / 8);
-                if (HD == 128) {
-                    const uint4 x = lds16(vc);
-                    w[r][0][0] = x.x, w[r][0][CW - 1] = x.y, w[r][1][0] = x.z, w[r][1][CW - 1] = x.w;
-                } else {
-                    const uint2 x = lds8(vc);
-                    w[r][0][0] = x.x, w[r][1][0] = x.y;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < CT; ++i) {  // channels (HD / 8) g + 2 i and + 1: nibbles 2 i, 2 i + 1 of the piece
-                uint32_t a[4];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const uint32_t two = __byte_perm(w[r][0][i / 4], w[r][1][i / 4], i % 4 < 2 ? 0x5410 : 0x7632);
-                    a[2 * r] = q4_scaled_f16x2(two, 2 * (i % 2), s16[r], s72[r]);
-                    a[2 * r + 1] = q4_scaled_f16x2(two, 2 * (i % 2) + 1, s16[r], s72[r]);
-                }
+                const float shrink = exp2_int(vexp - vnew);
+                vexp = vnew;
+                vscale = exp2_int(135 - vexp);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
-                    mma_f16_16816(o[nt][i], a[0], a[1], a[2], a[3], p[nt][0], p[nt][1], o[nt][i][0], o[nt][i][1], o[nt][i][2],
-                                  o[nt][i][3]);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float alpha = 1.f;
+                        if (top_m[nt][e] * fb > fmaf(mx[nt][e], fb, 8.f)) {
+                            alpha = exp2_fast((mx[nt][e] - top_m[nt][e]) * fb);
+                            mx[nt][e] = top_m[nt][e];
+                        }
+                        sum[nt][e] *= alpha;
+                        if (!ROW || lim[nt][e] == only) alpha *= shrink;
+#pragma unroll
+                        for (int i = 0; i < CT; ++i) o[nt][i][e] *= alpha, o[nt][i][e + 2] *= alpha;
+                    }
             }
-        }
-        if (odd) [[unlikely]] {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < CT; ++i)
+                for (int e = 0; e < 2; ++e) {
+                    // 2^7 p; nothing seen so far: every score is -inf
+                    const float off = mx[nt][e] == -INFINITY ? 0.f : fmaf(-mx[nt][e], fb, kKv4WeightBits);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[nt][i][e] += poison[nt][e & 1];
-        }
-        return false;
-    };
-    int stage = 0;
-    bool apart = false;
-    for (; base <= top; base += step) {
-        fetch();
-        cp_async_wait<D - 1>();
-        __syncwarp();
-        ok = ok_bits & 3u;
-        ok_bits >>= 2;
-        --in_count;
-        chunk = ring + stage * 2 * TB;
-        if (++stage == D) stage = 0;
-        if ((apart = work(std::false_type(), -1))) break;
-        __syncwarp();  // every lane has read the chunk before the ring comes round to it
-    }
-    // where O's units go: of the 32 / NJ lanes of a channel group the first four have two queries of each 8 each
-    float* units = sUnit + (warp * NJ + lane / (32 / NJ)) * NT * 8 + 2 * t;
-    auto unit = [&]() { return exp2_int(vexp - 135 - kKv4WeightBits); };  // no less than 2^-125
-    if (apart) {
-        const int before = vexp;
-        for (int only = low; only <= top; ++only) {
-            work(std::true_type(), only);
+                    for (int u = 0; u < 2; ++u) {
+                        s[nt][u][e] = exp2_fast(fmaf(s[nt][u][e], fb, off));
+                        s[nt][u][e + 2] = exp2_fast(fmaf(s[nt][u][e + 2], fb, off));
+                        sum[nt][e] += s[nt][u][e] + s[nt][u][e + 2];
+                    }
+                }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int u = 0; u < 2; ++u) {
+                constexpr int CW = HD / 64;  // code words of a lane's piece: channels (HD / 8) g ..
+                uint32_t p[NT][2], s16[2], s72[2], w[2][2][CW];  // w: [tokens 2 t, 2 t + 1 | 8 more][token][word]
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (lim[nt][e] == only && lane % (32 / NJ) < 4) units[nt * 8 + e] = unit();
-            vexp = before, vscale = exp2_int(135 - vexp);
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) p[nt][r] = movmatrix_trans(pack_f16(s[nt][u][2 * r], s[nt][u][2 * r + 1]));
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint32_t vs = pack_f16(bf16lo(sc[u][r]) * vscale, bf16hi(sc[u][r]) * vscale);
+                    s16[r] = mul_f16x2(vs, 0x2c002c00u), s72[r] = mul_f16x2(vs, 0xd480d480u);  // 1 / 16, -72
+                    const uint32_t vc = chunk + u * TB + 9 * HD + r * (4 * HD) + lane * (HD / 8);
+                    if (HD == 128) {
+                        const uint4 x = lds16(vc);
+                        w[r][0][0] = x.x, w[r][0][CW - 1] = x.y, w[r][1][0] = x.z, w[r][1][CW - 1] = x.w;
+                    } else {
+                        const uint2 x = lds8(vc);
+                        w[r][0][0] = x.x, w[r][1][0] = x.y;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < CT; ++i) {  // channels (HD / 8) g + 2 i and + 1: nibbles 2 i, 2 i + 1 of the piece
+                    uint32_t a[4];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const uint32_t two = __byte_perm(w[r][0][i / 4], w[r][1][i / 4], i % 4 < 2 ? 0x5410 : 0x7632);
+                        a[2 * r] = q4_scaled_f16x2(two, 2 * (i % 2), s16[r], s72[r]);
+                        a[2 * r + 1] = q4_scaled_f16x2(two, 2 * (i % 2) + 1, s16[r], s72[r]);
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        mma_f16_16816(o[nt][i], a[0], a[1], a[2], a[3], p[nt][0], p[nt][1], o[nt][i][0], o[nt][i][1], o[nt][i][2],
+                                      o[nt][i][3]);
+                }
+            }
+            if (odd) [[unlikely]] {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < CT; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[nt][i][e] += poison[nt][e & 1];
+            }
+            return false;
+        };
+        int stage = 0;
+        bool apart = false;
+        for (; base <= top; base += step) {
+            fetch();
+            cp_async_wait<D - 1>();
             __syncwarp();
+            ok = ok_bits & 3u;
+            ok_bits >>= 2;
+            --in_count;
+            chunk = ring + stage * 2 * TB;
+            if (++stage == D) stage = 0;
+            if ((apart = work(std::false_type(), -1))) break;
+            __syncwarp();  // every lane has read the chunk before the ring comes round to it
         }
-    } else if (lane % (32 / NJ) < 4) {
+        // where O's units go: of the 32 / NJ lanes of a channel group the first four have two queries of each 8 each
+        float* units = sUnit + (warp * NJ + lane / (32 / NJ)) * NT * 8 + 2 * t;
+        auto unit = [&]() { return exp2_int(vexp - 135 - kKv4WeightBits); };  // no less than 2^-125
+        if (apart) {
+            const int before = vexp;
+            for (int only = low; only <= top; ++only) {
+                work(std::true_type(), only);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<float2*>(units + nt * 8) = make_float2(unit(), unit());
-    }
-
-    // The next operation may come in from here on: earlier, its CTAs would take the free SMs two at a time (a layer of 4096
-    // channels over 16000 positions: 68 us, 66.5).
-    pdl_launch_dependents();
-    // ---- the warps' results, each where its ring was
-    cp_async_wait<0>();
-    __syncwarp();
-    float4* mineO = reinterpret_cast<float4*>(kv4_smem + warp * SM::kWarpRing);
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int i = 0; i < CT; ++i)
-            mineO[(nt * CT + i) * 32 + lane] = make_float4(o[nt][i][0], o[nt][i][1], o[nt][i][2], o[nt][i][3]);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 4);
-            sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 8);
-            sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 16);
-            if (g == 0) sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e] * exp2_int(-kKv4WeightBits));
-        }
-    }
-    __syncwarp();  // the cluster's barriers want whole warps
-    if (S > 1) cluster_wait();  // the others are there
-    __syncthreads();
-    // ---- the CTA's, sent to the CTA that finishes them: piece x holds two queries x two channels
-    const int share = fastdiv(SM::kItems + S - 1, S, div_S);  // pieces a CTA finishes; the last one may have fewer
-    for (int x = threadIdx.x; x < SM::kItems; x += W * 32) {
-        const int c = x / (CT * 32) * 8 + 2 * (x & 3);  // its first query
-        if (q0 + c >= Q) continue;
-        float m0 = -INFINITY, m1 = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < W; ++w) m0 = fmaxf(m0, sStat[w * NT * 8 + c].x), m1 = fmaxf(m1, sStat[w * NT * 8 + c + 1].x);
-        float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
-        float l0 = 0.f, l1 = 0.f;
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const float4 v = *reinterpret_cast<const float4*>(kv4_smem + w * SM::kWarpRing + x * 16);
-            const float2 s0 = sStat[w * NT * 8 + c], s1 = sStat[w * NT * 8 + c + 1];
-            const float f0 = m0 == -INFINITY ? 0.f : exp2_fast((s0.x - m0) * fb);
-            const float f1 = m1 == -INFINITY ? 0.f : exp2_fast((s1.x - m1) * fb);
-            const float2 unit = *reinterpret_cast<const float2*>(sUnit + (w * NJ + (x & 31) / (32 / NJ)) * NT * 8 + c);
-            l0 = fmaf(f0, s0.y, l0), l1 = fmaf(f1, s1.y, l1);
-            r.x = fmaf(f0 * unit.x, v.x, r.x), r.z = fmaf(f0 * unit.x, v.z, r.z);
-            r.y = fmaf(f1 * unit.y, v.y, r.y), r.w = fmaf(f1 * unit.y, v.w, r.w);
-        }
-        int to = 0;  // x / share
-        for (int edge = share; edge <= x; edge += share) ++to;
-        st_cluster_f4(map_cluster(smem_u32(sIn) + (rank * share + x - to * share) * 16, to), r);
-        if ((x / 4) % (CT * 8) == 0)  // one of the pieces with these queries: their statistics, to all
-            for (int d = 0; d < S; ++d) {
-                const uint32_t a = map_cluster(smem_u32(sInStat) + (rank * NT * 8 + c) * 8, d);
-                st_cluster_f2(a, m0, l0);
-                st_cluster_f2(a + 8, m1, l1);
+                    for (int e = 0; e < 2; ++e)
+                        if (lim[nt][e] == only && lane % (32 / NJ) < 4) units[nt * 8 + e] = unit();
+                vexp = before, vscale = exp2_int(135 - vexp);
+                __syncwarp();
             }
-    }
-    __syncwarp();
-    if (S > 1)
-        cluster_sync_all();  // after it nobody touches another CTA's memory
-    else
-        __syncthreads();
-    for (int y = threadIdx.x; y < 2 * share; y += W * 32) {  // one query and two channels a thread
-        const int x = rank * share + y / 2, e = y & 1, l = x & 31, c = x / (CT * 32) * 8 + 2 * (l & 3) + e, qi = q0 + c;
-        if (x >= SM::kItems || qi >= Q) continue;
-        float m = -INFINITY, sum_l = 0.f, v0 = 0.f, v1 = 0.f;
-        for (int r = 0; r < S; ++r) m = fmaxf(m, sInStat[r * NT * 8 + c].x);
-#pragma unroll 4
-        for (int r = 0; r < S; ++r) {
-            const float2 st = sInStat[r * NT * 8 + c];
-            const float f = m == -INFINITY ? 0.f : exp2_fast((st.x - m) * fb);
-            const float* v = reinterpret_cast<const float*>(sIn + r * share + y / 2);
-            sum_l = fmaf(f, st.y, sum_l), v0 = fmaf(f, v[e], v0), v1 = fmaf(f, v[e + 2], v1);
-        }
-        const int row = fastdiv(qi, G, div_G), ch = (l >> 2) * (HD / 8) + 2 * (x / 32 % CT);
-        if (splits > 1) {  // to be finished by combine_kv4_kernel
-            float* to = scratch + (kv4_partial(b, gridDim.y, blockIdx.y, splits, split) * (NT * 8) + c) * (HD + 2);
-            *reinterpret_cast<float2*>(to + ch) = make_float2(v0, v1);
-            if (ch == 0) *reinterpret_cast<float2*>(to + HD) = make_float2(m, sum_l);
-            continue;
-        }
-        const bool none = (long long)pos0 + row < 0 || (long long)pos0 + row >= cache.max_seq;
-        const float inv = 1.f / sum_l;
-        const uint32_t v = none ? 0u : pack_bf16(v0 * inv, v1 * inv);
-        *reinterpret_cast<uint32_t*>(out + (((long long)b * M + row) * Hq + head * G + qi - row * G) * HD + ch) = v;
-    }
-    if (NT == 1) break;
-    const int ahead = fastdiv(gridDim.x, S, div_S);
-    if ((split += ahead) >= splits) break;
-    __syncwarp();
-    if (S > 1) cluster_arrive();  // what the others sent here has been read
-    in_base = base0 += ahead * S * W * kKv4Chunk, in_stage = in_count = 0, ok_bits = 0;
-    look_up(base0);
+        } else if (lane % (32 / NJ) < 4) {
 #pragma unroll
-    for (int i = 0; i < D - 1; ++i) fetch();
+            for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<float2*>(units + nt * 8) = make_float2(unit(), unit());
+        }
+
+        // The next operation may come in from here on: earlier, its CTAs would take the free SMs two at a time (a layer of 4096
+        // channels over 16000 positions: 68 us, 66.5).
+        pdl_launch_dependents();
+        // ---- the warps' results, each where its ring was
+        cp_async_wait<0>();
+        __syncwarp();
+        float4* mineO = reinterpret_cast<float4*>(kv4_smem + warp * SM::kWarpRing);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int i = 0; i < CT; ++i)
+                mineO[(nt * CT + i) * 32 + lane] = make_float4(o[nt][i][0], o[nt][i][1], o[nt][i][2], o[nt][i][3]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 4);
+                sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 8);
+                sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 16);
+                if (g == 0) sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e] * exp2_int(-kKv4WeightBits));
+            }
+        }
+        __syncwarp();  // the cluster's barriers want whole warps
+        if (S > 1) cluster_wait();  // the others are there
+        __syncthreads();
+        // ---- the CTA's, sent to the CTA that finishes them: piece x holds two queries x two channels
+        const int share = fastdiv(SM::kItems + S - 1, S, div_S);  // pieces a CTA finishes; the last one may have fewer
+        for (int x = threadIdx.x; x < SM::kItems; x += W * 32) {
+            const int c = x / (CT * 32) * 8 + 2 * (x & 3);  // its first query
+            if (q0 + c >= Q) continue;
+            float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < W; ++w) m0 = fmaxf(m0, sStat[w * NT * 8 + c].x), m1 = fmaxf(m1, sStat[w * NT * 8 + c + 1].x);
+            float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+            float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float4 v = *reinterpret_cast<const float4*>(kv4_smem + w * SM::kWarpRing + x * 16);
+                const float2 s0 = sStat[w * NT * 8 + c], s1 = sStat[w * NT * 8 + c + 1];
+                const float f0 = m0 == -INFINITY ? 0.f : exp2_fast((s0.x - m0) * fb);
+                const float f1 = m1 == -INFINITY ? 0.f : exp2_fast((s1.x - m1) * fb);
+                const float2 unit = *reinterpret_cast<const float2*>(sUnit + (w * NJ + (x & 31) / (32 / NJ)) * NT * 8 + c);
+                l0 = fmaf(f0, s0.y, l0), l1 = fmaf(f1, s1.y, l1);
+                r.x = fmaf(f0 * unit.x, v.x, r.x), r.z = fmaf(f0 * unit.x, v.z, r.z);
+                r.y = fmaf(f1 * unit.y, v.y, r.y), r.w = fmaf(f1 * unit.y, v.w, r.w);
+            }
+            int to = 0;  // x / share
+            for (int edge = share; edge <= x; edge += share) ++to;
+            st_cluster_f4(map_cluster(smem_u32(sIn) + (rank * share + x - to * share) * 16, to), r);
+            if ((x / 4) % (CT * 8) == 0)  // one of the pieces with these queries: their statistics, to all
+                for (int d = 0; d < S; ++d) {
+                    const uint32_t a = map_cluster(smem_u32(sInStat) + (rank * NT * 8 + c) * 8, d);
+                    st_cluster_f2(a, m0, l0);
+                    st_cluster_f2(a + 8, m1, l1);
+                }
+        }
+        __syncwarp();
+        if (S > 1)
+            cluster_sync_all();  // after it nobody touches another CTA's memory
+        else
+            __syncthreads();
+        for (int y = threadIdx.x; y < 2 * share; y += W * 32) {  // one query and two channels a thread
+            const int x = rank * share + y / 2, e = y & 1, l = x & 31, c = x / (CT * 32) * 8 + 2 * (l & 3) + e, qi = q0 + c;
+            if (x >= SM::kItems || qi >= Q) continue;
+            float m = -INFINITY, sum_l = 0.f, v0 = 0.f, v1 = 0.f;
+            for (int r = 0; r < S; ++r) m = fmaxf(m, sInStat[r * NT * 8 + c].x);
+#pragma unroll 4
+            for (int r = 0; r < S; ++r) {
+                const float2 st = sInStat[r * NT * 8 + c];
+                const float f = m == -INFINITY ? 0.f : exp2_fast((st.x - m) * fb);
+                const float* v = reinterpret_cast<const float*>(sIn + r * share + y / 2);
+                sum_l = fmaf(f, st.y, sum_l), v0 = fmaf(f, v[e], v0), v1 = fmaf(f, v[e + 2], v1);
+            }
+            const int row = fastdiv(qi, G, div_G), ch = (l >> 2) * (HD / 8) + 2 * (x / 32 % CT);
+            if (splits > 1) {  // to be finished by combine_kv4_kernel
+                float* to = scratch + (kv4_partial(b, gridDim.y, blockIdx.y, splits, split) * (NT * 8) + c) * (HD + 2);
+                *reinterpret_cast<float2*>(to + ch) = make_float2(v0, v1);
+                if (ch == 0) *reinterpret_cast<float2*>(to + HD) = make_float2(m, sum_l);
+                continue;
+            }
+            const bool none = (long long)pos0 + row < 0 || (long long)pos0 + row >= cache.max_seq;
+            const float inv = 1.f / sum_l;
+            const uint32_t v = none ? 0u : pack_bf16(v0 * inv, v1 * inv);
+            *reinterpret_cast<uint32_t*>(out + (((long long)b * M + row) * Hq + head * G + qi - row * G) * HD + ch) = v;
+        }
+        if (NT == 1) break;
+        const int ahead = fastdiv(gridDim.x, S, div_S);
+        if ((split += ahead) >= splits) break;
+        __syncwarp();
+        if (S > 1) cluster_arrive();  // what the others sent here has been read
+        in_base = base0 += ahead * S * W * kKv4Chunk, in_stage = in_count = 0, ok_bits = 0;
+        look_up(base0);
+#pragma unroll
+        for (int i = 0; i < D - 1; ++i) fetch();
     }
 }
 
