@@ -358,7 +358,8 @@ int ls_op_prefill_attention(const void *q_bf16_dev, int32_t R, int32_t pos0, int
  * Number format.  A group of values shares a scale s, the group's largest |x| divided by 7 and
  * rounded UP to 5 significant bits, kept as bf16; a value stands for c * s with an integer
  * c = rint(x / s) in -7..7 (ties to even), stored as the nibble c + 8.  c * s is exactly a bf16
- * number, so expanding loses nothing.  A group with a NaN or an infinity stands for NaN.  Values up to
+ * number, so expanding loses nothing.  s is 0 (and c) if all x are, else at least 2^-126 and at most
+ * 1.125 * 2^125.  A group with a NaN or an infinity stands for NaN (s = 0x7fff, c = 0).  Values up to
  * 2^127 are represented; operations compute as if in fp32 and overflow as it does (attention: queries times
  * k scales beyond 2^100).
  * Groups are 32 consecutive channels of a head (cache) or 32, 64 or 128 consecutive columns (weights).

@@ -2047,6 +2047,9 @@ namespace {
 //   what 148 is not a multiple of (1 / 20 queries: 64 heads, 16000 positions 42.5 / 68.4 with clusters of 2, 35.7 / 66.5
 //   with 4; 96 heads 77 / 126 with 1, 48 / 88 with 3; 128 heads 77 / 126 with 1, 66 / 121 with 2; but 128 heads, 1000
 //   positions 9.7 / 17.6 and 10.9 / 23.4).
+// The figures of a comparison are of one run of one kernel; today's takes 1 to 3 % more for up to 8 queries, and less for
+// more than 24 (131072 positions, 8 heads, 1 / 20 / 64 queries: 42.4 / 78 / 196).  The numbers of SMs and clusters are a B200's:
+// they enter a row's arithmetic, and on another part they give a poor plan, not a wrong result.
 struct Kv4Plan {
     int S, splits;
 };

@@ -18,10 +18,11 @@
 // * p is rounded to f16's 11 bits (2^-12 of it), well below the rounding of a bf16 result.  2^7 p stands in f16: p is at most
 //   2^8 and the largest so far 1 or more, so that weights keep those bits down to 2^-21 and are off by 2^-32 below, which
 //   thousands of positions beside one that outweighs them by 2^25 need.  Scores, maxima, sums and O are fp32.
-// Some 320 instructions go into a tile of 16 tokens of one KV head (2304 bytes) and up to 8 queries, 85 more for each
-// further 8; two CTAs of 8 warps an SM issue 2.4 of them a cycle.  131072 tokens, 8 KV heads: 41.7 us (0.55 of the
-// measured copy rate; first form 130); 1030 tokens, 32 heads: 7.0 us, of which the launch is 1.4, the first loads and
-// the queries 2, a chunk 1.4, joining the warps and CTAs 2.
+// Some 360 instructions go into a tile of 16 tokens of one KV head (2304 bytes) and up to 8 queries, all else included, 85
+// more for each further 8; two CTAs of 8 warps an SM issue 2.4 of them a cycle.  131072 tokens, 8 KV heads: 42.4 us (0.54 of
+// the measured copy rate; first form 130); 1030 tokens, 32 heads: 6.9 us, of which the launch is 1.4, the first loads and
+// the queries 2, a chunk 1.4, joining the warps and CTAs 2.  With 25 to 32 queries of head size 128 a thread has 255 registers and
+// spills 23 more (64 queries over 131072 tokens: 196 us).
 #pragma once
 #include "ls_attention.cuh"
 #include "ls_w4.cuh"

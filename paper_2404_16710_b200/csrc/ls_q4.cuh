@@ -88,6 +88,8 @@ __device__ __forceinline__ uint32_t q4_word8(const uint4& v, float s, float r)
 __device__ __forceinline__ uint32_t q4_word(const uint4& v, float s, float r) { return q4_word8<true>(v, s, r); }         // a row's
 __device__ __forceinline__ uint32_t q4_word_plain(const uint4& v, float s, float r) { return q4_word8<false>(v, s, r); }  // lowest first (V)
 
+// Floats are made of nibbles by or-ing them into the mantissa of a power of two and subtracting it, a published method
+// (for 4-bit weights e.g. Kim et al. 2022, arXiv 2211.10017); the constants follow from the formats.
 // codes i and i + 4 of a word as two bf16 numbers c (exact): 0x4300 | u is 128 + u
 __device__ __forceinline__ uint32_t q4_bf16x2(uint32_t w, int i)
 {
@@ -154,9 +156,9 @@ __device__ __forceinline__ T ld_once(const void* p)
 }
 
 // ------------------------------------------------------------------ weights: bf16 -> blocks, blocks -> bf16
-// Both are bound by memory: 11008 x 4096, packed and expanded again: 37.5 us in two launches (0.83 of the measured copy
-// rate), 4096 x 4096: 17.6 (0.66).  A code costs about 5 instructions; with a division, floor and comparison each (16,
-// two of them on the quarter-rate conversion pipe) the latter took 25.7 us.
+// Both are bound by memory: 11008 x 4096, packed and expanded again: 39 us (0.80 of the measured copy rate), 4096 x 4096: 19.4
+// (0.60), in four launches: fence_kernel follows either and takes 0.8 us.  A code costs about 5 instructions; with a
+// division, floor and comparison each (16, two of them on the quarter-rate conversion pipe) the latter took 8 us more.
 // One warp per block of 16 rows x 128 columns: lane 4 g + t holds rows g and g + 8, columns 32 j + 8 t .. + 7.
 // NG groups of 128 / NG columns per block.  grid.x * warps covers the blocks of all rows, row blocks slowest.
 template <int NG>

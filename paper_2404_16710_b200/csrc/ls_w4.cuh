@@ -101,14 +101,16 @@ __device__ __forceinline__ void w4_block_mma(const W4Regs<NG>& w, const uint4 (&
 // One CTA per SM; its W warps form teams of 2^lks, and a team takes every (teams of the grid)-th group of TG tiles of
 // 16 rows (TG = 2 halves what is read of h in shared memory, which bounds the kernel for 16 rows of h).  Of a tile's
 // blocks each warp of the team has a fixed share, consecutive along K, and keeps the next blocks of its sequence (which
-// runs on across tiles) in flight in a ring of its own, of D blocks; the team meets once per tile, to add its sums up.  HS: h is copied to shared memory once (columns beyond K as
-// zeros); otherwise, for h larger than that, it comes through L1.
+// runs on across tiles) in flight in a ring of its own, of D blocks; the team meets once per tile, to add its sums up.  HS: h
+// is copied to shared memory once (columns beyond K as zeros); otherwise, for h larger than that, it comes through L1.
 // The codes are the A operand of mma.sync, the rows of h the B operand; a group's products are summed in fp32 by
 // the tensor cores and multiplied by the group's scale (a lane holds rows g and g + 8 of a tile) when they join
 // the running sum.  Turning codes into operands bounds the kernel: 11 instructions for 8 codes, 7 of them on the
 // half-rate integer pipe, which is 50 % busy on average and collides with the products of the other warps.  With the
 // conversion left out the loads alone take 43 us for 128256 x 4096 (the copy rate), 4.0 us for 4096 x 4096; with it, one
-// row of h: 55.8 us (0.77 of the measured copy rate) and 5.1 us (0.26: 2 us are the launch).  Tried and not kept: bulk
+// row of h: 56 us (0.77 of the measured copy rate) and 5.5 us (0.24: 2 us are the launch).  What HS = false costs, groups of
+// 64: 4096 x 11008, 7 rows 10.0 us, 8 rows (h no longer fits) 11.1, 9 12.7, 16 13.2; 8192 x 8192, 9 rows 14.4, 10 (no longer)
+// 17.0, 16 17.6; 4096 x 14336, 5 rows 11.0, 6 12.7.  Tried and not kept: bulk
 // copies with h from L1 (143 us, too few warps), blocks held in registers (94 to 104 us: the loads of several blocks end
 // up waiting for one another), f16 operands (3 to 5 % faster for one row, slower for 16: h has to be converted), h as two
 // e4m3 pieces (3 instructions for 8 codes, a nibble's byte being an e4m3 number; 79 us, mma.sync being slow on them).
