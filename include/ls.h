@@ -361,7 +361,8 @@ int ls_op_prefill_attention(const void *q_bf16_dev, int32_t R, int32_t pos0, int
  * number, so expanding loses nothing.  s is 0 (and c) if all x are, else at least 2^-126 and at most
  * 1.125 * 2^125.  A group with a NaN or an infinity stands for NaN (s = 0x7fff, c = 0).  Values up to
  * 2^127 are represented; operations compute as if in fp32 and overflow as it does (attention: queries times
- * k scales beyond 2^100).
+ * k scales beyond 2^100; sums of |v| over the positions beyond 2^120, as they are divided by the sum of the weights
+ * at the end).
  * Groups are 32 consecutive channels of a head (cache) or 32, 64 or 128 consecutive columns (weights).
  *
  * Packed weights of a matrix [N, K] (K a multiple of 8, at most 2^28): blocks of 16 rows x 128 columns, the

@@ -175,7 +175,8 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
     look_up(base0);
     const int pos0 = ld_now(pos0_dev + b);
 
-    // last position that this lane's two queries of each 8 see, and over the CTA's queries that see any the last and the first of those
+    // last position that this lane's two queries of each 8 see, and over the CTA's queries that see any the last and the
+    // first of those
     int lim[NT][2], top = -1, low = 0x7fffffff;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -273,8 +274,8 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = -INFINITY;
         float top_m[NT][2];
-        // O is kept in units of 2^(vexp - 135), and 2^7 of it for the weights'; vexp: no less than the exponent field of any V scale so far of this lane's
-        // channel group, at least 17
+        // O is kept in units of 2^(vexp - 135), and of 2^-7 for the weights; vexp: no less than the exponent field of any V
+        // scale so far of this lane's channel group, at least 17
         int vexp = 17;
         float vscale = exp2_int(135 - vexp);  // scales become less than 2^9, the largest [2^7, 2^8) when it raises vexp
 
@@ -388,7 +389,7 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
             bool odd = false;
             float poison[NT][2] = {};
             if (__any_sync(0xffffffffu, grown)) {
-                auto largest = [](const uint32_t (&v)[2][2]) {  // scale of this lane's channel group, which 32 / NJ neighbouring lanes share
+                auto largest = [](const uint32_t (&v)[2][2]) {  // scale of this lane's channel group: 32 / NJ lanes side by side
                     uint32_t x = __vmaxu2(__vmaxu2(v[0][0], v[0][1]), __vmaxu2(v[1][0], v[1][1]));
 #pragma unroll
                     for (int d = 1; d < 32 / NJ; d *= 2) x = __vmaxu2(x, __shfl_xor_sync(0xffffffffu, x, d));
@@ -562,7 +563,8 @@ attention_kv4_kernel(const uint16_t* __restrict__ q, int M, int G, const int32_t
                 sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 4);
                 sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 8);
                 sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], 16);
-                if (g == 0) sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e] * exp2_int(-kKv4WeightBits));
+                if (g == 0)
+                    sStat[warp * NT * 8 + nt * 8 + 2 * t + e] = make_float2(mx[nt][e], sum[nt][e] * exp2_int(-kKv4WeightBits));
             }
         }
         __syncwarp();  // the cluster's barriers want whole warps
