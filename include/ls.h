@@ -448,6 +448,56 @@ int ls_op_attention_kv4(const void *q_bf16_dev, int32_t n_seq, int32_t M, const 
                         int32_t table_stride, int32_t max_seq, const void *pages_dev, int32_t n_pages,
                         void *out_bf16_dev, void *scratch_dev, int32_t *status_dev, void *cuda_stream);
 
+/* ------------------------------------------------------------------------------
+ * 8-bit values with a scale for each block of 128: a layer's path in 8 bits, for any number of rows
+ * (one token to the prompt pass, whose projections the tensor cores do at twice the rate in 8 bits).
+ *
+ * Number format.  A block of values shares a scale s = 2^(e - 127), kept as the byte e; a value
+ * stands for c * s with an e4m3 code c (sign, 4 exponent bits, 3 mantissa bits; at most 448, no
+ * infinities).  A block is 128 columns of one row (block_rows = 1: activations) or 128 rows x 128
+ * columns (block_rows = 128: weights).  s is the smallest power of two with max |x| <= 448 s, held
+ * in 2^-117 .. 2^119, and c is x / s rounded to the nearest code, ties to the even one, at most 448 in
+ * size.  c * s is exactly a bf16 number.  A block with a NaN or an infinity stands for NaN (e = 255, c = 0).
+ * Codes are [rows][K] bytes, K a multiple of 16, 16-byte aligned.  Scale bytes are
+ * [ceil(rows / block_rows)][4 ceil(K / 512)], 4-byte aligned: the bytes of a row's ceil(K / 128)
+ * blocks, then zeros (ignored where they are read) up to whole 32-bit words.  Rows, M and N, are at most
+ * LS_F8_MAX_ROWS, K at most 2^28.
+ * Other tensors are LS_BF16 or LS_F32, their rows ld elements apart, 16-byte aligned (ld a multiple of
+ * 8 or 4; ignored for a single row).
+ * The first call of each kernel configuration (type, class of M and K) loads the kernel and sets
+ * its attributes: make it outside any stream capture.
+ * ------------------------------------------------------------------------------ */
+enum { LS_BF16 = 0, LS_F32 = 1 };
+#define LS_F8_MAX_ROWS (1 << 22)
+
+/* Bytes of the scales of [M, K]; 0 for a shape the format does not cover. */
+size_t ls_op_f8_scale_bytes(int32_t M, int32_t K, int32_t block_rows);
+/* x [M, K] -> codes and scales, and back to bf16 [M, K] (contiguous).  With block_rows = 128 (weights, or what
+ * bf16 operations may read as such) an empty launch follows either, as with ls_op_quantize_w4. */
+int ls_op_quantize_f8(const void *x_dev, int32_t type, int64_t ldx, int32_t M, int32_t K, int32_t block_rows,
+                      void *codes_dev, void *scales_dev, void *cuda_stream);
+int ls_op_expand_f8(const void *codes_dev, const void *scales_dev, int32_t M, int32_t K, int32_t block_rows,
+                    void *out_bf16_dev, void *cuda_stream);
+/* RMSNorm with the residual's addition: x' = x + delta, rounded to x's type and written to x_out (of x's type;
+ * may be x or delta itself, or NULL: not kept); codes and scales (block_rows = 1) of
+ * x'[m,i] / sqrt(mean_j x'[m,j]^2 + eps) * gain[i], gain bf16 [D].  delta may be NULL.  Sums in fp32. */
+int ls_op_rmsnorm_f8(const void *x_dev, int32_t x_type, int64_t ldx, const void *delta_dev, int32_t delta_type,
+                     int64_t ldd, void *x_out_dev, int64_t ldo, const void *gain_dev, int32_t M, int32_t D, float eps,
+                     void *codes_dev, void *scales_dev, void *cuda_stream);
+/* SwiGLU: codes and scales (block_rows = 1) of silu(gate[m,f]) * up[m,f]; gate and up of one type and row
+ * stride (two halves of one product's rows, or two tensors). */
+int ls_op_swiglu_f8(const void *gate_dev, const void *up_dev, int32_t type, int64_t ld, int32_t M, int32_t F,
+                    void *codes_dev, void *scales_dev, void *cuda_stream);
+/* out[m,n] = (add[m,n] +) sum_k h[m,k] w[n,k]: w [N, K] with block_rows = 128, h [M, K] with
+ * block_rows = 1; out and add (may be NULL; may be out itself) of one type, any alignment that the type has
+ * and any row strides.  fp32 accumulation, rounded once at the end.  A NaN block makes its
+ * rows NaN.  Up to LS_MAX_ROWS rows a row's result does not depend on how many rows
+ * share the call.  status_dev (device int32, may be NULL) receives 3 if one of the kernel's bounded waits ran out.
+ * Under ls_op_chain the weights are read ahead of the wait for the operation before. */
+int ls_op_linear_f8(const void *w_codes_dev, const void *w_scales_dev, const void *h_codes_dev, const void *h_scales_dev,
+                    int32_t M, int32_t N, int32_t K, void *out_dev, int32_t out_type, int64_t ldo, const void *add_dev,
+                    int64_t lda, int32_t *status_dev, void *cuda_stream);
+
 /* match + crop of Appendix A.4 on device arrays: n = number of leading i < d with
  * draft[i] == verified[i]; appends draft[0..n-1], verified[n] to out_ids (truncated at
  * max_new, and after the first eos_id if eos_id >= 0).

@@ -31,7 +31,8 @@ EXPORTS = (
     "ls_op_lm_head_argmax_static", "ls_op_rope_append", "ls_op_qkv_rope_append", "ls_op_attention", "ls_op_accept",
     "ls_op_gemm", "ls_op_prefill_attention", "ls_op_chain", "ls_op_w4_bytes", "ls_op_quantize_w4", "ls_op_expand_w4",
     "ls_op_linear_w4", "ls_op_kv4_page_bytes", "ls_op_append_kv4", "ls_op_expand_kv4", "ls_op_attention_kv4",
-    "ls_op_attention_kv4_scratch_bytes",
+    "ls_op_attention_kv4_scratch_bytes", "ls_op_f8_scale_bytes", "ls_op_quantize_f8", "ls_op_expand_f8", "ls_op_rmsnorm_f8",
+    "ls_op_swiglu_f8", "ls_op_linear_f8",
 )
 
 
@@ -128,6 +129,12 @@ def lib():
             "ls_op_expand_kv4": (C.c_int, [vp, i32, i32, i32, vp, i32, i32, i32, vp, i32, i32, vp, vp, vp, i32, vp, vp]),
             "ls_op_attention_kv4": (C.c_int, [vp, i32, i32, vp, i32, i32, i32, i32, vp, i32, i32, vp, i32, vp, vp, vp, vp]),
             "ls_op_attention_kv4_scratch_bytes": (C.c_size_t, [i32, i32, i32, i32, i32, i32]),
+            "ls_op_f8_scale_bytes": (C.c_size_t, [i32, i32, i32]),
+            "ls_op_quantize_f8": (C.c_int, [vp, i32, i64, i32, i32, i32, vp, vp, vp]),
+            "ls_op_expand_f8": (C.c_int, [vp, vp, i32, i32, i32, vp, vp]),
+            "ls_op_rmsnorm_f8": (C.c_int, [vp, i32, i64, vp, i32, i64, vp, i64, vp, i32, i32, C.c_float, vp, vp, vp]),
+            "ls_op_swiglu_f8": (C.c_int, [vp, vp, i32, i64, i32, i32, vp, vp, vp]),
+            "ls_op_linear_f8": (C.c_int, [vp, vp, vp, vp, i32, i32, i32, vp, i32, i64, vp, i64, vp, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -155,6 +162,7 @@ class _Torch:
     def load(self):
         import torch
         self.bf16, self.f32, self.i32, self.u8, self.empty = torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.empty
+        self.f8 = torch.float8_e4m3fn
         # torch.cuda.current_stream() builds a Stream object (3.4 us a call, as much as a launch); the raw handle costs 0.2
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.stream = raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
@@ -560,6 +568,87 @@ def ls_op_attention_kv4(q, pos0, Hkv, hd, page_size, table, max_seq, pages, out,
                                   _arg(table, _torch.i32, dev, "page table"), entries, max_seq, _arg(pages, _torch.u8, dev, "pages"), n_pages,
                                   _arg(out, _torch.bf16, dev, "out"), None if scratch is None else _arg(scratch, _torch.u8, dev, "scratch"), _status(status, dev),
                                   _stream_on(dev)), "ls_op_attention_kv4")
+
+
+# ---- 8-bit values with a scale for each block of 128
+LS_BF16, LS_F32 = 0, 1
+LS_F8_MAX_ROWS = 1 << 22
+
+
+@functools.lru_cache(maxsize=4096)
+def ls_op_f8_scale_bytes(M, K, block_rows=1):
+    return lib().ls_op_f8_scale_bytes(M, K, block_rows)
+
+
+def _held(codes, scales, block_rows, dev, what):
+    """device pointers of codes float8_e4m3fn [M, K] and their scales (uint8, ls_op_f8_scale_bytes of them)"""
+    M, K = codes.shape
+    if scales.numel() < ls_op_f8_scale_bytes(M, K, block_rows):
+        raise LsError(LS_ERR_CAPACITY, f"{what}: scales")
+    return _arg(codes, _torch.f8, dev, what + " codes"), _arg(scales, _torch.u8, dev, what + " scales")
+
+
+def _strided(t, shape, dev, what):
+    """(device pointer, type, row stride) of a bf16 or fp32 tensor of some shape [M, K] with contiguous columns"""
+    kind = LS_BF16 if t.dtype is _torch.bf16 else LS_F32 if t.dtype is _torch.f32 else _bad(f"{what}: bf16 or fp32")
+    if t.shape != shape or t.get_device() != dev or (t.stride(1) != 1 and shape[1] > 1):
+        _bad(f"{what}: a tensor {tuple(shape)} with contiguous columns, on the CUDA device of the others")
+    return t.data_ptr(), kind, t.stride(0)
+
+
+def ls_op_quantize_f8(x, codes, scales, block_rows=1):
+    """x [M, K], bf16 or fp32 -> codes (float8_e4m3fn [M, K]) and scales (uint8), of one row's or 128 rows' blocks of 128 columns"""
+    (M, K), dev = codes.shape, codes.get_device()
+    c, s = _held(codes, scales, block_rows, dev, "ls_op_quantize_f8")
+    xp, kind, ld = _strided(x, codes.shape, dev, "x")
+    _ck(lib().ls_op_quantize_f8(xp, kind, ld, M, K, block_rows, c, s, _stream_on(dev)), "ls_op_quantize_f8")
+
+
+def ls_op_expand_f8(codes, scales, out, block_rows=1):
+    """codes and scales -> bf16 [M, K]"""
+    (M, K), dev = codes.shape, codes.get_device()
+    c, s = _held(codes, scales, block_rows, dev, "ls_op_expand_f8")
+    if out.shape != codes.shape:
+        _bad("ls_op_expand_f8: out")
+    _ck(lib().ls_op_expand_f8(c, s, M, K, block_rows, _arg(out, _torch.bf16, dev, "out"), _stream_on(dev)), "ls_op_expand_f8")
+
+
+def ls_op_rmsnorm_f8(x, gain, eps, codes, scales, delta=None, x_out=None):
+    """codes and scales of the RMSNorm of x + delta [M, D], which goes to x_out (may be x) if it is given"""
+    (M, D), dev = codes.shape, codes.get_device()
+    c, s = _held(codes, scales, 1, dev, "ls_op_rmsnorm_f8")
+    xp, kind, ldx = _strided(x, codes.shape, dev, "x")
+    dp, dkind, ldd = (None, LS_F32, 0) if delta is None else _strided(delta, codes.shape, dev, "delta")
+    op, okind, ldo = (None, kind, 0) if x_out is None else _strided(x_out, codes.shape, dev, "x_out")
+    if okind != kind or gain.numel() != D:
+        _bad("ls_op_rmsnorm_f8: x_out of x's type, gain [D]")
+    _ck(lib().ls_op_rmsnorm_f8(xp, kind, ldx, dp, dkind, ldd, op, ldo, _arg(gain, _torch.bf16, dev, "gain"), M, D, eps, c, s, _stream_on(dev)),
+        "ls_op_rmsnorm_f8")
+
+
+def ls_op_swiglu_f8(gate, up, codes, scales):
+    """codes and scales of silu(gate) * up [M, F]; gate and up of one type and row stride"""
+    (M, F), dev = codes.shape, codes.get_device()
+    c, s = _held(codes, scales, 1, dev, "ls_op_swiglu_f8")
+    (gp, kind, ld), (upp, ukind, uld) = _strided(gate, codes.shape, dev, "gate"), _strided(up, codes.shape, dev, "up")
+    if kind != ukind or (ld != uld and M > 1):
+        _bad("ls_op_swiglu_f8: gate and up of one type and row stride")
+    _ck(lib().ls_op_swiglu_f8(gp, upp, kind, ld, M, F, c, s, _stream_on(dev)), "ls_op_swiglu_f8")
+
+
+def ls_op_linear_f8(w_codes, w_scales, h_codes, h_scales, out, add=None, status=None):
+    """out[M, N] = (add +) h @ W.T of weights [N, K] in blocks of 128 x 128 and tokens [M, K] in blocks of 1 x 128; out bf16
+    or fp32, add of its type (may be out)"""
+    (N, K), (M, Kh), dev = w_codes.shape, h_codes.shape, h_codes.get_device()
+    if K != Kh:
+        _bad("ls_op_linear_f8: columns of w and h")
+    wc, ws = _held(w_codes, w_scales, 128, dev, "w")
+    hc, hs = _held(h_codes, h_scales, 1, dev, "h")
+    op, kind, ldo = _strided(out, (M, N), dev, "out")
+    ap, akind, lda = (None, kind, 0) if add is None else _strided(add, (M, N), dev, "add")
+    if akind != kind:
+        _bad("ls_op_linear_f8: add of out's type")
+    _ck(lib().ls_op_linear_f8(wc, ws, hc, hs, M, N, K, op, kind, ldo, ap, lda, _status(status, dev), _stream_on(dev)), "ls_op_linear_f8")
 
 
 def ls_op_accept(draft, verified, d, state, out_ids, accepted):

@@ -13,6 +13,7 @@
 // then looks at the control words, so there is no host sync per token; steps launched
 // past the end see the done flag and return at once.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -25,6 +26,7 @@
 
 #include "ls.h"
 #include "ls_attention.cuh"
+#include "ls_f8_linear.cuh"
 #include "ls_kv4.cuh"
 #include "ls_linear.cuh"
 #include "ls_prefill.cuh"
@@ -554,6 +556,21 @@ int make_tile_map(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t K, 
     if (cache.size() >= 8192) cache.clear();
     cache.emplace(key, *map);
     return LS_OK;
+}
+
+// the same of a row-major matrix of bytes [rows, K]: boxes of 128 columns
+int make_f8_map(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t K, int box_rows)
+{
+    TensorMapEncodeFn fn = tensor_map_encoder();
+    if (!fn) return LS_ERR_UNSUPPORTED;
+    cuuint64_t dims[2] = {K, rows};
+    cuuint64_t strides[1] = {K};
+    cuuint32_t box[2] = {(cuuint32_t)kF8Block, (cuuint32_t)box_rows};
+    cuuint32_t es[2] = {1, 1};
+    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, es,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? LS_OK : LS_ERR_INVALID_ARG;
 }
 
 // C[M, N] (+)= A[M, K] B[N, K]^T on the tensor cores (tcgen05), A and B bf16, C fp32
@@ -1849,7 +1866,7 @@ static int64_t w4_blocks(int N, int K) { return ((int64_t)N + kQ4Rows - 1) / kQ4
 // it has finished.  Whether it may start early is its own attribute's matter, and the switch may be turned on after
 // the packing: so what writes weights is always followed by a launch that waits for it to the end and that the next
 // operation overlaps instead.
-static int w4_written(cudaStream_t stream)
+static int weights_written(cudaStream_t stream)
 {
     LS_CK(launch(LaunchCtx{stream, false}, fence_kernel, dim3(1), dim3(32), 0));
     return LS_OK;
@@ -1869,7 +1886,7 @@ int ls_op_quantize_w4(const void* w, int32_t N, int32_t K, int32_t group, void* 
     auto* kernel = group == 32 ? quantize_w4_kernel<4> : group == 64 ? quantize_w4_kernel<2> : quantize_w4_kernel<1>;
     LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, kernel, dim3((unsigned)((blocks + 7) / 8)), dim3(256), 0,
                  (const uint16_t*)w, N, K, w4_kblocks(K), blocks, (unsigned char*)packed));
-    return w4_written((cudaStream_t)stream);
+    return weights_written((cudaStream_t)stream);
 }
 
 int ls_op_expand_w4(const void* packed, int32_t N, int32_t K, int32_t group, void* out, void* stream)
@@ -1880,7 +1897,7 @@ int ls_op_expand_w4(const void* packed, int32_t N, int32_t K, int32_t group, voi
     auto* kernel = group == 32 ? expand_w4_kernel<4> : group == 64 ? expand_w4_kernel<2> : expand_w4_kernel<1>;
     LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, kernel, dim3((unsigned)((blocks + 7) / 8)), dim3(256), 0,
                  (const unsigned char*)packed, N, K, w4_kblocks(K), blocks, (uint16_t*)out));
-    return w4_written((cudaStream_t)stream);
+    return weights_written((cudaStream_t)stream);
 }
 
 }  // extern "C"
@@ -2169,6 +2186,187 @@ int ls_op_attention_kv4(const void* q, int32_t n_seq, int32_t M, const int32_t* 
     return (hd == 128 ? kv4_attn_launch_hd<128> : kv4_attn_launch_hd<64>)(
         kv4_plan(n_seq, Hkv, max_seq, scratch != nullptr), n_seq, (const uint16_t*)q, M, Hq / Hkv, pos0, c,
         (const unsigned char*)pages, (uint16_t*)out, (float*)scratch, status, lc);
+}
+
+// ---- 8-bit values with a scale for each block of 128 (ls_f8.cuh, ls_f8_linear.cuh)
+static bool f8_shape_ok(int M, int K) { return M >= 1 && M <= LS_F8_MAX_ROWS && K >= 16 && K <= 1 << 28 && K % 16 == 0; }
+static bool f8_type_ok(int type) { return type == LS_BF16 || type == LS_F32; }
+static int f8_pieces(int type) { return type == LS_F32 ? 4 : 8; }  // elements of 16 bytes
+static bool f8_rows_ok(const void* p, int type, int64_t ld, int M, int K)  // rows that begin at 16-byte boundaries
+{
+    return aligned16(p) && f8_type_ok(type) && (M == 1 || (ld >= K && ld % f8_pieces(type) == 0));
+}
+static bool f8_held_ok(const void* codes, const void* scales) { return aligned16(codes) && scales && ((uintptr_t)scales & 3u) == 0; }
+static int f8_parts(int K) { return (K + 511) / 512; }  // a warp's share of a row: a word of scale bytes
+
+size_t ls_op_f8_scale_bytes(int32_t M, int32_t K, int32_t block_rows)
+{
+    if (!f8_shape_ok(M, K) || (block_rows != 1 && block_rows != kF8Block)) return 0;
+    return (size_t)((M + block_rows - 1) / block_rows) * f8_scale_width(K);
+}
+
+int ls_op_quantize_f8(const void* x, int32_t type, int64_t ldx, int32_t M, int32_t K, int32_t block_rows, void* codes,
+                      void* scales, void* stream)
+{
+    if (!f8_shape_ok(M, K) || !f8_rows_ok(x, type, ldx, M, K) || !f8_held_ok(codes, scales) ||
+        (block_rows != 1 && block_rows != kF8Block))
+        return LS_ERR_INVALID_ARG;
+    const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
+    unsigned char *c = (unsigned char*)codes, *e = (unsigned char*)scales;
+    if (block_rows == 1) {
+        const int parts = f8_parts(K);
+        const long long items = (long long)M * parts;
+        if ((items + 7) / 8 > 0x7fffffff) return LS_ERR_UNSUPPORTED;
+        const dim3 grid((unsigned)((items + 7) / 8));
+        if (type == LS_F32) LS_CK(launch(lc, quantize_f8_rows_kernel<float>, grid, dim3(256), 0, (const float*)x, ldx, K, parts, items, c, e));
+        else LS_CK(launch(lc, quantize_f8_rows_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)x, ldx, K, parts, items, c, e));
+        return LS_OK;
+    }
+    const dim3 grid((K + kF8Block - 1) / kF8Block, (M + kF8Block - 1) / kF8Block);
+    if (type == LS_F32) LS_CK(launch(lc, quantize_f8_weights_kernel<float>, grid, dim3(256), 0, (const float*)x, ldx, M, K, c, e));
+    else LS_CK(launch(lc, quantize_f8_weights_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)x, ldx, M, K, c, e));
+    return weights_written((cudaStream_t)stream);
+}
+
+int ls_op_expand_f8(const void* codes, const void* scales, int32_t M, int32_t K, int32_t block_rows, void* out, void* stream)
+{
+    if (!f8_shape_ok(M, K) || !f8_held_ok(codes, scales) || !aligned16(out) || (block_rows != 1 && block_rows != kF8Block))
+        return LS_ERR_INVALID_ARG;
+    const int parts = f8_parts(K), weights = block_rows == kF8Block;
+    const long long items = (long long)M * parts;
+    if ((items + 7) / 8 > 0x7fffffff) return LS_ERR_UNSUPPORTED;
+    LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, expand_f8_kernel, dim3((unsigned)((items + 7) / 8)), dim3(256), 0,
+                 (const unsigned char*)codes, (const unsigned char*)scales, K, parts, items, weights ? 7 : 0, !weights, (uint16_t*)out));
+    return weights ? weights_written((cudaStream_t)stream) : LS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// cudaFuncAttributeMaxDynamicSharedMemorySize once per kernel (by value: instances of a template share a type) and device
+template <auto kernel>
+int allow_smem(size_t smem)
+{
+    static std::atomic<bool> allowed[64];
+    int dev = 0;
+    LS_CK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return LS_ERR_UNSUPPORTED;
+    if (!allowed[dev].load(std::memory_order_acquire)) {
+        LS_CK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        allowed[dev].store(true, std::memory_order_release);
+    }
+    return LS_OK;
+}
+
+struct NormArgs {
+    void *x, *x_out;
+    const void *d, *gain;
+    int64_t ldx, ldd, ldo;
+    int M, D;
+    float eps;
+    unsigned char *codes, *scales;
+};
+
+template <typename T, typename TD, int NV>
+int rmsnorm_f8_launch_nv(const NormArgs& a, int threads, const LaunchCtx& lc)
+{
+    LS_CK(launch(lc, rmsnorm_f8_kernel<T, TD, NV>, dim3((unsigned)a.M), dim3(threads), 0, (const T*)a.x, a.ldx, (const TD*)a.d, a.ldd,
+                 (T*)a.x_out, a.ldo, (const uint16_t*)a.gain, a.D, a.eps, a.codes, a.scales));
+    return LS_OK;
+}
+
+template <typename T, typename TD>
+int rmsnorm_f8_launch(const NormArgs& a, const LaunchCtx& lc)
+{
+    const int pieces = (int)f8_scale_width(a.D) * kF8Block / F8In<T>::V;  // 16-byte pieces of a row, whole warps of them
+    // A row is one CTA's. Few rows leave SMs idle: as many threads as there are pieces; with many, 256 threads of 4 to
+    // 8 pieces keep more loads in flight.
+    int threads = a.M <= 296 ? 1024 : 256;
+    while (threads < 512 && threads * 8 < pieces) threads *= 2;
+    while (threads > 64 && threads / 2 >= pieces) threads /= 2;
+    if (pieces <= threads) return rmsnorm_f8_launch_nv<T, TD, 1>(a, threads, lc);
+    if (pieces <= 2 * threads) return rmsnorm_f8_launch_nv<T, TD, 2>(a, threads, lc);
+    if (pieces <= 4 * threads) return rmsnorm_f8_launch_nv<T, TD, 4>(a, threads, lc);
+    if (pieces <= 8 * threads && threads <= 512) return rmsnorm_f8_launch_nv<T, TD, 8>(a, threads, lc);
+    return rmsnorm_f8_launch_nv<T, TD, 0>(a, threads, lc);
+}
+
+template <int NT>
+int linear_f8_launch(const void* wc, const void* hc, const F8Linear& p, int S, const LaunchCtx& lc)
+{
+    LS_TRY(allow_smem<linear_f8_kernel<NT>>(F8Cfg<NT>::kSmem));
+    CUtensorMap mw, mh;
+    LS_TRY(make_f8_map(&mw, wc, (uint64_t)p.N, (uint64_t)p.K, kF8Block));
+    LS_TRY(make_f8_map(&mh, hc, (uint64_t)p.M, (uint64_t)p.K, NT));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(S, (p.N + kF8Block - 1) / kF8Block, (p.M + NT - 1) / NT);
+    cfg.blockDim = dim3(kF8Threads);
+    cfg.dynamicSmemBytes = F8Cfg<NT>::kSmem;
+    cfg.stream = lc.st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = S;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = lc.pdl ? 2 : 1;
+    LS_CK(cudaLaunchKernelEx(&cfg, linear_f8_kernel<NT>, mw, mh, p));
+    return LS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ls_op_rmsnorm_f8(const void* x, int32_t x_type, int64_t ldx, const void* delta, int32_t delta_type, int64_t ldd, void* x_out,
+                     int64_t ldo, const void* gain, int32_t M, int32_t D, float eps, void* codes, void* scales, void* stream)
+{
+    if (!f8_shape_ok(M, D) || !f8_rows_ok(x, x_type, ldx, M, D) || (delta && !f8_rows_ok(delta, delta_type, ldd, M, D)) ||
+        (x_out && !f8_rows_ok(x_out, x_type, ldo, M, D)) || !aligned16(gain) || !f8_held_ok(codes, scales))
+        return LS_ERR_INVALID_ARG;
+    const NormArgs a = {const_cast<void*>(x), x_out, delta, gain, ldx, ldd, ldo, M, D, eps, (unsigned char*)codes, (unsigned char*)scales};
+    const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
+    const bool d32 = !delta || delta_type == LS_F32;
+    if (x_type == LS_F32) return d32 ? rmsnorm_f8_launch<float, float>(a, lc) : rmsnorm_f8_launch<float, uint16_t>(a, lc);
+    return d32 ? rmsnorm_f8_launch<uint16_t, float>(a, lc) : rmsnorm_f8_launch<uint16_t, uint16_t>(a, lc);
+}
+
+int ls_op_swiglu_f8(const void* gate, const void* up, int32_t type, int64_t ld, int32_t M, int32_t F, void* codes, void* scales,
+                    void* stream)
+{
+    if (!f8_shape_ok(M, F) || !f8_rows_ok(gate, type, ld, M, F) || !aligned16(up) || !f8_held_ok(codes, scales)) return LS_ERR_INVALID_ARG;
+    const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
+    const int parts = f8_parts(F);
+    const long long items = (long long)M * parts;
+    if ((items + 7) / 8 > 0x7fffffff) return LS_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)((items + 7) / 8));
+    unsigned char *c = (unsigned char*)codes, *e = (unsigned char*)scales;
+    if (type == LS_F32) LS_CK(launch(lc, swiglu_f8_kernel<float>, grid, dim3(256), 0, (const float*)gate, (const float*)up, ld, F, parts, items, c, e));
+    else LS_CK(launch(lc, swiglu_f8_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)gate, (const uint16_t*)up, ld, F, parts, items, c, e));
+    return LS_OK;
+}
+
+int ls_op_linear_f8(const void* w_codes, const void* w_scales, const void* h_codes, const void* h_scales, int32_t M, int32_t N,
+                    int32_t K, void* out, int32_t out_type, int64_t ldo, const void* add, int64_t lda, int32_t* status, void* stream)
+{
+    const uintptr_t odd = out_type == LS_F32 ? 3u : 1u;
+    if (!f8_shape_ok(M, K) || !f8_shape_ok(N, K) || !f8_held_ok(w_codes, w_scales) || !f8_held_ok(h_codes, h_scales) ||
+        !f8_type_ok(out_type) || !out || ((uintptr_t)out & odd) || ((uintptr_t)add & odd) || (M > 1 && (ldo < N || (add && lda < N))))
+        return LS_ERR_INVALID_ARG;
+    const F8Linear p = {(const unsigned char*)w_scales, (const unsigned char*)h_scales, M, N, K, out, add, ldo, lda, out_type == LS_BF16, status};
+    const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
+    const int NT = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, kb = (K + kF8Block - 1) / kF8Block;
+    // CTAs that share a tile: as many as keep one CTA an SM.  Up to 16 rows a function of the matrix alone: it enters a row's arithmetic.
+    const long long tiles = (long long)((N + kF8Block - 1) / kF8Block) * ((M + NT - 1) / NT);
+    int S = 1;
+    while (S < 8 && tiles * 2 * S <= 148 && kb >= 4 * S) S *= 2;
+    return NT == 16 ? linear_f8_launch<16>(w_codes, h_codes, p, S, lc)
+           : NT == 32 ? linear_f8_launch<32>(w_codes, h_codes, p, S, lc)
+           : NT == 64 ? linear_f8_launch<64>(w_codes, h_codes, p, S, lc)
+                      : linear_f8_launch<128>(w_codes, h_codes, p, S, lc);
 }
 
 int ls_op_accept(const int32_t* draft, const int32_t* verified, int32_t d, int32_t* state, int32_t* out_ids,
