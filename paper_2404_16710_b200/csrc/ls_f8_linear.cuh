@@ -5,6 +5,8 @@
 // sum goes to a tensor-memory buffer of its own; four warps read it back, multiply by the product of the two scales
 // and add it to fp32 registers, so what the tensor cores sum is never longer than 128 and the rest is plain fp32.
 #pragma once
+#include <type_traits>
+
 #include "ls_f8.cuh"
 #include "ls_prefill_attn.cuh"
 
@@ -37,19 +39,37 @@ struct F8Linear {
     void* out;
     const void* add;  // null or of out's type
     int64_t ldo, lda;
-    int bf16;
     int32_t* status;
 };
 
-// value (+ add) to out[m, n]
-__device__ __forceinline__ void f8_put(const F8Linear& p, long long m, int n, float v)
+// out[m .. m + 15, n] = v (+ add), `most` of them; all of add is asked for first, as out may be add
+template <bool BF16>
+__device__ __forceinline__ void f8_put16(const F8Linear& p, long long m, int n, const float* v, int most = 16)
 {
-    if (p.bf16) {
-        if (p.add) v += bf16f(__ldcg(reinterpret_cast<const uint16_t*>(p.add) + m * p.lda + n));
-        reinterpret_cast<uint16_t*>(p.out)[m * p.ldo + n] = f2bf(v);
-    } else {
-        if (p.add) v += __ldcg(reinterpret_cast<const float*>(p.add) + m * p.lda + n);
-        reinterpret_cast<float*>(p.out)[m * p.ldo + n] = v;
+    using T = std::conditional_t<BF16, uint16_t, float>;
+    const int rows = (int)min((long long)min(most, 16), p.M - m);
+    T* dst = reinterpret_cast<T*>(p.out) + m * p.ldo + n;
+    float a[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) a[j] = v[j];
+    if (p.add) {
+        const T* src = reinterpret_cast<const T*>(p.add) + m * p.lda + n;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if (j < rows) {
+                if constexpr (BF16) a[j] += bf16f(__ldcg(src));
+                else a[j] += __ldcg(src);
+            }
+            src += p.lda;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        if (j < rows) {
+            if constexpr (BF16) *dst = f2bf(a[j]);
+            else *dst = a[j];
+        }
+        dst += p.ldo;
     }
 }
 
@@ -76,7 +96,7 @@ struct F8Cfg {
 };
 
 // grid (S, tiles of 128 weight rows, tiles of NT tokens), clusters (S, 1, 1)
-template <int NT>
+template <int NT, bool BF16>
 __global__ void __launch_bounds__(kF8Threads, 1)
 linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h, const F8Linear p)
 {
@@ -253,27 +273,329 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     } else if (warp < 4 && n0 + tid < p.N) {
         if (S > 1) {
             const int per = NT / S;
-            for (int j = 0; j < per; ++j) {
-                const long long m = m0 + rank * per + j;
-                if (m >= p.M) break;
-                float v = 0.f;
-                for (int r = 0; r < S; ++r) {
-                    float u;
-                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(u) : "r"(part0 + 4u * ((r * per + j) * kF8Block + tid)) : "memory");
-                    v += u;
+            for (int c = 0; c < per; c += 16) {
+                float v[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    v[j] = 0.f;
+                    for (int r = 0; r < S && c + j < per; ++r) {
+                        float u;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(u) : "r"(part0 + 4u * ((r * per + c + j) * kF8Block + tid)) : "memory");
+                        v[j] += u;
+                    }
                 }
-                f8_put(p, m, n0 + tid, v);
+                f8_put16<BF16>(p, m0 + rank * per + c, n0 + tid, v, per - c);
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                if (m0 + j < p.M) f8_put(p, m0 + j, n0 + tid, acc[j]);
+            for (int j = 0; j < NT; j += 16) f8_put16<BF16>(p, m0 + j, n0 + tid, acc + j);
         }
     }
     tc_fence_before();
     __syncthreads();
     if (warp == 0)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kCols) : "memory");
+}
+
+// ------------------------------------------------------------------ many tokens: CTA pairs, scales in the tensor cores
+// Two CTAs of a cluster compute 256 rows of weights x nt tokens (nt a multiple of 16, at most 240) with
+// tcgen05.mma.cta_group::2 of kind mxf8f6f4: the tensor cores multiply each 32 columns' products by 2^(ew + eh) as they add
+// them up, so a block's four MMAs name the same scale byte and no sum leaves tensor memory before the tile is
+// done.  Scales go to tensor memory 512 columns at a time: a warp lays the words of 128 rows out as [row % 32][row / 32]
+// in shared memory, tcgen05.cp spreads them over the lanes; byte i of a word is the i-th block's, which the instruction
+// descriptor picks.  Weights are the 256-row operand, so that tiles follow the tokens' number in steps of 16 and a warp
+// stores 32 neighbouring outputs; at 240 tokens two accumulators and the scales fit the 512 columns of tensor memory:
+// a tile's sums are read while the next one's are made.
+// Persistent: pair p takes tiles p, p + P, ..., tokens fastest (pairs that run side by side share weights in L2).
+constexpr int kF8PairTokens = 240;
+constexpr int kF8PairStages = 7;
+constexpr int kF8PairStage = kF8WBytes + kF8PairTokens / 2 * kF8Block;  // a CTA's weights, and half of the tokens
+constexpr int kF8PairSlots = 4;
+constexpr int kF8PairChunk = 16;             // blocks along K that are summed in tensor memory
+constexpr int kF8PairSlot = 3 * 512;        // scale words of 128 rows of weights, of 256 tokens
+constexpr int kF8PairScaleCols = 2 * kF8PairTokens;  // two sets of 16 columns behind the accumulators
+constexpr int kF8PairThreads = 640;         // warps 0-15: sums and stores, 16: TMA, 17: MMA, 18, 19: scales
+constexpr size_t kF8PairSmem = (size_t)kF8PairStages * kF8PairStage + kF8PairSlots * kF8PairSlot + 1024 + 512;
+static_assert(kF8PairStage % 1024 == 0 && kF8PairSmem <= kF8SmemMax && kF8PairScaleCols + 32 <= 512, "shared and tensor memory");
+
+// D[tmem] (+)= (A * scales)(B * scales)^T, e4m3, a scale for 32 columns of a row
+__device__ __forceinline__ void tc_mma_f8_scaled_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa,
+                                                      uint32_t sb, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
+}
+// 32 rows of 16 bytes of either CTA's shared memory -> 4 columns of its tensor memory, in all four groups of 32 lanes
+__device__ __forceinline__ void tc_cp_scales_pair(uint32_t taddr, uint32_t smem)
+{
+    // rows 16 bytes apart, groups of 8 of them 128; no swizzle, descriptor version 1
+    const uint64_t d = (uint64_t)((smem >> 4) & 0x3fff) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(d) : "memory");
+}
+
+// true in one lane of a converged warp
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
+// mbar_wait for a barrier that the peer CTA arrives on too, after it has written what is read behind the wait
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
+{
+    for (uint32_t it = 0; it < (1u << 22); ++it) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (done) return true;
+        if (it > 1024) __nanosleep(200);
+    }
+    return false;
+}
+
+template <bool BF16>
+__global__ void __launch_bounds__(kF8PairThreads, 1)
+linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h, const F8Linear p,
+                      const int nt, const int token_tiles, const int n_tiles)
+{
+    extern __shared__ unsigned char f8_raw[];
+    __shared__ int failed;
+    const uint32_t base = (smem_u32(f8_raw) + 1023u) & ~1023u;
+    const uint32_t sc0 = base + kF8PairStages * kF8PairStage, bars = sc0 + kF8PairSlots * kF8PairSlot;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (kF8PairStages + s); };
+    auto accf = [&](int b) { return bars + 8u * (2 * kF8PairStages + b); };
+    auto acce = [&](int b) { return bars + 8u * (2 * kF8PairStages + 2 + b); };
+    auto sfull = [&](int b) { return bars + 8u * (2 * kF8PairStages + 4 + b); };
+    auto sempty = [&](int b) { return bars + 8u * (2 * kF8PairStages + 4 + kF8PairSlots + b); };
+    const uint32_t tslot = bars + 8u * (2 * kF8PairStages + 4 + 2 * kF8PairSlots);
+
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    uint32_t rank;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const int n_pairs = (int)gridDim.x / 2, pair = (int)blockIdx.x / 2;
+    const int nkb = (p.K + kF8Block - 1) / kF8Block, groups = (nkb + 3) / 4;
+
+    if (tid == 0) {
+        for (int s = 0; s < kF8PairStages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(accf(b), 1);
+            mbar_init(acce(b), 32);  // sixteen storing warps in each CTA of the pair
+        }
+        for (int b = 0; b < kF8PairSlots; ++b) {
+            mbar_init(sfull(b), 2);  // the scale warps of both
+            mbar_init(sempty(b), 1);
+        }
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tslot), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();  // the peer's barriers exist before anything signals them
+    tc_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tslot));
+
+    if (warp == 16) {
+        if (lane == 0) {
+            const uint32_t bytes = 2u * (uint32_t)(kF8WBytes + nt / 2 * kF8Block);
+            int it = 0;
+            bool ok = true;
+            for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+                const int w_row = (t / token_tiles * 2 + (int)rank) * kF8Block, h_row = t % token_tiles * nt + (int)rank * (nt / 2);
+                for (int kb = 0; kb < nkb; ++kb, ++it) {
+                    const int s = it % kF8PairStages;
+                    if (it >= kF8PairStages && !mbar_wait(empty(s), (it / kF8PairStages - 1) & 1)) {
+                        failed = 1;
+                        ok = false;
+                        break;
+                    }
+                    if (rank == 0) mbar_expect_tx(full(s), bytes);
+                    const uint32_t lead = full(s) & kPeerBitMask;
+                    tma_load_2d_pair(base + s * kF8PairStage, &map_w, kb * kF8Block, w_row, lead);
+                    tma_load_2d_pair(base + s * kF8PairStage + kF8WBytes, &map_h, kb * kF8Block, h_row, lead);
+                }
+            }
+        }
+    } else if (warp == 17) {
+        if (rank == 0) {
+            // The whole warp walks the loop and one lane issues: what an instruction names stays in uniform registers.
+            // instruction descriptor: scales 2^(e - 127), A and B e4m3, both K-major, N = nt, M = 256 (128 per CTA)
+            const uint32_t idesc = ((uint32_t)(nt >> 3) << 17) | (1u << 23) | (2u << 27);
+            const uint64_t desc0 = umma_desc_sw128(0);
+            const bool one = elect_one();
+            uint32_t s = 0, s_phase = 0, slot = 0, slot_phase = 0, set = 0;
+            uint32_t b = 0, b_phase = 1;  // an accumulator that was never used counts as read
+            bool ok = true;
+            for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+                for (int kb = 0; kb < nkb && ok; kb += 4) {
+                    const uint32_t d = tmem + b * kF8PairTokens;
+                    if (kb % kF8PairChunk == 0) {
+                        if (!mbar_wait(acce(b), b_phase)) {
+                            failed = 1;
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                    }
+                    // four blocks' scales; copies and products of a thread run in order
+                    if (!mbar_wait_cluster(sfull(slot), slot_phase)) {
+                        failed = 1;
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t sf = tmem + kF8PairScaleCols + set * 16u, src = sc0 + slot * kF8PairSlot;
+                    if (one) {
+                        tc_cp_scales_pair(sf, src);
+                        tc_cp_scales_pair(sf + 8, src + 512);
+                        if (nt > 128) tc_cp_scales_pair(sf + 12, src + 1024);
+                        tc_commit_pair(sempty(slot));
+                    }
+                    set ^= 1u;
+                    if (++slot == kF8PairSlots) slot = 0, slot_phase ^= 1u;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (kb + q >= nkb) break;
+                        if (!mbar_wait(full(s), s_phase)) {
+                            failed = 1;
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint64_t da = desc0 + ((base + s * kF8PairStage) >> 4), db = da + (kF8WBytes >> 4);
+                        if (one) {
+                            const uint32_t id = idesc | (uint32_t)q << 4 | (uint32_t)q << 29;
+#pragma unroll
+                            for (int k4 = 0; k4 < 4; ++k4)
+                                tc_mma_f8_scaled_pair(d, da + 2 * k4, db + 2 * k4, id, sf, sf + 8, (kb % kF8PairChunk | q | k4) != 0);
+                            tc_commit_pair(empty(s));
+                        }
+                        if (++s == kF8PairStages) s = 0, s_phase ^= 1u;
+                    }
+                    if (ok && ((kb + 4) % kF8PairChunk == 0 || kb + 4 >= nkb)) {
+                        if (one) tc_commit_pair(accf(b));
+                        b ^= 1u;
+                        if (b == 0) b_phase ^= 1u;
+                    }
+                }
+            }
+        }
+    } else if (warp >= 18) {
+        // Scale words of this CTA's weights (one for all its 128 rows) and of all the tile's tokens, four blocks at a time, the two warps
+        // in turn.  The fence waits for the warp's loads too, so the next words are asked for behind it, and two
+        // warps leave them the time of eight blocks (one warp: 2200 cycles for four, whatever the tile).
+        const int width = (int)f8_scale_width(p.K), w_rows = (p.N + kF8Block - 1) / kF8Block;
+        int t = pair, gi = warp - 18;  // next group to ask for
+        uint32_t w = 0, h[8];
+        auto settle = [&] {
+            while (gi >= groups) gi -= groups, t += n_pairs;
+        };
+        auto fetch = [&] {
+            const int wb = t / token_tiles * 2 + (int)rank;
+            const long long m0 = (long long)(t % token_tiles) * nt;
+            w = wb < w_rows ? __ldcg(reinterpret_cast<const uint32_t*>(p.ws + (long long)wb * width + 4 * gi)) : 0x7f7f7f7fu;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const long long m = m0 + 32 * j + lane;
+                h[j] = 32 * j + lane < nt && m < p.M ? __ldcg(reinterpret_cast<const uint32_t*>(p.hs + m * width + 4 * gi)) : 0x7f7f7f7fu;
+            }
+        };
+        uint32_t slot = warp - 18, phase = 1;  // a slot that was never used counts as free
+        settle();
+        if (t < n_tiles) fetch();
+        while (t < n_tiles) {
+            if (!mbar_wait(sempty(slot), phase)) {
+                failed = 1;
+                break;
+            }
+            const uint32_t dst = sc0 + slot * kF8PairSlot + lane * 16;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst), "r"(w) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + 512), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + 1024), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // tcgen05.cp reads what was just stored
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(cluster_map(sfull(slot), 0));
+            slot += 2;
+            if (slot >= kF8PairSlots) slot -= kF8PairSlots, phase ^= 1u;
+            gi += 2;
+            settle();
+            if (t < n_tiles) fetch();
+        }
+    } else {
+        // warp w reads lanes 32 (w % 4) .. of this CTA's accumulators, rows of weights, and a quarter of the tokens.  Sixteen
+        // warps, as each runs through its tokens once a tile: longer straight code waits for its instructions.
+        const uint32_t acce_leader[2] = {cluster_map(acce(0), 0), cluster_map(acce(1), 0)};
+        const int quarter = (nt / 4 + 15) / 16 * 16, c0 = (warp >> 2) * quarter, cols = min(quarter, nt - c0);
+        uint32_t b = 0, b_phase = 0;
+        bool ok = true;
+        for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+            const int n = (t / token_tiles * 2 + (int)rank) * kF8Block + (warp & 3) * 32 + lane;
+            const long long m0 = (long long)(t % token_tiles) * nt + c0;
+            if (p.add) {  // on its way into L2 while the products are made
+                using T = std::conditional_t<BF16, uint16_t, float>;
+                const int n_warp = n - lane;
+                for (int j = lane; j < cols; j += 32)
+                    if (m0 + j < p.M && n_warp < p.N)
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const T*>(p.add) + (m0 + j) * p.lda + n_warp));
+            }
+            float sum[64];
+            for (int kb = 0; kb < nkb; kb += kF8PairChunk) {
+                if (!mbar_wait(accf(b), b_phase)) {
+                    failed = 1;
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t tacc = tmem + ((uint32_t)((warp & 3) * 32) << 16) + b * kF8PairTokens + c0;
+#pragma unroll
+                for (int c = 0; c < 64; c += 16) {
+                    if (c < cols) {
+                        uint32_t v[16];
+                        tc_ld16(tacc + c, v);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[c + j] = kb ? sum[c + j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(acce_leader[b]);
+                b ^= 1u;
+                if (b == 0) b_phase ^= 1u;
+            }
+            if (ok && n < p.N) {
+#pragma unroll
+                for (int c = 0; c < 64; c += 16)
+                    if (c < cols) f8_put16<BF16>(p, m0 + c, n, sum + c, cols - c);
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (failed && tid == 0) {
+        if (p.status) *p.status = DEV_TIMEOUT;
+        __nanosleep(1000000);  // let copies that may still be in flight land before the CTA goes away
+    }
+    cluster_sync_all();  // both CTAs are done with tensor memory, and the MMAs with both shared memories
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
 }  // namespace ls

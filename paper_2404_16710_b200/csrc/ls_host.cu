@@ -568,7 +568,7 @@ int make_f8_map(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t K, in
     cuuint32_t box[2] = {(cuuint32_t)kF8Block, (cuuint32_t)box_rows};
     cuuint32_t es[2] = {1, 1};
     CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, es,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? LS_OK : LS_ERR_INVALID_ARG;
 }
@@ -2292,10 +2292,10 @@ int rmsnorm_f8_launch(const NormArgs& a, const LaunchCtx& lc)
     return rmsnorm_f8_launch_nv<T, TD, 0>(a, threads, lc);
 }
 
-template <int NT>
+template <int NT, bool BF16>
 int linear_f8_launch(const void* wc, const void* hc, const F8Linear& p, int S, const LaunchCtx& lc)
 {
-    LS_TRY(allow_smem<linear_f8_kernel<NT>>(F8Cfg<NT>::kSmem));
+    LS_TRY((allow_smem<linear_f8_kernel<NT, BF16>>(F8Cfg<NT>::kSmem)));
     CUtensorMap mw, mh;
     LS_TRY(make_f8_map(&mw, wc, (uint64_t)p.N, (uint64_t)p.K, kF8Block));
     LS_TRY(make_f8_map(&mh, hc, (uint64_t)p.M, (uint64_t)p.K, NT));
@@ -2313,8 +2313,71 @@ int linear_f8_launch(const void* wc, const void* hc, const F8Linear& p, int S, c
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = lc.pdl ? 2 : 1;
-    LS_CK(cudaLaunchKernelEx(&cfg, linear_f8_kernel<NT>, mw, mh, p));
+    LS_CK(cudaLaunchKernelEx(&cfg, linear_f8_kernel<NT, BF16>, mw, mh, p));
     return LS_OK;
+}
+
+template <bool BF16>
+int linear_f8_pair_launch(const void* wc, const void* hc, const F8Linear& p, const LaunchCtx& lc)
+{
+    static std::atomic<int> max_pairs[64];
+    int dev = 0;
+    LS_CK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return LS_ERR_UNSUPPORTED;
+    LS_TRY(allow_smem<linear_f8_pair_kernel<BF16>>(kF8PairSmem));
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 2;
+    at.val.clusterDim.y = 1;
+    at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    cfg.dynamicSmemBytes = kF8PairSmem;
+    cfg.blockDim = dim3(kF8PairThreads);
+    cfg.stream = lc.st;
+    int most = max_pairs[dev].load(std::memory_order_acquire);
+    if (!most) {
+        int sms = 0, n = 0;
+        LS_CK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+        cfg.gridDim = dim3(sms & ~1);
+        LS_CK(cudaOccupancyMaxActiveClusters(&n, linear_f8_pair_kernel<BF16>, &cfg));
+        if (n < 1) return LS_ERR_UNSUPPORTED;
+        most = n < sms / 2 ? n : sms / 2;
+        max_pairs[dev].store(most, std::memory_order_release);
+    }
+    // tokens of a tile: what makes the rounds of tiles over all pairs cost least
+    const int w_tiles = (p.N + 2 * kF8Block - 1) / (2 * kF8Block), least = (p.M + kF8PairTokens - 1) / kF8PairTokens;
+    int nt = kF8PairTokens, token_tiles = least;
+    long long best = 0;
+    for (int tt = least; tt <= least + 16; ++tt) {
+        const int n = ((p.M + tt - 1) / tt + 15) / 16 * 16, real = (p.M + n - 1) / n;
+        const long long cost = ((long long)w_tiles * real + most - 1) / most * (n + 64);
+        if (!best || cost < best) best = cost, nt = n, token_tiles = real;
+    }
+    const long long n_tiles = (long long)w_tiles * token_tiles;
+    if (n_tiles > 0x7fffffff) return LS_ERR_UNSUPPORTED;
+    CUtensorMap mw, mh;
+    LS_TRY(make_f8_map(&mw, wc, (uint64_t)p.N, (uint64_t)p.K, kF8Block));
+    LS_TRY(make_f8_map(&mh, hc, (uint64_t)p.M, (uint64_t)p.K, nt / 2));
+    cfg.gridDim = dim3(2 * (unsigned)(n_tiles < most ? n_tiles : most));
+    LS_CK(cudaLaunchKernelEx(&cfg, linear_f8_pair_kernel<BF16>, mw, mh, p, nt, token_tiles, (int)n_tiles));
+    return LS_OK;
+}
+
+template <bool BF16>
+int linear_f8_choose(const void* wc, const void* hc, const F8Linear& p, const LaunchCtx& lc)
+{
+    if (p.M > 128) return linear_f8_pair_launch<BF16>(wc, hc, p, lc);
+    const int NT = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128, kb = (p.K + kF8Block - 1) / kF8Block;
+    // CTAs that share a tile: as many as keep one CTA an SM.  Up to 16 rows a function of the matrix alone: it enters a row's arithmetic.
+    const long long tiles = (long long)((p.N + kF8Block - 1) / kF8Block) * ((p.M + NT - 1) / NT);
+    int S = 1;
+    while (S < 8 && tiles * 2 * S <= 148 && kb >= 4 * S) S *= 2;
+    return NT == 16 ? linear_f8_launch<16, BF16>(wc, hc, p, S, lc)
+           : NT == 32 ? linear_f8_launch<32, BF16>(wc, hc, p, S, lc)
+           : NT == 64 ? linear_f8_launch<64, BF16>(wc, hc, p, S, lc)
+                      : linear_f8_launch<128, BF16>(wc, hc, p, S, lc);
 }
 
 }  // namespace
@@ -2356,17 +2419,9 @@ int ls_op_linear_f8(const void* w_codes, const void* w_scales, const void* h_cod
     if (!f8_shape_ok(M, K) || !f8_shape_ok(N, K) || !f8_held_ok(w_codes, w_scales) || !f8_held_ok(h_codes, h_scales) ||
         !f8_type_ok(out_type) || !out || ((uintptr_t)out & odd) || ((uintptr_t)add & odd) || (M > 1 && (ldo < N || (add && lda < N))))
         return LS_ERR_INVALID_ARG;
-    const F8Linear p = {(const unsigned char*)w_scales, (const unsigned char*)h_scales, M, N, K, out, add, ldo, lda, out_type == LS_BF16, status};
+    const F8Linear p = {(const unsigned char*)w_scales, (const unsigned char*)h_scales, M, N, K, out, add, ldo, lda, status};
     const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
-    const int NT = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, kb = (K + kF8Block - 1) / kF8Block;
-    // CTAs that share a tile: as many as keep one CTA an SM.  Up to 16 rows a function of the matrix alone: it enters a row's arithmetic.
-    const long long tiles = (long long)((N + kF8Block - 1) / kF8Block) * ((M + NT - 1) / NT);
-    int S = 1;
-    while (S < 8 && tiles * 2 * S <= 148 && kb >= 4 * S) S *= 2;
-    return NT == 16 ? linear_f8_launch<16>(w_codes, h_codes, p, S, lc)
-           : NT == 32 ? linear_f8_launch<32>(w_codes, h_codes, p, S, lc)
-           : NT == 64 ? linear_f8_launch<64>(w_codes, h_codes, p, S, lc)
-                      : linear_f8_launch<128>(w_codes, h_codes, p, S, lc);
+    return out_type == LS_BF16 ? linear_f8_choose<true>(w_codes, h_codes, p, lc) : linear_f8_choose<false>(w_codes, h_codes, p, lc);
 }
 
 int ls_op_accept(const int32_t* draft, const int32_t* verified, int32_t d, int32_t* state, int32_t* out_ids,
