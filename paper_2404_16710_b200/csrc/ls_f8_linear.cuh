@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "ls_f8.cuh"
+#include "ls_attention.cuh"
 #include "ls_prefill_attn.cuh"
 
 namespace ls {
@@ -22,8 +23,15 @@ __device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t a_desc, uint
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// true in one lane of a converged warp
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
 // 16 columns of the thread's lane; the caller waits (tc_wait_ld)
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&v)[16])
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t* v)
 {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -31,6 +39,20 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&v)[16])
         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
           "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(taddr));
+}
+
+// acc[j] += t[j] * scale[j], scales in shared memory
+template <int N>
+__device__ __forceinline__ void f8_add_scaled(float* acc, const uint32_t* t, uint32_t scales)
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+        const uint4 f = lds16(scales + 4u * j);
+        acc[j] = fmaf(__uint_as_float(t[j]), __uint_as_float(f.x), acc[j]);
+        acc[j + 1] = fmaf(__uint_as_float(t[j + 1]), __uint_as_float(f.y), acc[j + 1]);
+        acc[j + 2] = fmaf(__uint_as_float(t[j + 2]), __uint_as_float(f.z), acc[j + 2]);
+        acc[j + 3] = fmaf(__uint_as_float(t[j + 3]), __uint_as_float(f.w), acc[j + 3]);
+    }
 }
 
 struct F8Linear {
@@ -42,6 +64,24 @@ struct F8Linear {
     int32_t* status;
 };
 
+// out[m, n] = v (+ add)
+template <bool BF16>
+__device__ __forceinline__ void f8_put(const F8Linear& p, long long m, int n, float v)
+{
+    if constexpr (BF16) {
+        if (p.add) v += bf16f(__ldcg(reinterpret_cast<const uint16_t*>(p.add) + m * p.lda + n));
+        reinterpret_cast<uint16_t*>(p.out)[m * p.ldo + n] = f2bf(v);
+    } else {
+        if (p.add) v += __ldcg(reinterpret_cast<const float*>(p.add) + m * p.lda + n);
+        reinterpret_cast<float*>(p.out)[m * p.ldo + n] = v;
+    }
+}
+__device__ __forceinline__ float lds_f32(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
 // out[m .. m + 15, n] = v (+ add), `most` of them; all of add is asked for first, as out may be add
 template <bool BF16>
 __device__ __forceinline__ void f8_put16(const F8Linear& p, long long m, int n, const float* v, int most = 16)
@@ -82,25 +122,54 @@ constexpr int kF8WBytes = kF8Block * kF8Block;
 constexpr int kF8SmemMax = 227 * 1024;
 constexpr int kF8Slots = 4;  // slots of scales, one word of scale bytes (four blocks) each
 
-template <int NT>
+template <int NT, int CTAS>  // CTAs that fit an SM
 struct F8Cfg {
     static constexpr int kStage = kF8WBytes + NT * kF8Block;
     static constexpr int kScale = kF8Slots * 4 * NT * 4;      // floats [slot][block][token]
     static constexpr int kPart = NT * kF8Block * 4;           // what the cluster's CTAs send: [rank][token][row]
     static constexpr int kFixed = 1024 + kScale + kPart + 512;
-    static constexpr int kFit = (kF8SmemMax - kFixed) / kStage;
-    static constexpr int kStages = kFit < 10 ? kFit : 10;
-    static constexpr int kBufs = NT <= 64 ? 4 : 2;            // tensor-memory buffers
-    static constexpr int kCols = kBufs * NT < 32 ? 32 : kBufs * NT;
+    static constexpr int kFit = (kF8SmemMax / CTAS - 1024 - kFixed) / kStage;
+    static constexpr int kStages = kFit < 11 ? kFit : 11;
+    static constexpr int kUnit = NT <= 16 ? 4 : NT <= 32 ? 2 : 1;  // blocks along K that change hands together
+    static constexpr int kBufs = NT == 64 ? 4 : 2;            // tensor-memory buffers of kUnit * NT columns
+    static constexpr int kCols = kBufs * kUnit * NT;
     static constexpr size_t kSmem = (size_t)kStages * kStage + kFixed;
 };
 
+// sums of the first `rows` tokens to the CTAs that own them: token j is the (j / S)-th of CTA j % S
+template <int NT, int S>
+__device__ __forceinline__ void f8_send(const float* acc, uint32_t row, int rows)
+{
+#pragma unroll
+    for (int r = 0; r < S; ++r) {
+        const uint32_t to = cluster_map(row, r);
+#pragma unroll
+        for (int j = r; j < NT; j += S)
+            if (j < rows)
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4u * (j / S * S * kF8Block)), "f"(acc[j]) : "memory");
+    }
+}
+// the tokens m, m + S, ... of this CTA: sums of the cluster's CTAs in order
+template <int NT, int S, bool BF16>
+__device__ __forceinline__ void f8_join(const F8Linear& p, long long m, int n, uint32_t row)
+{
+#pragma unroll 1
+    for (int j = 0; j < NT / S && m < p.M; ++j, m += S) {
+        float u[S], v = 0.f;
+#pragma unroll
+        for (int r = 0; r < S; ++r) u[r] = lds_f32(row + 4u * ((j * S + r) * kF8Block));
+#pragma unroll
+        for (int r = 0; r < S; ++r) v += u[r];
+        f8_put<BF16>(p, m, n, v);
+    }
+}
+
 // grid (S, tiles of 128 weight rows, tiles of NT tokens), clusters (S, 1, 1)
-template <int NT, bool BF16>
-__global__ void __launch_bounds__(kF8Threads, 1)
+template <int NT, bool BF16, int CTAS>
+__global__ void __launch_bounds__(kF8Threads, CTAS)
 linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h, const F8Linear p)
 {
-    using C = F8Cfg<NT>;
+    using C = F8Cfg<NT, CTAS>;
     extern __shared__ unsigned char f8_raw[];
     __shared__ int failed;
     const uint32_t base = (smem_u32(f8_raw) + 1023u) & ~1023u;
@@ -114,28 +183,34 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const uint32_t tslot = bars + 8u * (2 * C::kStages + 16);
     static_assert(8 * (2 * C::kStages + 17) <= 512, "barriers");
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int S = gridDim.x, rank = blockIdx.x;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const int S = gridDim.x, rank = blockIdx.x;  // S: 1, 2, 4 or 8
     const int n0 = blockIdx.y * kF8Block;
     const long long m0 = (long long)blockIdx.z * NT;
     const int nkb = (p.K + kF8Block - 1) / kF8Block;
     const int kb0 = (int)((long long)nkb * rank / S), kb1 = (int)((long long)nkb * (rank + 1) / S);
 
-    if (tid == 0) {
-        for (int s = 0; s < C::kStages; ++s) {
-            mbar_init(full(s), 1);
-            mbar_init(empty(s), 1);
+    const int ahead = min(kb1 - kb0, C::kStages);
+    if (warp == 4) {  // barriers, and at once the weights of the first stages: they need not wait for the operation ahead
+        if (lane < 2 * C::kStages) mbar_init(bars + 8u * lane, 1);
+        if (lane < C::kBufs) {
+            mbar_init(tfull(lane), 1);
+            mbar_init(tempty(lane), 4);
         }
-        for (int b = 0; b < C::kBufs; ++b) {
-            mbar_init(tfull(b), 1);
-            mbar_init(tempty(b), 4);
+        if (lane < kF8Slots) {
+            mbar_init(sfull(lane), 1);
+            mbar_init(sempty(lane), 4);
         }
-        for (int b = 0; b < kF8Slots; ++b) {
-            mbar_init(sfull(b), 1);
-            mbar_init(sempty(b), 4);
-        }
-        failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            failed = 0;
+            for (int i = 0; i < ahead; ++i) {
+                mbar_expect_tx(full(i), C::kStage);
+                tma_load_2d(base + i * C::kStage, &map_w, (kb0 + i) * kF8Block, n0, full(i));
+            }
+        }
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tslot), "r"(C::kCols) : "memory");
@@ -147,16 +222,11 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tslot));
-    if (S > 1) cluster_sync_all();  // every CTA of the cluster runs before any sends to it
+    if (S > 1) cluster_arrive_relaxed();  // "this CTA runs": a release here takes 1.9 us
 
     float acc[NT];
     if (warp == 4) {
-        if (lane == 0) {  // TMA: the weights of the first stages before the wait for the operation ahead
-            const int ahead = min(kb1 - kb0, C::kStages);
-            for (int i = 0; i < ahead; ++i) {
-                mbar_expect_tx(full(i), C::kStage);
-                tma_load_2d(base + i * C::kStage, &map_w, (kb0 + i) * kF8Block, n0, full(i));
-            }
+        if (lane == 0) {
             pdl_wait();
             for (int i = 0; i < ahead; ++i)
                 tma_load_2d(base + i * C::kStage + kF8WBytes, &map_h, (kb0 + i) * kF8Block, (int)m0, full(i));
@@ -172,99 +242,142 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             }
         }
     } else if (warp == 5) {
-        if (lane == 0) {
-            // instruction descriptor: D fp32, A and B e4m3, both K-major, N = NT, M = 128
-            const uint32_t idesc = (1u << 4) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(kF8Block >> 4) << 24);
-            for (int i = 0; i < kb1 - kb0; ++i) {
-                const int s = i % C::kStages, b = i % C::kBufs;
-                if ((i >= C::kBufs && !mbar_wait(tempty(b), (i / C::kBufs - 1) & 1)) || !mbar_wait(full(s), (i / C::kStages) & 1)) {
-                    failed = 1;
-                    break;
-                }
+        // the whole warp walks the loop and one lane issues: what an instruction names stays in uniform registers
+        // instruction descriptor: D fp32, A and B e4m3, both K-major, N = NT, M = 128
+        constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(kF8Block >> 4) << 24);
+        const uint64_t desc0 = umma_desc_sw128(0);
+        const bool one = elect_one();
+        uint32_t s = 0, s_phase = 0, b = 0, b_phase = 1;  // a buffer that was never used counts as read
+        bool ok = true;
+        for (int kb = kb0; kb < kb1 && ok;) {
+            ok = mbar_wait(tempty(b), b_phase);
+            // blocks up to the next multiple of kUnit, block q of it in columns q * NT
+            do {
+                ok = ok && mbar_wait(full(s), s_phase);
+                if (!ok) break;
                 tc_fence_after();
-                const uint64_t da = umma_desc_sw128(base + s * C::kStage), db = umma_desc_sw128(base + s * C::kStage + kF8WBytes);
+                const uint64_t da = desc0 + ((base + s * C::kStage) >> 4), db = da + (kF8WBytes >> 4);
+                if (one) {
 #pragma unroll
-                for (int k4 = 0; k4 < 4; ++k4)  // 32 bytes further along K per MMA
-                    tc_mma_f8(tmem + (uint32_t)(b * NT), da + 2 * k4, db + 2 * k4, idesc, k4 != 0);
-                tc_commit(empty(s));
-                tc_commit(tfull(b));
-            }
+                    for (int k4 = 0; k4 < 4; ++k4)  // 32 bytes further along K per MMA
+                        tc_mma_f8(tmem + (b * C::kUnit + kb % C::kUnit) * NT, da + 2 * k4, db + 2 * k4, idesc, k4 != 0);
+                    tc_commit(empty(s));
+                }
+                if (++s == C::kStages) s = 0, s_phase ^= 1u;
+                ++kb;
+            } while (kb < kb1 && kb % C::kUnit);
+            if (one && ok) tc_commit(tfull(b));
+            if (++b == C::kBufs) b = 0, b_phase ^= 1u;
         }
+        if (!ok) failed = 1;
     } else if (warp == 6) {
-        // products of the scales of four blocks at a time, as floats
-        const int width = (int)f8_scale_width(p.K);
+        // products of the scales of four blocks at a time, as floats; words are asked for AHEAD times four blocks before
+        constexpr int AHEAD = 3, R = (NT + 31) / 32;
+        const int width = (int)f8_scale_width(p.K), g0 = kb0 / 4, gn = (kb1 + 3) / 4;
+        uint32_t w[AHEAD + 1], h[AHEAD + 1][R];
+        auto fetch = [&](int g, uint32_t& fw, uint32_t (&fh)[R]) {
+            if (g >= gn) return;
+            fw = __ldcg(reinterpret_cast<const uint32_t*>(p.ws + (long long)blockIdx.y * width + 4 * g));
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int t = 32 * r + lane;
+                fh[r] = t < NT && m0 + t < p.M ? __ldcg(reinterpret_cast<const uint32_t*>(p.hs + (m0 + t) * width + 4 * g)) : 0u;
+            }
+        };
         pdl_wait();
-        for (int g = kb0 / 4, i = 0; g * 4 < kb1; ++g, ++i) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) fetch(g0 + i, w[i], h[i]);
+        for (int g = g0, i = 0; g < gn; ++g, ++i) {
             const int s = i % kF8Slots;
+            fetch(g + AHEAD, w[AHEAD], h[AHEAD]);
             if (i >= kF8Slots && !mbar_wait(sempty(s), (i / kF8Slots - 1) & 1)) {
                 failed = 1;
                 break;
             }
-            const uint32_t w = __ldcg(reinterpret_cast<const uint32_t*>(p.ws + (long long)blockIdx.y * width + 4 * g));
 #pragma unroll
-            for (int t = lane; t < NT; t += 32) {
-                const uint32_t h = m0 + t < p.M ? __ldcg(reinterpret_cast<const uint32_t*>(p.hs + (m0 + t) * width + 4 * g)) : 0u;
+            for (int r = 0; r < R; ++r) {
+                const int t = 32 * r + lane;
+                if (t < NT) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float f = f8_scale(w >> (8 * j) & 255u) * f8_scale(h >> (8 * j) & 255u);
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(sc0 + 4u * ((s * 4 + j) * NT + t)), "f"(f) : "memory");
+                    for (int j = 0; j < 4; ++j) {
+                        const float f = f8_scale(w[0] >> (8 * j) & 255u) * f8_scale(h[0][r] >> (8 * j) & 255u);
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(sc0 + 4u * ((s * 4 + j) * NT + t)), "f"(f) : "memory");
+                    }
                 }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(sfull(s));
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                w[k] = w[k + 1];
+#pragma unroll
+                for (int r = 0; r < R; ++r) h[k][r] = h[k + 1][r];
+            }
         }
     } else {
         // lane 32 w + l of tensor memory is row n0 + 32 w + l of the weights
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[j] = 0.f;
         bool ok = true;
+        uint32_t b = 0, b_phase = 0;
 #pragma unroll 1
-        for (int kb = kb0; kb < kb1; ++kb) {
-            const int i = kb - kb0, b = i % C::kBufs, gi = kb / 4 - kb0 / 4, s = gi % kF8Slots;
-            if (i == 0 || kb % 4 == 0) ok = mbar_wait(sfull(s), (gi / kF8Slots) & 1);
-            ok = ok && mbar_wait(tfull(b), (i / C::kBufs) & 1);
+        for (int kb = kb0; kb < kb1;) {
+            const int gi = kb / 4 - kb0 / 4, s = gi % kF8Slots, end = min(kb1, (kb / C::kUnit + 1) * C::kUnit);
+            if (kb == kb0 || kb % 4 == 0) ok = mbar_wait(sfull(s), (gi / kF8Slots) & 1);
+            ok = ok && mbar_wait(tfull(b), b_phase);
             if (!ok) {
                 failed = 1;
                 break;
             }
             tc_fence_after();
-            const uint32_t t0 = tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)(b * NT);
-            const uint32_t s0 = sc0 + 4u * ((s * 4 + kb % 4) * NT);
+            const uint32_t t0 = tmem + ((uint32_t)(warp * 32) << 16) + b * (C::kUnit * NT);
+            const uint32_t s0 = sc0 + 4u * (s * 4 * NT);
+            if constexpr (C::kUnit > 1) {
+                uint32_t t[C::kUnit][NT];
 #pragma unroll
-            for (int c = 0; c < NT; c += 16) {
-                uint32_t t[16];
-                tc_ld16(t0 + c, t);
+                for (int q = 0; q < C::kUnit; ++q)
+#pragma unroll
+                    for (int c = 0; c < NT; c += 16) tc_ld16(t0 + q * NT + c, &t[q][c]);
                 tc_wait_ld();
+                const int q0 = kb % C::kUnit, q1 = q0 + end - kb, g0 = kb / C::kUnit * C::kUnit % 4;
 #pragma unroll
-                for (int j = 0; j < 16; j += 4) {
-                    const uint4 f = lds16(s0 + 4u * (c + j));
-                    acc[c + j] = fmaf(__uint_as_float(t[j]), __uint_as_float(f.x), acc[c + j]);
-                    acc[c + j + 1] = fmaf(__uint_as_float(t[j + 1]), __uint_as_float(f.y), acc[c + j + 1]);
-                    acc[c + j + 2] = fmaf(__uint_as_float(t[j + 2]), __uint_as_float(f.z), acc[c + j + 2]);
-                    acc[c + j + 3] = fmaf(__uint_as_float(t[j + 3]), __uint_as_float(f.w), acc[c + j + 3]);
+                for (int q = 0; q < C::kUnit; ++q)
+                    if (q >= q0 && q < q1) f8_add_scaled<NT>(acc, t[q], s0 + 4u * ((g0 + q) * NT));
+            } else {
+#pragma unroll
+                for (int c = 0; c < NT; c += 16) {
+                    uint32_t t[16];
+                    tc_ld16(t0 + c, t);
+                    tc_wait_ld();
+                    f8_add_scaled<16>(acc + c, t, s0 + 4u * (kb % 4 * NT + c));
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive(tempty(b));
-                if (kb % 4 == 3) mbar_arrive(sempty(s));
+                if (end % 4 == 0) mbar_arrive(sempty(s));
             }
+            if (++b == C::kBufs) b = 0, b_phase ^= 1u;
+            kb = end;
         }
         pdl_wait();
-        if (S > 1) {
-            // token j belongs to CTA j / (NT / S): send it there
-            const int per = NT / S;
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const uint32_t to = cluster_map(part0 + 4u * ((rank * per + j % per) * kF8Block + tid), j / per);
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(acc[j]) : "memory");
-            }
-        }
     }
     __syncwarp();
-    if (S > 1) cluster_sync_all();
-    else __syncthreads();
+    if (S > 1) {
+        cluster_wait();  // every CTA of the cluster runs
+        // token j belongs to CTA j % S: send it there, as its (j / S)-th, beside those of the other CTAs
+        if (warp < 4) {
+            const uint32_t row = part0 + 4u * (rank * kF8Block + tid);
+            const int rows = (int)min((long long)NT, p.M - m0);
+            if (S == 2) f8_send<NT, 2>(acc, row, rows);
+            else if (S == 4) f8_send<NT, 4>(acc, row, rows);
+            else f8_send<NT, 8>(acc, row, rows);
+        }
+        cluster_sync_all();
+    } else {
+        __syncthreads();
+    }
     if (failed) {
         if (tid == 0) {
             if (p.status) *p.status = DEV_TIMEOUT;
@@ -272,20 +385,10 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         }
     } else if (warp < 4 && n0 + tid < p.N) {
         if (S > 1) {
-            const int per = NT / S;
-            for (int c = 0; c < per; c += 16) {
-                float v[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    v[j] = 0.f;
-                    for (int r = 0; r < S && c + j < per; ++r) {
-                        float u;
-                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(u) : "r"(part0 + 4u * ((r * per + c + j) * kF8Block + tid)) : "memory");
-                        v[j] += u;
-                    }
-                }
-                f8_put16<BF16>(p, m0 + rank * per + c, n0 + tid, v, per - c);
-            }
+            const uint32_t row = part0 + 4u * tid;
+            if (S == 2) f8_join<NT, 2, BF16>(p, m0 + rank, n0 + tid, row);
+            else if (S == 4) f8_join<NT, 4, BF16>(p, m0 + rank, n0 + tid, row);
+            else f8_join<NT, 8, BF16>(p, m0 + rank, n0 + tid, row);
         } else {
 #pragma unroll
             for (int j = 0; j < NT; j += 16) f8_put16<BF16>(p, m0 + j, n0 + tid, acc + j);
@@ -337,13 +440,6 @@ __device__ __forceinline__ void tc_cp_scales_pair(uint32_t taddr, uint32_t smem)
     asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(d) : "memory");
 }
 
-// true in one lane of a converged warp
-__device__ __forceinline__ bool elect_one()
-{
-    uint32_t one;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
-    return one != 0;
-}
 // mbar_wait for a barrier that the peer CTA arrives on too, after it has written what is read behind the wait
 __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
 {
@@ -407,7 +503,8 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     }
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();  // the peer's barriers exist before anything signals them
+    cluster_arrive_relaxed();  // behind the fence above: the peer's barriers exist before anything signals them
+    cluster_wait();
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tslot));
