@@ -58,57 +58,91 @@ __device__ __forceinline__ uint32_t f8_values2(uint32_t codes, float s)
     return pack_bf16(lo * s, hi * s);
 }
 
-// 16 bytes of a row as floats: four of fp32, eight of bf16.  Coherent loads past L1 (the operation ahead may have
-// written them, and under programmatic dependent launch been running when this kernel started).
+// 32 bytes of a row: eight values of fp32, sixteen of bf16.  One access where `wide` says that rows begin at 32-byte boundaries,
+// else two.  Coherent loads that L1 does not keep (the operation ahead may have written the data, and under programmatic
+// dependent launch been running when this kernel started).
+struct F8Raw {
+    uint32_t w[8];
+};
+__device__ __forceinline__ F8Raw f8_ld32(const void* p, bool wide)
+{
+    F8Raw r;
+    if (wide) {
+        asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
+                     : "l"(p)
+                     : "memory");
+    } else {
+        const uint4 a = __ldcg(reinterpret_cast<const uint4*>(p)), b = __ldcg(reinterpret_cast<const uint4*>(p) + 1);
+        r.w[0] = a.x, r.w[1] = a.y, r.w[2] = a.z, r.w[3] = a.w, r.w[4] = b.x, r.w[5] = b.y, r.w[6] = b.z, r.w[7] = b.w;
+    }
+    return r;
+}
+__device__ __forceinline__ void f8_st32(void* p, const uint32_t (&w)[8], bool wide)
+{
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
 template <typename T>
 struct F8In;
 template <>
 struct F8In<float> {
-    static constexpr int V = 4;
-    static __device__ __forceinline__ void load(const float* p, float (&v)[4])
+    static constexpr int V = 8;
+    static __device__ __forceinline__ void unpack(const F8Raw& r, float (&v)[8])
     {
-        const float4 f = __ldcg(reinterpret_cast<const float4*>(p));
-        v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i]);
     }
-    static __device__ __forceinline__ void store(float* p, const float (&v)[4])
+    static __device__ __forceinline__ void store(float* p, const float (&v)[8], bool wide)
     {
-        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
+        f8_st32(p, w, wide);
     }
     static __device__ __forceinline__ float kept(float v) { return v; }
 };
 template <>
 struct F8In<uint16_t> {  // bf16
-    static constexpr int V = 8;
-    static __device__ __forceinline__ void load(const uint16_t* p, float (&v)[8])
+    static constexpr int V = 16;
+    static __device__ __forceinline__ void unpack(const F8Raw& r, float (&v)[16])
     {
-        const uint4 u = __ldcg(reinterpret_cast<const uint4*>(p));
-        v[0] = bf16lo(u.x), v[1] = bf16hi(u.x), v[2] = bf16lo(u.y), v[3] = bf16hi(u.y);
-        v[4] = bf16lo(u.z), v[5] = bf16hi(u.z), v[6] = bf16lo(u.w), v[7] = bf16hi(u.w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[2 * i] = bf16lo(r.w[i]), v[2 * i + 1] = bf16hi(r.w[i]);
     }
-    static __device__ __forceinline__ void store(uint16_t* p, const float (&v)[8])
+    static __device__ __forceinline__ void store(uint16_t* p, const float (&v)[16], bool wide)
     {
-        *reinterpret_cast<uint4*>(p) =
-            make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+        f8_st32(p, w, wide);
     }
     static __device__ __forceinline__ float kept(float v) { return bf16f(f2bf(v)); }  // the value that store() leaves
 };
 
-template <int V>
-__device__ __forceinline__ uint32_t f8_absmax(const float (&v)[V])  // bits, not values: NaN counts as largest
+__device__ __forceinline__ float max_nan(float a, float b)  // a NaN wins
 {
-    uint32_t a = 0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) a = max(a, __float_as_uint(v[i]) & 0x7fffffffu);
-    return a;
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
 }
-// largest over the 128 / V lanes that hold a block
 template <int V>
-__device__ __forceinline__ uint32_t f8_block_max(uint32_t a)
+__device__ __forceinline__ uint32_t f8_absmax(const float (&v)[V])  // bits of the largest |v|; a NaN's are larger than any number's
 {
-    if (V == 4) return __reduce_max_sync(0xffffffffu, a);
+    float a[V / 2];
 #pragma unroll
-    for (int o = 64 / V; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
-    return a;
+    for (int i = 0; i < V / 2; ++i) a[i] = max_nan(fabsf(v[2 * i]), fabsf(v[2 * i + 1]));
+#pragma unroll
+    for (int n = V / 4; n > 0; n /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i) a[i] = max_nan(a[i], a[i + n]);
+    return __float_as_uint(a[0]) & 0x7fffffffu;
 }
 template <int V>
 __device__ __forceinline__ void f8_store_codes(unsigned char* p, const float (&v)[V], float r)
@@ -116,8 +150,8 @@ __device__ __forceinline__ void f8_store_codes(unsigned char* p, const float (&v
     uint32_t w[V / 4];
 #pragma unroll
     for (int i = 0; i < V / 4; ++i) w[i] = f8_codes4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], r);
-    if (V == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
-    else *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[V / 4 - 1]);
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 // A warp's 32 V columns of a row, from column k0 (a multiple of 128; lane l holds columns k0 + V l ..): codes and scale
 // bytes, and zeros behind the row's last block.  Lanes beyond K hold zeros.
@@ -125,57 +159,72 @@ template <int V>
 __device__ __forceinline__ void f8_store_row_part(const float (&v)[V], int k0, int K, int width, unsigned char* codes,
                                                   unsigned char* scales)
 {
-    const int lane = threadIdx.x & 31, k = k0 + V * lane;
-    const uint32_t e = f8_scale_byte(f8_block_max<V>(f8_absmax<V>(v)));
+    const int k = k0 + V * (threadIdx.x & 31);
+    uint32_t a = f8_absmax<V>(v);
+#pragma unroll
+    for (int o = 64 / V; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));  // the 128 / V lanes of a block
+    const uint32_t e = f8_scale_byte(a);
     if (k < K) f8_store_codes<V>(codes + k, v, f8_inverse(e));
     if (k % kF8Block == 0 && k / kF8Block < width) scales[k / kF8Block] = k < K ? (unsigned char)e : 0;
 }
 
 // ------------------------------------------------------------------ rows and weights -> 8 bits, and back
-// Rows: a warp takes 512 columns of a row, one word of scales.  grid.x * 8 warps cover the parts of all rows.
+// Rows: a warp takes 1024 columns of a row.  grid.x * 8 warps cover the parts of all rows.
+constexpr int kF8RowPart = 1024;
 template <typename T>
-__global__ void __launch_bounds__(256) quantize_f8_rows_kernel(const T* __restrict__ x, int64_t ldx, int K, int parts, long long items,
+__global__ void __launch_bounds__(256) quantize_f8_rows_kernel(const T* __restrict__ x, int64_t ldx, int K, int parts, long long items, int wide,
                                                                unsigned char* __restrict__ codes, unsigned char* __restrict__ scales)
 {
-    constexpr int V = F8In<T>::V, STEP = 32 * V, N = 512 / STEP;
+    constexpr int V = F8In<T>::V, STEP = 32 * V, N = kF8RowPart / STEP;
     pdl_launch_dependents();
     pdl_wait();
     const long long it = (long long)blockIdx.x * 8 + threadIdx.x / 32;
     if (it >= items) return;  // whole warps
     const long long m = it / parts;
-    const int k0 = (int)(it - m * parts) * 512, lane = threadIdx.x & 31, width = 4 * parts;
-    float v[N][V];
+    const int k0 = (int)(it - m * parts) * kF8RowPart, lane = threadIdx.x & 31, width = (int)f8_scale_width(K);
+    F8Raw raw[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int k = k0 + i * STEP + V * lane;
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[i][j] = 0.f;
-        if (k < K) F8In<T>::load(x + m * ldx + k, v[i]);  // K is a multiple of 16: the octet is in or out
+        raw[i] = F8Raw{};
+        if (k < K) raw[i] = f8_ld32(x + m * ldx + k, wide);  // K is a multiple of 16: all of the piece is in or out
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) f8_store_row_part<V>(v[i], k0 + i * STEP, K, width, codes + m * K, scales + m * width);
+    for (int i = 0; i < N; ++i) {
+        float v[V];
+        F8In<T>::unpack(raw[i], v);
+        if (k0 + i * STEP < K || k0 + i * STEP < width * kF8Block) f8_store_row_part<V>(v, k0 + i * STEP, K, width, codes + m * K, scales + m * width);
+    }
 }
 
-// Weights: a CTA takes a block of 128 x 128.  grid (blocks of a row of them, rows of blocks).
+// Weights: a CTA takes a block of 128 x 128.  grid (blocks of a row of them, rows of blocks).  Bound by the loads of a CTA's only
+// block: pieces stay as they were loaded (32 registers of bf16), so that more CTAs fit an SM (11008 x 4096: 31 us, 4.4 TB/s; as
+// floats 60).
 template <typename T>
-__global__ void __launch_bounds__(256) quantize_f8_weights_kernel(const T* __restrict__ x, int64_t ldx, int M, int K,
-                                                                  unsigned char* __restrict__ codes, unsigned char* __restrict__ scales)
+__global__ void __launch_bounds__(256, F8In<T>::V == 16 ? 3 : 2)
+quantize_f8_weights_kernel(const T* __restrict__ x, int64_t ldx, int M, int K, int wide, unsigned char* __restrict__ codes,
+                           unsigned char* __restrict__ scales)
 {
     constexpr int V = F8In<T>::V, LANES = kF8Block / V, ROWS = 256 / LANES, N = kF8Block / ROWS;  // ROWS rows a step
     __shared__ uint32_t wmax[8];
     pdl_wait();
     const int tid = threadIdx.x, k = blockIdx.x * kF8Block + V * (tid % LANES);
     const long long m0 = (long long)blockIdx.y * kF8Block + tid / LANES;
-    float v[N][V];
+    F8Raw raw[N];
     uint32_t a = 0;
+    const T* src = x + m0 * ldx + k;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[i][j] = 0.f;
-        if (k < K && m0 + i * ROWS < M) F8In<T>::load(x + (m0 + i * ROWS) * ldx + k, v[i]);
+        raw[i] = F8Raw{};
+        if (k < K && m0 + i * ROWS < M) raw[i] = f8_ld32(src, wide);
+        src += ROWS * ldx;
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) a = max(a, f8_absmax<V>(v[i]));
+    for (int i = 0; i < N; ++i) {
+        float v[V];
+        F8In<T>::unpack(raw[i], v);
+        a = max(a, f8_absmax<V>(v));
+    }
     a = __reduce_max_sync(0xffffffffu, a);
     if ((tid & 31) == 0) wmax[tid >> 5] = a;
     __syncthreads();
@@ -183,44 +232,64 @@ __global__ void __launch_bounds__(256) quantize_f8_weights_kernel(const T* __res
     for (int w = 0; w < 8; ++w) a = max(a, wmax[w]);
     const uint32_t e = f8_scale_byte(a);
     const float r = f8_inverse(e);
+    unsigned char* dst = codes + m0 * K + k;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (k < K && m0 + i * ROWS < M) f8_store_codes<V>(codes + (m0 + i * ROWS) * K + k, v[i], r);
+    for (int i = 0; i < N; ++i) {
+        float v[V];
+        F8In<T>::unpack(raw[i], v);
+        if (k < K && m0 + i * ROWS < M) f8_store_codes<V>(dst, v, r);
+        dst += (int64_t)ROWS * K;
+    }
     const int width = (int)f8_scale_width(K);
     unsigned char* row = scales + (long long)blockIdx.y * width;
     if (tid == 0) row[blockIdx.x] = (unsigned char)e;
     if (blockIdx.x + 1 == gridDim.x && tid > 0 && (int)blockIdx.x + tid < width) row[blockIdx.x + tid] = 0;  // at most 3
 }
 
-// Codes and scales -> bf16 [M, K].  A warp takes 512 columns of a row; `shift`: log2 of a block's rows.
+// Codes and scales -> bf16 [M, K].  A warp takes 2048 columns of a row, a lane 16 neighbouring ones at a time: 32 bytes of
+// output.  `shift`: log2 of a block's rows.
+constexpr int kF8ExpandPart = 2048;
 __global__ void __launch_bounds__(256) expand_f8_kernel(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
-                                                        int K, int parts, long long items, int shift, int signal, uint16_t* __restrict__ out)
+                                                        int K, int parts, long long items, int shift, int signal, int wide,
+                                                        uint16_t* __restrict__ out)
 {
+    constexpr int N = kF8ExpandPart / 512;
     if (signal) pdl_launch_dependents();
     pdl_wait();
     const long long it = (long long)blockIdx.x * 8 + threadIdx.x / 32;
     if (it >= items) return;
     const long long m = it / parts;
-    const int k = (int)(it - m * parts) * 512 + 16 * (threadIdx.x & 31);
-    if (k >= K) return;
-    const float s = f8_scale(__ldcg(scales + (m >> shift) * (4ll * parts) + k / kF8Block));
-    const uint4 c = __ldcg(reinterpret_cast<const uint4*>(codes + m * K + k));
-    uint4 lo, hi;
-    lo.x = f8_values2(c.x, s), lo.y = f8_values2(c.x >> 16, s), lo.z = f8_values2(c.y, s), lo.w = f8_values2(c.y >> 16, s);
-    hi.x = f8_values2(c.z, s), hi.y = f8_values2(c.z >> 16, s), hi.z = f8_values2(c.w, s), hi.w = f8_values2(c.w >> 16, s);
-    uint4* dst = reinterpret_cast<uint4*>(out + m * K + k);
-    dst[0] = lo;
-    dst[1] = hi;
+    const int k0 = (int)(it - m * parts) * kF8ExpandPart + 16 * (threadIdx.x & 31);
+    const unsigned char *row = scales + (m >> shift) * f8_scale_width(K), *src = codes + m * K + k0;
+    uint4 c[N];
+    uint32_t e[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (k0 + 512 * i < K) {
+            c[i] = __ldcg(reinterpret_cast<const uint4*>(src + 512 * i));
+            e[i] = __ldcg(row + (k0 + 512 * i) / kF8Block);
+        }
+    uint16_t* dst = out + m * K + k0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (k0 + 512 * i < K) {
+            const float s = f8_scale(e[i]);
+            const uint32_t u[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[2 * j] = f8_values2(u[j], s), w[2 * j + 1] = f8_values2(u[j] >> 16, s);
+            f8_st32(dst + 512 * i, w, wide);
+        }
 }
 
 // ------------------------------------------------------------------ RMSNorm with the residual's addition, into 8 bits
 // x' = x + d rounded to x's type, y = x' / sqrt(mean x'^2 + eps) * gain, sums in fp32.  A CTA takes a row; with NV > 0 a
 // thread keeps its NV pieces of it in registers, else (rows too long for that) x' is read again, from x_out where it was
-// written.  d and x_out may be null, x_out may be x.
+// written.  d and x_out may be null, x_out may be x or d.
 template <typename T, typename TD, int NV>
-__global__ void __launch_bounds__(NV == 8 ? 512 : 1024)
-rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, int64_t ldo, const uint16_t* __restrict__ gain, int D,
-                  float eps, unsigned char* __restrict__ codes, unsigned char* __restrict__ scales)
+__global__ void __launch_bounds__(NV >= 4 ? 512 : 1024)
+rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, int64_t ldo, const uint16_t* gain, int D, float eps, int wide,
+                  unsigned char* __restrict__ codes, unsigned char* __restrict__ scales)
 {
     constexpr int V = F8In<T>::V, KEEP = NV > 0 ? NV : 1;
     __shared__ float part[32];
@@ -233,20 +302,21 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
     if (x_out) x_out += m * ldo;
     const int width = (int)f8_scale_width(D), cover = width * kF8Block;  // columns with a scale byte
     auto fetch = [&](int k, float (&v)[V]) {
-        F8In<T>::load(x + k, v);
+        F8In<T>::unpack(f8_ld32(x + k, wide), v);
         if (d) {
             float a[V];
             if constexpr (F8In<TD>::V == V) {
-                F8In<TD>::load(d + k, a);
-            } else if constexpr (V == 8) {  // fp32 d for bf16 x
-                float lo[4], hi[4];
-                F8In<float>::load(d + k, lo);
-                F8In<float>::load(d + k + 4, hi);
+                F8In<TD>::unpack(f8_ld32(d + k, wide), a);
+            } else if constexpr (V == 16) {  // fp32 d for bf16 x
+                float lo[8], hi[8];
+                F8In<float>::unpack(f8_ld32(d + k, wide), lo);
+                F8In<float>::unpack(f8_ld32(d + k + 8, wide), hi);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) a[j] = lo[j], a[4 + j] = hi[j];
+                for (int j = 0; j < 8; ++j) a[j] = lo[j], a[8 + j] = hi[j];
             } else {
-                const uint2 u = __ldcg(reinterpret_cast<const uint2*>(d + k));
+                const uint4 u = __ldcg(reinterpret_cast<const uint4*>(d + k));
                 a[0] = bf16lo(u.x), a[1] = bf16hi(u.x), a[2] = bf16lo(u.y), a[3] = bf16hi(u.y);
+                a[4] = bf16lo(u.z), a[5] = bf16hi(u.z), a[6] = bf16lo(u.w), a[7] = bf16hi(u.w);
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = F8In<T>::kept(v[j] + a[j]);
@@ -254,10 +324,10 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
     };
     float v[KEEP][V], ss = 0.f;
     auto square = [&](const float (&u)[V]) {
-        float s = 0.f;
+        float s[2] = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < V; ++j) s = fmaf(u[j], u[j], s);
-        ss += s;
+        for (int j = 0; j < V; ++j) s[j & 1] = fmaf(u[j], u[j], s[j & 1]);
+        ss += s[0] + s[1];
     };
     if (NV > 0) {
 #pragma unroll
@@ -270,13 +340,13 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
             const int k = (i * T0 + tid) * V;
-            if (x_out && k < D) F8In<T>::store(x_out + k, v[i]);
+            if (x_out && k < D) F8In<T>::store(x_out + k, v[i], wide);
             square(v[i]);
         }
     } else {
         for (int k = tid * V; k < D; k += T0 * V) {
             fetch(k, v[0]);
-            if (x_out) F8In<T>::store(x_out + k, v[0]);
+            if (x_out) F8In<T>::store(x_out + k, v[0], wide);
             square(v[0]);
         }
     }
@@ -290,15 +360,16 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
     const float r = 1.0f / sqrtf(ss / (float)D + eps);
     auto finish = [&](int k, float (&u)[V]) {  // whole warps
         if (k < D) {
-            float g[V];
-            if constexpr (V == 8) {
-                F8In<uint16_t>::load(gain + k, g);
-            } else {
-                const uint2 w = __ldcg(reinterpret_cast<const uint2*>(gain + k));
-                g[0] = bf16lo(w.x), g[1] = bf16hi(w.x), g[2] = bf16lo(w.y), g[3] = bf16hi(w.y);
-            }
 #pragma unroll
-            for (int j = 0; j < V; ++j) u[j] = u[j] * r * g[j];
+            for (int j = 0; j < V; j += 8) {
+                const uint4 g = ld_reuse16(gain + k + j);
+                const uint32_t w[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    u[j + 2 * q] = u[j + 2 * q] * r * bf16lo(w[q]);
+                    u[j + 2 * q + 1] = u[j + 2 * q + 1] * r * bf16hi(w[q]);
+                }
+            }
         }
         f8_store_row_part<V>(u, k - V * (tid & 31), D, width, codes + m * D, scales + m * width);
     };
@@ -311,7 +382,7 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
 #pragma unroll
             for (int j = 0; j < V; ++j) v[0][j] = 0.f;
             if (k < D) {
-                if (x_out) F8In<T>::load(x_out + k, v[0]);  // this thread wrote it
+                if (x_out) F8In<T>::unpack(f8_ld32(x_out + k, wide), v[0]);  // this thread wrote it
                 else fetch(k, v[0]);
             }
             finish(k, v[0]);
@@ -320,10 +391,25 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
 }
 
 // ------------------------------------------------------------------ SwiGLU into 8 bits
-// y = gate / (1 + exp(-gate)) * up.  A warp takes 512 features of a row.
+// y = gate / (1 + exp(-gate)) * up.  exp(-g) = 2^t (1 + d ln 2), t = -g log2 e rounded, d what it was rounded by (the product's
+// error, which the fma gives exactly, and that of log2 e), so that the exponential is off by little more than ex2.approx,
+// 2^-22 of its value, however large g.  (With expf and a division the kernel issued 2.75 instructions a cycle and took
+// 86 us where this takes XX, 4096 x 11008 bf16.)  From t = 126 on (gates below -87.3) the
+// reciprocal is not a normal number and counts as 0.
+__device__ __forceinline__ float f8_silu_times(float g, float u)
+{
+    const float c = -1.44269502e+00f, c_lo = -1.92596299e-08f, ln2 = 0.693147182f;  // -log2 e in two parts
+    const float t = g * c, d = fmaf(g, c_lo, fmaf(g, c, -t));
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fminf(t, 127.f)));
+    e = fmaf(e, d * ln2, e);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return g * r * u;
+}
+// A warp takes 512 features of a row.
 template <typename T>
 __global__ void __launch_bounds__(256) swiglu_f8_kernel(const T* __restrict__ gate, const T* __restrict__ up, int64_t ld, int F, int parts,
-                                                        long long items, unsigned char* __restrict__ codes,
+                                                        long long items, int wide, unsigned char* __restrict__ codes,
                                                         unsigned char* __restrict__ scales)
 {
     constexpr int V = F8In<T>::V, STEP = 32 * V, N = 512 / STEP;
@@ -333,22 +419,24 @@ __global__ void __launch_bounds__(256) swiglu_f8_kernel(const T* __restrict__ ga
     if (it >= items) return;
     const long long m = it / parts;
     const int k0 = (int)(it - m * parts) * 512, lane = threadIdx.x & 31, width = 4 * parts;
-    float g[N][V], u[N][V];
+    F8Raw g[N], u[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int k = k0 + i * STEP + V * lane;
-#pragma unroll
-        for (int j = 0; j < V; ++j) g[i][j] = u[i][j] = 0.f;
+        g[i] = u[i] = F8Raw{};
         if (k < F) {
-            F8In<T>::load(gate + m * ld + k, g[i]);
-            F8In<T>::load(up + m * ld + k, u[i]);
+            g[i] = f8_ld32(gate + m * ld + k, wide);
+            u[i] = f8_ld32(up + m * ld + k, wide);
         }
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+        float a[V], b[V];
+        F8In<T>::unpack(g[i], a);
+        F8In<T>::unpack(u[i], b);
 #pragma unroll
-        for (int j = 0; j < V; ++j) g[i][j] = g[i][j] / (1.0f + expf(-g[i][j])) * u[i][j];
-        f8_store_row_part<V>(g[i], k0 + i * STEP, F, width, codes + m * F, scales + m * width);
+        for (int j = 0; j < V; ++j) a[j] = f8_silu_times(a[j], b[j]);
+        f8_store_row_part<V>(a, k0 + i * STEP, F, width, codes + m * F, scales + m * width);
     }
 }
 

@@ -2197,7 +2197,11 @@ static bool f8_rows_ok(const void* p, int type, int64_t ld, int M, int K)  // ro
     return aligned16(p) && f8_type_ok(type) && (M == 1 || (ld >= K && ld % f8_pieces(type) == 0));
 }
 static bool f8_held_ok(const void* codes, const void* scales) { return aligned16(codes) && scales && ((uintptr_t)scales & 3u) == 0; }
-static int f8_parts(int K) { return (K + 511) / 512; }  // a warp's share of a row: a word of scale bytes
+// rows that begin at 32-byte boundaries (element counts of 32 bytes: twice f8_pieces)
+static bool f8_wide(const void* p, int type, int64_t ld, int M)
+{
+    return !p || (((uintptr_t)p & 31u) == 0 && (M == 1 || ld % (2 * f8_pieces(type)) == 0));
+}
 
 size_t ls_op_f8_scale_bytes(int32_t M, int32_t K, int32_t block_rows)
 {
@@ -2213,18 +2217,19 @@ int ls_op_quantize_f8(const void* x, int32_t type, int64_t ldx, int32_t M, int32
         return LS_ERR_INVALID_ARG;
     const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
     unsigned char *c = (unsigned char*)codes, *e = (unsigned char*)scales;
+    const int wide = f8_wide(x, type, ldx, M);
     if (block_rows == 1) {
-        const int parts = f8_parts(K);
+        const int parts = (K + kF8RowPart - 1) / kF8RowPart;
         const long long items = (long long)M * parts;
         if ((items + 7) / 8 > 0x7fffffff) return LS_ERR_UNSUPPORTED;
         const dim3 grid((unsigned)((items + 7) / 8));
-        if (type == LS_F32) LS_CK(launch(lc, quantize_f8_rows_kernel<float>, grid, dim3(256), 0, (const float*)x, ldx, K, parts, items, c, e));
-        else LS_CK(launch(lc, quantize_f8_rows_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)x, ldx, K, parts, items, c, e));
+        if (type == LS_F32) LS_CK(launch(lc, quantize_f8_rows_kernel<float>, grid, dim3(256), 0, (const float*)x, ldx, K, parts, items, wide, c, e));
+        else LS_CK(launch(lc, quantize_f8_rows_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)x, ldx, K, parts, items, wide, c, e));
         return LS_OK;
     }
     const dim3 grid((K + kF8Block - 1) / kF8Block, (M + kF8Block - 1) / kF8Block);
-    if (type == LS_F32) LS_CK(launch(lc, quantize_f8_weights_kernel<float>, grid, dim3(256), 0, (const float*)x, ldx, M, K, c, e));
-    else LS_CK(launch(lc, quantize_f8_weights_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)x, ldx, M, K, c, e));
+    if (type == LS_F32) LS_CK(launch(lc, quantize_f8_weights_kernel<float>, grid, dim3(256), 0, (const float*)x, ldx, M, K, wide, c, e));
+    else LS_CK(launch(lc, quantize_f8_weights_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)x, ldx, M, K, wide, c, e));
     return weights_written((cudaStream_t)stream);
 }
 
@@ -2232,11 +2237,11 @@ int ls_op_expand_f8(const void* codes, const void* scales, int32_t M, int32_t K,
 {
     if (!f8_shape_ok(M, K) || !f8_held_ok(codes, scales) || !aligned16(out) || (block_rows != 1 && block_rows != kF8Block))
         return LS_ERR_INVALID_ARG;
-    const int parts = f8_parts(K), weights = block_rows == kF8Block;
+    const int parts = (K + kF8ExpandPart - 1) / kF8ExpandPart, weights = block_rows == kF8Block;
     const long long items = (long long)M * parts;
     if ((items + 7) / 8 > 0x7fffffff) return LS_ERR_UNSUPPORTED;
     LS_CK(launch(LaunchCtx{(cudaStream_t)stream, g_op_chain}, expand_f8_kernel, dim3((unsigned)((items + 7) / 8)), dim3(256), 0,
-                 (const unsigned char*)codes, (const unsigned char*)scales, K, parts, items, weights ? 7 : 0, !weights, (uint16_t*)out));
+                 (const unsigned char*)codes, (const unsigned char*)scales, K, parts, items, weights ? 7 : 0, !weights, (int)f8_wide(out, LS_BF16, K, M), (uint16_t*)out));
     return weights ? weights_written((cudaStream_t)stream) : LS_OK;
 }
 
@@ -2263,7 +2268,7 @@ struct NormArgs {
     void *x, *x_out;
     const void *d, *gain;
     int64_t ldx, ldd, ldo;
-    int M, D;
+    int M, D, wide;
     float eps;
     unsigned char *codes, *scales;
 };
@@ -2272,23 +2277,22 @@ template <typename T, typename TD, int NV>
 int rmsnorm_f8_launch_nv(const NormArgs& a, int threads, const LaunchCtx& lc)
 {
     LS_CK(launch(lc, rmsnorm_f8_kernel<T, TD, NV>, dim3((unsigned)a.M), dim3(threads), 0, (const T*)a.x, a.ldx, (const TD*)a.d, a.ldd,
-                 (T*)a.x_out, a.ldo, (const uint16_t*)a.gain, a.D, a.eps, a.codes, a.scales));
+                 (T*)a.x_out, a.ldo, (const uint16_t*)a.gain, a.D, a.eps, a.wide, a.codes, a.scales));
     return LS_OK;
 }
 
 template <typename T, typename TD>
 int rmsnorm_f8_launch(const NormArgs& a, const LaunchCtx& lc)
 {
-    const int pieces = (int)f8_scale_width(a.D) * kF8Block / F8In<T>::V;  // 16-byte pieces of a row, whole warps of them
-    // A row is one CTA's. Few rows leave SMs idle: as many threads as there are pieces; with many, 256 threads of 4 to
-    // 8 pieces keep more loads in flight.
+    const int pieces = (int)f8_scale_width(a.D) * kF8Block / F8In<T>::V;  // 32-byte pieces of a row (fp32), whole warps of them
+    // A row is one CTA's.  Few rows leave SMs idle: as many threads as there are pieces, up to 1024; with many, 256 threads of
+    // two pieces and more: several rows an SM, whose loads and stores overlap.
     int threads = a.M <= 296 ? 1024 : 256;
-    while (threads < 512 && threads * 8 < pieces) threads *= 2;
+    while (threads < 512 && threads * 4 < pieces) threads *= 2;
     while (threads > 64 && threads / 2 >= pieces) threads /= 2;
     if (pieces <= threads) return rmsnorm_f8_launch_nv<T, TD, 1>(a, threads, lc);
     if (pieces <= 2 * threads) return rmsnorm_f8_launch_nv<T, TD, 2>(a, threads, lc);
-    if (pieces <= 4 * threads) return rmsnorm_f8_launch_nv<T, TD, 4>(a, threads, lc);
-    if (pieces <= 8 * threads && threads <= 512) return rmsnorm_f8_launch_nv<T, TD, 8>(a, threads, lc);
+    if (pieces <= 4 * threads && threads <= 512) return rmsnorm_f8_launch_nv<T, TD, 4>(a, threads, lc);
     return rmsnorm_f8_launch_nv<T, TD, 0>(a, threads, lc);
 }
 
@@ -2402,7 +2406,8 @@ int ls_op_rmsnorm_f8(const void* x, int32_t x_type, int64_t ldx, const void* del
     if (!f8_shape_ok(M, D) || !f8_rows_ok(x, x_type, ldx, M, D) || (delta && !f8_rows_ok(delta, delta_type, ldd, M, D)) ||
         (x_out && !f8_rows_ok(x_out, x_type, ldo, M, D)) || !aligned16(gain) || !f8_held_ok(codes, scales))
         return LS_ERR_INVALID_ARG;
-    const NormArgs a = {const_cast<void*>(x), x_out, delta, gain, ldx, ldd, ldo, M, D, eps, (unsigned char*)codes, (unsigned char*)scales};
+    const int wide = f8_wide(x, x_type, ldx, M) && f8_wide(delta, delta_type, ldd, M) && f8_wide(x_out, x_type, ldo, M);
+    const NormArgs a = {const_cast<void*>(x), x_out, delta, gain, ldx, ldd, ldo, M, D, wide, eps, (unsigned char*)codes, (unsigned char*)scales};
     const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
     const bool d32 = !delta || delta_type == LS_F32;
     if (x_type == LS_F32) return d32 ? rmsnorm_f8_launch<float, float>(a, lc) : rmsnorm_f8_launch<float, uint16_t>(a, lc);
@@ -2414,13 +2419,13 @@ int ls_op_swiglu_f8(const void* gate, const void* up, int32_t type, int64_t ld, 
 {
     if (!f8_shape_ok(M, F) || !f8_rows_ok(gate, type, ld, M, F) || !aligned16(up) || !f8_held_ok(codes, scales)) return LS_ERR_INVALID_ARG;
     const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
-    const int parts = f8_parts(F);
+    const int parts = (F + 511) / 512, wide = f8_wide(gate, type, ld, M) && f8_wide(up, type, ld, M);
     const long long items = (long long)M * parts;
     if ((items + 7) / 8 > 0x7fffffff) return LS_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)((items + 7) / 8));
     unsigned char *c = (unsigned char*)codes, *e = (unsigned char*)scales;
-    if (type == LS_F32) LS_CK(launch(lc, swiglu_f8_kernel<float>, grid, dim3(256), 0, (const float*)gate, (const float*)up, ld, F, parts, items, c, e));
-    else LS_CK(launch(lc, swiglu_f8_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)gate, (const uint16_t*)up, ld, F, parts, items, c, e));
+    if (type == LS_F32) LS_CK(launch(lc, swiglu_f8_kernel<float>, grid, dim3(256), 0, (const float*)gate, (const float*)up, ld, F, parts, items, wide, c, e));
+    else LS_CK(launch(lc, swiglu_f8_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)gate, (const uint16_t*)up, ld, F, parts, items, wide, c, e));
     return LS_OK;
 }
 
