@@ -580,46 +580,49 @@ def ls_op_f8_scale_bytes(M, K, block_rows=1):
     return lib().ls_op_f8_scale_bytes(M, K, block_rows)
 
 
-def _held(codes, scales, block_rows, dev, what):
+def _held(codes, scales, M, K, block_rows, dev, what):
     """device pointers of codes float8_e4m3fn [M, K] and their scales (uint8, ls_op_f8_scale_bytes of them)"""
-    M, K = codes.shape
     if scales.numel() < ls_op_f8_scale_bytes(M, K, block_rows):
-        raise LsError(LS_ERR_CAPACITY, f"{what}: scales")
-    return _arg(codes, _torch.f8, dev, what + " codes"), _arg(scales, _torch.u8, dev, what + " scales")
+        raise LsError(LS_ERR_CAPACITY, what + ": scales")
+    return _arg(codes, _torch.f8, dev, what), _arg(scales, _torch.u8, dev, what)
 
 
 def _strided(t, shape, dev, what):
     """(device pointer, type, row stride) of a bf16 or fp32 tensor of some shape [M, K] with contiguous columns"""
-    kind = LS_BF16 if t.dtype is _torch.bf16 else LS_F32 if t.dtype is _torch.f32 else _bad(f"{what}: bf16 or fp32")
-    if t.shape != shape or t.get_device() != dev or (t.stride(1) != 1 and shape[1] > 1):
-        _bad(f"{what}: a tensor {tuple(shape)} with contiguous columns, on the CUDA device of the others")
-    return t.data_ptr(), kind, t.stride(0)
+    dtype, stride = t.dtype, t.stride()
+    kind = LS_F32 if dtype is _torch.f32 else LS_BF16 if dtype is _torch.bf16 else -1
+    if kind < 0 or t.shape != shape or t.get_device() != dev or (stride[1] != 1 and shape[1] > 1):
+        _bad(f"{what}: a bf16 or fp32 tensor {tuple(shape)} with contiguous columns is needed, on the CUDA device of the others")
+    return t.data_ptr(), kind, stride[0]
 
 
 def ls_op_quantize_f8(x, codes, scales, block_rows=1):
     """x [M, K], bf16 or fp32 -> codes (float8_e4m3fn [M, K]) and scales (uint8), of one row's or 128 rows' blocks of 128 columns"""
-    (M, K), dev = codes.shape, codes.get_device()
-    c, s = _held(codes, scales, block_rows, dev, "ls_op_quantize_f8")
-    xp, kind, ld = _strided(x, codes.shape, dev, "x")
+    shape, dev = codes.shape, codes.get_device()
+    M, K = shape
+    c, s = _held(codes, scales, M, K, block_rows, dev, "ls_op_quantize_f8")
+    xp, kind, ld = _strided(x, shape, dev, "x")
     _ck(lib().ls_op_quantize_f8(xp, kind, ld, M, K, block_rows, c, s, _stream_on(dev)), "ls_op_quantize_f8")
 
 
 def ls_op_expand_f8(codes, scales, out, block_rows=1):
     """codes and scales -> bf16 [M, K]"""
-    (M, K), dev = codes.shape, codes.get_device()
-    c, s = _held(codes, scales, block_rows, dev, "ls_op_expand_f8")
-    if out.shape != codes.shape:
+    shape, dev = codes.shape, codes.get_device()
+    M, K = shape
+    c, s = _held(codes, scales, M, K, block_rows, dev, "ls_op_expand_f8")
+    if out.shape != shape:
         _bad("ls_op_expand_f8: out")
     _ck(lib().ls_op_expand_f8(c, s, M, K, block_rows, _arg(out, _torch.bf16, dev, "out"), _stream_on(dev)), "ls_op_expand_f8")
 
 
 def ls_op_rmsnorm_f8(x, gain, eps, codes, scales, delta=None, x_out=None):
     """codes and scales of the RMSNorm of x + delta [M, D], which goes to x_out (may be x) if it is given"""
-    (M, D), dev = codes.shape, codes.get_device()
-    c, s = _held(codes, scales, 1, dev, "ls_op_rmsnorm_f8")
-    xp, kind, ldx = _strided(x, codes.shape, dev, "x")
-    dp, dkind, ldd = (None, LS_F32, 0) if delta is None else _strided(delta, codes.shape, dev, "delta")
-    op, okind, ldo = (None, kind, 0) if x_out is None else _strided(x_out, codes.shape, dev, "x_out")
+    shape, dev = codes.shape, codes.get_device()
+    M, D = shape
+    c, s = _held(codes, scales, M, D, 1, dev, "ls_op_rmsnorm_f8")
+    xp, kind, ldx = _strided(x, shape, dev, "x")
+    dp, dkind, ldd = (None, LS_F32, 0) if delta is None else _strided(delta, shape, dev, "delta")
+    op, okind, ldo = (xp, kind, ldx) if x_out is x else (None, kind, 0) if x_out is None else _strided(x_out, shape, dev, "x_out")
     if okind != kind or gain.numel() != D:
         _bad("ls_op_rmsnorm_f8: x_out of x's type, gain [D]")
     _ck(lib().ls_op_rmsnorm_f8(xp, kind, ldx, dp, dkind, ldd, op, ldo, _arg(gain, _torch.bf16, dev, "gain"), M, D, eps, c, s, _stream_on(dev)),
@@ -628,9 +631,11 @@ def ls_op_rmsnorm_f8(x, gain, eps, codes, scales, delta=None, x_out=None):
 
 def ls_op_swiglu_f8(gate, up, codes, scales):
     """codes and scales of silu(gate) * up [M, F]; gate and up of one type and row stride"""
-    (M, F), dev = codes.shape, codes.get_device()
-    c, s = _held(codes, scales, 1, dev, "ls_op_swiglu_f8")
-    (gp, kind, ld), (upp, ukind, uld) = _strided(gate, codes.shape, dev, "gate"), _strided(up, codes.shape, dev, "up")
+    shape, dev = codes.shape, codes.get_device()
+    M, F = shape
+    c, s = _held(codes, scales, M, F, 1, dev, "ls_op_swiglu_f8")
+    gp, kind, ld = _strided(gate, shape, dev, "gate")
+    upp, ukind, uld = _strided(up, shape, dev, "up")
     if kind != ukind or (ld != uld and M > 1):
         _bad("ls_op_swiglu_f8: gate and up of one type and row stride")
     _ck(lib().ls_op_swiglu_f8(gp, upp, kind, ld, M, F, c, s, _stream_on(dev)), "ls_op_swiglu_f8")
@@ -642,13 +647,14 @@ def ls_op_linear_f8(w_codes, w_scales, h_codes, h_scales, out, add=None, status=
     (N, K), (M, Kh), dev = w_codes.shape, h_codes.shape, h_codes.get_device()
     if K != Kh:
         _bad("ls_op_linear_f8: columns of w and h")
-    wc, ws = _held(w_codes, w_scales, 128, dev, "w")
-    hc, hs = _held(h_codes, h_scales, 1, dev, "h")
+    wc, ws = _held(w_codes, w_scales, N, K, 128, dev, "ls_op_linear_f8: w")
+    hc, hs = _held(h_codes, h_scales, M, K, 1, dev, "ls_op_linear_f8: h")
     op, kind, ldo = _strided(out, (M, N), dev, "out")
-    ap, akind, lda = (None, kind, 0) if add is None else _strided(add, (M, N), dev, "add")
+    ap, akind, lda = (None, kind, 0) if add is None else (op, kind, ldo) if add is out else _strided(add, (M, N), dev, "add")
     if akind != kind:
         _bad("ls_op_linear_f8: add of out's type")
-    _ck(lib().ls_op_linear_f8(wc, ws, hc, hs, M, N, K, op, kind, ldo, ap, lda, _status(status, dev), _stream_on(dev)), "ls_op_linear_f8")
+    _ck(lib().ls_op_linear_f8(wc, ws, hc, hs, M, N, K, op, kind, ldo, ap, lda, None if status is None else _status(status, dev), _stream_on(dev)),
+        "ls_op_linear_f8")
 
 
 def ls_op_accept(draft, verified, d, state, out_ids, accepted):

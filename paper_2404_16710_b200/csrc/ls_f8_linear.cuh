@@ -82,12 +82,12 @@ __device__ __forceinline__ float lds_f32(uint32_t addr)
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
 }
-// out[m .. m + 15, n] = v (+ add), `most` of them; all of add is asked for first, as out may be add
+// out[m .. m + 15, n] = v (+ add); all of add is asked for first, as out may be add
 template <bool BF16>
-__device__ __forceinline__ void f8_put16(const F8Linear& p, long long m, int n, const float* v, int most = 16)
+__device__ __forceinline__ void f8_put16(const F8Linear& p, long long m, int n, const float* v)
 {
     using T = std::conditional_t<BF16, uint16_t, float>;
-    const int rows = (int)min((long long)min(most, 16), p.M - m);
+    const int rows = (int)min(16ll, p.M - m);
     T* dst = reinterpret_cast<T*>(p.out) + m * p.ldo + n;
     float a[16];
 #pragma unroll
@@ -411,15 +411,21 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 // a tile's sums are read while the next one's are made.
 // Persistent: pair p takes tiles p, p + P, ..., tokens fastest (pairs that run side by side share weights in L2).
 constexpr int kF8PairTokens = 240;
-constexpr int kF8PairStages = 7;
-constexpr int kF8PairStage = kF8WBytes + kF8PairTokens / 2 * kF8Block;  // a CTA's weights, and half of the tokens
+constexpr int kF8PairRing = 7 * (kF8WBytes + kF8PairTokens / 2 * kF8Block);  // as many stages as fit, 7 at 240 tokens
+constexpr int kF8PairMaxStages = 12;
+// a stage: a CTA's weights, and half of the tokens
+__host__ __device__ constexpr int f8_pair_stage(int nt) { return kF8WBytes + nt / 2 * kF8Block; }
+__host__ __device__ constexpr int f8_pair_stages(int nt)
+{
+    return kF8PairRing / f8_pair_stage(nt) < kF8PairMaxStages ? kF8PairRing / f8_pair_stage(nt) : kF8PairMaxStages;
+}
 constexpr int kF8PairSlots = 4;
 constexpr int kF8PairChunk = 16;             // blocks along K that are summed in tensor memory
 constexpr int kF8PairSlot = 3 * 512;        // scale words of 128 rows of weights, of 256 tokens
 constexpr int kF8PairScaleCols = 2 * kF8PairTokens;  // two sets of 16 columns behind the accumulators
 constexpr int kF8PairThreads = 640;         // warps 0-15: sums and stores, 16: TMA, 17: MMA, 18, 19: scales
-constexpr size_t kF8PairSmem = (size_t)kF8PairStages * kF8PairStage + kF8PairSlots * kF8PairSlot + 1024 + 512;
-static_assert(kF8PairStage % 1024 == 0 && kF8PairSmem <= kF8SmemMax && kF8PairScaleCols + 32 <= 512, "shared and tensor memory");
+constexpr size_t kF8PairSmem = (size_t)kF8PairRing + kF8PairSlots * kF8PairSlot + 1024 + 512;
+static_assert(f8_pair_stage(16) % 1024 == 0 && kF8PairSmem <= kF8SmemMax && kF8PairScaleCols + 32 <= 512, "shared and tensor memory");
 
 // D[tmem] (+)= (A * scales)(B * scales)^T, e4m3, a scale for 32 columns of a row
 __device__ __forceinline__ void tc_mma_f8_scaled_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa,
@@ -458,6 +464,20 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
     return false;
 }
 
+// whether the phase is complete, without waiting
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+
 template <bool BF16>
 __global__ void __launch_bounds__(kF8PairThreads, 1)
 linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h, const F8Linear p,
@@ -466,14 +486,15 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     extern __shared__ unsigned char f8_raw[];
     __shared__ int failed;
     const uint32_t base = (smem_u32(f8_raw) + 1023u) & ~1023u;
-    const uint32_t sc0 = base + kF8PairStages * kF8PairStage, bars = sc0 + kF8PairSlots * kF8PairSlot;
+    const uint32_t sc0 = base + kF8PairRing, bars = sc0 + kF8PairSlots * kF8PairSlot;
+    const int stages = f8_pair_stages(nt), stage = f8_pair_stage(nt);
     auto full = [&](int s) { return bars + 8u * s; };
-    auto empty = [&](int s) { return bars + 8u * (kF8PairStages + s); };
-    auto accf = [&](int b) { return bars + 8u * (2 * kF8PairStages + b); };
-    auto acce = [&](int b) { return bars + 8u * (2 * kF8PairStages + 2 + b); };
-    auto sfull = [&](int b) { return bars + 8u * (2 * kF8PairStages + 4 + b); };
-    auto sempty = [&](int b) { return bars + 8u * (2 * kF8PairStages + 4 + kF8PairSlots + b); };
-    const uint32_t tslot = bars + 8u * (2 * kF8PairStages + 4 + 2 * kF8PairSlots);
+    auto empty = [&](int s) { return bars + 8u * (kF8PairMaxStages + s); };
+    auto accf = [&](int b) { return bars + 8u * (2 * kF8PairMaxStages + b); };
+    auto acce = [&](int b) { return bars + 8u * (2 * kF8PairMaxStages + 2 + b); };
+    auto sfull = [&](int b) { return bars + 8u * (2 * kF8PairMaxStages + 4 + b); };
+    auto sempty = [&](int b) { return bars + 8u * (2 * kF8PairMaxStages + 4 + kF8PairSlots + b); };
+    const uint32_t tslot = bars + 8u * (2 * kF8PairMaxStages + 4 + 2 * kF8PairSlots);
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     uint32_t rank;
@@ -482,7 +503,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     const int nkb = (p.K + kF8Block - 1) / kF8Block, groups = (nkb + 3) / 4;
 
     if (tid == 0) {
-        for (int s = 0; s < kF8PairStages; ++s) {
+        for (int s = 0; s < stages; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
         }
@@ -512,21 +533,21 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     if (warp == 16) {
         if (lane == 0) {
             const uint32_t bytes = 2u * (uint32_t)(kF8WBytes + nt / 2 * kF8Block);
-            int it = 0;
+            uint32_t s = 0, phase = 1;  // a stage that was never used counts as free
             bool ok = true;
             for (int t = pair; t < n_tiles && ok; t += n_pairs) {
                 const int w_row = (t / token_tiles * 2 + (int)rank) * kF8Block, h_row = t % token_tiles * nt + (int)rank * (nt / 2);
-                for (int kb = 0; kb < nkb; ++kb, ++it) {
-                    const int s = it % kF8PairStages;
-                    if (it >= kF8PairStages && !mbar_wait(empty(s), (it / kF8PairStages - 1) & 1)) {
+                for (int kb = 0; kb < nkb; ++kb) {
+                    if (!mbar_wait(empty(s), phase)) {
                         failed = 1;
                         ok = false;
                         break;
                     }
                     if (rank == 0) mbar_expect_tx(full(s), bytes);
                     const uint32_t lead = full(s) & kPeerBitMask;
-                    tma_load_2d_pair(base + s * kF8PairStage, &map_w, kb * kF8Block, w_row, lead);
-                    tma_load_2d_pair(base + s * kF8PairStage + kF8WBytes, &map_h, kb * kF8Block, h_row, lead);
+                    tma_load_2d_pair(base + s * stage, &map_w, kb * kF8Block, w_row, lead);
+                    tma_load_2d_pair(base + s * stage + kF8WBytes, &map_h, kb * kF8Block, h_row, lead);
+                    if (++s == stages) s = 0, phase ^= 1u;
                 }
             }
         }
@@ -539,7 +560,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             const bool one = elect_one();
             uint32_t s = 0, s_phase = 0, slot = 0, slot_phase = 0, set = 0;
             uint32_t b = 0, b_phase = 1;  // an accumulator that was never used counts as read
-            bool ok = true;
+            bool ok = true, ready = false;
             for (int t = pair; t < n_tiles && ok; t += n_pairs) {
                 for (int kb = 0; kb < nkb && ok; kb += 4) {
                     const uint32_t d = tmem + b * kF8PairTokens;
@@ -570,21 +591,23 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         if (kb + q >= nkb) break;
-                        if (!mbar_wait(full(s), s_phase)) {
+                        if (!ready && !mbar_wait(full(s), s_phase)) {
                             failed = 1;
                             ok = false;
                             break;
                         }
                         tc_fence_after();
-                        const uint64_t da = desc0 + ((base + s * kF8PairStage) >> 4), db = da + (kF8WBytes >> 4);
+                        const uint64_t da = desc0 + ((base + s * stage) >> 4), db = da + (kF8WBytes >> 4);
+                        const uint32_t s_now = s;
+                        if (++s == stages) s = 0, s_phase ^= 1u;
+                        ready = mbar_test(full(s), s_phase);  // the next stage: its answer comes while the products are issued
                         if (one) {
                             const uint32_t id = idesc | (uint32_t)q << 4 | (uint32_t)q << 29;
 #pragma unroll
                             for (int k4 = 0; k4 < 4; ++k4)
                                 tc_mma_f8_scaled_pair(d, da + 2 * k4, db + 2 * k4, id, sf, sf + 8, (kb % kF8PairChunk | q | k4) != 0);
-                            tc_commit_pair(empty(s));
+                            tc_commit_pair(empty(s_now));
                         }
-                        if (++s == kF8PairStages) s = 0, s_phase ^= 1u;
                     }
                     if (ok && ((kb + 4) % kF8PairChunk == 0 || kb + 4 >= nkb)) {
                         if (one) tc_commit_pair(accf(b));
@@ -645,14 +668,23 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         for (int t = pair; t < n_tiles && ok; t += n_pairs) {
             const int n = (t / token_tiles * 2 + (int)rank) * kF8Block + (warp & 3) * 32 + lane;
             const long long m0 = (long long)(t % token_tiles) * nt + c0;
-            if (p.add) {  // on its way into L2 while the products are made
-                using T = std::conditional_t<BF16, uint16_t, float>;
-                const int n_warp = n - lane;
-                for (int j = lane; j < cols; j += 32)
-                    if (m0 + j < p.M && n_warp < p.N)
-                        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const T*>(p.add) + (m0 + j) * p.lda + n_warp));
-            }
+            // sums begin with add, which comes while the first products are made
             float sum[64];
+            const int rows = (int)min((long long)cols, p.M - m0);
+#pragma unroll
+            for (int j = 0; j < 64; ++j) sum[j] = 0.f;
+            if (p.add && n < p.N) {
+                using T = std::conditional_t<BF16, uint16_t, float>;
+                const T* src = reinterpret_cast<const T*>(p.add) + m0 * p.lda + n;
+#pragma unroll
+                for (int j = 0; j < 64; ++j) {
+                    if (j < rows) {
+                        if constexpr (BF16) sum[j] = bf16f(__ldcg(src));
+                        else sum[j] = __ldcg(src);
+                    }
+                    src += p.lda;
+                }
+            }
             for (int kb = 0; kb < nkb; kb += kF8PairChunk) {
                 if (!mbar_wait(accf(b), b_phase)) {
                     failed = 1;
@@ -668,7 +700,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                         tc_ld16(tacc + c, v);
                         tc_wait_ld();
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) sum[c + j] = kb ? sum[c + j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
+                        for (int j = 0; j < 16; ++j) sum[c + j] += __uint_as_float(v[j]);
                     }
                 }
                 tc_fence_before();
@@ -678,9 +710,16 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 if (b == 0) b_phase ^= 1u;
             }
             if (ok && n < p.N) {
+                using T = std::conditional_t<BF16, uint16_t, float>;
+                T* dst = reinterpret_cast<T*>(p.out) + m0 * p.ldo + n;
 #pragma unroll
-                for (int c = 0; c < 64; c += 16)
-                    if (c < cols) f8_put16<BF16>(p, m0 + c, n, sum + c, cols - c);
+                for (int j = 0; j < 64; ++j) {
+                    if (j < rows) {
+                        if constexpr (BF16) *dst = f2bf(sum[j]);
+                        else *dst = sum[j];
+                    }
+                    dst += p.ldo;
+                }
             }
         }
     }

@@ -3,8 +3,8 @@
 Conversions are exact: bytes have to be equal.  Tolerances of the computed results, derived:
 * linear: products of two codes are exact (4 by 4 significant bits).  Every one of the K / 32 tensor-core sums, the
   K / 128 scaled additions and the 8 that join parts is off by at most one unit of its result's last place (the tensor
-  cores may truncate), 2^-23, of a partial sum that is at most sum |h w|; the addition of `add` likewise 2^-24 of its
-  result; a bf16 result is rounded once, 2^-8 of its value.
+  cores may truncate), 2^-23, of a partial sum that is at most sum |h w|; sums that begin with `add` are rounded when a part of 2048
+  columns is added, K / 2048 + 1 times by 2^-24 of at most |add| + sum |h w|; a bf16 result is rounded once, 2^-8 of its value.
 * rmsnorm, swiglu: y is off by at most delta before it is rounded to a code, so the scale byte is that of y (1 - delta) or
   of y (1 + delta), and the code lies between those of y (1 - delta) and y (1 + delta) under that scale.
   rmsnorm: a sum of D squares of which no more than D / 64 + 32 are added in a chain, half of that (the root), the
@@ -289,7 +289,7 @@ def linear_tol(K, spread, out_type, ref, base=None):
     tol = (K / 32 + K / 128 + 12) * 2.0 ** -23 * spread
     total = ref if base is None else ref + base
     if base is not None:
-        tol = tol + 2.0 ** -24 * total.abs()
+        tol = tol + (K / 2048 + 1) * 2.0 ** -24 * (base.abs() + spread)
     return tol + (2.0 ** -8 * total.abs() if out_type is BF16 else 0.0)
 
 
