@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(256) quantize_f8_rows_kernel(const T* __restri
     for (int i = 0; i < N; ++i) {
         float v[V];
         F8In<T>::unpack(raw[i], v);
-        if (k0 + i * STEP < K || k0 + i * STEP < width * kF8Block) f8_store_row_part<V>(v, k0 + i * STEP, K, width, codes + m * K, scales + m * width);
+        if (k0 + i * STEP < width * kF8Block) f8_store_row_part<V>(v, k0 + i * STEP, K, width, codes + m * K, scales + m * width);
     }
 }
 

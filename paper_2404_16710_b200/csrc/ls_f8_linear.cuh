@@ -164,7 +164,7 @@ __device__ __forceinline__ void f8_join(const F8Linear& p, long long m, int n, u
     }
 }
 
-// grid (S, tiles of 128 weight rows, tiles of NT tokens), clusters (S, 1, 1)
+// grid (S, tiles of 128 weight rows), clusters (S, 1, 1); at most NT tokens
 template <int NT, bool BF16, int CTAS>
 __global__ void __launch_bounds__(kF8Threads, CTAS)
 linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h, const F8Linear p)
@@ -186,7 +186,6 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int S = gridDim.x, rank = blockIdx.x;  // S: 1, 2, 4 or 8
     const int n0 = blockIdx.y * kF8Block;
-    const long long m0 = (long long)blockIdx.z * NT;
     const int nkb = (p.K + kF8Block - 1) / kF8Block;
     const int kb0 = (int)((long long)nkb * rank / S), kb1 = (int)((long long)nkb * (rank + 1) / S);
 
@@ -224,12 +223,13 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tslot));
     if (S > 1) cluster_arrive_relaxed();  // "this CTA runs": a release here takes 1.9 us
 
+    pdl_wait();  // before any bounded wait: the operation ahead may take its time
+
     float acc[NT];
     if (warp == 4) {
         if (lane == 0) {
-            pdl_wait();
             for (int i = 0; i < ahead; ++i)
-                tma_load_2d(base + i * C::kStage + kF8WBytes, &map_h, (kb0 + i) * kF8Block, (int)m0, full(i));
+                tma_load_2d(base + i * C::kStage + kF8WBytes, &map_h, (kb0 + i) * kF8Block, 0, full(i));
             for (int i = ahead; i < kb1 - kb0; ++i) {
                 const int s = i % C::kStages;
                 if (!mbar_wait(empty(s), (i / C::kStages - 1) & 1)) {
@@ -238,7 +238,7 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                 }
                 mbar_expect_tx(full(s), C::kStage);
                 tma_load_2d(base + s * C::kStage, &map_w, (kb0 + i) * kF8Block, n0, full(s));
-                tma_load_2d(base + s * C::kStage + kF8WBytes, &map_h, (kb0 + i) * kF8Block, (int)m0, full(s));
+                tma_load_2d(base + s * C::kStage + kF8WBytes, &map_h, (kb0 + i) * kF8Block, 0, full(s));
             }
         }
     } else if (warp == 5) {
@@ -281,10 +281,9 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int t = 32 * r + lane;
-                fh[r] = t < NT && m0 + t < p.M ? __ldcg(reinterpret_cast<const uint32_t*>(p.hs + (m0 + t) * width + 4 * g)) : 0u;
+                fh[r] = t < p.M ? __ldcg(reinterpret_cast<const uint32_t*>(p.hs + (long long)t * width + 4 * g)) : 0u;
             }
         };
-        pdl_wait();
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) fetch(g0 + i, w[i], h[i]);
         for (int g = g0, i = 0; g < gn; ++g, ++i) {
@@ -361,7 +360,6 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             if (++b == C::kBufs) b = 0, b_phase ^= 1u;
             kb = end;
         }
-        pdl_wait();
     }
     __syncwarp();
     if (S > 1) {
@@ -369,10 +367,9 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         // token j belongs to CTA j % S: send it there, as its (j / S)-th, beside those of the other CTAs
         if (warp < 4) {
             const uint32_t row = part0 + 4u * (rank * kF8Block + tid);
-            const int rows = (int)min((long long)NT, p.M - m0);
-            if (S == 2) f8_send<NT, 2>(acc, row, rows);
-            else if (S == 4) f8_send<NT, 4>(acc, row, rows);
-            else f8_send<NT, 8>(acc, row, rows);
+            if (S == 2) f8_send<NT, 2>(acc, row, p.M);
+            else if (S == 4) f8_send<NT, 4>(acc, row, p.M);
+            else f8_send<NT, 8>(acc, row, p.M);
         }
         cluster_sync_all();
     } else {
@@ -386,12 +383,12 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     } else if (warp < 4 && n0 + tid < p.N) {
         if (S > 1) {
             const uint32_t row = part0 + 4u * tid;
-            if (S == 2) f8_join<NT, 2, BF16>(p, m0 + rank, n0 + tid, row);
-            else if (S == 4) f8_join<NT, 4, BF16>(p, m0 + rank, n0 + tid, row);
-            else f8_join<NT, 8, BF16>(p, m0 + rank, n0 + tid, row);
+            if (S == 2) f8_join<NT, 2, BF16>(p, rank, n0 + tid, row);
+            else if (S == 4) f8_join<NT, 4, BF16>(p, rank, n0 + tid, row);
+            else f8_join<NT, 8, BF16>(p, rank, n0 + tid, row);
         } else {
 #pragma unroll
-            for (int j = 0; j < NT; j += 16) f8_put16<BF16>(p, m0 + j, n0 + tid, acc + j);
+            for (int j = 0; j < NT; j += 16) f8_put16<BF16>(p, j, n0 + tid, acc + j);
         }
     }
     tc_fence_before();
@@ -558,7 +555,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             const uint32_t idesc = ((uint32_t)(nt >> 3) << 17) | (1u << 23) | (2u << 27);
             const uint64_t desc0 = umma_desc_sw128(0);
             const bool one = elect_one();
-            uint32_t s = 0, s_phase = 0, slot = 0, slot_phase = 0, set = 0;
+            uint32_t s = 0, s_phase = 0, slot = 0, slot_phase = 0, old_phase = 1;
             uint32_t b = 0, b_phase = 1;  // an accumulator that was never used counts as read
             bool ok = true, ready = false;
             for (int t = pair; t < n_tiles && ok; t += n_pairs) {
@@ -578,16 +575,19 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                         ok = false;
                         break;
                     }
+                    // the columns that the copies overwrite: the products of the group before the last have read them
+                    if (!mbar_wait(sempty((slot + kF8PairSlots - 2) % kF8PairSlots), old_phase)) {
+                        failed = 1;
+                        ok = false;
+                        break;
+                    }
                     tc_fence_after();
-                    const uint32_t sf = tmem + kF8PairScaleCols + set * 16u, src = sc0 + slot * kF8PairSlot;
+                    const uint32_t sf = tmem + kF8PairScaleCols + (slot & 1u) * 16u, src = sc0 + slot * kF8PairSlot;
                     if (one) {
                         tc_cp_scales_pair(sf, src);
                         tc_cp_scales_pair(sf + 8, src + 512);
                         if (nt > 128) tc_cp_scales_pair(sf + 12, src + 1024);
-                        tc_commit_pair(sempty(slot));
                     }
-                    set ^= 1u;
-                    if (++slot == kF8PairSlots) slot = 0, slot_phase ^= 1u;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         if (kb + q >= nkb) break;
@@ -609,6 +609,9 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                             tc_commit_pair(empty(s_now));
                         }
                     }
+                    if (one && ok) tc_commit_pair(sempty(slot));  // copies and products of these four blocks are done
+                    if (++slot == kF8PairSlots) slot = 0, slot_phase ^= 1u;
+                    if (slot == 2) old_phase ^= 1u;
                     if (ok && ((kb + 4) % kF8PairChunk == 0 || kb + 4 >= nkb)) {
                         if (one) tc_commit_pair(accf(b));
                         b ^= 1u;

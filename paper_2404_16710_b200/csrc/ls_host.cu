@@ -2304,7 +2304,7 @@ int linear_f8_launch(const void* wc, const void* hc, const F8Linear& p, int S, c
     LS_TRY(make_f8_map(&mw, wc, (uint64_t)p.N, (uint64_t)p.K, kF8Block));
     LS_TRY(make_f8_map(&mh, hc, (uint64_t)p.M, (uint64_t)p.K, NT));
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(S, (p.N + kF8Block - 1) / kF8Block, (p.M + NT - 1) / NT);
+    cfg.gridDim = dim3(S, (p.N + kF8Block - 1) / kF8Block);
     cfg.blockDim = dim3(kF8Threads);
     cfg.dynamicSmemBytes = F8Cfg<NT, CTAS>::kSmem;
     cfg.stream = lc.st;
@@ -2367,7 +2367,7 @@ int linear_f8_pair_launch(const void* wc, const void* hc, const F8Linear& p, con
         if (!best || cost < best) best = cost, nt = n, token_tiles = real;
     }
     const long long n_tiles = (long long)w_tiles * token_tiles;
-    if (n_tiles > 0x7fffffff) return LS_ERR_UNSUPPORTED;
+    if (n_tiles > 0x7fffffff - 1024) return LS_ERR_UNSUPPORTED;
     CUtensorMap mw, mh;
     LS_TRY(make_f8_map(&mw, wc, (uint64_t)p.N, (uint64_t)p.K, kF8Block));
     LS_TRY(make_f8_map(&mh, hc, (uint64_t)p.M, (uint64_t)p.K, nt / 2));
