@@ -122,18 +122,22 @@ constexpr int kF8WBytes = kF8Block * kF8Block;
 constexpr int kF8SmemMax = 227 * 1024;
 constexpr int kF8Slots = 4;  // slots of scales, one word of scale bytes (four blocks) each
 
+constexpr int kF8MaxStages = 11;
 template <int NT, int CTAS>  // CTAs that fit an SM
 struct F8Cfg {
     static constexpr int kStage = kF8WBytes + NT * kF8Block;
     static constexpr int kScale = kF8Slots * 4 * NT * 4;      // floats [slot][block][token]
-    static constexpr int kPart = NT * kF8Block * 4;           // what the cluster's CTAs send: [rank][token][row]
-    static constexpr int kFixed = 1024 + kScale + kPart + 512;
-    static constexpr int kFit = (kF8SmemMax / CTAS - 1024 - kFixed) / kStage;
-    static constexpr int kStages = kFit < 11 ? kFit : 11;
+    static constexpr int kPart = NT * kF8Block * 4;           // what the cluster's CTAs send: [token / S][rank][row]
     static constexpr int kUnit = NT <= 16 ? 4 : NT <= 32 ? 2 : 1;  // blocks along K that change hands together
     static constexpr int kBufs = NT == 64 ? 4 : 2;            // tensor-memory buffers of kUnit * NT columns
     static constexpr int kCols = kBufs * kUnit * NT;
-    static constexpr size_t kSmem = (size_t)kStages * kStage + kFixed;
+    static constexpr int fixed(int S) { return 1024 + kScale + (S > 1 ? kPart : 0) + 512; }
+    static constexpr int stages(int S)
+    {
+        const int fit = (kF8SmemMax / CTAS - 1024 - fixed(S)) / kStage;
+        return fit < kF8MaxStages ? fit : kF8MaxStages;
+    }
+    static constexpr size_t smem(int S) { return (size_t)stages(S) * kStage + fixed(S); }
 };
 
 // sums of the first `rows` tokens to the CTAs that own them: token j is the (j / S)-th of CTA j % S
@@ -167,31 +171,31 @@ __device__ __forceinline__ void f8_join(const F8Linear& p, long long m, int n, u
 // grid (S, tiles of 128 weight rows), clusters (S, 1, 1); at most NT tokens
 template <int NT, bool BF16, int CTAS>
 __global__ void __launch_bounds__(kF8Threads, CTAS)
-linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h, const F8Linear p)
+linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h, const F8Linear p, const int stages)
 {
     using C = F8Cfg<NT, CTAS>;
     extern __shared__ unsigned char f8_raw[];
     __shared__ int failed;
     const uint32_t base = (smem_u32(f8_raw) + 1023u) & ~1023u;
-    const uint32_t sc0 = base + C::kStages * C::kStage, part0 = sc0 + C::kScale, bars = part0 + C::kPart;
+    const int S = gridDim.x, rank = blockIdx.x;  // S: 1, 2, 4 or 8
+    const uint32_t sc0 = base + stages * C::kStage, part0 = sc0 + C::kScale, bars = part0 + (S > 1 ? C::kPart : 0);
     auto full = [&](int s) { return bars + 8u * s; };
-    auto empty = [&](int s) { return bars + 8u * (C::kStages + s); };
-    auto tfull = [&](int b) { return bars + 8u * (2 * C::kStages + b); };
-    auto tempty = [&](int b) { return bars + 8u * (2 * C::kStages + 4 + b); };
-    auto sfull = [&](int b) { return bars + 8u * (2 * C::kStages + 8 + b); };
-    auto sempty = [&](int b) { return bars + 8u * (2 * C::kStages + 12 + b); };
-    const uint32_t tslot = bars + 8u * (2 * C::kStages + 16);
-    static_assert(8 * (2 * C::kStages + 17) <= 512, "barriers");
+    auto empty = [&](int s) { return bars + 8u * (kF8MaxStages + s); };
+    auto tfull = [&](int b) { return bars + 8u * (2 * kF8MaxStages + b); };
+    auto tempty = [&](int b) { return bars + 8u * (2 * kF8MaxStages + 4 + b); };
+    auto sfull = [&](int b) { return bars + 8u * (2 * kF8MaxStages + 8 + b); };
+    auto sempty = [&](int b) { return bars + 8u * (2 * kF8MaxStages + 12 + b); };
+    const uint32_t tslot = bars + 8u * (2 * kF8MaxStages + 16);
+    static_assert(8 * (2 * kF8MaxStages + 17) <= 512, "barriers");
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-    const int S = gridDim.x, rank = blockIdx.x;  // S: 1, 2, 4 or 8
     const int n0 = blockIdx.y * kF8Block;
     const int nkb = (p.K + kF8Block - 1) / kF8Block;
     const int kb0 = (int)((long long)nkb * rank / S), kb1 = (int)((long long)nkb * (rank + 1) / S);
 
-    const int ahead = min(kb1 - kb0, C::kStages);
+    const int ahead = min(kb1 - kb0, stages);
     if (warp == 4) {  // barriers, and at once the weights of the first stages: they need not wait for the operation ahead
-        if (lane < 2 * C::kStages) mbar_init(bars + 8u * lane, 1);
+        if (lane < 2 * kF8MaxStages) mbar_init(bars + 8u * lane, 1);
         if (lane < C::kBufs) {
             mbar_init(tfull(lane), 1);
             mbar_init(tempty(lane), 4);
@@ -231,8 +235,8 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             for (int i = 0; i < ahead; ++i)
                 tma_load_2d(base + i * C::kStage + kF8WBytes, &map_h, (kb0 + i) * kF8Block, 0, full(i));
             for (int i = ahead; i < kb1 - kb0; ++i) {
-                const int s = i % C::kStages;
-                if (!mbar_wait(empty(s), (i / C::kStages - 1) & 1)) {
+                const int s = i % stages;
+                if (!mbar_wait(empty(s), (i / stages - 1) & 1)) {
                     failed = 1;
                     break;
                 }
@@ -263,7 +267,7 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                         tc_mma_f8(tmem + (b * C::kUnit + kb % C::kUnit) * NT, da + 2 * k4, db + 2 * k4, idesc, k4 != 0);
                     tc_commit(empty(s));
                 }
-                if (++s == C::kStages) s = 0, s_phase ^= 1u;
+                if (++s == stages) s = 0, s_phase ^= 1u;
                 ++kb;
             } while (kb < kb1 && kb % C::kUnit);
             if (one && ok) tc_commit(tfull(b));

@@ -2299,14 +2299,15 @@ int rmsnorm_f8_launch(const NormArgs& a, const LaunchCtx& lc)
 template <int NT, bool BF16, int CTAS>
 int linear_f8_launch(const void* wc, const void* hc, const F8Linear& p, int S, const LaunchCtx& lc)
 {
-    LS_TRY((allow_smem<linear_f8_kernel<NT, BF16, CTAS>>(F8Cfg<NT, CTAS>::kSmem)));
+    using C = F8Cfg<NT, CTAS>;
+    LS_TRY((allow_smem<linear_f8_kernel<NT, BF16, CTAS>>(std::max(C::smem(1), C::smem(2)))));
     CUtensorMap mw, mh;
     LS_TRY(make_f8_map(&mw, wc, (uint64_t)p.N, (uint64_t)p.K, kF8Block));
     LS_TRY(make_f8_map(&mh, hc, (uint64_t)p.M, (uint64_t)p.K, NT));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(S, (p.N + kF8Block - 1) / kF8Block);
     cfg.blockDim = dim3(kF8Threads);
-    cfg.dynamicSmemBytes = F8Cfg<NT, CTAS>::kSmem;
+    cfg.dynamicSmemBytes = C::smem(S);
     cfg.stream = lc.st;
     cudaLaunchAttribute at[3];
     int n = 0;
@@ -2324,7 +2325,7 @@ int linear_f8_launch(const void* wc, const void* hc, const F8Linear& p, int S, c
     }
     cfg.attrs = at;
     cfg.numAttrs = n;
-    LS_CK(cudaLaunchKernelEx(&cfg, linear_f8_kernel<NT, BF16, CTAS>, mw, mh, p));
+    LS_CK(cudaLaunchKernelEx(&cfg, linear_f8_kernel<NT, BF16, CTAS>, mw, mh, p, C::stages(S)));
     return LS_OK;
 }
 
@@ -2381,9 +2382,8 @@ int linear_f8_choose(const void* wc, const void* hc, const F8Linear& p, const La
 {
     const int w_tiles = (p.N + kF8Block - 1) / kF8Block, kb = (p.K + kF8Block - 1) / kF8Block;
     // CTA pairs from 129 tokens on, or from 65 where there is more than one tile of weights an SM (172 tiles, K = 4096, 65 / 128
-    // tokens: 29.0 / 30.8 us, 34.9 / 35.6 without; 96 tiles 17.7 / 19.2, 18.4 / 18.9; 32 tiles 14.4 / 14.6, 11.1 / 13.3), or from 33
-    // where there are more than four (1002 tiles, 33 tokens: 89.7, 96.1; 172 tiles 28.2, 28.0)
-    if (p.M > 128 || (p.M > 64 && w_tiles > 148) || (p.M > 32 && w_tiles > 592)) return linear_f8_pair_launch<BF16>(wc, hc, p, lc);
+    // tokens: 29.0 / 30.8 us, 34.9 / 35.6 without; 96 tiles 17.7 / 19.2, 18.4 / 18.9; 32 tiles 14.4 / 14.6, 11.1 / 13.3)
+    if (p.M > 128 || (p.M > 64 && w_tiles > 148)) return linear_f8_pair_launch<BF16>(wc, hc, p, lc);
     const int NT = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
     // CTAs that share a tile: as many as keep one CTA an SM and two blocks a CTA.  A function of the matrix alone: it enters a
     // row's arithmetic.  (32 tiles, K = 4096, one token, 1 / 2 / 4 / 8 CTAs: 10.9 / 8.6 / 7.6 / 9.1 us; 86 tiles: 12.8 / 12.4 / 13.9 / 15.5,
@@ -2392,7 +2392,7 @@ int linear_f8_choose(const void* wc, const void* hc, const F8Linear& p, const La
     while (S < 8 && w_tiles * 2 * S <= 148 && kb >= 4 * S) S *= 2;
     return NT == 16 ? linear_f8_launch<16, BF16, 2>(wc, hc, p, S, lc)
            : NT == 32 ? linear_f8_launch<32, BF16, 2>(wc, hc, p, S, lc)
-           : NT == 64 ? linear_f8_launch<64, BF16, 1>(wc, hc, p, S, lc)
+           : NT == 64 ? linear_f8_launch<64, BF16, 2>(wc, hc, p, S, lc)
                       : linear_f8_launch<128, BF16, 1>(wc, hc, p, S, lc);
 }
 
