@@ -503,21 +503,22 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     const int n_pairs = (int)gridDim.x / 2, pair = (int)blockIdx.x / 2;
     const int nkb = (p.K + kF8Block - 1) / kF8Block, groups = (nkb + 3) / 4;
 
-    if (tid == 0) {
-        for (int s = 0; s < stages; ++s) {
-            mbar_init(full(s), 1);
-            mbar_init(empty(s), 1);
+    if (warp == 16) {
+        if (lane < kF8PairMaxStages) {
+            mbar_init(full(lane), 1);
+            mbar_init(empty(lane), 1);
         }
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(accf(b), 1);
-            mbar_init(acce(b), 32);  // sixteen storing warps in each CTA of the pair
+        if (lane < 2) {
+            mbar_init(accf(lane), 1);
+            mbar_init(acce(lane), 32);  // sixteen storing warps in each CTA of the pair
         }
-        for (int b = 0; b < kF8PairSlots; ++b) {
-            mbar_init(sfull(b), 2);  // the scale warps of both
-            mbar_init(sempty(b), 1);
+        if (lane < kF8PairSlots) {
+            mbar_init(sfull(lane), 2);  // the scale warps of both
+            mbar_init(sempty(lane), 1);
         }
-        failed = 0;
+        if (lane == 0) failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        __syncwarp();
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tslot), "r"(512) : "memory");
@@ -668,6 +669,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     } else {
         // warp w reads lanes 32 (w % 4) .. of this CTA's accumulators, rows of weights, and a quarter of the tokens.  Sixteen
         // warps, as each runs through its tokens once a tile: longer straight code waits for its instructions.
+        using T = std::conditional_t<BF16, uint16_t, float>;
         const uint32_t acce_leader[2] = {cluster_map(acce(0), 0), cluster_map(acce(1), 0)};
         const int quarter = (nt / 4 + 15) / 16 * 16, c0 = (warp >> 2) * quarter, cols = min(quarter, nt - c0);
         uint32_t b = 0, b_phase = 0;
@@ -681,7 +683,6 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
 #pragma unroll
             for (int j = 0; j < 64; ++j) sum[j] = 0.f;
             if (p.add && n < p.N) {
-                using T = std::conditional_t<BF16, uint16_t, float>;
                 const T* src = reinterpret_cast<const T*>(p.add) + m0 * p.lda + n;
 #pragma unroll
                 for (int j = 0; j < 64; ++j) {
@@ -716,16 +717,18 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 b ^= 1u;
                 if (b == 0) b_phase ^= 1u;
             }
-            if (ok && n < p.N) {
-                using T = std::conditional_t<BF16, uint16_t, float>;
-                T* dst = reinterpret_cast<T*>(p.out) + m0 * p.ldo + n;
 #pragma unroll
-                for (int j = 0; j < 64; ++j) {
-                    if (j < rows) {
-                        if constexpr (BF16) *dst = f2bf(sum[j]);
-                        else *dst = sum[j];
+            for (int c = 0; c < 64; c += 16) {
+                if (ok && n < p.N && c < rows) {
+                    T* dst = reinterpret_cast<T*>(p.out) + (m0 + c) * p.ldo + n;
+#pragma unroll
+                    for (int j = c; j < c + 16; ++j) {
+                        if (j < rows) {
+                            if constexpr (BF16) *dst = f2bf(sum[j]);
+                            else *dst = sum[j];
+                        }
+                        dst += p.ldo;
                     }
-                    dst += p.ldo;
                 }
             }
         }
@@ -737,7 +740,8 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         if (p.status) *p.status = DEV_TIMEOUT;
         __nanosleep(1000000);  // let copies that may still be in flight land before the CTA goes away
     }
-    cluster_sync_all();  // both CTAs are done with tensor memory, and the MMAs with both shared memories
+    cluster_arrive_relaxed();  // both CTAs are done with tensor memory, and the MMAs with both shared memories
+    cluster_wait();
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
