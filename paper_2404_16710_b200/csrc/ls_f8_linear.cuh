@@ -465,6 +465,12 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
     return false;
 }
 
+__device__ __forceinline__ void tc_commit_to(uint32_t bar, uint16_t ctas)  // arrives on `bar` in these CTAs of the cluster
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"(ctas)
+                 : "memory");
+}
 // whether the phase is complete, without waiting
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
 {
@@ -479,10 +485,43 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
     return done != 0;
 }
 
+// add of the tokens m0 .. m0 + rows - 1 (at most 64), row n of the weights
 template <bool BF16>
+__device__ __forceinline__ void f8_fetch_add(const F8Linear& p, long long m0, int n, int rows, float* sum)
+{
+    using T = std::conditional_t<BF16, uint16_t, float>;
+    const T* src = reinterpret_cast<const T*>(p.add) + m0 * p.lda + n;
+#pragma unroll
+    for (int j = 0; j < 64; ++j) {
+        if (j < rows) {
+            if constexpr (BF16) sum[j] = bf16f(__ldcg(src));
+            else sum[j] = __ldcg(src);
+        }
+        src += p.lda;
+    }
+}
+// out of up to 16 tokens from m on
+template <bool BF16>
+__device__ __forceinline__ void f8_store16(const F8Linear& p, long long m, int n, int rows, const float* sum)
+{
+    using T = std::conditional_t<BF16, uint16_t, float>;
+    T* dst = reinterpret_cast<T*>(p.out) + m * p.ldo + n;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        if (j < rows) {
+            if constexpr (BF16) *dst = f2bf(sum[j]);
+            else *dst = sum[j];
+        }
+        dst += p.ldo;
+    }
+}
+
+// SPLIT: a cluster of sk pairs shares a tile, each taking a stretch along K; a pair's sums of 16 tokens go to the pair that
+// owns them, through the rings, which by then are idle.  Every cluster has one tile then.
+template <bool BF16, bool SPLIT>
 __global__ void __launch_bounds__(kF8PairThreads, 1)
 linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h, const F8Linear p,
-                      const int nt, const int token_tiles, const int n_tiles)
+                      const int nt, const int token_tiles, const int n_tiles, const int sk)
 {
     extern __shared__ unsigned char f8_raw[];
     __shared__ int failed;
@@ -498,10 +537,14 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     const uint32_t tslot = bars + 8u * (2 * kF8PairMaxStages + 4 + 2 * kF8PairSlots);
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-    uint32_t rank;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    const int n_pairs = (int)gridDim.x / 2, pair = (int)blockIdx.x / 2;
-    const int nkb = (p.K + kF8Block - 1) / kF8Block, groups = (nkb + 3) / 4;
+    uint32_t cluster_rank;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(cluster_rank));
+    const uint32_t rank = cluster_rank & 1u, leader = cluster_rank & ~1u;
+    // tiles of this pair, and its blocks along K
+    const int first = SPLIT ? (int)blockIdx.x / (2 * sk) : (int)blockIdx.x / 2, step = SPLIT ? n_tiles : (int)gridDim.x / 2;
+    const int nkb = (p.K + kF8Block - 1) / kF8Block, all = (nkb + 3) / 4, own = SPLIT ? (int)cluster_rank / 2 : 0;
+    const int g0 = SPLIT ? all * own / sk : 0, groups = SPLIT ? all * (own + 1) / sk - g0 : all;
+    const int kb0 = 4 * g0, kb1 = min(nkb, kb0 + 4 * groups);
 
     if (warp == 16) {
         if (lane < kF8PairMaxStages) {
@@ -532,14 +575,19 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tslot));
 
+    // Of a tile, warp w < 16 reads lanes 32 (w % 4) .. of this CTA's accumulators, rows of weights, and a quarter of the tokens.
+    // Sixteen warps, as each runs through its tokens once a tile: longer straight code waits for its instructions.
+    const int quarter = (nt / 4 + 15) / 16 * 16, c0 = (warp >> 2 & 3) * quarter, cols = min(quarter, nt - c0);
+    auto row_of = [&](int t) { return (t / token_tiles * 2 + (int)rank) * kF8Block + (warp & 3) * 32 + lane; };
+    float sum[64];
     if (warp == 16) {
         if (lane == 0) {
             const uint32_t bytes = 2u * (uint32_t)(kF8WBytes + nt / 2 * kF8Block);
             uint32_t s = 0, phase = 1;  // a stage that was never used counts as free
             bool ok = true;
-            for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+            for (int t = first; t < n_tiles && ok; t += step) {
                 const int w_row = (t / token_tiles * 2 + (int)rank) * kF8Block, h_row = t % token_tiles * nt + (int)rank * (nt / 2);
-                for (int kb = 0; kb < nkb; ++kb) {
+                for (int kb = kb0; kb < kb1; ++kb) {
                     if (!mbar_wait(empty(s), phase)) {
                         failed = 1;
                         ok = false;
@@ -560,13 +608,14 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             const uint32_t idesc = ((uint32_t)(nt >> 3) << 17) | (1u << 23) | (2u << 27);
             const uint64_t desc0 = umma_desc_sw128(0);
             const bool one = elect_one();
+            const uint16_t both = (uint16_t)(3u << leader);  // the pair's CTAs in the cluster
             uint32_t s = 0, s_phase = 0, slot = 0, slot_phase = 0, old_phase = 1;
             uint32_t b = 0, b_phase = 1;  // an accumulator that was never used counts as read
             bool ok = true, ready = false;
-            for (int t = pair; t < n_tiles && ok; t += n_pairs) {
-                for (int kb = 0; kb < nkb && ok; kb += 4) {
+            for (int t = first; t < n_tiles && ok; t += step) {
+                for (int kb = kb0; kb < kb1 && ok; kb += 4) {
                     const uint32_t d = tmem + b * kF8PairTokens;
-                    if (kb % kF8PairChunk == 0) {
+                    if ((kb - kb0) % kF8PairChunk == 0) {
                         if (!mbar_wait(acce(b), b_phase)) {
                             failed = 1;
                             ok = false;
@@ -595,7 +644,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                     }
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        if (kb + q >= nkb) break;
+                        if (kb + q >= kb1) break;
                         if (!ready && !mbar_wait(full(s), s_phase)) {
                             failed = 1;
                             ok = false;
@@ -610,15 +659,15 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                             const uint32_t id = idesc | (uint32_t)q << 4 | (uint32_t)q << 29;
 #pragma unroll
                             for (int k4 = 0; k4 < 4; ++k4)
-                                tc_mma_f8_scaled_pair(d, da + 2 * k4, db + 2 * k4, id, sf, sf + 8, (kb % kF8PairChunk | q | k4) != 0);
-                            tc_commit_pair(empty(s_now));
+                                tc_mma_f8_scaled_pair(d, da + 2 * k4, db + 2 * k4, id, sf, sf + 8, ((kb - kb0) % kF8PairChunk | q | k4) != 0);
+                            tc_commit_to(empty(s_now), both);
                         }
                     }
-                    if (one && ok) tc_commit_pair(sempty(slot));  // copies and products of these four blocks are done
+                    if (one && ok) tc_commit_to(sempty(slot), both);  // copies and products of these four blocks are done
                     if (++slot == kF8PairSlots) slot = 0, slot_phase ^= 1u;
                     if (slot == 2) old_phase ^= 1u;
-                    if (ok && ((kb + 4) % kF8PairChunk == 0 || kb + 4 >= nkb)) {
-                        if (one) tc_commit_pair(accf(b));
+                    if (ok && ((kb - kb0 + 4) % kF8PairChunk == 0 || kb + 4 >= kb1)) {
+                        if (one) tc_commit_to(accf(b), both);
                         b ^= 1u;
                         if (b == 0) b_phase ^= 1u;
                     }
@@ -630,19 +679,19 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         // in turn.  The fence waits for the warp's loads too, so the next words are asked for behind it, and two
         // warps leave them the time of eight blocks (one warp: 2200 cycles for four, whatever the tile).
         const int width = (int)f8_scale_width(p.K), w_rows = (p.N + kF8Block - 1) / kF8Block;
-        int t = pair, gi = warp - 18;  // next group to ask for
+        int t = first, gi = warp - 18;  // next group to ask for
         uint32_t w = 0, h[8];
         auto settle = [&] {
-            while (gi >= groups) gi -= groups, t += n_pairs;
+            while (gi >= groups) gi -= groups, t += step;
         };
         auto fetch = [&] {
             const int wb = t / token_tiles * 2 + (int)rank;
             const long long m0 = (long long)(t % token_tiles) * nt;
-            w = wb < w_rows ? __ldcg(reinterpret_cast<const uint32_t*>(p.ws + (long long)wb * width + 4 * gi)) : 0x7f7f7f7fu;
+            w = wb < w_rows ? __ldcg(reinterpret_cast<const uint32_t*>(p.ws + (long long)wb * width + 4 * (g0 + gi))) : 0x7f7f7f7fu;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const long long m = m0 + 32 * j + lane;
-                h[j] = 32 * j + lane < nt && m < p.M ? __ldcg(reinterpret_cast<const uint32_t*>(p.hs + m * width + 4 * gi)) : 0x7f7f7f7fu;
+                h[j] = 32 * j + lane < nt && m < p.M ? __ldcg(reinterpret_cast<const uint32_t*>(p.hs + m * width + 4 * (g0 + gi))) : 0x7f7f7f7fu;
             }
         };
         uint32_t slot = warp - 18, phase = 1;  // a slot that was never used counts as free
@@ -659,7 +708,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + 1024), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // tcgen05.cp reads what was just stored
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(cluster_map(sfull(slot), 0));
+            if (lane == 0) mbar_arrive_cluster(cluster_map(sfull(slot), leader));
             slot += 2;
             if (slot >= kF8PairSlots) slot -= kF8PairSlots, phase ^= 1u;
             gi += 2;
@@ -667,33 +716,18 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             if (t < n_tiles) fetch();
         }
     } else {
-        // warp w reads lanes 32 (w % 4) .. of this CTA's accumulators, rows of weights, and a quarter of the tokens.  Sixteen
-        // warps, as each runs through its tokens once a tile: longer straight code waits for its instructions.
-        using T = std::conditional_t<BF16, uint16_t, float>;
-        const uint32_t acce_leader[2] = {cluster_map(acce(0), 0), cluster_map(acce(1), 0)};
-        const int quarter = (nt / 4 + 15) / 16 * 16, c0 = (warp >> 2) * quarter, cols = min(quarter, nt - c0);
+        const uint32_t acce_leader[2] = {cluster_map(acce(0), leader), cluster_map(acce(1), leader)};
         uint32_t b = 0, b_phase = 0;
         bool ok = true;
-        for (int t = pair; t < n_tiles && ok; t += n_pairs) {
-            const int n = (t / token_tiles * 2 + (int)rank) * kF8Block + (warp & 3) * 32 + lane;
+        for (int t = first; t < n_tiles && ok; t += step) {
+            const int n = row_of(t);
             const long long m0 = (long long)(t % token_tiles) * nt + c0;
-            // sums begin with add, which comes while the first products are made
-            float sum[64];
             const int rows = (int)min((long long)cols, p.M - m0);
+            // sums begin with add, which comes while the first products are made
 #pragma unroll
             for (int j = 0; j < 64; ++j) sum[j] = 0.f;
-            if (p.add && n < p.N) {
-                const T* src = reinterpret_cast<const T*>(p.add) + m0 * p.lda + n;
-#pragma unroll
-                for (int j = 0; j < 64; ++j) {
-                    if (j < rows) {
-                        if constexpr (BF16) sum[j] = bf16f(__ldcg(src));
-                        else sum[j] = __ldcg(src);
-                    }
-                    src += p.lda;
-                }
-            }
-            for (int kb = 0; kb < nkb; kb += kF8PairChunk) {
+            if (p.add && n < p.N && own == 0) f8_fetch_add<BF16>(p, m0, n, rows, sum);
+            for (int kb = kb0; kb < kb1; kb += kF8PairChunk) {
                 if (!mbar_wait(accf(b), b_phase)) {
                     failed = 1;
                     ok = false;
@@ -717,18 +751,45 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 b ^= 1u;
                 if (b == 0) b_phase ^= 1u;
             }
+            if (!SPLIT && ok && n < p.N) {
+#pragma unroll
+                for (int c = 0; c < 64; c += 16)
+                    if (c < rows) f8_store16<BF16>(p, m0 + c, n, rows - c, sum + c);
+            }
+        }
+    }
+    if constexpr (SPLIT) {
+        // the 16 tokens from c on belong to pair c / 16 % sk; part [pair][c / 16 / sk][warp][token][lane]
+        __syncwarp();
+        cluster_sync_all();  // every pair's products are made: nothing uses the rings any more
+        const uint32_t part = base + 4u * (uint32_t)(warp * 512 + lane), each = 4u * (uint32_t)(4 / sk) * 8192u;
+        if (warp < 16) {
 #pragma unroll
             for (int c = 0; c < 64; c += 16) {
-                if (ok && n < p.N && c < rows) {
-                    T* dst = reinterpret_cast<T*>(p.out) + (m0 + c) * p.ldo + n;
+                const int to = c / 16 % sk;
+                if (c < cols && to != own) {
+                    const uint32_t dst = cluster_map(part + (uint32_t)own * each + 4u * (uint32_t)(c / 16 / sk) * 8192u, 2u * to + rank);
 #pragma unroll
-                    for (int j = c; j < c + 16; ++j) {
-                        if (j < rows) {
-                            if constexpr (BF16) *dst = f2bf(sum[j]);
-                            else *dst = sum[j];
-                        }
-                        dst += p.ldo;
+                    for (int j = 0; j < 16; ++j)
+                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst + 128u * j), "f"(sum[c + j]) : "memory");
+                }
+            }
+        }
+        cluster_sync_all();
+        const int n = row_of(first);
+        const long long m0 = (long long)(first % token_tiles) * nt + c0;
+        const int rows = (int)min((long long)cols, p.M - m0);
+        if (warp < 16 && !failed) {
+#pragma unroll
+            for (int c = 0; c < 64; c += 16) {
+                if (c < rows && c / 16 % sk == own) {
+                    for (int from = 0; from < sk; ++from) {
+                        if (from == own) continue;
+                        const uint32_t src = part + (uint32_t)from * each + 4u * (uint32_t)(c / 16 / sk) * 8192u;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[c + j] += lds_f32(src + 128u * j);
                     }
+                    if (n < p.N) f8_store16<BF16>(p, m0 + c, n, rows - c, sum + c);
                 }
             }
         }

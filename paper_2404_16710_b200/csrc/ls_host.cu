@@ -2329,52 +2329,93 @@ int linear_f8_launch(const void* wc, const void* hc, const F8Linear& p, int S, c
     return LS_OK;
 }
 
-template <bool BF16>
-int linear_f8_pair_launch(const void* wc, const void* hc, const F8Linear& p, const LaunchCtx& lc)
+// most clusters of 2 sk CTAs of the kernel that are resident at once (0: none)
+template <bool BF16, bool SPLIT>
+int f8_pair_clusters(int sk, int* most)
 {
-    static std::atomic<int> max_pairs[64];
+    static std::atomic<int> known[64][5];
     int dev = 0;
     LS_CK(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return LS_ERR_UNSUPPORTED;
-    LS_TRY(allow_smem<linear_f8_pair_kernel<BF16>>(kF8PairSmem));
+    int n = known[dev][sk].load(std::memory_order_acquire);
+    if (!n) {
+        LS_TRY((allow_smem<linear_f8_pair_kernel<BF16, SPLIT>>(kF8PairSmem)));
+        int sms = 0;
+        LS_CK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute at;
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = 2 * sk;
+        at.val.clusterDim.y = 1;
+        at.val.clusterDim.z = 1;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        cfg.dynamicSmemBytes = kF8PairSmem;
+        cfg.blockDim = dim3(kF8PairThreads);
+        cfg.gridDim = dim3(sms / (2 * sk) * 2 * sk);
+        LS_CK(cudaOccupancyMaxActiveClusters(&n, linear_f8_pair_kernel<BF16, SPLIT>, &cfg));
+        n = std::min(n, sms / (2 * sk));
+        known[dev][sk].store(n > 0 ? n : -1, std::memory_order_release);
+    }
+    *most = n > 0 ? n : 0;
+    return LS_OK;
+}
+
+template <bool BF16, bool SPLIT>
+int linear_f8_pair_launch_as(const CUtensorMap& mw, const CUtensorMap& mh, const F8Linear& p, int nt, int token_tiles, int n_tiles, int clusters,
+                             int sk, const LaunchCtx& lc)
+{
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = 2;
+    at.val.clusterDim.x = 2 * sk;
     at.val.clusterDim.y = 1;
     at.val.clusterDim.z = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
     cfg.dynamicSmemBytes = kF8PairSmem;
     cfg.blockDim = dim3(kF8PairThreads);
+    cfg.gridDim = dim3(2 * sk * (unsigned)clusters);
     cfg.stream = lc.st;
-    int most = max_pairs[dev].load(std::memory_order_acquire);
-    if (!most) {
-        int sms = 0, n = 0;
-        LS_CK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-        cfg.gridDim = dim3(sms & ~1);
-        LS_CK(cudaOccupancyMaxActiveClusters(&n, linear_f8_pair_kernel<BF16>, &cfg));
-        if (n < 1) return LS_ERR_UNSUPPORTED;
-        most = n < sms / 2 ? n : sms / 2;
-        max_pairs[dev].store(most, std::memory_order_release);
+    LS_CK(cudaLaunchKernelEx(&cfg, linear_f8_pair_kernel<BF16, SPLIT>, mw, mh, p, nt, token_tiles, n_tiles, sk));
+    return LS_OK;
+}
+
+template <bool BF16>
+int linear_f8_pair_launch(const void* wc, const void* hc, const F8Linear& p, const LaunchCtx& lc)
+{
+    int most[5] = {0, 0, 0, 0, 0};
+    LS_TRY((f8_pair_clusters<BF16, false>(1, &most[1])));
+    LS_TRY((f8_pair_clusters<BF16, true>(2, &most[2])));
+    LS_TRY((f8_pair_clusters<BF16, true>(4, &most[4])));
+    if (most[1] < 1) return LS_ERR_UNSUPPORTED;
+    // Tokens of a tile, and pairs that share one along K: what costs least.  In cycles, a block along K takes 400 up to 175 tokens
+    // (what the ring hides of the loads' latency) and 1.6 a token beyond (products, and loads from L2), a tile's end 4000 for 240
+    // tokens, which the next tile's products cover where there is one and they are longer, and the larger cluster and joining 10000 (512x512, K = 14336,
+    // 512 tokens: 18.0 us with four pairs, 29.8 with one; 4096x11008, 256 tokens: 22.4 with two, 26.2; 4096x4096, 160 tokens 15.7, 13.5).
+    const int w_tiles = (p.N + 2 * kF8Block - 1) / (2 * kF8Block), groups = ((p.K + kF8Block - 1) / kF8Block + 3) / 4;
+    int nt = 0, token_tiles = 0, sk = 1;
+    double best = 0;
+    for (int n = kF8PairTokens; n >= 16; n -= 16) {
+        const int tt = (p.M + n - 1) / n;
+        const double tiles = (double)w_tiles * tt, block = std::max(400.0, 120 + 1.6 * n);
+        for (int k = 1; k <= 4; k *= 2) {
+            if (k > 1 && (tiles > most[k] || groups < 2 * k)) continue;
+            const double end = 4000.0 * n / kF8PairTokens;
+            const double cost = k == 1 ? std::ceil(tiles / most[1]) * std::max(4 * groups * block, end) + end
+                                       : 4.0 * ((groups + k - 1) / k) * block + end + 10000;
+            if (!nt || cost < best) best = cost, nt = n, token_tiles = tt, sk = k;
+        }
     }
-    // tokens of a tile: what makes the rounds of tiles over all pairs cost least
-    const int w_tiles = (p.N + 2 * kF8Block - 1) / (2 * kF8Block), least = (p.M + kF8PairTokens - 1) / kF8PairTokens;
-    int nt = kF8PairTokens, token_tiles = least;
-    long long best = 0;
-    for (int tt = least; tt <= least + 16; ++tt) {
-        const int n = ((p.M + tt - 1) / tt + 15) / 16 * 16, real = (p.M + n - 1) / n;
-        const long long cost = ((long long)w_tiles * real + most - 1) / most * (n + 64);
-        if (!best || cost < best) best = cost, nt = n, token_tiles = real;
-    }
+    // as few tokens a tile as that many tiles need
+    nt = ((p.M + token_tiles - 1) / token_tiles + 15) / 16 * 16;
     const long long n_tiles = (long long)w_tiles * token_tiles;
     if (n_tiles > 0x7fffffff - 1024) return LS_ERR_UNSUPPORTED;
     CUtensorMap mw, mh;
     LS_TRY(make_f8_map(&mw, wc, (uint64_t)p.N, (uint64_t)p.K, kF8Block));
     LS_TRY(make_f8_map(&mh, hc, (uint64_t)p.M, (uint64_t)p.K, nt / 2));
-    cfg.gridDim = dim3(2 * (unsigned)(n_tiles < most ? n_tiles : most));
-    LS_CK(cudaLaunchKernelEx(&cfg, linear_f8_pair_kernel<BF16>, mw, mh, p, nt, token_tiles, (int)n_tiles));
-    return LS_OK;
+    if (sk > 1) return linear_f8_pair_launch_as<BF16, true>(mw, mh, p, nt, token_tiles, (int)n_tiles, (int)n_tiles, sk, lc);
+    return linear_f8_pair_launch_as<BF16, false>(mw, mh, p, nt, token_tiles, (int)n_tiles, (int)std::min(n_tiles, (long long)most[1]), 1, lc);
 }
 
 template <bool BF16>
