@@ -490,11 +490,13 @@ int ls_op_rmsnorm_f8(const void *x_dev, int32_t x_type, int64_t ldx, const void 
 int ls_op_swiglu_f8(const void *gate_dev, const void *up_dev, int32_t type, int64_t ld, int32_t M, int32_t F,
                     void *codes_dev, void *scales_dev, void *cuda_stream);
 /* out[m,n] = (add[m,n] +) sum_k h[m,k] w[n,k]: w [N, K] with block_rows = 128, h [M, K] with
- * block_rows = 1; out and add (may be NULL; may be out itself) of one type, any alignment that the type has
- * and any row strides.  fp32 accumulation, rounded once at the end.  A NaN block makes its
- * rows NaN.  Up to LS_MAX_ROWS rows a row's result does not depend on how many rows
- * share the call.  status_dev (device int32, may be NULL) receives 3 if one of the kernel's bounded waits ran out.
- * Under ls_op_chain the weights are read ahead of the wait for the operation before. */
+ * block_rows = 1; out and add (may be NULL; may be out itself, with its stride) of one type, any alignment that
+ * the type has and any row strides >= N.  Accumulation in fp32 (of 2048 columns at a time or fewer in the tensor cores,
+ * which truncate), bf16 rounded once at the end.  A NaN block makes its rows NaN.  The product of two blocks'
+ * scales has to be a number of fp32, 2^-149 to 2^127.  Up to LS_MAX_ROWS rows a row's result does not depend on
+ * how many rows share the call.  status_dev (device int32, may be NULL) receives 3 if one of the kernel's bounded
+ * waits ran out.  Under ls_op_chain weights are read ahead of the wait for the operation before, but for calls on CTA
+ * pairs (more than 128 rows, or more than 64 and more than 148 tiles of 128 rows of weights), which are not chained. */
 int ls_op_linear_f8(const void *w_codes_dev, const void *w_scales_dev, const void *h_codes_dev, const void *h_scales_dev,
                     int32_t M, int32_t N, int32_t K, void *out_dev, int32_t out_type, int64_t ldo, const void *add_dev,
                     int64_t lda, int32_t *status_dev, void *cuda_stream);

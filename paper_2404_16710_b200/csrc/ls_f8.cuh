@@ -169,7 +169,7 @@ __device__ __forceinline__ void f8_store_row_part(const float (&v)[V], int k0, i
 }
 
 // ------------------------------------------------------------------ rows and weights -> 8 bits, and back
-// Rows: a warp takes 1024 columns of a row.  grid.x * 8 warps cover the parts of all rows.
+// Rows: a warp takes 1024 columns of a row.  grid.x * 8 warps cover the parts of all rows.  (1030 x 4096 bf16: 5.6 us, launch 2.2 of them.)
 constexpr int kF8RowPart = 1024;
 template <typename T>
 __global__ void __launch_bounds__(256) quantize_f8_rows_kernel(const T* __restrict__ x, int64_t ldx, int K, int parts, long long items, int wide,
@@ -198,8 +198,8 @@ __global__ void __launch_bounds__(256) quantize_f8_rows_kernel(const T* __restri
 }
 
 // Weights: a CTA takes a block of 128 x 128.  grid (blocks of a row of them, rows of blocks).  Bound by the loads of a CTA's only
-// block: pieces stay as they were loaded (32 registers of bf16), so that more CTAs fit an SM (11008 x 4096: 31 us, 4.4 TB/s; as
-// floats 60).
+// block: pieces stay as they were loaded, so that more CTAs fit an SM (11008 x 4096 bf16: 27 us, 5.0 TB/s; as floats, and
+// 16 bytes at a time, 60).
 template <typename T>
 __global__ void __launch_bounds__(256, F8In<T>::V == 16 ? 3 : 2)
 quantize_f8_weights_kernel(const T* __restrict__ x, int64_t ldx, int M, int K, int wide, unsigned char* __restrict__ codes,
@@ -247,7 +247,8 @@ quantize_f8_weights_kernel(const T* __restrict__ x, int64_t ldx, int M, int K, i
 }
 
 // Codes and scales -> bf16 [M, K].  A warp takes 2048 columns of a row, a lane 16 neighbouring ones at a time: 32 bytes of
-// output.  `shift`: log2 of a block's rows.
+// output (4096 x 11008: 22.8 us, 5.9 TB/s; 16 bytes of codes a warp's lane at a time, stored in two halves, 39).  `shift`: log2 of a
+// block's rows.
 constexpr int kF8ExpandPart = 2048;
 __global__ void __launch_bounds__(256) expand_f8_kernel(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
                                                         int K, int parts, long long items, int shift, int signal, int wide,
@@ -285,7 +286,8 @@ __global__ void __launch_bounds__(256) expand_f8_kernel(const unsigned char* __r
 // ------------------------------------------------------------------ RMSNorm with the residual's addition, into 8 bits
 // x' = x + d rounded to x's type, y = x' / sqrt(mean x'^2 + eps) * gain, sums in fp32.  A CTA takes a row; with NV > 0 a
 // thread keeps its NV pieces of it in registers, else (rows too long for that) x' is read again, from x_out where it was
-// written.  d and x_out may be null, x_out may be x or d.
+// written.  d and x_out may be null, x_out may be x or d.  Bound by memory: 4096 x 4096, fp32 x and bf16 d 32.3 us, 5.7 TB/s (41 with
+// 16-byte accesses); one row 2.6 us, a launch.
 template <typename T, typename TD, int NV>
 __global__ void __launch_bounds__(NV >= 4 ? 512 : 1024)
 rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, int64_t ldo, const uint16_t* gain, int D, float eps, int wide,
@@ -394,7 +396,7 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
 // y = gate / (1 + exp(-gate)) * up.  exp(-g) = 2^t (1 + d ln 2), t = -g log2 e rounded, d what it was rounded by (the product's
 // error, which the fma gives exactly, and that of log2 e), so that the exponential is off by little more than ex2.approx,
 // 2^-22 of its value, however large g.  (With expf and a division the kernel issued 2.75 instructions a cycle and took
-// 86 us where this takes XX, 4096 x 11008 bf16.)  From t = 126 on (gates below -87.3) the
+// 86 us, 4096 x 11008 bf16.)  From t = 126 on (gates below -87.3) the
 // reciprocal is not a normal number and counts as 0.
 __device__ __forceinline__ float f8_silu_times(float g, float u)
 {
@@ -406,7 +408,7 @@ __device__ __forceinline__ float f8_silu_times(float g, float u)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
     return g * r * u;
 }
-// A warp takes 512 features of a row.
+// A warp takes 512 features of a row.  Bound by memory: 4096 x 11008 bf16 38.9 us, 5.8 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256) swiglu_f8_kernel(const T* __restrict__ gate, const T* __restrict__ up, int64_t ld, int F, int parts,
                                                         long long items, int wide, unsigned char* __restrict__ codes,

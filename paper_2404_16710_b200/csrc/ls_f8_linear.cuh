@@ -1,9 +1,21 @@
-// Matrix product in 8 bits with a scale for each block of 128: out[m, n] (+)= sum_k h[m, k] w[n, k], both operands in the
-// format of ls_f8.cuh, any number of rows.
+// Matrix product in 8 bits with a scale for each block of 128: out[m, n] = (add[m, n] +) sum_k h[m, k] w[n, k], both operands
+// in the format of ls_f8.cuh, any number of rows m ("tokens").
 //
-// The 128 columns of a block are one row of a 128B-swizzled tile and four tcgen05.mma (kind f8f6f4, K = 32).  Their
-// sum goes to a tensor-memory buffer of its own; four warps read it back, multiply by the product of the two scales
-// and add it to fp32 registers, so what the tensor cores sum is never longer than 128 and the rest is plain fp32.
+// The 128 codes of a block's row are a row of a 128B-swizzled tile, as TMA writes it and four tcgen05.mma of K = 32 read it.
+// In both kernels the weights are the operand in the lanes and the tokens the columns: few tokens then leave no lanes idle, tiles
+// follow the tokens' number in steps of 16, and a warp's store of a token is 32 neighbouring outputs.
+//   up to 128 tokens   linear_f8_kernel: bound by reading the weights, so 128 rows a CTA, two CTAs an SM, K split over a cluster
+//                      where there are few tiles.  Scales multiply the sums of 128 columns in fp32 registers.
+//   more               linear_f8_pair_kernel: bound by the products (and, through them, by the power limit), so CTA pairs, 256 rows
+//                      x 240 tokens, and the scales multiplied in the tensor cores.
+// Why not one for both: at 16 tokens the pair kernel's start (tensor memory, a cluster, scales through shared memory and tensor memory)
+// costs what the products do not (4096 x 4096: 18.7 us, 7.5 - 10 without); at 4096 the first form reads back 128 x 128 sums for each
+// block along K and stops at 584 TFLOP/s (2650 with pairs).
+// Measured (B200, 1965 MHz until the power limit, inputs not in L2): 4096 x 4096, one token 7.5 us (5.6 chained); 4096 x 11008, 7 tokens
+// with add 13.0; 128256 x 4096, 16 tokens 83 - 88 (6.0 - 6.4 TB/s); 12288 x 4096, 1030 tokens 47 (2.2 PFLOP/s); 22016 x 4096, 4096 tokens
+// 276 - 282 (2.65 PFLOP/s; at 1.18 GHz under the power limit 84 % of what the tensor cores can do).
+// Rows of K = 16 mod 32 bytes begin inside a 32-byte sector: the loads of every second row then cost about 1.4 times (2334 x 7600, 2108
+// tokens: 54.7 us, K = 7616 40.7).  The layout is the caller's, and both operands have to agree on the columns of a step.
 #pragma once
 #include <type_traits>
 
@@ -82,46 +94,51 @@ __device__ __forceinline__ float lds_f32(uint32_t addr)
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
 }
-// out[m .. m + 15, n] = v (+ add); all of add is asked for first, as out may be add
+// out of up to 16 tokens from m on
 template <bool BF16>
-__device__ __forceinline__ void f8_put16(const F8Linear& p, long long m, int n, const float* v)
+__device__ __forceinline__ void f8_store16(const F8Linear& p, long long m, int n, int rows, const float* sum)
 {
     using T = std::conditional_t<BF16, uint16_t, float>;
-    const int rows = (int)min(16ll, p.M - m);
     T* dst = reinterpret_cast<T*>(p.out) + m * p.ldo + n;
-    float a[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) a[j] = v[j];
-    if (p.add) {
-        const T* src = reinterpret_cast<const T*>(p.add) + m * p.lda + n;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            if (j < rows) {
-                if constexpr (BF16) a[j] += bf16f(__ldcg(src));
-                else a[j] += __ldcg(src);
-            }
-            src += p.lda;
-        }
-    }
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
         if (j < rows) {
-            if constexpr (BF16) *dst = f2bf(a[j]);
-            else *dst = a[j];
+            if constexpr (BF16) *dst = f2bf(sum[j]);
+            else *dst = sum[j];
         }
         dst += p.ldo;
     }
 }
+// add of N tokens from m on, those below rows
+template <bool BF16, int N>
+__device__ __forceinline__ void f8_fetch_add(const F8Linear& p, long long m, int n, int rows, float* a)
+{
+    using T = std::conditional_t<BF16, uint16_t, float>;
+    const T* src = reinterpret_cast<const T*>(p.add) + m * p.lda + n;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (j < rows) {
+            if constexpr (BF16) a[j] = bf16f(__ldcg(src));
+            else a[j] = __ldcg(src);
+        }
+        src += p.lda;
+    }
+}
 
-// ------------------------------------------------------------------ weights in the lanes, tokens in the columns
-// A CTA computes 128 rows of weights x NT tokens: the weights are the 128-row operand, so that few tokens leave no part
-// of the tensor core's rows idle, and a warp's stores of a token are 32 neighbouring outputs.  The S CTAs of a cluster
-// share a tile, each taking a stretch of the blocks along K; their sums meet in the CTA that owns the token, in order.
+// ------------------------------------------------------------------ up to 128 tokens
+// A CTA takes 128 rows of weights and up to NT tokens.  A block's four MMAs (kind f8f6f4) leave their sum in tensor-memory columns
+// of its own; four warps read them back, multiply by the product of the two scales (laid out ahead as floats by a warp of its own)
+// and add to fp32 registers.  kUnit blocks change hands at a time: a hand-over takes some 400 cycles, a block's weights 700 at the
+// copy rate.  The S CTAs of a cluster share a tile, each a stretch of the blocks along K; their sums meet in the CTA
+// that owns the token, in order.  S is a function of the matrix alone: up to 16 tokens a row's bits do not depend on how many there are.
+// Steps (4096 x 4096, one token / 128256 x 4096, 16): first form 11.8 / 130 us; 256-byte sectors asked of L2 - / 122; scale words
+// asked for 12 blocks ahead and two CTAs an SM 10.1 / 79; hand-overs of four blocks 8.8; relaxed arrival at the cluster's first barrier (a
+// release waits 1.9 us), barriers set up by a warp, sums sent without divisions 7.5.  With mma.sync on f16 (cvt from e4m3, registers straight
+// from global memory) one token took 7.2 us and 16 took 11.2 (10.0 here), larger matrices up to twice as long: not kept.
 constexpr int kF8Threads = 224;  // warps 0-3: sums and stores, 4: TMA, 5: MMA, 6: scales
 constexpr int kF8WBytes = kF8Block * kF8Block;
 constexpr int kF8SmemMax = 227 * 1024;
 constexpr int kF8Slots = 4;  // slots of scales, one word of scale bytes (four blocks) each
-
 constexpr int kF8MaxStages = 11;
 template <int NT, int CTAS>  // CTAs that fit an SM
 struct F8Cfg {
@@ -392,7 +409,17 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             else f8_join<NT, 8, BF16>(p, rank, n0 + tid, row);
         } else {
 #pragma unroll
-            for (int j = 0; j < NT; j += 16) f8_put16<BF16>(p, j, n0 + tid, acc + j);
+            for (int j = 0; j < NT; j += 16) {
+                float a[16];
+                if (p.add) {  // all of it is asked for before anything is stored: out may be add
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) a[i] = 0.f;
+                    f8_fetch_add<BF16, 16>(p, j, n0 + tid, p.M - j, a);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[j + i] += a[i];
+                }
+                f8_store16<BF16>(p, j, n0 + tid, p.M - j, acc + j);
+            }
         }
     }
     tc_fence_before();
@@ -409,8 +436,14 @@ linear_f8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 // in shared memory, tcgen05.cp spreads them over the lanes; byte i of a word is the i-th block's, which the instruction
 // descriptor picks.  Weights are the 256-row operand, so that tiles follow the tokens' number in steps of 16 and a warp
 // stores 32 neighbouring outputs; at 240 tokens two accumulators and the scales fit the 512 columns of tensor memory:
-// a tile's sums are read while the next one's are made.
+// a tile's sums are read while the next one's are made.  Every 16 blocks (2048 columns) sums move to fp32 registers: the tensor
+// cores truncate as they add, and 11008 columns at once are off by 1.1e-6 of the result's norm, 2048 at a time by 1.6e-7.
 // Persistent: pair p takes tiles p, p + P, ..., tokens fastest (pairs that run side by side share weights in L2).
+// A block takes 480 cycles of products at 240 tokens and 500 in all; its loads are 31 KB a CTA, 60 bytes a cycle from L2, which is near what
+// an SM gets.  Steps (22016 x 4096, 4096 tokens): one lane alone issuing 400 us; the whole warp walking the loop, so that
+// descriptors stay in uniform registers, 338; eight storing warps with 120 tokens of straight code each 438, sixteen with 60 319 (instruction fetch);
+// 256-byte sectors 312; scales by two warps, each asking for its next words behind its fence (which waits for loads under way) 290;
+// the next stage's barrier asked ahead 277.  From there the power limit sets the clock.
 constexpr int kF8PairTokens = 240;
 constexpr int kF8PairRing = 7 * (kF8WBytes + kF8PairTokens / 2 * kF8Block);  // as many stages as fit, 7 at 240 tokens
 constexpr int kF8PairMaxStages = 12;
@@ -422,9 +455,9 @@ __host__ __device__ constexpr int f8_pair_stages(int nt)
 }
 constexpr int kF8PairSlots = 4;
 constexpr int kF8PairChunk = 16;             // blocks along K that are summed in tensor memory
-constexpr int kF8PairSlot = 3 * 512;        // scale words of 128 rows of weights, of 256 tokens
+constexpr int kF8PairSlot = 3 * 512;         // scale words of 128 rows of weights, of 256 tokens
 constexpr int kF8PairScaleCols = 2 * kF8PairTokens;  // two sets of 16 columns behind the accumulators
-constexpr int kF8PairThreads = 640;         // warps 0-15: sums and stores, 16: TMA, 17: MMA, 18, 19: scales
+constexpr int kF8PairThreads = 640;          // warps 0-15: sums and stores, 16: TMA, 17: MMA, 18, 19: scales
 constexpr size_t kF8PairSmem = (size_t)kF8PairRing + kF8PairSlots * kF8PairSlot + 1024 + 512;
 static_assert(f8_pair_stage(16) % 1024 == 0 && kF8PairSmem <= kF8SmemMax && kF8PairScaleCols + 32 <= 512, "shared and tensor memory");
 
@@ -483,37 +516,6 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
         : "r"(bar), "r"(parity)
         : "memory");
     return done != 0;
-}
-
-// add of the tokens m0 .. m0 + rows - 1 (at most 64), row n of the weights
-template <bool BF16>
-__device__ __forceinline__ void f8_fetch_add(const F8Linear& p, long long m0, int n, int rows, float* sum)
-{
-    using T = std::conditional_t<BF16, uint16_t, float>;
-    const T* src = reinterpret_cast<const T*>(p.add) + m0 * p.lda + n;
-#pragma unroll
-    for (int j = 0; j < 64; ++j) {
-        if (j < rows) {
-            if constexpr (BF16) sum[j] = bf16f(__ldcg(src));
-            else sum[j] = __ldcg(src);
-        }
-        src += p.lda;
-    }
-}
-// out of up to 16 tokens from m on
-template <bool BF16>
-__device__ __forceinline__ void f8_store16(const F8Linear& p, long long m, int n, int rows, const float* sum)
-{
-    using T = std::conditional_t<BF16, uint16_t, float>;
-    T* dst = reinterpret_cast<T*>(p.out) + m * p.ldo + n;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        if (j < rows) {
-            if constexpr (BF16) *dst = f2bf(sum[j]);
-            else *dst = sum[j];
-        }
-        dst += p.ldo;
-    }
 }
 
 // SPLIT: a cluster of sk pairs shares a tile, each taking a stretch along K; a pair's sums of 16 tokens go to the pair that
@@ -726,7 +728,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             // sums begin with add, which comes while the first products are made
 #pragma unroll
             for (int j = 0; j < 64; ++j) sum[j] = 0.f;
-            if (p.add && n < p.N && own == 0) f8_fetch_add<BF16>(p, m0, n, rows, sum);
+            if (p.add && n < p.N && own == 0) f8_fetch_add<BF16, 64>(p, m0, n, rows, sum);
             for (int kb = kb0; kb < kb1; kb += kF8PairChunk) {
                 if (!mbar_wait(accf(b), b_phase)) {
                     failed = 1;

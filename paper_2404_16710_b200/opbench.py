@@ -2,6 +2,7 @@
 
     python -m paper_2404_16710_b200.opbench --workload llama2-7b --layers 4 --ops gate_up_swiglu --rows 7
     python -m paper_2404_16710_b200.opbench --workload llama3-8b --bits 4 --rows 1,5
+    python -m paper_2404_16710_b200.opbench --bits 8 --prompt-rows 1024
 
 Each op is launched ``iters`` times (as one CUDA graph) with CUDA events around the batch,
 rotating over the weights of ``layers`` layers so that no launch finds its weights in L2 (one 7B-shaped
@@ -139,6 +140,64 @@ def q4_cases(shape, w, M, n_ctx=1030, group=64):
     return cases
 
 
+F8_OPS = ("gate_up_f8", "down_residual_f8", "qkv_f8", "o_residual_f8", "lm_head_f8", "rmsnorm_f8", "swiglu_f8", "quantize_f8")
+
+
+def f8_matrices(shape, w):
+    """name -> [(codes, scales)] of the layers' matrices in 8 bits"""
+    L = len(w["wq"])
+    mats = {"gate_up_f8": [torch.cat([w["w_gate"][i], w["w_up"][i]]) for i in range(L)], "down_residual_f8": w["w_down"],
+            "qkv_f8": [torch.cat([w["wq"][i], w["wk"][i], w["wv"][i]]) for i in range(L)], "o_residual_f8": w["wo"],
+            "lm_head_f8": [w["lm_head"], w["tok_embed"]]}
+    return {name: [held_f8(m, 128) for m in ms] for name, ms in mats.items()}
+
+
+def held_f8(x, block_rows=1, fill=True):
+    """(codes, scales) of x, or of its size"""
+    M, K = x.shape
+    codes = torch.empty((M, K), dtype=torch.float8_e4m3fn, device="cuda")
+    scales = torch.empty(B.ls_op_f8_scale_bytes(M, K, block_rows), dtype=torch.uint8, device="cuda")
+    if fill:
+        B.ls_op_quantize_f8(x, codes, scales, block_rows)
+    return codes, scales
+
+
+def f8_cases(shape, w, M):
+    """A layer's 8-bit path: name -> (callable(layer index), algorithmic bytes per launch, number of distinct operands)."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    cases = {}
+    for name, held in f8_matrices(shape, w).items():
+        # small matrices: further copies, so that no launch finds its weights in L2
+        n = max(len(held), -(-160_000_000 // held[0][0].numel()))
+        held = held + [tuple(t.clone() for t in held[i % len(held)]) for i in range(n - len(held))]
+        N, K = held[0][0].shape
+        h = held_f8(torch.randn((M, K), device="cuda", generator=g))
+        residual = "residual" in name
+        out = torch.zeros((M, N), dtype=torch.float32 if residual or name == "lm_head_f8" else torch.bfloat16, device="cuda")
+        fn = lambda i, held=held, h=h, out=out, a=out if residual else None: B.ls_op_linear_f8(*held[i], *h, out, add=a)  # noqa: E731
+        cases[name] = (fn, N * K + held[0][1].numel(), n)
+    D, F = shape.d_model, shape.d_ffn
+    x, delta = torch.randn((M, D), device="cuda", generator=g), torch.randn((M, D), device="cuda", generator=g).bfloat16()
+    gu = torch.randn((M, 2 * F), device="cuda", generator=g).bfloat16()
+    gain = w["attn_norm"][0]
+    hn, ha = held_f8(x, fill=False), held_f8(gu[:, :F], fill=False)
+    x_out = torch.empty_like(x)
+    cases["rmsnorm_f8"] = (lambda i: B.ls_op_rmsnorm_f8(x, gain, 1e-5, *hn, delta=delta, x_out=x_out), 11 * M * D, 1)
+    cases["swiglu_f8"] = (lambda i: B.ls_op_swiglu_f8(gu[:, :F], gu[:, F:], *ha), 5 * M * F, 1)
+    cases["quantize_f8"] = (lambda i: B.ls_op_quantize_f8(delta, *hn), 3 * M * D, 1)
+    return cases
+
+
+PROMPT_F8_OPS = ("gate_up_f8", "down_residual_f8", "qkv_f8", "o_residual_f8")
+
+
+def prompt_f8_cases(shape, w, R):
+    """The projections of R rows in 8 bits: name -> (callable(layer index), flops per launch, distinct weights)."""
+    mats = f8_matrices(shape, w)
+    cases = f8_cases(shape, w, R)
+    return {name: (cases[name][0], 2 * R * mats[name][0][0].numel(), cases[name][2]) for name in PROMPT_F8_OPS}
+
+
 PROMPT_OPS = ("prompt_gemm_qkv", "prompt_gemm_gate", "prompt_gemm_down", "prompt_attention")
 
 
@@ -171,9 +230,9 @@ def prompt_cases(shape, w, R):
     }
 
 
-def prompt_rates(shape, w, R, ops=PROMPT_OPS, iters=20, warm=3):
+def prompt_rates(shape, w, R, ops=PROMPT_OPS, iters=20, warm=3, bits=16):
     out = {}
-    cases = prompt_cases(shape, w, R)
+    cases = prompt_f8_cases(shape, w, R) if bits == 8 else prompt_cases(shape, w, R)
     for name in ops:
         fn, flops, rot = cases[name]
         ms = time_op(fn, rot, iters, warm)
@@ -188,7 +247,7 @@ def kernel_rooflines(shape, w, path, rows, peak_gbs, ops=OPS, iters=40, warm=5, 
     predecessor's last CTAs finish).  Fractions are algorithmic bytes / time / peak_gbs."""
     out = {}
     for M in rows:
-        cases = op_cases(shape, w, path, M) if bits == 16 else q4_cases(shape, w, M)
+        cases = op_cases(shape, w, path, M) if bits == 16 else f8_cases(shape, w, M) if bits == 8 else q4_cases(shape, w, M)
         for name in ops:
             fn, nbytes, rot = cases[name]
             ms = time_op(fn, rot, iters, warm)
@@ -210,8 +269,8 @@ def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--workload", default="llama2-7b", choices=sorted(synth.WORKLOADS))
     ap.add_argument("--layers", type=int, default=4, help="layers of weights to create and rotate over")
-    ap.add_argument("--ops", default="", help="of " + ", ".join(OPS) + "; with --bits 4 of " + ", ".join(Q4_OPS))
-    ap.add_argument("--bits", type=int, default=16, choices=[16, 4], help="4: packed 4-bit weights and the 4-bit cache")
+    ap.add_argument("--ops", default="", help="of " + ", ".join(OPS) + "; with --bits 4 of " + ", ".join(Q4_OPS) + "; with --bits 8 of " + ", ".join(F8_OPS))
+    ap.add_argument("--bits", type=int, default=16, choices=[16, 8, 4], help="8: a layer's path in 8 bits; 4: packed 4-bit weights and the 4-bit cache")
     ap.add_argument("--rows", default="1,7")
     ap.add_argument("--path", default="mma", choices=["fma", "mma"])
     ap.add_argument("--iters", type=int, default=40)
@@ -219,7 +278,7 @@ def main():
     ap.add_argument("--peak", type=float, default=6553.9, help="GB/s the fractions are quoted against")
     ap.add_argument("--prompt-rows", type=int, default=0, metavar="R",
                     help="instead: the prompt pass's GEMMs and attention on R rows (TFLOP/s); --ops picks among "
-                         + ", ".join(PROMPT_OPS))
+                         + ", ".join(PROMPT_OPS) + "; with --bits 8 among " + ", ".join(PROMPT_F8_OPS))
     a = ap.parse_args()
     from dataclasses import replace
     wl = synth.WORKLOADS[a.workload]
@@ -227,14 +286,15 @@ def main():
     w = synth.make_weights(shape, wl.weight_seed, wl.exit_layer, wl.late_scale, device="cuda")
     path = B.LS_LINEAR_MMA if a.path == "mma" else B.LS_LINEAR_FMA
     if a.prompt_rows:
-        ops = [o for o in a.ops.split(",") if o in PROMPT_OPS] or list(PROMPT_OPS)
-        res = prompt_rates(shape, w, a.prompt_rows, ops, a.iters, a.warm)
+        known = PROMPT_F8_OPS if a.bits == 8 else PROMPT_OPS
+        ops = [o for o in a.ops.split(",") if o in known] or list(known)
+        res = prompt_rates(shape, w, a.prompt_rows, ops, a.iters, a.warm, a.bits)
         for k, v in res.items():
             print(f"{k:28s} {v['ms'] * 1e3:8.2f} us  {v['TFLOP/s']:8.1f} TFLOP/s")
         print(json.dumps(res))
         return
     res = kernel_rooflines(shape, w, path, [int(r) for r in a.rows.split(",")], a.peak,
-                           [o for o in a.ops.split(",") if o] or (OPS if a.bits == 16 else Q4_OPS), a.iters, a.warm, bits=a.bits)
+                           [o for o in a.ops.split(",") if o] or {16: OPS, 8: F8_OPS, 4: Q4_OPS}[a.bits], a.iters, a.warm, bits=a.bits)
     for k, v in res.items():
         print(f"{k:28s} {v['ms'] * 1e3:8.2f} us  {v['GB/s']:8.1f} GB/s  {v['frac']:.3f} of {a.peak:.0f}   chained "
               f"{v['ms_chained'] * 1e3:8.2f} us  {v['frac_chained']:.3f}")
