@@ -582,9 +582,12 @@ def ls_op_f8_scale_bytes(M, K, block_rows=1):
 
 def _held(codes, scales, M, K, block_rows, dev, what):
     """device pointers of codes float8_e4m3fn [M, K] and their scales (uint8, ls_op_f8_scale_bytes of them)"""
+    if codes.dtype is not _torch.f8 or scales.dtype is not _torch.u8 or codes.get_device() != dev or scales.get_device() != dev or \
+            not codes.is_contiguous() or not scales.is_contiguous():
+        _bad(f"{what}: contiguous codes (float8_e4m3fn) and scales (uint8) are needed, on the CUDA device of the others")
     if scales.numel() < ls_op_f8_scale_bytes(M, K, block_rows):
-        raise LsError(LS_ERR_CAPACITY, what + ": scales")
-    return _arg(codes, _torch.f8, dev, what), _arg(scales, _torch.u8, dev, what)
+        raise LsError(LS_ERR_CAPACITY, f"{what}: scales")
+    return codes.data_ptr(), scales.data_ptr()
 
 
 def _strided(t, shape, dev, what):
@@ -602,7 +605,9 @@ def ls_op_quantize_f8(x, codes, scales, block_rows=1):
     M, K = shape
     c, s = _held(codes, scales, M, K, block_rows, dev, "ls_op_quantize_f8")
     xp, kind, ld = _strided(x, shape, dev, "x")
-    _ck(lib().ls_op_quantize_f8(xp, kind, ld, M, K, block_rows, c, s, _stream_on(dev)), "ls_op_quantize_f8")
+    rc = lib().ls_op_quantize_f8(xp, kind, ld, M, K, block_rows, c, s, _stream_on(dev))
+    if rc:
+        raise LsError(rc, "ls_op_quantize_f8")
 
 
 def ls_op_expand_f8(codes, scales, out, block_rows=1):
@@ -612,7 +617,9 @@ def ls_op_expand_f8(codes, scales, out, block_rows=1):
     c, s = _held(codes, scales, M, K, block_rows, dev, "ls_op_expand_f8")
     if out.shape != shape:
         _bad("ls_op_expand_f8: out")
-    _ck(lib().ls_op_expand_f8(c, s, M, K, block_rows, _arg(out, _torch.bf16, dev, "out"), _stream_on(dev)), "ls_op_expand_f8")
+    rc = lib().ls_op_expand_f8(c, s, M, K, block_rows, _arg(out, _torch.bf16, dev, "out"), _stream_on(dev))
+    if rc:
+        raise LsError(rc, "ls_op_expand_f8")
 
 
 def ls_op_rmsnorm_f8(x, gain, eps, codes, scales, delta=None, x_out=None):
@@ -625,8 +632,9 @@ def ls_op_rmsnorm_f8(x, gain, eps, codes, scales, delta=None, x_out=None):
     op, okind, ldo = (xp, kind, ldx) if x_out is x else (None, kind, 0) if x_out is None else _strided(x_out, shape, dev, "x_out")
     if okind != kind or gain.numel() != D:
         _bad("ls_op_rmsnorm_f8: x_out of x's type, gain [D]")
-    _ck(lib().ls_op_rmsnorm_f8(xp, kind, ldx, dp, dkind, ldd, op, ldo, _arg(gain, _torch.bf16, dev, "gain"), M, D, eps, c, s, _stream_on(dev)),
-        "ls_op_rmsnorm_f8")
+    rc = lib().ls_op_rmsnorm_f8(xp, kind, ldx, dp, dkind, ldd, op, ldo, _arg(gain, _torch.bf16, dev, "gain"), M, D, eps, c, s, _stream_on(dev))
+    if rc:
+        raise LsError(rc, "ls_op_rmsnorm_f8")
 
 
 def ls_op_swiglu_f8(gate, up, codes, scales):
@@ -638,7 +646,9 @@ def ls_op_swiglu_f8(gate, up, codes, scales):
     upp, ukind, uld = _strided(up, shape, dev, "up")
     if kind != ukind or (ld != uld and M > 1):
         _bad("ls_op_swiglu_f8: gate and up of one type and row stride")
-    _ck(lib().ls_op_swiglu_f8(gp, upp, kind, ld, M, F, c, s, _stream_on(dev)), "ls_op_swiglu_f8")
+    rc = lib().ls_op_swiglu_f8(gp, upp, kind, ld, M, F, c, s, _stream_on(dev))
+    if rc:
+        raise LsError(rc, "ls_op_swiglu_f8")
 
 
 def ls_op_linear_f8(w_codes, w_scales, h_codes, h_scales, out, add=None, status=None):
@@ -653,8 +663,9 @@ def ls_op_linear_f8(w_codes, w_scales, h_codes, h_scales, out, add=None, status=
     ap, akind, lda = (None, kind, 0) if add is None else (op, kind, ldo) if add is out else _strided(add, (M, N), dev, "add")
     if akind != kind:
         _bad("ls_op_linear_f8: add of out's type")
-    _ck(lib().ls_op_linear_f8(wc, ws, hc, hs, M, N, K, op, kind, ldo, ap, lda, None if status is None else _status(status, dev), _stream_on(dev)),
-        "ls_op_linear_f8")
+    rc = lib().ls_op_linear_f8(wc, ws, hc, hs, M, N, K, op, kind, ldo, ap, lda, None if status is None else _status(status, dev), _stream_on(dev))
+    if rc:
+        raise LsError(rc, "ls_op_linear_f8")
 
 
 def ls_op_accept(draft, verified, d, state, out_ids, accepted):

@@ -2426,11 +2426,15 @@ int linear_f8_choose(const void* wc, const void* hc, const F8Linear& p, const La
     // tokens: 29.0 / 30.8 us, 34.9 / 35.6 without; 96 tiles 17.7 / 19.2, 18.4 / 18.9; 32 tiles 14.4 / 14.6, 11.1 / 13.3)
     if (p.M > 128 || (p.M > 64 && w_tiles > 148)) return linear_f8_pair_launch<BF16>(wc, hc, p, lc);
     const int NT = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
-    // CTAs that share a tile: as many as keep one CTA an SM and two blocks a CTA.  A function of the matrix alone: it enters a
-    // row's arithmetic.  (32 tiles, K = 4096, one token, 1 / 2 / 4 / 8 CTAs: 10.9 / 8.6 / 7.6 / 9.1 us; 86 tiles: 12.8 / 12.4 / 13.9 / 15.5,
+    // CTAs that share a tile: as many as keep one CTA an SM and more than two blocks a CTA (2304x2048, 2 / 4 / 8 CTAs: 5.2 / 4.4 / 5.0 us;
+    // 2048x8192 11.7 / 8.4 / 7.6).  A function of the matrix alone: it enters a row's arithmetic.  (32 tiles, K = 4096, one token, 1 / 2 / 4 / 8 CTAs: 10.9 / 8.6 / 7.6 / 9.1 us; 86 tiles: 12.8 / 12.4 / 13.9 / 15.5,
     // 16 tokens 13.0 / 14.3 / 16.3 / 18.3)
     int S = 1;
-    while (S < 8 && w_tiles * 2 * S <= 148 && kb >= 4 * S) S *= 2;
+    while (S < 8 && w_tiles * 2 * S <= 148 && kb > 4 * S) S *= 2;
+    // Up to 16 tokens and one CTA an SM at most: its ring as long as an SM allows, 11 stages instead of 5 (4096x11008 one token 11.1 us,
+    // 11.8; 11008x4096 12.8, 13.4; 4096x4096 7.5 either way), unless the next operation is to move in beside it (chained
+    // 4096x4096: 5.6 us, 7.0), or clusters of 8 do not all find room (2048x8192: 11.5 us, 7.7).
+    if (NT == 16 && !lc.pdl && S <= 4 && w_tiles * S <= 148) return linear_f8_launch<16, BF16, 1>(wc, hc, p, S, lc);
     return NT == 16 ? linear_f8_launch<16, BF16, 2>(wc, hc, p, S, lc)
            : NT == 32 ? linear_f8_launch<32, BF16, 2>(wc, hc, p, S, lc)
            : NT == 64 ? linear_f8_launch<64, BF16, 2>(wc, hc, p, S, lc)
