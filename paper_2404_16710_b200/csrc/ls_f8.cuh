@@ -64,10 +64,16 @@ __device__ __forceinline__ uint32_t f8_values2(uint32_t codes, float s)
 struct F8Raw {
     uint32_t w[8];
 };
+template <bool LAST = false>  // LAST: nobody reads it again, L2 may drop it first
 __device__ __forceinline__ F8Raw f8_ld32(const void* p, bool wide)
 {
     F8Raw r;
-    if (wide) {
+    if (LAST && wide) {
+        asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
+                     : "l"(p)
+                     : "memory");
+    } else if (wide) {
         asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                      : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
                      : "l"(p)
@@ -187,7 +193,7 @@ __global__ void __launch_bounds__(256) quantize_f8_rows_kernel(const T* __restri
     for (int i = 0; i < N; ++i) {
         const int k = k0 + i * STEP + V * lane;
         raw[i] = F8Raw{};
-        if (k < K) raw[i] = f8_ld32(x + m * ldx + k, wide);  // K is a multiple of 16: all of the piece is in or out
+        if (k < K) raw[i] = f8_ld32<true>(x + m * ldx + k, wide);  // K is a multiple of 16: all of the piece is in or out
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -216,7 +222,7 @@ quantize_f8_weights_kernel(const T* __restrict__ x, int64_t ldx, int M, int K, i
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         raw[i] = F8Raw{};
-        if (k < K && m0 + i * ROWS < M) raw[i] = f8_ld32(src, wide);
+        if (k < K && m0 + i * ROWS < M) raw[i] = f8_ld32<true>(src, wide);
         src += ROWS * ldx;
     }
 #pragma unroll
@@ -427,8 +433,8 @@ __global__ void __launch_bounds__(256) swiglu_f8_kernel(const T* __restrict__ ga
         const int k = k0 + i * STEP + V * lane;
         g[i] = u[i] = F8Raw{};
         if (k < F) {
-            g[i] = f8_ld32(gate + m * ld + k, wide);
-            u[i] = f8_ld32(up + m * ld + k, wide);
+            g[i] = f8_ld32<true>(gate + m * ld + k, wide);
+            u[i] = f8_ld32<true>(up + m * ld + k, wide);
         }
     }
 #pragma unroll

@@ -2389,8 +2389,8 @@ int linear_f8_pair_launch(const void* wc, const void* hc, const F8Linear& p, con
     LS_TRY((f8_pair_clusters<BF16, true>(2, &most[2])));
     LS_TRY((f8_pair_clusters<BF16, true>(4, &most[4])));
     if (most[1] < 1) return LS_ERR_UNSUPPORTED;
-    // Tokens of a tile, and pairs that share one along K: what costs least.  In cycles, a block along K takes 400 up to 175 tokens
-    // (what the ring hides of the loads' latency) and 1.6 a token beyond (products, and loads from L2), a tile's end 4000 for 240
+    // Tokens of a tile, and pairs that share one along K: what costs least.  In cycles, a block along K takes 390 or 277 and 0.93 a
+    // token (60 bytes a cycle of a CTA's loads from L2: 391 for 64 tokens, 396 for 128, 500 for 240), a tile's end 4000 for 240
     // tokens, which the next tile's products cover where there is one and they are longer, and the larger cluster and joining 10000 (512x512, K = 14336,
     // 512 tokens: 18.0 us with four pairs, 29.8 with one; 4096x11008, 256 tokens: 22.4 with two, 26.2; 4096x4096, 160 tokens 15.7, 13.5).
     const int w_tiles = (p.N + 2 * kF8Block - 1) / (2 * kF8Block), groups = ((p.K + kF8Block - 1) / kF8Block + 3) / 4;
@@ -2398,7 +2398,7 @@ int linear_f8_pair_launch(const void* wc, const void* hc, const F8Linear& p, con
     double best = 0;
     for (int n = kF8PairTokens; n >= 16; n -= 16) {
         const int tt = (p.M + n - 1) / n;
-        const double tiles = (double)w_tiles * tt, block = std::max(400.0, 120 + 1.6 * n);
+        const double tiles = (double)w_tiles * tt, block = std::max(390.0, 277 + 0.93 * n);
         for (int k = 1; k <= 4; k *= 2) {
             if (k > 1 && (tiles > most[k] || groups < 2 * k)) continue;
             const double end = 4000.0 * n / kF8PairTokens;
