@@ -763,7 +763,9 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     if constexpr (SPLIT) {
         // the 16 tokens from c on belong to pair c / 16 % sk; part [pair][c / 16 / sk][warp][token][lane]
         __syncwarp();
-        cluster_sync_all();  // every pair's products are made: nothing uses the rings any more
+        // every pair's products are made: nothing uses the rings any more (reads that are complete need no release, which takes 0.4 us)
+        cluster_arrive_relaxed();
+        cluster_wait();
         const uint32_t part = base + 4u * (uint32_t)(warp * 512 + lane), each = 4u * (uint32_t)(4 / sk) * 8192u;
         if (warp < 16) {
 #pragma unroll

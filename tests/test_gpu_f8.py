@@ -359,6 +359,23 @@ def test_linear_rows_do_not_depend_on_pass_size(N, K):
         assert torch.equal(out, full[m0:m0 + M]), M
 
 
+@pytest.mark.parametrize("M", [1, 16, 30, 64, 100, 300])
+def test_linear_chained_gives_the_same_bits(M):
+    """chained operations run beside one another, on shorter rings of stages: the sums are the same"""
+    N, K = 1000, 4112
+    w, h = pair_of(M, N, K, 17)
+    alone, chained = (torch.full((M, N), float("nan"), device="cuda") for _ in range(2))
+    B.ls_op_linear_f8(*w, *h, alone)
+    torch.cuda.synchronize()
+    B.ls_op_chain(True)
+    try:
+        for _ in range(3):
+            B.ls_op_linear_f8(*w, *h, chained)
+    finally:
+        B.ls_op_chain(False)
+    assert torch.equal(alone, chained)
+
+
 @pytest.mark.parametrize("M,N,K", [(5, 300, 1040), (90, 300, 1040), (300, 700, 1040)])
 def test_linear_any_scales_and_blocks_that_are_not_finite(M, N, K):
     """bytes of other quantisers, rubbish behind the last block's byte, NaN blocks on either side"""
