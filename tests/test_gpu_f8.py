@@ -307,7 +307,8 @@ SHAPES = [(1, 1, 16), (1, 128, 128), (1, 4096, 4096), (2, 200, 144), (7, 333, 10
           (16, 1000, 14336), (5, 32000, 528), (17, 300, 1040), (32, 129, 4096), (33, 4096, 656), (64, 257, 2048), (65, 500, 400),
           (100, 1000, 4096), (128, 4096, 1040), (129, 384, 1040), (255, 256, 528), (256, 512, 4096), (257, 1030, 1040), (300, 129, 4112),
           (1030, 770, 2064), (1025, 2600, 400), (2050, 300, 144), (700, 4096, 4096),
-          (130, 300, 8208), (512, 512, 4112), (300, 129, 14336), (241, 1000, 4096), (777, 1030, 9232), (1919, 134, 2448), (2050, 250, 4624)]
+          (130, 300, 8208), (512, 512, 4112), (300, 129, 14336), (241, 1000, 4096), (777, 1030, 9232), (1919, 134, 2448), (2050, 250, 4624),
+          (3, 70, 262160), (150, 70, 262160)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
