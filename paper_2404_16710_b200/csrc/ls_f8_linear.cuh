@@ -14,8 +14,8 @@
 // Measured (B200, 1965 MHz until the power limit, inputs not in L2): 4096 x 4096, one token 7.5 us (5.6 chained); 4096 x 11008, 7 tokens
 // with add 12.4; 128256 x 4096, 16 tokens 83 - 88 (6.0 - 6.4 TB/s); 12288 x 4096, 1030 tokens 47 (2.2 PFLOP/s); 22016 x 4096, 4096 tokens
 // 276 - 282 (2.65 PFLOP/s; at 1.18 GHz under the power limit 84 % of what the tensor cores can do).
-// Rows of K = 16 mod 32 bytes begin inside a 32-byte sector: the loads of every second row then cost about 1.4 times (2334 x 7600, 2108
-// tokens: 54.7 us, K = 7616 40.7).  The layout is the caller's, and both operands have to agree on the columns of a step.
+// Rows of K = 16 mod 32 bytes begin inside a 32-byte sector: the loads of every second row then cost more (2334 x 7600, 2108 tokens:
+// 49.3 us, K = 7616 40.4).  The layout is the caller's, and both operands have to agree on the columns of a step.
 #pragma once
 #include <type_traits>
 
