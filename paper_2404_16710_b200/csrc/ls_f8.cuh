@@ -113,6 +113,7 @@ struct F8In<float> {
         f8_st32(p, w, wide);
     }
     static __device__ __forceinline__ float kept(float v) { return v; }
+    static __device__ __forceinline__ float value(float v) { return v; }
 };
 template <>
 struct F8In<uint16_t> {  // bf16
@@ -130,6 +131,7 @@ struct F8In<uint16_t> {  // bf16
         f8_st32(p, w, wide);
     }
     static __device__ __forceinline__ float kept(float v) { return bf16f(f2bf(v)); }  // the value that store() leaves
+    static __device__ __forceinline__ float value(uint16_t v) { return bf16f(v); }
 };
 
 __device__ __forceinline__ float max_nan(float a, float b)  // a NaN wins
@@ -159,19 +161,80 @@ __device__ __forceinline__ void f8_store_codes(unsigned char* p, const float (&v
     if constexpr (V == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
+// largest over the 128 / V lanes that hold a block
+template <int V>
+__device__ __forceinline__ uint32_t f8_block_max(uint32_t a)
+{
+#pragma unroll
+    for (int o = 64 / V; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
+    return a;
+}
+// A double as a float, rounded to odd: where it is inexact the last bit is set, so that a later rounding to fewer bits, and a
+// comparison with a number of fewer bits, decide as the double would.
+__device__ __forceinline__ float f8_odd(double y)
+{
+    const float n = (float)y, f = __double2float_rz(y);
+    return (double)n == y || isinf(n) ? n : __uint_as_float(__float_as_uint(f) | 1u);
+}
+// Values computed in fp32, off by up to W 2^-24 of theirs, are rounded to 4 bits here.  What lies so near a border between two
+// codes (one value in 2^20 / 2 W) or two scales is computed again, by fix(k) for column k: in 64 bits, rounded to odd, so
+// that codes and scales are those of the exact values (of 18 million, fp32 alone gave 10 the neighbouring code).  Borders
+// have 0x80000 in the 20 bits behind the code's three; of t (1 + W 2^-24), with t near one, they are up to 2 W + 1 above
+// that.  Codes below 2^-6 s (8 of the 127, a fixed distance apart) keep the fp32 value's rounding.
+__device__ __forceinline__ uint32_t f8_above_border(float t) { return (__float_as_uint(t) ^ 0x80000u) & 0xfffffu; }
+struct F8AsIs {};  // with W = 0: the values are what they are
+// The two rare ways are calls, whose registers and instructions the others do not carry: the columns of a lane that `todo`
+// names, and a warp's whole part where the scale is in doubt.
+template <typename Fix>
+__device__ __noinline__ void f8_fix_codes(Fix fix, int k, uint32_t todo, float r, unsigned char* codes)
+{
+    for (; todo; todo &= todo - 1) {
+        const int j = __ffs(todo) - 1;
+        codes[k + j] = (unsigned char)f8_codes4(fix(k + j), 0.f, 0.f, 0.f, r);
+    }
+}
+template <int V, typename Fix>
+__device__ __noinline__ void f8_fix_part(Fix fix, int k, int K, int width, unsigned char* codes, unsigned char* scales)
+{
+    uint32_t a = 0;
+#pragma unroll 1
+    for (int j = 0; j < V; ++j)
+        if (k < K) a = max(a, __float_as_uint(fix(k + j)) & 0x7fffffffu);
+    const uint32_t e = f8_scale_byte(f8_block_max<V>(a));
+    if (k < K) f8_fix_codes(fix, k, (1u << V) - 1, f8_inverse(e), codes);
+    if (k % kF8Block == 0 && k / kF8Block < width) scales[k / kF8Block] = k < K ? (unsigned char)e : 0;
+}
 // A warp's 32 V columns of a row, from column k0 (a multiple of 128; lane l holds columns k0 + V l ..): codes and scale
 // bytes, and zeros behind the row's last block.  Lanes beyond K hold zeros.
-template <int V>
+template <int V, int W, typename Fix>
 __device__ __forceinline__ void f8_store_row_part(const float (&v)[V], int k0, int K, int width, unsigned char* codes,
-                                                  unsigned char* scales)
+                                                  unsigned char* scales, Fix fix)
 {
     const int k = k0 + V * (threadIdx.x & 31);
-    uint32_t a = f8_absmax<V>(v);
-#pragma unroll
-    for (int o = 64 / V; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));  // the 128 / V lanes of a block
+    const uint32_t a = f8_block_max<V>(f8_absmax<V>(v));
+    if constexpr (W > 0) {
+        if (__any_sync(0xffffffffu, (a & 0x7fffffu) - (0x600000u - W) <= 2u * W)) {  // 448 = 1.75 2^8
+            f8_fix_part<V>(fix, k, K, width, codes, scales);
+            return;
+        }
+    }
     const uint32_t e = f8_scale_byte(a);
-    if (k < K) f8_store_codes<V>(codes + k, v, f8_inverse(e));
+    const float r = f8_inverse(e);
+    if (k < K) f8_store_codes<V>(codes + k, v, r);
     if (k % kF8Block == 0 && k / kF8Block < width) scales[k / kF8Block] = k < K ? (unsigned char)e : 0;
+    if constexpr (W > 0) {
+        const float q = r * (1.f + W * 0x1p-24f);
+        uint32_t near = 0xfffffu;
+#pragma unroll
+        for (int j = 0; j < V; j += 2) near = __vimin3_u32(near, f8_above_border(v[j] * q), f8_above_border(v[j + 1] * q));
+        if (near <= 2 * W + 1) {
+            uint32_t todo = 0;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (f8_above_border(v[j] * q) <= 2 * W + 1) todo |= 1u << j;
+            f8_fix_codes(fix, k, todo, r, codes);
+        }
+    }
 }
 
 // ------------------------------------------------------------------ rows and weights -> 8 bits, and back
@@ -199,7 +262,7 @@ __global__ void __launch_bounds__(256) quantize_f8_rows_kernel(const T* __restri
     for (int i = 0; i < N; ++i) {
         float v[V];
         F8In<T>::unpack(raw[i], v);
-        if (k0 + i * STEP < width * kF8Block) f8_store_row_part<V>(v, k0 + i * STEP, K, width, codes + m * K, scales + m * width);
+        if (k0 + i * STEP < width * kF8Block) f8_store_row_part<V, 0>(v, k0 + i * STEP, K, width, codes + m * K, scales + m * width, F8AsIs{});
     }
 }
 
@@ -290,17 +353,23 @@ __global__ void __launch_bounds__(256) expand_f8_kernel(const unsigned char* __r
 }
 
 // ------------------------------------------------------------------ RMSNorm with the residual's addition, into 8 bits
-// x' = x + d rounded to x's type, y = x' / sqrt(mean x'^2 + eps) * gain, sums in fp32.  A CTA takes a row; with NV > 0 a
-// thread keeps its NV pieces of it in registers, else (rows too long for that) x' is read again, from x_out where it was
-// written.  d and x_out may be null, x_out may be x or d.  Bound by memory: 4096 x 4096, fp32 x and bf16 d 32.3 us, 5.7 TB/s (41 with
-// 16-byte accesses); one row 2.6 us, a launch.
+// x' = x + d rounded to x's type, y = x' / sqrt(mean x'^2 + eps) * gain.  Squares are added in fp32 within a thread's 32-byte piece (two
+// sums) and in 64 bits from there on; the rest is fp32, off by 5.5 2^-24: 7 roundings, three of them under the root.  A CTA
+// takes a row; with NV > 0 a thread keeps its NV pieces of it in registers, else (rows too long for that) x' is read again,
+// from x_out where it was written.  d and x_out may be null, x_out may be x or d.  Bound by memory and, since the borders
+// are checked, by registers: 4096 x 4096, fp32 x and bf16 d 36.1 us, 5.1 TB/s (without the check 31.5; that with 16-byte
+// accesses 41); one row 2.8 us, a launch.
+__device__ __forceinline__ float f8_norm_exact(float x, float g, double ss, int D, float eps)
+{
+    return f8_odd((double)x * (1.0 / sqrt(ss / D + (double)eps)) * (double)g);
+}
 template <typename T, typename TD, int NV>
 __global__ void __launch_bounds__(NV >= 4 ? 512 : 1024)
 rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, int64_t ldo, const uint16_t* gain, int D, float eps, int wide,
                   unsigned char* __restrict__ codes, unsigned char* __restrict__ scales)
 {
     constexpr int V = F8In<T>::V, KEEP = NV > 0 ? NV : 1;
-    __shared__ float part[32];
+    __shared__ double part[32];
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, T0 = blockDim.x;
@@ -330,12 +399,13 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
             for (int j = 0; j < V; ++j) v[j] = F8In<T>::kept(v[j] + a[j]);
         }
     };
-    float v[KEEP][V], ss = 0.f;
+    float v[KEEP][V];
+    double ss = 0;
     auto square = [&](const float (&u)[V]) {
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < V; ++j) s[j & 1] = fmaf(u[j], u[j], s[j & 1]);
-        ss += s[0] + s[1];
+        ss += (double)s[0] + (double)s[1];
     };
     if (NV > 0) {
 #pragma unroll
@@ -362,10 +432,15 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
     for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     if ((tid & 31) == 0) part[tid >> 5] = ss;
     __syncthreads();
-    ss = (tid & 31) < T0 / 32 ? part[tid & 31] : 0.f;
+    ss = (tid & 31) < T0 / 32 ? part[tid & 31] : 0.0;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    const float r = 1.0f / sqrtf(ss / (float)D + eps);
+    const float r = 1.0f / sqrtf((float)ss / (float)D + eps);
+    auto exact = [=](int k) {
+        float u = F8In<T>::value(x_out ? x_out[k] : x[k]);
+        if (!x_out && d) u = F8In<T>::kept(u + F8In<TD>::value(d[k]));
+        return f8_norm_exact(u, bf16f(gain[k]), ss, D, eps);
+    };
     auto finish = [&](int k, float (&u)[V]) {  // whole warps
         if (k < D) {
 #pragma unroll
@@ -379,7 +454,7 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
                 }
             }
         }
-        f8_store_row_part<V>(u, k - V * (tid & 31), D, width, codes + m * D, scales + m * width);
+        f8_store_row_part<V, 8>(u, k - V * (tid & 31), D, width, codes + m * D, scales + m * width, exact);
     };
     if (NV > 0) {
 #pragma unroll
@@ -401,7 +476,7 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
 // ------------------------------------------------------------------ SwiGLU into 8 bits
 // y = gate / (1 + exp(-gate)) * up.  exp(-g) = 2^t (1 + d ln 2), t = -g log2 e rounded, d what it was rounded by (the product's
 // error, which the fma gives exactly, and that of log2 e), so that the exponential is off by little more than ex2.approx,
-// 2^-22 of its value, however large g.  (With expf and a division the kernel issued 2.75 instructions a cycle and took
+// 2^-22 of its value, however large g; in all y is off by 10 2^-24 of its value.  (With expf and a division the kernel issued 2.75 instructions a cycle and took
 // 86 us, 4096 x 11008 bf16.)  From t = 126 on (gates below -87.3) the
 // reciprocal is not a normal number and counts as 0.
 __device__ __forceinline__ float f8_silu_times(float g, float u)
@@ -414,37 +489,50 @@ __device__ __forceinline__ float f8_silu_times(float g, float u)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
     return g * r * u;
 }
-// A warp takes 512 features of a row.  Bound by memory: 4096 x 11008 bf16 38.9 us, 5.8 TB/s.
-template <typename T>
-__global__ void __launch_bounds__(256) swiglu_f8_kernel(const T* __restrict__ gate, const T* __restrict__ up, int64_t ld, int F, int parts,
-                                                        long long items, int wide, unsigned char* __restrict__ codes,
-                                                        unsigned char* __restrict__ scales)
+__device__ __forceinline__ float f8_silu_exact(float g, float u)
 {
-    constexpr int V = F8In<T>::V, STEP = 32 * V, N = 512 / STEP;
+    return f8_odd((double)g / (1.0 + exp(-(double)g)) * (double)u);
+}
+// A warp takes 32 V features of a row at a time, and loads its next piece before it works on this one: the check of the borders
+// leaves 32 warps an SM, whose loads alone would not cover the memory's latency (4096 x 11008 bf16: 51 us without, 46.4 with;
+// unrolled twice 50).  4.9 TB/s; without the check 39, 5.8.
+template <typename T>
+__global__ void __launch_bounds__(256, 4) swiglu_f8_kernel(const T* __restrict__ gate, const T* __restrict__ up, int64_t ld, int M, int F,
+                                                           int parts, int dm, int dp, int wide, unsigned char* __restrict__ codes,
+                                                           unsigned char* __restrict__ scales)
+{
+    constexpr int V = F8In<T>::V, STEP = 32 * V;
     pdl_launch_dependents();
     pdl_wait();
-    const long long it = (long long)blockIdx.x * 8 + threadIdx.x / 32;
-    if (it >= items) return;
-    const long long m = it / parts;
-    const int k0 = (int)(it - m * parts) * 512, lane = threadIdx.x & 31, width = 4 * parts;
-    F8Raw g[N], u[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int k = k0 + i * STEP + V * lane;
-        g[i] = u[i] = F8Raw{};
-        if (k < F) {
-            g[i] = f8_ld32<true>(gate + m * ld + k, wide);
-            u[i] = f8_ld32<true>(up + m * ld + k, wide);
+    const int it = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x & 31, width = parts * STEP / kF8Block;
+    uint32_t m = it / parts;  // m1 may pass 2^31
+    int p = it - (int)m * parts;
+    F8Raw g, u;
+    auto load = [&](uint32_t m, int p, F8Raw& g, F8Raw& u) {
+        const int k = p * STEP + V * lane;
+        g = u = F8Raw{};
+        if (m < (uint32_t)M && k < F) {
+            g = f8_ld32<true>(gate + m * ld + k, wide);
+            u = f8_ld32<true>(up + m * ld + k, wide);
         }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
+    };
+    load(m, p, g, u);
+#pragma unroll 1
+    while (m < (uint32_t)M) {
+        F8Raw g1, u1;
+        uint32_t m1 = m + dm;
+        int p1 = p + dp;
+        if (p1 >= parts) ++m1, p1 -= parts;
+        load(m1, p1, g1, u1);
         float a[V], b[V];
-        F8In<T>::unpack(g[i], a);
-        F8In<T>::unpack(u[i], b);
+        F8In<T>::unpack(g, a);
+        F8In<T>::unpack(u, b);
 #pragma unroll
         for (int j = 0; j < V; ++j) a[j] = f8_silu_times(a[j], b[j]);
-        f8_store_row_part<V>(a, k0 + i * STEP, F, width, codes + m * F, scales + m * width);
+        const T *gm = gate + m * ld, *um = up + m * ld;
+        auto exact = [=](int k) { return f8_silu_exact(F8In<T>::value(gm[k]), F8In<T>::value(um[k])); };
+        f8_store_row_part<V, 12>(a, p * STEP, F, width, codes + (int64_t)m * F, scales + (int64_t)m * width, exact);
+        m = m1, p = p1, g = g1, u = u1;
     }
 }
 

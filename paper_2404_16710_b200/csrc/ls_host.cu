@@ -2468,13 +2468,14 @@ int ls_op_swiglu_f8(const void* gate, const void* up, int32_t type, int64_t ld, 
 {
     if (!f8_shape_ok(M, F) || !f8_rows_ok(gate, type, ld, M, F) || !aligned16(up) || !f8_held_ok(codes, scales)) return LS_ERR_INVALID_ARG;
     const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
-    const int parts = (F + 511) / 512, wide = f8_wide(gate, type, ld, M) && f8_wide(up, type, ld, M);
-    const long long items = (long long)M * parts;
-    if ((items + 7) / 8 > 0x7fffffff) return LS_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((items + 7) / 8));
+    const int wide = f8_wide(gate, type, ld, M) && f8_wide(up, type, ld, M);
+    const int parts = (int)f8_scale_width(F) / (type == LS_F32 ? 2 : 4);  // of 256 or 512 columns
+    const int64_t ctas = std::min<int64_t>(((int64_t)M * parts + 7) / 8, 148 * 4);  // as many as are resident
+    const int dm = (int)(ctas * 8 / parts), dp = (int)(ctas * 8 % parts);
+    const dim3 grid((unsigned)ctas);
     unsigned char *c = (unsigned char*)codes, *e = (unsigned char*)scales;
-    if (type == LS_F32) LS_CK(launch(lc, swiglu_f8_kernel<float>, grid, dim3(256), 0, (const float*)gate, (const float*)up, ld, F, parts, items, wide, c, e));
-    else LS_CK(launch(lc, swiglu_f8_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)gate, (const uint16_t*)up, ld, F, parts, items, wide, c, e));
+    if (type == LS_F32) LS_CK(launch(lc, swiglu_f8_kernel<float>, grid, dim3(256), 0, (const float*)gate, (const float*)up, ld, M, F, parts, dm, dp, wide, c, e));
+    else LS_CK(launch(lc, swiglu_f8_kernel<uint16_t>, grid, dim3(256), 0, (const uint16_t*)gate, (const uint16_t*)up, ld, M, F, parts, dm, dp, wide, c, e));
     return LS_OK;
 }
 

@@ -516,3 +516,70 @@ def test_captured_replayed_and_on_two_streams():
         torch.cuda.synchronize()
         for (_, _, eager, _, x), y in zip(sets, got):
             assert torch.equal(x, eager[i]) and torch.equal(y, eager[i])
+
+
+# ------------------------------------------------------------------ borders
+# A value computed in fp32 next to a border between two codes is decided in 64 bits: codes at and above 2^-6 s and all scales are those
+# of the values in 64 bits.
+def check_exact(codes, scales, want):
+    assert np.array_equal(scales.cpu().numpy(), R.scale_bytes(want, 1))
+    s = R.scales(scales.cpu().numpy(), *want.shape, 1)
+    assert ((bits(codes) == R.codes(want, 1)) | (np.abs(want) < 2.0 ** -6 * (1 + 2.0 ** -20) * s)).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,F", [(1000, 2064), (300, 12304), (500, 4112)])
+def test_swiglu_codes_next_to_a_border(M, F, dtype):
+    gu = (2 * rnd((M, 2 * F), 5)).to(dtype)
+    codes, scales = empty_held(M, F)
+    B.ls_op_swiglu_f8(gu[:, :F], gu[:, F:], codes, scales)
+    g, u = f64(gu[:, :F]), f64(gu[:, F:])
+    check_exact(codes, scales, g / (1 + np.exp(-g)) * u)
+
+
+def test_swiglu_scales_next_to_a_border():
+    """each block's largest value lies within a few units of 448 2^k, on either side, in every place of the block"""
+    M, F = 64, 1040
+    rng = np.random.default_rng(3)
+    g = rng.uniform(-3, 3, (M, F)).astype(np.float32)
+    u = rng.uniform(-1, 1, (M, F)).astype(np.float32)
+    for m in range(M):
+        for b in range(-(-F // 128)):
+            k = min(128 * b + (2 * m + b) % 128, F - 1)
+            g[m, k] = rng.uniform(0.5, 4)
+            y = float(g[m, k]) / (1 + np.exp(-float(g[m, k])))
+            v = np.float32(448 * 2.0 ** rng.integers(-4, 5) / y)
+            for _ in range(m % 3):
+                v = np.nextafter(v, np.float32(0 if b % 2 else 1e9))
+            u[m, k] = v
+    codes, scales = empty_held(M, F)
+    B.ls_op_swiglu_f8(torch.from_numpy(g).cuda(), torch.from_numpy(u).cuda(), codes, scales)
+    x = g.astype(np.float64)
+    check_exact(codes, scales, x / (1 + np.exp(-x)) * u.astype(np.float64))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,D", [(700, 2064), (400, 4096), (300, 8208), (40, 12304), (9, 40000)])
+@pytest.mark.parametrize("form", ["alone", "added", "kept"])
+def test_norm_codes_next_to_a_border(M, D, dtype, form):
+    """multiples of 1/4 up to 4: their squares' sums are exact, so that nothing but the borders decides"""
+    g = torch.Generator(device="cuda").manual_seed(M + D)
+    x = (torch.randint(-8, 9, (M, D), generator=g, device="cuda") / 4).to(dtype)
+    d = None if form == "alone" else (torch.randint(-8, 9, (M, D), generator=g, device="cuda") / 4).to(BF16)
+    gain = (1 + 0.1 * rnd((D,), 3)).to(BF16)
+    codes, scales = empty_held(M, D)
+    out = torch.empty_like(x) if form == "kept" else None
+    want = normed(added(x, d), gain, 2.0 ** -17)
+    B.ls_op_rmsnorm_f8(x, gain, 2.0 ** -17, codes, scales, delta=d, x_out=out)
+    check_exact(codes, scales, want)
+
+
+def test_swiglu_many_rows_of_one_piece():
+    """more pieces than warps that are resident, one and two a row, and a last round that only some warps have"""
+    for M, F in ((20011, 16), (9001, 528), (4736 * 2 + 1, 256)):
+        for dtype in (BF16, F32):
+            gu = rnd((M, 2 * F), F).to(dtype)
+            codes, scales = empty_held(M, F)
+            B.ls_op_swiglu_f8(gu[:, :F], gu[:, F:], codes, scales)
+            g, u = f64(gu[:, :F]), f64(gu[:, F:])
+            check_exact(codes, scales, g / (1 + np.exp(-g)) * u)
