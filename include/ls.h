@@ -480,13 +480,14 @@ int ls_op_expand_f8(const void *codes_dev, const void *scales_dev, int32_t M, in
                     void *out_bf16_dev, void *cuda_stream);
 /* RMSNorm with the residual's addition: x' = x + delta, rounded to x's type and written to x_out (of x's type;
  * may be x or delta itself, or NULL: not kept); codes and scales (block_rows = 1) of
- * x'[m,i] / sqrt(mean_j x'[m,j]^2 + eps) * gain[i], gain bf16 [D].  delta may be NULL.  Sums in fp32. */
+ * x'[m,i] / sqrt(mean_j x'[m,j]^2 + eps) * gain[i], gain bf16 [D].  delta may be NULL.  In fp32, squares
+ * joined in 64 bits; values next to a border between two codes are decided in 64 bits. */
 int ls_op_rmsnorm_f8(const void *x_dev, int32_t x_type, int64_t ldx, const void *delta_dev, int32_t delta_type,
                      int64_t ldd, void *x_out_dev, int64_t ldo, const void *gain_dev, int32_t M, int32_t D, float eps,
                      void *codes_dev, void *scales_dev, void *cuda_stream);
 /* SwiGLU: codes and scales (block_rows = 1) of silu(gate[m,f]) * up[m,f]; gate and up of one type and row
- * stride (two halves of one product's rows, or two tensors).  fp32; silu is 0 below -87.3, where exp(-x) leaves its normal
- * numbers. */
+ * stride (two halves of one product's rows, or two tensors).  fp32, next to a border between two codes 64 bits; silu is 0
+ * below -87.3, where exp(-x) leaves its normal numbers. */
 int ls_op_swiglu_f8(const void *gate_dev, const void *up_dev, int32_t type, int64_t ld, int32_t M, int32_t F,
                     void *codes_dev, void *scales_dev, void *cuda_stream);
 /* out[m,n] = (add[m,n] +) sum_k h[m,k] w[n,k]: w [N, K] with block_rows = 128, h [M, K] with
