@@ -486,8 +486,8 @@ int ls_op_rmsnorm_f8(const void *x_dev, int32_t x_type, int64_t ldx, const void 
                      int64_t ldd, void *x_out_dev, int64_t ldo, const void *gain_dev, int32_t M, int32_t D, float eps,
                      void *codes_dev, void *scales_dev, void *cuda_stream);
 /* SwiGLU: codes and scales (block_rows = 1) of silu(gate[m,f]) * up[m,f]; gate and up of one type and row
- * stride (two halves of one product's rows, or two tensors).  fp32, next to a border between two codes 64 bits; silu is 0
- * below -87.3, where exp(-x) leaves its normal numbers. */
+ * stride (two halves of one product's rows, or two tensors).  fp32, next to a border between two codes (of 2^-6 s and more) 64 bits;
+ * silu is 0 below -87.3, where exp(-x) leaves its normal numbers, and x above 88. */
 int ls_op_swiglu_f8(const void *gate_dev, const void *up_dev, int32_t type, int64_t ld, int32_t M, int32_t F,
                     void *codes_dev, void *scales_dev, void *cuda_stream);
 /* out[m,n] = (add[m,n] +) sum_k h[m,k] w[n,k]: w [N, K] with block_rows = 128, h [M, K] with

@@ -474,28 +474,33 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
 }
 
 // ------------------------------------------------------------------ SwiGLU into 8 bits
-// y = gate / (1 + exp(-gate)) * up.  exp(-g) = 2^t (1 + d ln 2), t = -g log2 e rounded, d what it was rounded by (the product's
+// y = gate / (1 + exp(-gate)) * up.  exp(-g) = 2^t (1 + d ln 2), t = -g log2 e rounded down, d what it was rounded by (the product's
 // error, which the fma gives exactly, and that of log2 e), so that the exponential is off by little more than ex2.approx,
-// 2^-22 of its value, however large g; in all y is off by 10 2^-24 of its value.  (With expf and a division the kernel issued 2.75 instructions a cycle and took
+// 2^-22 of its value; in all y is off by 10 2^-24 of its value.  (With expf and a division the kernel issued 2.75 instructions a cycle and took
 // 86 us, 4096 x 11008 bf16.)  From t = 126 on (gates below -87.3) the
 // reciprocal is not a normal number and counts as 0.
+// d is held to 0 .. 1, which costs nothing: of far gates t overflows, or is rounded by more than it may be.  As t is rounded down, d is
+// negative only for positive gates, by log2 e's part: with exp(-g) beside 1 that is less than 2^-27 of y.
+// The reciprocal is multiplied by up first: that cannot overflow, and the bits it loses below the normal numbers are below the
+// codes'; half of a subnormal gate would lose bits that count.
 __device__ __forceinline__ float f8_silu_times(float g, float u)
 {
     const float c = -1.44269502e+00f, c_lo = -1.92596299e-08f, ln2 = 0.693147182f;  // -log2 e in two parts
-    const float t = g * c, d = fmaf(g, c_lo, fmaf(g, c, -t));
+    const float t = __fmul_rd(g, c), d = __saturatef(fmaf(g, c_lo, fmaf(g, c, -t)));  // of a NaN: 0
     float e, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fminf(t, 127.f)));
     e = fmaf(e, d * ln2, e);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-    return g * r * u;
+    return g * (r * u);
 }
 __device__ __forceinline__ float f8_silu_exact(float g, float u)
 {
-    return f8_odd((double)g / (1.0 + exp(-(double)g)) * (double)u);
+    const double q = 1.0 + exp(-(double)g);
+    return f8_odd((q > 0x1p126 ? (double)g * 0.0 : (double)g / q) * (double)u);
 }
 // A warp takes 32 V features of a row at a time, and loads its next piece before it works on this one: the check of the borders
-// leaves 32 warps an SM, whose loads alone would not cover the memory's latency (4096 x 11008 bf16: 51 us without, 46.4 with;
-// unrolled twice 50).  4.9 TB/s; without the check 39, 5.8.
+// leaves 32 warps an SM, whose loads alone would not cover the memory's latency (4096 x 11008 bf16: 51 us without, 46.4 with (46.8 since
+// far gates are right); unrolled twice 50).  4.8 TB/s; without the check 39, 5.8.
 template <typename T>
 __global__ void __launch_bounds__(256, 4) swiglu_f8_kernel(const T* __restrict__ gate, const T* __restrict__ up, int64_t ld, int M, int F,
                                                            int parts, int dm, int dp, int wide, unsigned char* __restrict__ codes,

@@ -583,3 +583,62 @@ def test_swiglu_many_rows_of_one_piece():
             B.ls_op_swiglu_f8(gu[:, :F], gu[:, F:], codes, scales)
             g, u = f64(gu[:, :F]), f64(gu[:, F:])
             check_exact(codes, scales, g / (1 + np.exp(-g)) * u)
+
+
+# ------------------------------------------------------------------ the ends of SwiGLU's range
+LAST_GATE = 126 * np.log(2.0)  # beyond, 1 + exp(-gate) is 2^126 and more: silu is 0
+
+
+def silu64(g):
+    with np.errstate(over="ignore"):
+        return np.where(g < -LAST_GATE, 0.0, g / (1 + np.exp(-g)))
+
+
+def partners(g, rng):
+    """fp32 values u for rows of one gate each: neither silu(g) u nor silu'(g) = silu(g) / g times u leaves the normal numbers"""
+    e = np.frexp(g.astype(np.float64))[1][:, None]
+    k = np.where(e > 8, -np.minimum(e, 100), np.where((g[:, None] < -16), rng.integers(3, 20, (len(g), 128)), np.minimum(-e, 120)))
+    return (np.ldexp(rng.uniform(0.5, 1, (len(g), 128)), k) * rng.choice([-1.0, 1.0], (len(g), 128))).astype(np.float32)
+
+
+def check_gates(g, dtype, seed):
+    """rows of 128 columns, each of one gate, so that nothing larger hides what becomes of it"""
+    u = torch.from_numpy(partners(g, np.random.default_rng(seed))).cuda().to(dtype)
+    gate = torch.from_numpy(g).cuda().to(dtype)[:, None].expand(-1, 128).contiguous()
+    codes, scales = empty_held(*u.shape)
+    B.ls_op_swiglu_f8(gate, u, codes, scales)
+    with np.errstate(invalid="ignore"):
+        check_rounded(codes, scales, silu64(f64(gate)) * f64(u), SWIGLU_DELTA)
+
+
+def far_from_the_last(g):
+    g = g[np.isfinite(g)]
+    return g[np.abs(g.astype(np.float64) + LAST_GATE) > 1e-4]
+
+
+def test_swiglu_every_bf16_gate():
+    g = (np.arange(65536, dtype=np.uint32) << 16).view(np.float32)
+    check_gates(far_from_the_last(g), BF16, 1)
+
+
+def test_swiglu_fp32_gates_of_every_binade():
+    rng = np.random.default_rng(2)
+    g = np.ldexp(rng.uniform(1, 2, (277, 60)), np.arange(-149, 128)[:, None])
+    far = np.ldexp(rng.uniform(1, 2, 8000), rng.integers(23, 32, 8000))  # -t's last place: 1 and more
+    g = np.concatenate([g.ravel(), far, [2.0 ** -149, 88, 1e30, 2.35e38, 2.36e38, 3e38, np.finfo(np.float32).max]]).astype(np.float32)
+    g = np.concatenate([g, -g, rng.uniform(-88, -87, 2000).astype(np.float32)])
+    check_gates(far_from_the_last(g), F32, 3)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_swiglu_gates_that_count_as_0_beside_a_scale_in_doubt(dtype):
+    """a block whose largest value is 448 s is computed again in 64 bits, by the same definition: silu(-88) is 0"""
+    g = torch.zeros((2, 512), device="cuda").to(dtype)
+    u = torch.ones_like(g)
+    g[:, 0::128], u[:, 0::128] = 448, 2.0 ** -16
+    g[:, 7::9] = -88
+    u[:, 7::9] = 2.0 ** 103  # exp(-88) of it: 2^-16 * 0.36
+    codes, scales = empty_held(2, 512)
+    B.ls_op_swiglu_f8(g, u, codes, scales)
+    check_exact(codes, scales, silu64(f64(g)) * f64(u))
+    assert not held_values(codes, scales)[:, 7::9].any()
