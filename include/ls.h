@@ -480,8 +480,9 @@ int ls_op_expand_f8(const void *codes_dev, const void *scales_dev, int32_t M, in
                     void *out_bf16_dev, void *cuda_stream);
 /* RMSNorm with the residual's addition: x' = x + delta, rounded to x's type and written to x_out (of x's type;
  * may be x or delta itself, or NULL: not kept); codes and scales (block_rows = 1) of
- * x'[m,i] / sqrt(mean_j x'[m,j]^2 + eps) * gain[i], gain bf16 [D].  delta may be NULL.  In fp32, squares
- * joined in 64 bits; values next to a border between two codes are decided in 64 bits. */
+ * x'[m,i] / sqrt(mean_j x'[m,j]^2 + eps) * gain[i], gain bf16 [D].  delta may be NULL.  Squares and
+ * their mean in 64 bits, so that rows of any finite size have their norm; the rest in fp32, next to a border between two codes (of 2^-6 s
+ * and more) 64 bits. */
 int ls_op_rmsnorm_f8(const void *x_dev, int32_t x_type, int64_t ldx, const void *delta_dev, int32_t delta_type,
                      int64_t ldd, void *x_out_dev, int64_t ldo, const void *gain_dev, int32_t M, int32_t D, float eps,
                      void *codes_dev, void *scales_dev, void *cuda_stream);

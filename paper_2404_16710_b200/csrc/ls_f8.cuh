@@ -353,19 +353,18 @@ __global__ void __launch_bounds__(256) expand_f8_kernel(const unsigned char* __r
 }
 
 // ------------------------------------------------------------------ RMSNorm with the residual's addition, into 8 bits
-// x' = x + d rounded to x's type, y = x' / sqrt(mean x'^2 + eps) * gain.  Squares are added in fp32 within a thread's 32-byte piece (two
-// sums) and in 64 bits from there on; the rest is fp32, off by 5.5 2^-24: 7 roundings, three of them under the root.  A CTA
+// x' = x + d rounded to x's type, y = x' / sqrt(mean x'^2 + eps) * gain.  Squares are added in 64 bits (exact products, so that the sum's
+// error is nothing beside a rounding to fp32, and no row's squares overflow or vanish); the rest is fp32, off by 4.5 2^-24: the mean's rounding,
+// halved by the root, and those of root, reciprocal and two products.  Where the mean is not a normal number of fp32, x' is
+// multiplied by p, a power of two, and the mean by p^2.  A CTA
 // takes a row; with NV > 0 a thread keeps its NV pieces of it in registers, else (rows too long for that) x' is read again,
 // from x_out where it was written.  d and x_out may be null, x_out may be x or d.  Bound by memory and, since the borders
-// are checked, by registers: 4096 x 4096, fp32 x and bf16 d 36.1 us, 5.1 TB/s (without the check 31.5; that with 16-byte
-// accesses 41); one row 2.8 us, a launch.
-__device__ __forceinline__ float f8_norm_exact(float x, float g, double ss, int D, float eps)
-{
-    return f8_odd((double)x * (1.0 / sqrt(ss / D + (double)eps)) * (double)g);
-}
+// are checked, by registers: 4096 x 4096, fp32 x and bf16 d 37.1 us, 5.0 TB/s (36.8 with squares in
+// fp32; without the check 31.5; that with 16-byte accesses 41); one row 2.8 us, a launch.
+__device__ __forceinline__ float f8_norm_exact(float x, float g, double mean) { return f8_odd((double)x * (1.0 / sqrt(mean)) * (double)g); }
 template <typename T, typename TD, int NV>
 __global__ void __launch_bounds__(NV >= 4 ? 512 : 1024)
-rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, int64_t ldo, const uint16_t* gain, int D, float eps, int wide,
+rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, int64_t ldo, const uint16_t* gain, int D, double inv_D, float eps, int wide,
                   unsigned char* __restrict__ codes, unsigned char* __restrict__ scales)
 {
     constexpr int V = F8In<T>::V, KEEP = NV > 0 ? NV : 1;
@@ -400,12 +399,13 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
         }
     };
     float v[KEEP][V];
-    double ss = 0;
+    double ss = 0, ss1 = 0;  // two chains
     auto square = [&](const float (&u)[V]) {
-        float s[2] = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < V; ++j) s[j & 1] = fmaf(u[j], u[j], s[j & 1]);
-        ss += (double)s[0] + (double)s[1];
+        for (int j = 0; j < V; j += 2) {
+            ss = fma((double)u[j], (double)u[j], ss);
+            ss1 = fma((double)u[j + 1], (double)u[j + 1], ss1);
+        }
     };
     if (NV > 0) {
 #pragma unroll
@@ -428,6 +428,7 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
             square(v[0]);
         }
     }
+    ss += ss1;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     if ((tid & 31) == 0) part[tid >> 5] = ss;
@@ -435,13 +436,18 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
     ss = (tid & 31) < T0 / 32 ? part[tid & 31] : 0.0;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    const float r = 1.0f / sqrtf((float)ss / (float)D + eps);
+    const double mean = ss * inv_D + (double)eps;
+    const float p = mean > 0x1p127 ? 0x1p-65f : mean < 0x1p-126 ? 0x1p100f : 1.f;
+    const float r = 1.0f / sqrtf((float)(mean * p * p));
     auto exact = [=](int k) {
         float u = F8In<T>::value(x_out ? x_out[k] : x[k]);
         if (!x_out && d) u = F8In<T>::kept(u + F8In<TD>::value(d[k]));
-        return f8_norm_exact(u, bf16f(gain[k]), ss, D, eps);
+        return f8_norm_exact(u, bf16f(gain[k]), mean);
     };
     auto finish = [&](int k, float (&u)[V]) {  // whole warps
+        if (p != 1.f)
+#pragma unroll
+            for (int j = 0; j < V; ++j) u[j] *= p;
         if (k < D) {
 #pragma unroll
             for (int j = 0; j < V; j += 8) {

@@ -2278,7 +2278,7 @@ template <typename T, typename TD, int NV>
 int rmsnorm_f8_launch_nv(const NormArgs& a, int threads, const LaunchCtx& lc)
 {
     LS_CK(launch(lc, rmsnorm_f8_kernel<T, TD, NV>, dim3((unsigned)a.M), dim3(threads), 0, (const T*)a.x, a.ldx, (const TD*)a.d, a.ldd,
-                 (T*)a.x_out, a.ldo, (const uint16_t*)a.gain, a.D, a.eps, a.wide, a.codes, a.scales));
+                 (T*)a.x_out, a.ldo, (const uint16_t*)a.gain, a.D, 1.0 / a.D, a.eps, a.wide, a.codes, a.scales));
     return LS_OK;
 }
 

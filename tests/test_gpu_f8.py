@@ -642,3 +642,78 @@ def test_swiglu_gates_that_count_as_0_beside_a_scale_in_doubt(dtype):
     B.ls_op_swiglu_f8(g, u, codes, scales)
     check_exact(codes, scales, silu64(f64(g)) * f64(u))
     assert not held_values(codes, scales)[:, 7::9].any()
+
+
+# ------------------------------------------------------------------ the norm's sum
+def next_to_a_border(x, gain, eps, seed):
+    """x (fp32 [M, D]) with one value of each row moved until its result is one of the two fp32 neighbours of a border between codes"""
+    rng = np.random.default_rng(seed)
+    M, D = x.shape
+    rows, at = np.arange(M), rng.integers(0, D, M)
+    v = x.astype(np.float64)
+    rest = (v * v).sum(1) - v[rows, at] ** 2
+    y = v[rows, at] / np.sqrt((rest + v[rows, at] ** 2) / D + eps) * gain[at]
+    e = np.floor(np.log2(np.abs(y)))
+    border = (np.floor(np.abs(y) / np.exp2(e - 3)) + 0.5) * np.exp2(e - 3)
+    t = (border / np.abs(gain[at])) ** 2  # v^2 = t (rest + v^2) / D + t eps
+    ok = t < D / 2
+    size = np.sqrt(np.where(ok, t * (rest / D + eps) / np.where(ok, 1 - t / D, 1), v[rows, at] ** 2))
+    near = size.astype(np.float32)
+    below = np.where(near <= size, near, np.nextafter(near, np.float32(0)))
+    near = np.where(rng.random(M) < 0.5, below, np.nextafter(below, np.float32(np.inf)))
+    x = x.copy()
+    x[rows, at] = np.copysign(near, x[rows, at])
+    return x
+
+
+@pytest.mark.parametrize("form", ["alone", "added", "kept"])
+@pytest.mark.parametrize("M,D", [(20000, 16), (4000, 272), (600, 4112), (24, 40000)])
+def test_norm_codes_that_the_sum_decides(M, D, form):
+    """a few loud columns and many whose squares are lost one by one in 24 bits, and a value of each row next to a border: the error
+    of the sum has to be far below that of a rounding"""
+    rng = np.random.default_rng(D)
+    x = rng.standard_normal((M, D)) * np.where(rng.random((M, D)) < 4 / D, 1, 2.0 ** -12.5)
+    x[:, :2] = rng.uniform(0.5, 1.5, (M, 2)) * rng.choice([-1, 1], (M, 2))
+    x = (x * np.exp(rng.standard_normal((M, 1)))).astype(np.float32)
+    gain = (1 + 0.1 * rnd((D,), 3)).to(BF16)
+    eps = 2.0 ** -17
+    x = torch.from_numpy(next_to_a_border(x, f64(gain), eps, 1)).cuda()
+    d = None if form == "alone" else (rnd((M, D), 4) * 2.0 ** -30).to(BF16)
+    if d is not None:
+        x = x - d.float()
+        x = torch.from_numpy(next_to_a_border(added(x, d).cpu().numpy(), f64(gain), eps, 2)).cuda() - d.float()
+    want = normed(added(x, d), gain, eps)
+    codes, scales = empty_held(M, D)
+    B.ls_op_rmsnorm_f8(x, gain, eps, codes, scales, delta=d, x_out=x if form == "kept" else None)
+    check_exact(codes, scales, want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,D", [(9, 16), (300, 272), (7, 4112), (5, 40000)])
+def test_norm_codes_of_ordinary_rows(M, D, dtype):
+    x = (rnd((M, D), M + D) * torch.exp(rnd((M, 1), 1))).to(dtype)
+    gain = (1 + 0.1 * rnd((D,), 3)).to(BF16)
+    codes, scales = empty_held(M, D)
+    B.ls_op_rmsnorm_f8(x, gain, 2.0 ** -17, codes, scales)
+    check_exact(codes, scales, normed(x, gain, 2.0 ** -17))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [16, 528, 4096, 40000])
+def test_norm_of_rows_of_any_size(D, dtype):
+    """rows whose squares, or their mean, are no numbers of fp32; without eps"""
+    sizes = torch.tensor([2.0 ** k for k in (-130, -100, -76, -70, -64, -60, -30, 0, 30, 60, 63, 64, 65, 90, 120, 126)], device="cuda")
+    x = (rnd((len(sizes), D), D).clamp(-1.9, 1.9) * sizes[:, None]).to(dtype)
+    x[:, 3] = x[:, 2] * 0.125
+    gain = (1 + 0.1 * rnd((D,), 3)).to(BF16)
+    codes, scales = empty_held(*x.shape)
+    for eps in (0.0, 2.0 ** -17):
+        x_out = torch.empty_like(x)
+        B.ls_op_rmsnorm_f8(x, gain, eps, codes, scales, x_out=x_out)
+        assert torch.equal(x_out, x)
+        check_exact(codes, scales, normed(x, gain, eps))
+    # the largest numbers throughout: every value is its gain
+    x = torch.full((2, D), torch.finfo(dtype).max, dtype=dtype, device="cuda")
+    codes, scales = empty_held(2, D)
+    B.ls_op_rmsnorm_f8(x, torch.ones(D, dtype=BF16, device="cuda"), 1e-5, codes, scales)
+    assert (held_values(codes, scales) == 1).all()
