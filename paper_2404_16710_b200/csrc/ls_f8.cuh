@@ -113,7 +113,7 @@ struct F8In<float> {
         f8_st32(p, w, wide);
     }
     static __device__ __forceinline__ float kept(float v) { return v; }
-    static __device__ __forceinline__ float value(float v) { return v; }
+    static __device__ __forceinline__ float load(const float* p) { return __ldcg(p); }
 };
 template <>
 struct F8In<uint16_t> {  // bf16
@@ -131,7 +131,7 @@ struct F8In<uint16_t> {  // bf16
         f8_st32(p, w, wide);
     }
     static __device__ __forceinline__ float kept(float v) { return bf16f(f2bf(v)); }  // the value that store() leaves
-    static __device__ __forceinline__ float value(uint16_t v) { return bf16f(v); }
+    static __device__ __forceinline__ float load(const uint16_t* p) { return bf16f(__ldcg(p)); }
 };
 
 __device__ __forceinline__ float max_nan(float a, float b)  // a NaN wins
@@ -185,6 +185,7 @@ __device__ __forceinline__ uint32_t f8_above_border(float t) { return (__float_a
 struct F8AsIs {};  // with W = 0: the values are what they are
 // The two rare ways are calls, whose registers and instructions the others do not carry: the columns of a lane that `todo`
 // names, and a warp's whole part where the scale is in doubt.
+// fix() loads from L2, as f8_ld32 does not leave lines in L1: one that an operation of the chain left there may be older than the data.
 template <typename Fix>
 __device__ __noinline__ void f8_fix_codes(Fix fix, int k, uint32_t todo, float r, unsigned char* codes)
 {
@@ -440,8 +441,8 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
     const float p = mean > 0x1p127 ? 0x1p-65f : mean < 0x1p-126 ? 0x1p100f : 1.f;
     const float r = 1.0f / sqrtf((float)(mean * p * p));
     auto exact = [=](int k) {
-        float u = F8In<T>::value(x_out ? x_out[k] : x[k]);
-        if (!x_out && d) u = F8In<T>::kept(u + F8In<TD>::value(d[k]));
+        float u = F8In<T>::load(x_out ? x_out + k : x + k);
+        if (!x_out && d) u = F8In<T>::kept(u + F8In<TD>::load(d + k));
         return f8_norm_exact(u, bf16f(gain[k]), mean);
     };
     auto finish = [&](int k, float (&u)[V]) {  // whole warps
@@ -541,7 +542,7 @@ __global__ void __launch_bounds__(256, 4) swiglu_f8_kernel(const T* __restrict__
 #pragma unroll
         for (int j = 0; j < V; ++j) a[j] = f8_silu_times(a[j], b[j]);
         const T *gm = gate + m * ld, *um = up + m * ld;
-        auto exact = [=](int k) { return f8_silu_exact(F8In<T>::value(gm[k]), F8In<T>::value(um[k])); };
+        auto exact = [=](int k) { return f8_silu_exact(F8In<T>::load(gm + k), F8In<T>::load(um + k)); };
         f8_store_row_part<V, 12>(a, p * STEP, F, width, codes + (int64_t)m * F, scales + (int64_t)m * width, exact);
         m = m1, p = p1, g = g1, u = u1;
     }

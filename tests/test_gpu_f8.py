@@ -717,3 +717,25 @@ def test_norm_of_rows_of_any_size(D, dtype):
     codes, scales = empty_held(2, D)
     B.ls_op_rmsnorm_f8(x, torch.ones(D, dtype=BF16, device="cuda"), 1e-5, codes, scales)
     assert (held_values(codes, scales) == 1).all()
+
+
+def test_norm_in_a_chain_reads_what_the_operation_ahead_wrote_in_the_64_bit_path_too():
+    """rows of one number x and gains that put every result on a border: all of them are computed twice, whatever x is; x grows by one between
+    chained norms, and a value of an earlier x among the new ones would be off by far more than a code"""
+    M, D, steps = 100, 4096, 48
+    gain = torch.full((D,), 1.0625, dtype=BF16, device="cuda")
+    w = quantised(torch.full((D, 16), 0.25, device="cuda"), 128)
+    h = quantised(torch.full((M, 16), 0.25, device="cuda"))
+    x = torch.ones((M, D), device="cuda")
+    held = [empty_held(M, D) for _ in range(steps)]
+    torch.cuda.synchronize()
+    B.ls_op_chain(True)
+    try:
+        for codes, scales in held:
+            B.ls_op_rmsnorm_f8(x, gain, 0.0, codes, scales)
+            B.ls_op_linear_f8(*w, *h, x, add=x)
+    finally:
+        B.ls_op_chain(False)
+    assert (x == 1 + steps).all()
+    for i, (codes, scales) in enumerate(held):  # 1.0625 is halfway between 1 and 1.125
+        assert (held_values(codes, scales) == 1).all(), i
