@@ -739,3 +739,34 @@ def test_norm_in_a_chain_reads_what_the_operation_ahead_wrote_in_the_64_bit_path
     assert (x == 1 + steps).all()
     for i, (codes, scales) in enumerate(held):  # 1.0625 is halfway between 1 and 1.125
         assert (held_values(codes, scales) == 1).all(), i
+
+
+# ------------------------------------------------------------------ which form of the product runs
+# both sides of the rule by which 65 to 128 rows go to CTA pairs (more than 148 tiles of 128 rows of weights), and of those at 64 and 128 rows
+MANY_TILES = [(M, N, K) for M in (64, 65, 97, 128, 129) for N, K in ((18944, 272), (18945, 272), (19073, 528))] + \
+    [(65, 32000, 400), (80, 22016, 1040), (112, 19200, 2064), (128, 22016, 4112)]
+
+
+@pytest.mark.parametrize("M,N,K", MANY_TILES)
+@pytest.mark.parametrize("out_type,add", [(F32, True), (BF16, False)])
+def test_linear_many_tiles_of_weights(M, N, K, out_type, add):
+    test_linear(M, N, K, out_type, add)
+
+
+@pytest.mark.parametrize("M", [1, 7, 16])
+@pytest.mark.parametrize("N,K", [(4096, 4112), (5504, 1040), (11008, 4096), (18944, 528), (2048, 8208)])
+@pytest.mark.parametrize("add", [False, True])
+def test_linear_chained_and_alone_with_and_without_a_long_ring(M, N, K, add):
+    """alone, up to 16 rows on at most one CTA an SM and clusters of at most four use the whole SM for stages; chained, half of it"""
+    w, h = pair_of(M, N, K, 19)
+    base = rnd((M, N), 6) if add else None
+    alone, chained = (torch.full((M, N), float("nan"), device="cuda") for _ in range(2))
+    B.ls_op_linear_f8(*w, *h, alone, add=base)
+    torch.cuda.synchronize()
+    B.ls_op_chain(True)
+    try:
+        for _ in range(3):
+            B.ls_op_linear_f8(*w, *h, chained, add=base)
+    finally:
+        B.ls_op_chain(False)
+    assert torch.equal(alone, chained)
