@@ -577,6 +577,8 @@ LS_F8_MAX_ROWS = 1 << 22
 
 @functools.lru_cache(maxsize=4096)
 def ls_op_f8_scale_bytes(M, K, block_rows=1):
+    if not (0 < M <= LS_F8_MAX_ROWS and 0 < K <= 1 << 28 and block_rows in (1, 128)):  # 32 bits of them go to the library
+        return 0
     return lib().ls_op_f8_scale_bytes(M, K, block_rows)
 
 
@@ -585,7 +587,10 @@ def _held(codes, scales, M, K, block_rows, dev, what):
     if codes.dtype is not _torch.f8 or scales.dtype is not _torch.u8 or codes.get_device() != dev or scales.get_device() != dev or \
             not codes.is_contiguous() or not scales.is_contiguous():
         _bad(f"{what}: contiguous codes (float8_e4m3fn) and scales (uint8) are needed, on the CUDA device of the others")
-    if scales.numel() < ls_op_f8_scale_bytes(M, K, block_rows):
+    need = ls_op_f8_scale_bytes(M, K, block_rows)
+    if not need:
+        _bad(f"{what}: a shape of the format is needed, in blocks of 1 or 128 rows")
+    if scales.numel() < need:
         raise LsError(LS_ERR_CAPACITY, f"{what}: scales")
     return codes.data_ptr(), scales.data_ptr()
 

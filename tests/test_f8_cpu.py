@@ -154,3 +154,45 @@ def test_the_binding_refuses_tensors_of_another_device(monkeypatch):
             with pytest.raises(B.LsError) as e:
                 f(*a)
             assert e.value.status == BAD, (f.__name__, odd)
+
+
+def test_sizes_beyond_32_bits_are_not_taken_for_small_ones(monkeypatch):
+    """rows and columns go to the library as 32-bit integers: 2^32 + 4 rows are refused, not 4 done"""
+    big = (1 << 32) + 4
+    for shape in ((big, 16, 1), (4, (1 << 32) + 256, 1), (4, 256, (1 << 32) + 1), (big, 256, 128), (4 - (1 << 32), 256, 1)):
+        assert B.ls_op_f8_scale_bytes(*shape) == 0, shape
+
+    class Unreached:
+        def __getattr__(self, name):
+            raise AssertionError(f"{name} is called")
+
+    class On:  # a tensor of some shape on the current device
+        def __init__(self, t):
+            self.t = t
+
+        def __getattr__(self, name):
+            return getattr(self.t, name)
+
+        def get_device(self):
+            return 0
+
+    monkeypatch.setattr(B._torch, "device", lambda: 0)
+    monkeypatch.setattr(B._torch, "stream", lambda dev: 0)
+    monkeypatch.setattr(B, "lib", Unreached)
+    B.ls_op_f8_scale_bytes.cache_clear()
+    bf = torch.bfloat16
+
+    def on(*shape, dtype=torch.float8_e4m3fn):
+        return On(torch.empty(shape, dtype=dtype, device="meta"))
+
+    codes, scales, x, gain = on(big, 256), on(big, 4, dtype=torch.uint8), on(big, 256, dtype=bf), on(256, dtype=bf)
+    few, fs = on(4, 256), on(4, 4, dtype=torch.uint8)
+    cases = [
+        (B.ls_op_quantize_f8, (x, codes, scales)), (B.ls_op_quantize_f8, (x, codes, scales, 128)), (B.ls_op_expand_f8, (codes, scales, x)),
+        (B.ls_op_rmsnorm_f8, (x, gain, 1e-5, codes, scales)), (B.ls_op_swiglu_f8, (x, x, codes, scales)),
+        (B.ls_op_linear_f8, (codes, scales, few, fs, on(4, big, dtype=bf))), (B.ls_op_linear_f8, (few, fs, codes, scales, on(big, 4, dtype=bf))),
+    ]
+    for f, args in cases:
+        with pytest.raises(B.LsError) as e:
+            f(*args)
+        assert e.value.status == BAD, f.__name__
