@@ -163,6 +163,8 @@ def test_sizes_beyond_32_bits_are_not_taken_for_small_ones(monkeypatch):
         assert B.ls_op_f8_scale_bytes(*shape) == 0, shape
 
     class Unreached:
+        ls_op_f8_scale_bytes, ls_strerror = B.lib().ls_op_f8_scale_bytes, B.lib().ls_strerror
+
         def __getattr__(self, name):
             raise AssertionError(f"{name} is called")
 
