@@ -479,7 +479,7 @@ int ls_op_quantize_f8(const void *x_dev, int32_t type, int64_t ldx, int32_t M, i
 int ls_op_expand_f8(const void *codes_dev, const void *scales_dev, int32_t M, int32_t K, int32_t block_rows,
                     void *out_bf16_dev, void *cuda_stream);
 /* RMSNorm with the residual's addition: x' = x + delta, rounded to x's type and written to x_out (of x's type;
- * may be x or delta itself, or NULL: not kept); codes and scales (block_rows = 1) of
+ * may be x, or delta of x's type, itself, with its stride; NULL: not kept); codes and scales (block_rows = 1) of
  * x'[m,i] / sqrt(mean_j x'[m,j]^2 + eps) * gain[i], gain bf16 [D].  delta may be NULL.  Squares and
  * their mean in 64 bits, so that rows of any finite size have their norm; the rest in fp32, next to a border between two codes (of 2^-6 s
  * and more) 64 bits. */

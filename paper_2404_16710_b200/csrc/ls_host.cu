@@ -2198,6 +2198,8 @@ static bool f8_rows_ok(const void* p, int type, int64_t ld, int M, int K)  // ro
     return aligned16(p) && f8_type_ok(type) && (M == 1 || (ld >= K && ld % f8_pieces(type) == 0));
 }
 static bool f8_held_ok(const void* codes, const void* scales) { return aligned16(codes) && scales && ((uintptr_t)scales & 3u) == 0; }
+// an output that begins where an input does: the same rows, each read before it is written
+static bool f8_in_place_ok(const void* out, int64_t ldo, const void* in, int64_t ld, int M) { return out != in || M == 1 || ldo == ld; }
 // rows that begin at 32-byte boundaries (element counts of 32 bytes: twice f8_pieces)
 static bool f8_wide(const void* p, int type, int64_t ld, int M)
 {
@@ -2455,6 +2457,8 @@ int ls_op_rmsnorm_f8(const void* x, int32_t x_type, int64_t ldx, const void* del
     if (!f8_shape_ok(M, D) || !f8_rows_ok(x, x_type, ldx, M, D) || (delta && !f8_rows_ok(delta, delta_type, ldd, M, D)) ||
         (x_out && !f8_rows_ok(x_out, x_type, ldo, M, D)) || !aligned16(gain) || !f8_held_ok(codes, scales))
         return LS_ERR_INVALID_ARG;
+    if (x_out && (!f8_in_place_ok(x_out, ldo, x, ldx, M) || !f8_in_place_ok(x_out, ldo, delta, ldd, M) || (x_out == delta && x_type != delta_type)))
+        return LS_ERR_INVALID_ARG;
     const int wide = f8_wide(x, x_type, ldx, M) && f8_wide(delta, delta_type, ldd, M) && f8_wide(x_out, x_type, ldo, M);
     const NormArgs a = {const_cast<void*>(x), x_out, delta, gain, ldx, ldd, ldo, M, D, wide, eps, (unsigned char*)codes, (unsigned char*)scales};
     const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};
@@ -2484,7 +2488,8 @@ int ls_op_linear_f8(const void* w_codes, const void* w_scales, const void* h_cod
 {
     const uintptr_t odd = out_type == LS_F32 ? 3u : 1u;
     if (!f8_shape_ok(M, K) || !f8_shape_ok(N, K) || !f8_held_ok(w_codes, w_scales) || !f8_held_ok(h_codes, h_scales) ||
-        !f8_type_ok(out_type) || !out || ((uintptr_t)out & odd) || ((uintptr_t)add & odd) || (M > 1 && (ldo < N || (add && lda < N))))
+        !f8_type_ok(out_type) || !out || ((uintptr_t)out & odd) || ((uintptr_t)add & odd) || (M > 1 && (ldo < N || (add && lda < N))) ||
+        !f8_in_place_ok(out, ldo, add, lda, M))
         return LS_ERR_INVALID_ARG;
     const F8Linear p = {(const unsigned char*)w_scales, (const unsigned char*)h_scales, M, N, K, out, add, ldo, lda, status};
     const LaunchCtx lc = {(cudaStream_t)stream, g_op_chain};

@@ -198,3 +198,11 @@ def test_sizes_beyond_32_bits_are_not_taken_for_small_ones(monkeypatch):
         with pytest.raises(B.LsError) as e:
             f(*args)
         assert e.value.status == BAD, f.__name__
+
+
+def test_an_output_over_an_input_of_another_stride_is_refused():
+    """in place means row over row: rows that begin together and lie differently would be written before they are read"""
+    L = B.lib()
+    refused(L.ls_op_rmsnorm_f8, [P, B.LS_F32, 512, 2 * P, B.LS_F32, 512, P, 512, P, 4, 256, 1e-5, P, P, None], [
+        (2, 256), (7, 256), ((6, 7), (2 * P, 256)), ((4, 6), (B.LS_BF16, 2 * P)), ((5, 6), (1024, 2 * P))])
+    refused(L.ls_op_linear_f8, [P, P, P, P, 4, 128, 256, 2 * P, B.LS_F32, 256, 2 * P, 256, None, None], [(9, 128), (11, 128), (11, 512)])
