@@ -185,7 +185,7 @@ __device__ __forceinline__ uint32_t f8_above_border(float t) { return (__float_a
 struct F8AsIs {};  // with W = 0: the values are what they are
 // The two rare ways are calls, whose registers and instructions the others do not carry: the columns of a lane that `todo`
 // names, and a warp's whole part where the scale is in doubt.
-// fix() loads from L2, as f8_ld32 does not leave lines in L1: one that an operation of the chain left there may be older than the data.
+// fix() loads from L2: a line that an operation of the chain left in L1 may be older than the data (f8_ld32 leaves none).
 template <typename Fix>
 __device__ __noinline__ void f8_fix_codes(Fix fix, int k, uint32_t todo, float r, unsigned char* codes)
 {
@@ -461,7 +461,7 @@ rmsnorm_f8_kernel(const T* x, int64_t ldx, const TD* d, int64_t ldd, T* x_out, i
                 }
             }
         }
-        f8_store_row_part<V, 8>(u, k - V * (tid & 31), D, width, codes + m * D, scales + m * width, exact);
+        f8_store_row_part<V, 6>(u, k - V * (tid & 31), D, width, codes + m * D, scales + m * width, exact);
     };
     if (NV > 0) {
 #pragma unroll
